@@ -16,7 +16,10 @@
  * softmax statistics (more_route_lowrank_train), the training backward pass
  * (more_route_lowrank_backward), the full-rank baselines (more_route_fullrank,
  * more_route_fullrank_fused), the per-expert histogram and the dispatch bookkeeping
- * (more_dispatch_sort).
+ * (more_dispatch_sort); and the layer around the router: the experts' gated feed-forward block with
+ * its backward pass (more_expert_ffn, more_expert_ffn_backward), the norms after and before a block
+ * fused with its gate and residual scale (more_block_norm, more_block_norm_backward) and the clipping
+ * of all gradients by their common norm (more_grad_clip).
  *
  * Conventions shared by every call
  * --------------------------------
@@ -314,6 +317,133 @@ more_status more_route_lowrank_noalloc(const uint16_t* x, const uint16_t* R1t, c
                                        int64_t T, int32_t h, int32_t r, int32_t M, int32_t k,
                                        int32_t* idx, float* gate, float* topval, int32_t* counts,
                                        void* stream);
+
+/*
+ * The experts of the layer: a gated feed-forward block per expert, applied to the entries of a
+ * selection ("MoE layer", SwiGLU experts f_i and sum_i g_i f_i; the efficiency appendix's expert linear
+ * (N, h) -> (N k, 2s), SwiGLU, linear (N k, s) -> (N, h)).  For every entry p = t k + j with expert
+ * e = idx[t][j] and gate g_p:
+ *   A_p = silu(x_t Wg_e^T) * (x_t Wu_e^T)       y_p = g_p (A_p W2_e^T)
+ * The layer's output is sum_j y[t k + j] (more_block_norm takes the k rows as they are).  One dense
+ * block is M = 1, k = 1, idx = 0.
+ *   x        bf16 [T][h]
+ *   W1t      bf16 [M][2s][h]   per expert the s gate rows Wg_e, then the s up rows Wu_e
+ *   W2t      bf16 [M][h][s]    per expert W2_e, one row per output column
+ *   idx      int32 [T][k]      the selection; entries with an id outside [0, M) are dropped: their y
+ *                              rows are zero, and their gates are not read
+ *   offsets  int32 [M + 1]     from more_dispatch_sort of this idx
+ *   sorted   int32 [T k]       from more_dispatch_sort of this idx
+ *   gate     fp32 [T][k]       or NULL (all ones)
+ *   y        bf16 [T k][h] out
+ *   workspace / workspace_bytes   at least more_expert_ffn_workspace_size() bytes, 256-byte aligned
+ *                              (NULL allowed when T == 0)
+ * Limits: h a positive multiple of 16, s a positive multiple of 8, both at most 65536;
+ * 1 <= k <= MORE_K_MAX (k may exceed M: an id may occur more than once in a token); T k <= 2^31 - 1,
+ * M < 2^30.  T == 0 writes nothing.  offsets and sorted that are not those of idx give undefined values
+ * in y (no access outside the buffers).
+ * Numerics: fp32 accumulation of exact bf16 products; A is rounded to bf16 once, between the two
+ * contractions; activation and gate in fp32.  The sums run in a fixed order.
+ */
+more_status more_expert_ffn(const uint16_t* x, const uint16_t* W1t, const uint16_t* W2t, int64_t T,
+                            int32_t h, int32_t s, int32_t M, int32_t k, const int32_t* idx,
+                            const int32_t* offsets, const int32_t* sorted, const float* gate,
+                            uint16_t* y, void* workspace, size_t workspace_bytes, void* stream);
+more_status more_expert_ffn_workspace_size(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k,
+                                           size_t* bytes);
+
+/*
+ * Backward pass of more_expert_ffn with recompute of the hidden units (nothing is kept from the forward
+ * pass).  du is the gradient with respect to sum_j y[t k + j], the same for a token's k entries.
+ *   x .. gate  as in more_expert_ffn
+ *   du       bf16 [T][h]
+ *   dx       bf16 [T][h]       out
+ *   dW1t     bf16 [M][2s][h]   out, zero for experts without entries (all zero when T == 0)
+ *   dW2t     bf16 [M][h][s]    out, likewise
+ *   dgate    fp32 [T][k]       out, or NULL; zero for dropped entries.  NULL where gate is NULL
+ *   workspace / workspace_bytes   at least more_expert_ffn_backward_workspace_size() bytes, 256-byte
+ *                              aligned (NULL allowed when T == 0)
+ * Limits as for more_expert_ffn.  Numerics: bf16 operands with fp32 accumulation; the gradients of the
+ * pre-activations and gate A are rounded to bf16 once, the entries' shares of dx are added in fp32,
+ * dgate comes from unrounded fp32 values.  Nothing is added atomically: a call gives the same bits on
+ * every run.
+ */
+more_status more_expert_ffn_backward(const uint16_t* x, const uint16_t* W1t, const uint16_t* W2t,
+                                     int64_t T, int32_t h, int32_t s, int32_t M, int32_t k,
+                                     const int32_t* idx, const int32_t* offsets, const int32_t* sorted,
+                                     const float* gate, const uint16_t* du, uint16_t* dx,
+                                     uint16_t* dW1t, uint16_t* dW2t, float* dgate, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+more_status more_expert_ffn_backward_workspace_size(int64_t T, int32_t h, int32_t s, int32_t M,
+                                                    int32_t k, size_t* bytes);
+
+/*
+ * The end of a block and the norm before the next one, in one pass:
+ *   u  = sum_{j < k} y[t][j]                       r' = alpha r + gate[t] (w_after * n)
+ *   n  = u / rms(u) if norm_after, else u          xn = w_before * r' / rms(r')
+ * with rms(v) = sqrt(mean(v^2) + eps).
+ *   r         [T][h]            the residual, fp32 (resid_bits == 32) or bf16 (resid_bits == 16)
+ *   y         bf16 [T][k][h]    the block's output as k addends, e.g. the rows of more_expert_ffn;
+ *                               k == 0 and y == NULL: no block, r' = r, and w_after, gate, r_out and u
+ *                               are NULL (the norm before the first block)
+ *   w_after   fp32 [h] or NULL (ones)
+ *   w_before  fp32 [h], NULL exactly where xn is NULL (no norm follows; then there must be a block)
+ *   gate      fp32 [T] or NULL (ones)
+ *   r_out     [T][h] out        r', in the residual's type; may be r itself (in place)
+ *   u         bf16 [T][h] out   or NULL; the backward pass takes it
+ *   xn        bf16 [T][h] out   or NULL
+ * Limits: h a multiple of 16 up to MORE_NORM_H_MAX, k <= 65536, T k <= 2^31 - 1, eps > 0, alpha finite.
+ * No workspace.  Numerics: fp32 throughout, each output rounded once (xn from the unrounded r').
+ */
+#define MORE_NORM_H_MAX 8192
+more_status more_block_norm(const void* r, int32_t resid_bits, const uint16_t* y, int64_t T, int32_t h,
+                            int32_t k, const float* w_after, const float* w_before, const float* gate,
+                            float alpha, float eps, int32_t norm_after, void* r_out, uint16_t* u,
+                            uint16_t* xn, void* stream);
+
+/*
+ * Backward pass of more_block_norm.
+ *   u         bf16 [T][h]       of the forward pass; NULL: no block (then gate, w_after, du, dw_after
+ *                               and dgate are NULL and alpha is taken as 1)
+ *   r_out     [T][h]            r' of the forward pass, of type resid_bits
+ *   dr_out    [T][h]            gradient with respect to r', of that type, or NULL (zero)
+ *   dxn       bf16 [T][h]       gradient with respect to xn, or NULL
+ *   dxn32     fp32 [T][h]       a second addend of it (the router's dx), or NULL
+ *                               (w_before is NULL exactly where both are NULL; not all three are NULL)
+ *   dr        [T][h] out        gradient with respect to r, of type resid_bits; may be dr_out itself
+ *   du        bf16 [T][h] out   gradient with respect to u, that is to each of the k rows y[t][j]
+ *   dw_after  fp32 [h] out      or NULL
+ *   dw_before fp32 [h] out      or NULL; NULL where w_before is NULL
+ *   dgate     fp32 [T] out      or NULL; NULL where gate is NULL
+ *   workspace / workspace_bytes   at least more_block_norm_backward_workspace_size() bytes, 16-byte
+ *                               aligned (NULL allowed when T == 0)
+ * T == 0 writes zeros to dw_after and dw_before.  The weights' gradients are summed in a fixed order in
+ * fp32: a shape gives the same bits on every run.
+ */
+more_status more_block_norm_backward(const uint16_t* u, const void* r_out, int32_t resid_bits,
+                                     const void* dr_out, const uint16_t* dxn, const float* dxn32,
+                                     int64_t T, int32_t h, const float* w_after, const float* w_before,
+                                     const float* gate, float alpha, float eps, int32_t norm_after,
+                                     void* dr, uint16_t* du, float* dw_after, float* dw_before,
+                                     float* dgate, void* workspace, size_t workspace_bytes, void* stream);
+more_status more_block_norm_backward_workspace_size(int64_t T, int32_t h, size_t* bytes);
+
+/*
+ * The 2-norm N of n gradients together, and the gradients scaled by c = min(1, max_norm / (N + eps)).
+ *   in, out  host arrays of n device pointers; out[i] == in[i] scales in place (and writes nothing when
+ *            c is 1).  An output may not overlap another tensor.  Elements must be aligned to their
+ *            size (16-byte aligned tensors are faster)
+ *   numel    host, elements of each tensor (0 allowed, then its pointers are not read)
+ *   bits     host, 32 (fp32) or 16 (bf16) per tensor
+ *   norm     fp32 [1] out, or NULL: N
+ *   workspace / workspace_bytes   at least more_grad_clip_workspace_size() bytes, 16-byte aligned
+ * The host arrays are read during the call only.  n >= 0, max_norm >= 0, eps > 0, both finite.  The
+ * squares are added in fp64 in a fixed order.  Where N is infinite c is 0 (infinite elements become
+ * NaN, the others 0); a NaN among the elements makes N, c and every element NaN.
+ */
+more_status more_grad_clip(const void* const* in, void* const* out, const int64_t* numel,
+                           const int32_t* bits, int32_t n, float max_norm, float eps, float* norm,
+                           void* workspace, size_t workspace_bytes, void* stream);
+more_status more_grad_clip_workspace_size(const int64_t* numel, int32_t n, size_t* bytes);
 
 /* Static, never NULL. */
 const char* more_status_string(more_status s);

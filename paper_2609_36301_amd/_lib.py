@@ -15,11 +15,12 @@ K_MAX = 32
 LOWRANK_K_MAX = 32
 LOWRANK_TRAIN_K_MAX = 16
 ROUTE_WIDE = 4
+NORM_H_MAX = 8192
 NOALLOC_SCRATCH_BYTES = 256 << 20
 
 # (name, restype, argtypes) for every symbol declared in include/more.h
 _P = ctypes.c_void_p
-_I64, _I32, _SZ = ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t
+_I64, _I32, _SZ, _F32 = ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t, ctypes.c_float
 _PSZ = ctypes.POINTER(ctypes.c_size_t)
 _PI32 = ctypes.POINTER(ctypes.c_int32)
 SIGNATURES = {
@@ -49,6 +50,19 @@ SIGNATURES = {
     "more_dispatch_sort_workspace_size": (_I32, [_I64, _I32, _I32, _PSZ]),
     "more_route_lowrank_noalloc": (_I32, [_P, _P, _P, _I64, _I32, _I32, _I32, _I32, _P, _P, _P,
                                           _P, _P]),
+    "more_expert_ffn": (_I32, [_P, _P, _P, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _P, _P,
+                               _SZ, _P]),
+    "more_expert_ffn_workspace_size": (_I32, [_I64, _I32, _I32, _I32, _I32, _PSZ]),
+    "more_expert_ffn_backward": (_I32, [_P, _P, _P, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _P,
+                                        _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "more_expert_ffn_backward_workspace_size": (_I32, [_I64, _I32, _I32, _I32, _I32, _PSZ]),
+    "more_block_norm": (_I32, [_P, _I32, _P, _I64, _I32, _I32, _P, _P, _P, _F32, _F32, _I32, _P,
+                               _P, _P, _P]),
+    "more_block_norm_backward": (_I32, [_P, _P, _I32, _P, _P, _P, _I64, _I32, _P, _P, _P, _F32,
+                                        _F32, _I32, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "more_block_norm_backward_workspace_size": (_I32, [_I64, _I32, _PSZ]),
+    "more_grad_clip": (_I32, [_P, _P, _P, _P, _I32, _F32, _F32, _P, _P, _SZ, _P]),
+    "more_grad_clip_workspace_size": (_I32, [_P, _I32, _PSZ]),
     "more_status_string": (ctypes.c_char_p, [_I32]),
     "more_version": (ctypes.c_char_p, []),
 }

@@ -20,7 +20,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmore.so")
 SOURCES = ["lowrank.hip", "bucket.hip", "fullrank.hip", "histogram.hip", "dispatch.hip", "stats.hip", "fullrank_fused.hip",
            "backward.hip", "wide.hip",
-           "noalloc.hip", "more_api.cpp"]
+           "noalloc.hip", "more_api.cpp", "ffn.hip", "ffn_backward.hip", "block_norm.hip",
+           "grad_clip.hip", "layer_api.cpp"]
 ARCH = "gfx950"
 
 

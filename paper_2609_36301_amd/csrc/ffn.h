@@ -1,0 +1,43 @@
+// Plans and launch entry points of the experts' gated feed-forward block (ffn.hip, ffn_backward.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace more {
+
+struct FfnArgs {
+    const uint16_t* x;       // [T][h]
+    const uint16_t* W1t;     // [M][2s][h], gate rows then up rows
+    const uint16_t* W2t;     // [M][h][s]
+    int32_t T, h, s, M, k;
+    const int32_t* idx;      // [T][k]
+    const int32_t* offsets;  // [M + 1]
+    const int32_t* sorted;   // [T k]
+    const float* gate;       // [T][k] or NULL (all ones)
+    // backward
+    const uint16_t* du;      // [T][h]
+    uint16_t* dx;            // [T][h]
+    uint16_t* dW1t;          // [M][2s][h]
+    uint16_t* dW2t;          // [M][h][s]
+    float* dgate;            // [T][k] or NULL
+};
+
+struct FfnPlan {
+    int64_t n;        // T k entries
+    int32_t bm;       // rows of a tile (all of one expert)
+    int64_t tiles;    // bound on the number of tiles
+    size_t off_tiles, off_hidden, off_dgu, off_dxs, off_dgp;
+    size_t workspace_bytes;
+};
+
+void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p);
+void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p);
+hipError_t ffn_launch(const FfnPlan& p, const FfnArgs& a, uint16_t* y, void* workspace, hipStream_t stream);
+hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspace, hipStream_t stream);
+
+// Lists the tiles (shared by both directions).
+hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* tiles, hipStream_t stream);
+
+}  // namespace more

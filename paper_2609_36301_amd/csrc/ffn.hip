@@ -1,0 +1,355 @@
+// The experts' gated feed-forward block for gfx950: for every entry p = t k + j of a selection with
+// expert e = idx[t][j],
+//   A_p = silu(x_t Wg_e^T) * (x_t Wu_e^T)      [s]
+//   y_p = gate_p * (A_p W2_e^T)                [h]
+// with W1t[e] = [Wg_e; Wu_e] and W2t[e] = W2_e.  The entries are taken in the order of Sort + Count, so
+// the rows of an expert are neighbours; they are cut into tiles of at most `bm` rows of one expert.
+//
+// Kernels of one call:
+//   ffn_tiles   lists the tiles
+//   ffn_up      both projections, the activation and the product of one tile and 64 hidden units:
+//               A (bf16, sorted order) into the workspace
+//   ffn_down    A W2^T times the gate, to the entry's row of y
+// Numerics: both contractions take bf16 operands with fp32 accumulation; A is rounded to bf16 once (the
+// matrix cores' operand type), the activation and the gate are applied in fp32.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "ffn.h"
+#include "ffn_device.h"
+
+namespace more {
+
+// ------------------------------------------------------------------------------ tiles
+// A workgroup lists the tiles of 4096 experts, four per thread; it counts the tiles of all earlier
+// experts itself (one launch, no cross-workgroup sum).  The last workgroup adds the tiles of the dropped
+// entries.  Offsets that Sort + Count cannot have written are cut to [0, n], and tiles past the list's
+// end are not written, so that no call reads or writes outside its buffers.
+constexpr int kTileThreads = 1024;
+constexpr int kTileExperts = 4 * kTileThreads;
+
+__device__ __forceinline__ int32_t ffn_cut(int32_t v, int32_t n) { return v < 0 ? 0 : v > n ? n : v; }
+
+__global__ __launch_bounds__(kTileThreads) void ffn_tiles_kernel(const int32_t* __restrict__ offsets, int32_t M,
+                                                                 int32_t n, int32_t log_bm, int64_t bound,
+                                                                 int32_t* __restrict__ list) {
+    FfnTile* tiles = reinterpret_cast<FfnTile*>(reinterpret_cast<char*>(list) + kFfnTileHeader);
+    __shared__ int32_t part[kTileThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int32_t bm1 = (1 << log_bm) - 1;
+    const int32_t e0 = (int32_t)blockIdx.x * kTileExperts;
+    int32_t before = 0;
+#pragma unroll 8
+    for (int32_t e = tid; e < e0; e += kTileThreads) {
+        const int32_t a = ffn_cut(offsets[e], n), b = ffn_cut(offsets[e + 1], n);
+        before += b > a ? (b - a + bm1) >> log_bm : 0;
+    }
+    int32_t start[4], len[4], mine = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int32_t e = e0 + 4 * tid + j;
+        start[j] = len[j] = 0;
+        if (e < M) {
+            start[j] = ffn_cut(offsets[e], n);
+            len[j] = ffn_cut(offsets[e + 1], n) - start[j];
+            len[j] = len[j] > 0 ? len[j] : 0;
+        }
+        mine += (len[j] + bm1) >> log_bm;
+    }
+    // inclusive scan of `mine` over the workgroup, and the sum of `before`
+    int32_t scan = mine, sum = before;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int32_t o = __shfl_up(scan, d, 64);
+        scan += lane >= d ? o : 0;
+        sum += __shfl_xor(sum, d, 64);
+    }
+    __shared__ int32_t part2[kTileThreads / 64];
+    if (lane == 63) part[wave] = scan;
+    if (lane == 0) part2[wave] = sum;
+    __syncthreads();
+    int32_t base = 0, total = 0;
+    for (int w = 0; w < kTileThreads / 64; ++w) {
+        total += part[w] + part2[w];
+        base += part2[w] + (w < wave ? part[w] : 0);
+    }
+    int64_t at = (int64_t)base + scan - mine;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        for (int32_t r = 0; r < len[j]; r += bm1 + 1, ++at)
+            if (at < bound)
+                tiles[at] = FfnTile{e0 + 4 * tid + j, start[j] + r, min(len[j] - r, bm1 + 1), 0};
+    if (blockIdx.x == gridDim.x - 1) {
+        const int32_t valid = ffn_cut(offsets[M], n);
+        const int32_t extra = (n - valid + bm1) >> log_bm;
+        for (int32_t r = tid; r < extra; r += kTileThreads)
+            if ((int64_t)total + r < bound) {
+                const int32_t row = valid + (r << log_bm);
+                tiles[(int64_t)total + r] = FfnTile{-1, row, min(n - row, bm1 + 1), 0};
+            }
+        if (tid == 0) *list = (int32_t)std::min<int64_t>((int64_t)total + extra, bound);
+    }
+}
+
+// ------------------------------------------------------------------------------ up
+// A workgroup computes A of one tile and 64 hidden units: the 64 gate rows and 64 up rows of W1t are the
+// M side of the matrix product, the tile's token rows the N side.  A wave holds WS hidden units (both
+// projections) times WN tokens, so the activation meets both its factors in the same lane.
+template <int BM>
+struct UpShape {
+    static constexpr int kWavesS = BM >= 64 ? 2 : 4;  // waves along the hidden units
+    static constexpr int kS = 64 / kWavesS / 16;      // 16-unit tiles per wave
+    static constexpr int kN = BM / (4 / kWavesS) / 16;
+    static constexpr int kStages = BM >= 128 ? 2 : 3;
+    static constexpr int kStageBytes = (128 + BM) * 128;
+    static constexpr int kLoads = 4 + BM / 32;
+};
+
+template <int BM>
+__global__ __launch_bounds__(kFfnThreads, 2) void ffn_up_kernel(FfnArgs a, const void* __restrict__ list,
+                                                             uint16_t* __restrict__ hidden) {
+    using S = UpShape<BM>;
+    __shared__ __attribute__((aligned(1024))) char smem_raw[S::kStages * S::kStageBytes];
+    LdsChar* smem = (LdsChar*)smem_raw;
+    const FfnTile* tiles = ffn_tile_list(list);
+    const int32_t s = a.s, h = a.h;
+    const int32_t n = a.T * a.k;
+    const int32_t cols = (s + 63) / 64;
+    const int wave = ffn_wave(), lane = ffn_lane();
+    const int ws = wave % S::kWavesS, wn = wave / S::kWavesS;
+    const int64_t total = (int64_t)*static_cast<const int32_t*>(list) * cols;
+    ffn_for_each(total, [&](int64_t item) {
+        const FfnTile tile = tiles[item / cols];
+        if (tile.expert < 0) return;
+        const int32_t s0 = (int32_t)(item % cols) * 64;
+        RowTileLoader<128> weights;
+        const uint16_t* W = a.W1t + (int64_t)tile.expert * 2 * s * h;
+        weights.init([&](int i) {
+            const int32_t u = min(s0 + (i & 63), s - 1);
+            return W + (int64_t)((i >> 6) * s + u) * h;
+        });
+        RowTileLoader<BM> tokens;
+        tokens.init([&](int i) {
+            const uint32_t p = a.sorted[tile.row0 + min(i, tile.rows - 1)];
+            return a.x + (int64_t)(p < (uint32_t)n ? p / (uint32_t)a.k : 0) * h;
+        });
+        f32x4 g[S::kS][S::kN], u[S::kS][S::kN];
+#pragma unroll
+        for (int i = 0; i < S::kS; ++i)
+#pragma unroll
+            for (int j = 0; j < S::kN; ++j) g[i][j] = u[i][j] = zero_f32x4();
+        ffn_pipeline<S::kStages, S::kLoads>(
+            (h + kFfnBK - 1) / kFfnBK,
+            [&](int step, int slot) {
+                LdsChar* at = smem + slot * S::kStageBytes;
+                weights.load(at, step * kFfnBK, h);
+                tokens.load(at + 128 * 128, step * kFfnBK, h);
+            },
+            [&](int step, int slot) {
+                LdsChar* at = smem + slot * S::kStageBytes;
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) {
+                    bf16x8 b[S::kN];
+#pragma unroll
+                    for (int j = 0; j < S::kN; ++j) b[j] = row_fragment(at + 128 * 128, 16 * (wn * S::kN + j), kk);
+#pragma unroll
+                    for (int i = 0; i < S::kS; ++i) {
+                        const bf16x8 fg = row_fragment(at, 16 * (ws * S::kS + i), kk);
+                        const bf16x8 fu = row_fragment(at, 64 + 16 * (ws * S::kS + i), kk);
+#pragma unroll
+                        for (int j = 0; j < S::kN; ++j) {
+                            g[i][j] = mfma_16x16x32(fg, b[j], g[i][j]);
+                            u[i][j] = mfma_16x16x32(fu, b[j], u[i][j]);
+                        }
+                    }
+                }
+            });
+        // lane l holds token l % 16 and hidden units 4 (l / 16) .. + 3 of each 16 x 16 tile
+#pragma unroll
+        for (int j = 0; j < S::kN; ++j) {
+            const int32_t row = 16 * (wn * S::kN + j) + (lane & 15);
+            if (row >= tile.rows) continue;
+            uint16_t* out = hidden + (int64_t)(tile.row0 + row) * s;
+#pragma unroll
+            for (int i = 0; i < S::kS; ++i) {
+                const int32_t c = s0 + 16 * (ws * S::kS + i) + 4 * (lane >> 4);
+                if (c >= s) continue;
+                float v[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[q] = g[i][j][q] * ffn_sigmoid(g[i][j][q]) * u[i][j][q];
+                *reinterpret_cast<uint2*>(out + c) = pack_bf16x4(v[0], v[1], v[2], v[3]);
+            }
+        }
+    });
+}
+
+// ------------------------------------------------------------------------------ down
+// A workgroup computes y of one tile and `hspan` columns in steps of 128: the rows of W2t are the M
+// side, the tile's rows of A the N side.  The pipeline runs over (column step, contraction step) pairs,
+// so that the short contraction of small experts (one step up to s = 64) does not drain it.
+template <int BM>
+struct DownShape {
+    static constexpr int kWavesM = BM >= 64 ? 2 : 4;
+    static constexpr int kM = 128 / kWavesM / 16;
+    static constexpr int kN = BM / (4 / kWavesM) / 16;
+    static constexpr int kStages = BM >= 128 ? 2 : 3;
+    static constexpr int kStageBytes = (128 + BM) * 128;
+    static constexpr int kLoads = 4 + BM / 32;
+};
+
+template <int BM>
+__global__ __launch_bounds__(kFfnThreads, 2) void ffn_down_kernel(FfnArgs a, const void* __restrict__ list,
+                                                               const uint16_t* __restrict__ hidden, int32_t hspan,
+                                                               uint16_t* __restrict__ y) {
+    using S = DownShape<BM>;
+    __shared__ __attribute__((aligned(1024))) char smem_raw[S::kStages * S::kStageBytes];
+    LdsChar* smem = (LdsChar*)smem_raw;
+    const FfnTile* tiles = ffn_tile_list(list);
+    const int32_t s = a.s, h = a.h;
+    const int32_t n = a.T * a.k;
+    const int32_t spans = (h + hspan - 1) / hspan;
+    const int wave = ffn_wave(), lane = ffn_lane();
+    const int wm = wave % S::kWavesM, wn = wave / S::kWavesM;
+    const int64_t total = (int64_t)*static_cast<const int32_t*>(list) * spans;
+    ffn_for_each(total, [&](int64_t item) {
+        const FfnTile tile = tiles[item / spans];
+        const int32_t h0 = (int32_t)(item % spans) * hspan, h1 = min(h, h0 + hspan);
+        if (tile.expert < 0) {  // dropped entries: zero rows
+            const int32_t pieces = (h1 - h0) / 8;
+            for (int32_t i = threadIdx.x; i < tile.rows * pieces; i += kFfnThreads) {
+                const uint32_t p = a.sorted[tile.row0 + i / pieces];
+                if (p < (uint32_t)n)
+                    *reinterpret_cast<u32x4*>(y + (int64_t)p * h + h0 + 8 * (i % pieces)) = u32x4{0u, 0u, 0u, 0u};
+            }
+            return;
+        }
+        const uint16_t* W = a.W2t + (int64_t)tile.expert * h * s;
+        RowTileLoader<BM> rows;
+        rows.init([&](int i) { return hidden + (int64_t)(tile.row0 + min(i, tile.rows - 1)) * s; });
+        uint32_t place[S::kN];
+        float gate[S::kN];
+#pragma unroll
+        for (int j = 0; j < S::kN; ++j) {
+            const int32_t row = 16 * (wn * S::kN + j) + (lane & 15);
+            place[j] = row < tile.rows ? (uint32_t)a.sorted[tile.row0 + row] : 0xFFFFFFFFu;
+            gate[j] = a.gate && place[j] < (uint32_t)n ? a.gate[place[j]] : 1.0f;
+        }
+        f32x4 acc[S::kM][S::kN];
+#pragma unroll
+        for (int i = 0; i < S::kM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::kN; ++j) acc[i][j] = zero_f32x4();
+        const int32_t ksteps = (s + kFfnBK - 1) / kFfnBK;
+        const int32_t hsteps = (h1 - h0 + 127) / 128;
+        // (column step, contraction step) of the next load and of the next compute
+        int32_t lh = h0, lk = 0, ch = h0, ck = 0;
+        ffn_pipeline<S::kStages, S::kLoads>(
+            ksteps * hsteps,
+            [&](int, int slot) {
+                LdsChar* at = smem + slot * S::kStageBytes;
+                RowTileLoader<128> weights;
+                weights.init([&](int i) { return W + (int64_t)min(lh + i, h - 1) * s; });
+                weights.load(at, lk * kFfnBK, s);
+                rows.load(at + 128 * 128, lk * kFfnBK, s);
+                if (++lk == ksteps) {
+                    lk = 0;
+                    lh += 128;
+                }
+            },
+            [&](int, int slot) {
+                LdsChar* at = smem + slot * S::kStageBytes;
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) {
+                    bf16x8 b[S::kN];
+#pragma unroll
+                    for (int j = 0; j < S::kN; ++j) b[j] = row_fragment(at + 128 * 128, 16 * (wn * S::kN + j), kk);
+#pragma unroll
+                    for (int i = 0; i < S::kM; ++i) {
+                        const bf16x8 f = row_fragment(at, 16 * (wm * S::kM + i), kk);
+#pragma unroll
+                        for (int j = 0; j < S::kN; ++j) acc[i][j] = mfma_16x16x32(f, b[j], acc[i][j]);
+                    }
+                }
+                if (++ck < ksteps) return;
+#pragma unroll
+                for (int j = 0; j < S::kN; ++j) {
+#pragma unroll
+                    for (int i = 0; i < S::kM; ++i) {
+                        const int32_t c = ch + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
+                        const f32x4 v = acc[i][j] * gate[j];
+                        if (place[j] < (uint32_t)n && c < h1)
+                            *reinterpret_cast<uint2*>(y + (int64_t)place[j] * h + c) =
+                                pack_bf16x4(v[0], v[1], v[2], v[3]);
+                        acc[i][j] = zero_f32x4();
+                    }
+                }
+                ck = 0;
+                ch += 128;
+            });
+    });
+}
+
+// ------------------------------------------------------------------------------ host
+namespace {
+
+size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
+constexpr int64_t kMaxBlocks = 1 << 19;
+
+// a multiple of 8 workgroups, at most one per item
+unsigned grid_of(int64_t items) {
+    return (unsigned)(std::min<int64_t>((items + 7) / 8, kMaxBlocks / 8) * 8);
+}
+
+// Rows of a tile: the mean number of rows of an expert decides.
+int32_t tile_rows(int64_t n, int32_t M) {
+    const int64_t mean = n / std::max<int64_t>(1, std::min<int64_t>(n, M));
+    return mean >= 96 ? 128 : mean >= 40 ? 64 : 32;
+}
+
+void tiles_plan(int64_t T, int32_t M, int32_t k, FfnPlan* p) {
+    p->n = T * k;
+    p->bm = tile_rows(p->n, M);
+    p->tiles = p->n / p->bm + std::min<int64_t>(M, p->n) + 1;
+    p->off_tiles = 0;
+}
+
+template <int BM>
+hipError_t forward(const FfnPlan& p, const FfnArgs& a, uint16_t* y, char* ws, hipStream_t stream) {
+    uint16_t* hidden = reinterpret_cast<uint16_t*>(ws + p.off_hidden);
+    ffn_up_kernel<BM><<<grid_of(p.tiles * ((a.s + 63) / 64)), kFfnThreads, 0, stream>>>(
+        a, ws + p.off_tiles, hidden);
+    const int32_t hspan = 512;
+    ffn_down_kernel<BM><<<grid_of(p.tiles * ((a.h + hspan - 1) / hspan)), kFfnThreads, 0,
+                          stream>>>(a, ws + p.off_tiles, hidden, hspan, y);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {
+    tiles_plan(T, M, k, p);
+    p->off_hidden = align256(kFfnTileHeader + (size_t)p->tiles * sizeof(FfnTile));
+    p->workspace_bytes = p->off_hidden + align256((size_t)p->n * s * 2);
+}
+
+hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* tiles, hipStream_t stream) {
+    const unsigned blocks = (unsigned)((a.M + kTileExperts - 1) / kTileExperts);
+    ffn_tiles_kernel<<<blocks, kTileThreads, 0, stream>>>(a.offsets, a.M, (int32_t)p.n, __builtin_ctz(p.bm), p.tiles,
+                                                          static_cast<int32_t*>(tiles));
+    return hipGetLastError();
+}
+
+hipError_t ffn_launch(const FfnPlan& p, const FfnArgs& a, uint16_t* y, void* workspace, hipStream_t stream) {
+    char* ws = static_cast<char*>(workspace);
+    hipError_t e = ffn_tiles_launch(p, a, ws + p.off_tiles, stream);
+    if (e != hipSuccess) return e;
+    switch (p.bm) {
+        case 128: return forward<128>(p, a, y, ws, stream);
+        case 64: return forward<64>(p, a, y, ws, stream);
+        default: return forward<32>(p, a, y, ws, stream);
+    }
+}
+
+}  // namespace more

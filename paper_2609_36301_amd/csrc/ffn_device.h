@@ -1,0 +1,207 @@
+// Device helpers of the experts' feed-forward kernels (gfx950): the tile list, LDS tiles filled by
+// direct-to-LDS loads, their fragments for the 16x16x32 bf16 MFMA, and the work loop.
+//
+// A workgroup has four waves.  An operand tile is one of two kinds, 128 bytes of K per row or column:
+//   row tile     ROWS x 64: row m or n holds 64 consecutive values of the contraction axis
+//   column tile  64 x COLS: row kappa holds COLS consecutive values of the other axis; its fragments are
+//                read with the transposing 8-byte LDS read (ds_read_b64_tr_b16)
+// A direct-to-LDS load writes lane l's 16 bytes at 16 l, so the layout is permuted at the source: the
+// 16-byte piece (row tile) or 32-byte piece (column tile) that lies at a place is XORed with bits of the
+// row, which spreads the 16 rows that a fragment read touches over all banks.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "device_common.h"
+
+namespace more {
+
+constexpr int kFfnThreads = 256;
+constexpr int kFfnBK = 64;  // contraction values per stage
+
+// A tile: rows [row0, row0 + rows) of the sorted entries, all of expert `expert` (-1: dropped entries).
+struct FfnTile {
+    int32_t expert, row0, rows, pad;
+};
+// The tile list: a count, then (256 bytes on) the tiles.
+constexpr size_t kFfnTileHeader = 256;
+__device__ __forceinline__ const FfnTile* ffn_tile_list(const void* tiles) {
+    return reinterpret_cast<const FfnTile*>(static_cast<const char*>(tiles) + kFfnTileHeader);
+}
+
+// Source of the pieces that lie outside a matrix (zero, never written).
+static __device__ __attribute__((aligned(16))) uint16_t ffn_zeros[64];
+
+typedef __attribute__((address_space(3))) char LdsChar;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x4 mfma_16x16x32(bf16x8 a, bf16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// s_waitcnt immediate: at most n vector memory operations outstanding, all LDS operations done.
+__host__ __device__ constexpr int ffn_wait_imm(int n) {
+    return (n & 15) | ((n >> 4) << 14) | (7 << 4);
+}
+// Direct-to-LDS load of 16 bytes per lane: lane l of the wave writes lds + 16 l (lds wave-uniform).
+__device__ __forceinline__ void ffn_dma16(const uint16_t* g, LdsChar* lds) {
+    __builtin_amdgcn_global_load_lds(g, lds, 16, 0, 0);
+}
+// Workgroup barrier that leaves at most VM of the wave's own vector memory operations outstanding.
+template <int VM>
+__device__ __forceinline__ void ffn_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(ffn_wait_imm(VM));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+__device__ __forceinline__ int ffn_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+__device__ __forceinline__ int ffn_lane() { return threadIdx.x & 63; }
+
+// Fills a row tile.  Lane l of a load takes row l / 8 of eight and the piece (l % 8) ^ (l / 8) of its
+// 128 bytes; a wave fills ROWS / 4 rows.
+template <int ROWS>
+struct RowTileLoader {
+    static constexpr int kLoads = ROWS / 32;
+    static constexpr int kBytes = ROWS * 128;
+    const uint16_t* p[kLoads];
+    int piece;
+
+    // row_of(i): the first element of tile row i (any readable row where row i is not wanted)
+    template <typename F>
+    __device__ __forceinline__ void init(F row_of) {
+        const int l = ffn_lane(), w = ffn_wave();
+        piece = ((l & 7) ^ (l >> 3)) * 8;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) p[i] = row_of(w * (ROWS / 4) + 8 * i + (l >> 3)) + piece;
+    }
+    // contraction values [k0, k0 + 64) of K (a multiple of 8); past K: zeros
+    __device__ __forceinline__ void load(LdsChar* lds, int k0, int K) const {
+        const int w = ffn_wave();
+        LdsChar* at = lds + w * (ROWS / 4) * 128;
+        if (k0 + kFfnBK <= K) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) ffn_dma16(p[i] + k0, at + i * 1024);
+        } else {
+            const bool in = k0 + piece < K;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) ffn_dma16(in ? p[i] + k0 : ffn_zeros, at + i * 1024);
+        }
+    }
+};
+// Fragment of 16 rows and contraction values 32 kk .. 32 kk + 31: lane l gets row l % 16, values
+// 8 (l / 16) .. + 7.
+__device__ __forceinline__ bf16x8 row_fragment(const LdsChar* lds, int row0, int kk) {
+    const int l = ffn_lane();
+    const int row = row0 + (l & 15);
+    const int piece = (4 * kk + (l >> 4)) ^ (row & 7);
+    return __builtin_bit_cast(
+        bf16x8, *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(lds + row * 128 + piece * 16));
+}
+
+// The 32-byte piece of a column tile's row kappa that holds columns 16 q .. 16 q + 15 lies at
+// q ^ column_swizzle(kappa): a transposing read takes rows 0-3, 8-11, 16-19 and 24-27 (or four on) of
+// 32, and these then meet every 32 bytes of the 256-byte bank row twice.
+template <int COLS>
+__device__ __forceinline__ int column_swizzle(int kappa) {
+    static_assert(COLS == 64 || COLS == 128, "128- or 256-byte rows");
+    return COLS == 128 ? ((kappa & 3) << 1) | ((kappa >> 3) & 1)
+                       : ((kappa >> 1) & 1) | (((kappa >> 3) & 1) << 1);
+}
+
+// Fills a column tile: a load takes 512 / COLS rows, a wave 16 rows.
+template <int COLS>
+struct ColTileLoader {
+    static constexpr int kRows = 512 / COLS;      // rows per load
+    static constexpr int kLoads = 16 / kRows;     // per wave
+    static constexpr int kLanes = 64 / kRows;     // lanes per row
+    static constexpr int kBytes = COLS * 128;
+    int col[kLoads];   // first column of the lane's piece
+
+    __device__ __forceinline__ int row_in_tile(int i) const {
+        return ffn_wave() * 16 + i * kRows + ffn_lane() / kLanes;
+    }
+    __device__ __forceinline__ void init() {
+        const int c = ffn_lane() % kLanes;  // 16-byte place in the row
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            col[i] = 16 * ((c >> 1) ^ column_swizzle<COLS>(row_in_tile(i))) + 8 * (c & 1);
+    }
+    // row_of(i, kappa): the address of column 0 of tile row kappa (the lane's i-th), or NULL (zeros);
+    // columns from `cols` on (a multiple of 8) are zeros
+    template <typename F>
+    __device__ __forceinline__ void load(LdsChar* lds, int cols, F row_of) const {
+        LdsChar* at = lds + ffn_wave() * 16 * (COLS * 2);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const uint16_t* r = row_of(i, row_in_tile(i));
+            ffn_dma16(r && col[i] < cols ? r + col[i] : ffn_zeros, at + i * 1024);
+        }
+    }
+};
+// Fragment of columns col0 .. col0 + 15 (col0 a multiple of 16) and rows 32 kk .. 32 kk + 31: lane l
+// gets column l % 16, rows 8 (l / 16) .. + 7.
+template <int COLS>
+__device__ __forceinline__ bf16x8 col_fragment(LdsChar* lds, int col0, int kk) {
+    const int l = ffn_lane();
+    const int kappa = 32 * kk + 8 * (l >> 4) + ((l & 15) >> 2);
+    LdsChar* a = lds + kappa * (COLS * 2) + (((col0 >> 4) ^ column_swizzle<COLS>(kappa)) << 5) + ((l & 3) << 3);
+    // rows kappa + 4 have the same swizzle
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4*>(a));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        reinterpret_cast<__attribute__((address_space(3))) s16x4*>(a + 4 * (COLS * 2)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Work items [0, total) over the grid (a multiple of 8 workgroups): workgroups are dealt to the 8 XCDs
+// in turn, so item q of XCD d is d ceil(total / 8) + q and neighbouring items share an L2.
+template <typename F>
+__device__ __forceinline__ void ffn_for_each(int64_t total, F body) {
+    const int64_t chunk = (total + 7) / 8;
+    const int64_t base = (int64_t)(blockIdx.x & 7) * chunk;
+    for (int64_t q = blockIdx.x >> 3; q < chunk; q += gridDim.x >> 3) {
+        if (base + q >= total) break;
+        body(base + q);
+    }
+}
+
+// Software pipeline over `steps` stages of an LDS ring of STAGES: load(step, slot) issues LOADS
+// direct-to-LDS loads per wave, compute(step, slot) reads them.  The loads of a step are STAGES - 1
+// steps ahead; the barrier that lets a step's data be read also ends all reads of the slot that is
+// filled next.
+template <int STAGES, int LOADS, typename L, typename C>
+__device__ __forceinline__ void ffn_pipeline(int steps, L load, C compute) {
+    constexpr int kAhead = STAGES - 1;
+    ffn_barrier<0>();  // the previous work item's reads are over
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (i < steps) load(i, i);
+    int slot = 0;
+    for (int step = 0; step < steps; ++step) {
+        if (step + kAhead <= steps) {
+            ffn_barrier<(kAhead - 1) * LOADS>();
+        } else {
+            ffn_barrier<0>();
+        }
+        if (step + kAhead < steps) load(step + kAhead, slot == 0 ? STAGES - 1 : slot - 1);
+        compute(step, slot);
+        slot = slot + 1 == STAGES ? 0 : slot + 1;
+    }
+}
+
+__device__ __forceinline__ f32x4 zero_f32x4() { return f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
+
+// four fp32 -> four bf16 (round to nearest even)
+__device__ __forceinline__ uint2 pack_bf16x4(float a, float b, float c, float d) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(uint2, bf16x4{(__bf16)a, (__bf16)b, (__bf16)c, (__bf16)d});
+}
+
+// 1 / (1 + e^-v): v_exp_f32 and v_rcp_f32 (1 ulp each); e^-v = inf gives 0.
+__device__ __forceinline__ float ffn_sigmoid(float v) {
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * v));
+}
+
+}  // namespace more

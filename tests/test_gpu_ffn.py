@@ -1,0 +1,195 @@
+"""The experts' gated feed-forward block and its backward pass against the 64-bit reference, entry by
+entry within the bound that follows from the kernels' stated roundings (layer_ref.py) (marked `gpu`).
+
+The shapes cover tiles of every size with ragged rows, hidden units and columns (the mean number of rows
+per expert picks the tile), experts without rows, one expert with nearly all rows, dropped entries,
+tokens whose entries are all dropped, an id several times in a token, one token, and the dense block.
+"""
+import numpy as np
+import pytest
+
+import layer_ref as ref
+from gpu_util import announce, require_gpu, to_dev
+
+pytestmark = pytest.mark.gpu
+
+
+def make(T, h, s, M, k, *, drop=0.0, hot=0.0, gated=True, repeat=False, seed=0):
+    """Inputs as bf16 bits / fp32, and the same in float64."""
+    rng = np.random.default_rng(1000 * seed + T + h + s + M + k)
+    idx = rng.integers(0, M, size=(T, k)).astype(np.int32)
+    if not repeat and k <= M:
+        idx = np.argsort(rng.random((T, M)), axis=1)[:, :k].astype(np.int32)
+    idx[rng.random((T, k)) < hot] = M // 2
+    idx[rng.random((T, k)) < drop] = rng.choice([-1, M, M + 7, 2 ** 31 - 1])
+    bits = {"x": rng.standard_normal((T, h)), "W1t": rng.standard_normal((M, 2 * s, h)) * h ** -0.5,
+            "W2t": rng.standard_normal((M, h, s)) * s ** -0.5, "du": rng.standard_normal((T, h)) * 0.1}
+    bits = {name: ref.to_bf16(v) for name, v in bits.items()}
+    gate = rng.random((T, k)).astype(np.float32) if gated else None
+    exact = {name: ref.from_bf16(v) for name, v in bits.items()}
+    exact["gate"] = None if gate is None else gate.astype(np.float64)
+    return idx, bits, gate, exact
+
+
+def on_device(idx, bits, gate, M):
+    offsets, srt = ref.dispatch(idx, M)
+    d = {name: to_dev(v) for name, v in bits.items()}
+    return d, to_dev(idx), to_dev(offsets), to_dev(srt), None if gate is None else to_dev(gate)
+
+
+def check(name, got, want, bound, tag):
+    got = got.astype(np.float64)
+    assert got.shape == want.shape, (tag, name)
+    assert np.all(np.isfinite(got)), (tag, name)
+    off = np.abs(got - want) - bound
+    worst = np.unravel_index(np.argmax(off), off.shape) if off.size else None
+    assert not off.size or off[worst] <= 0, "%s %s at %s: %r against %r, bound %r" % (
+        tag, name, worst, got[worst], want[worst], bound[worst])
+
+
+CASES = {
+    "one_token": dict(T=1, h=512, s=64, M=64, k=8),
+    "one_value": dict(T=1, h=16, s=8, M=1, k=1),
+    "three_tokens": dict(T=3, h=48, s=24, M=5, k=2),
+    "all_experts": dict(T=7, h=128, s=64, M=3, k=3),
+    "more_slots_than_experts": dict(T=5, h=64, s=16, M=2, k=32, repeat=True),
+    "dense": dict(T=64, h=64, s=72, M=1, k=1, gated=False),
+    "dense_long": dict(T=300, h=96, s=200, M=1, k=1, gated=False),
+    "ragged_dropped": dict(T=200, h=528, s=72, M=9, k=6, drop=0.1),
+    "all_dropped": dict(T=20, h=64, s=16, M=4, k=2, drop=1.1),
+    "tile128": dict(T=130, h=256, s=136, M=2, k=2),
+    "tile128_ragged": dict(T=515, h=1040, s=200, M=3, k=2),
+    "tile64": dict(T=100, h=272, s=64, M=4, k=2),
+    "tile64_hot": dict(T=301, h=144, s=40, M=16, k=3, hot=0.6, drop=0.03),
+    "hot_expert": dict(T=400, h=64, s=16, M=300, k=2, hot=0.9),
+    "many_experts": dict(T=33, h=64, s=8, M=5000, k=4, drop=0.2),
+    "repeated_ids": dict(T=50, h=80, s=32, M=6, k=4, repeat=True),
+    "many_rows": dict(T=3000, h=64, s=16, M=5, k=3, drop=0.01),
+}
+
+
+@pytest.mark.parametrize("name", list(CASES))
+def test_forward(name):
+    kw = CASES[name]
+    M = kw["M"]
+    idx, bits, gate, exact = make(**kw)
+    torch = require_gpu()
+    from paper_2609_36301_amd import layer
+    announce("expert_ffn %s %s" % (name, kw))
+    d, i, o, s, g = on_device(idx, bits, gate, M)
+    if g is not None:  # the gates of dropped entries are not read
+        g = torch.where((i >= 0) & (i < M), g, torch.nan)
+    y = layer.expert_ffn(d["x"], d["W1t"], d["W2t"], i, o, s, g)
+    torch.cuda.synchronize()
+    want, bound = ref.ffn(exact["x"], exact["W1t"], exact["W2t"], idx, exact["gate"])
+    check("y", y.float().cpu().numpy(), want, bound, name)
+    dropped = (idx.ravel() < 0) | (idx.ravel() >= M)
+    assert np.all(y.float().cpu().numpy()[dropped] == 0)
+
+
+@pytest.mark.parametrize("name", list(CASES))
+def test_backward(name):
+    kw = CASES[name]
+    M = kw["M"]
+    idx, bits, gate, exact = make(**kw, seed=1)
+    torch = require_gpu()
+    from paper_2609_36301_amd import layer
+    announce("expert_ffn_backward %s %s" % (name, kw))
+    d, i, o, s, g = on_device(idx, bits, gate, M)
+    if g is not None:
+        g = torch.where((i >= 0) & (i < M), g, torch.nan)
+    got = layer.expert_ffn_backward(d["x"], d["W1t"], d["W2t"], i, o, s, g, d["du"])
+    torch.cuda.synchronize()
+    want, bound = ref.ffn_backward(exact["x"], exact["W1t"], exact["W2t"], idx, exact["gate"], exact["du"])
+    for field, v, b in zip(("dx", "dW1t", "dW2t", "dgate"), want, bound):
+        out = getattr(got, field)
+        if out is None:
+            assert gate is None and field == "dgate"
+            continue
+        check(field, out.float().cpu().numpy(), v, b, name)
+
+
+def test_empty_batch():
+    torch = require_gpu()
+    from paper_2609_36301_amd import layer
+    h, s, M, k = 64, 16, 3, 2
+    x = torch.empty((0, h), dtype=torch.bfloat16, device="cuda")
+    W1, W2 = torch.ones((M, 2 * s, h), dtype=torch.bfloat16, device="cuda"), torch.ones((M, h, s), dtype=torch.bfloat16, device="cuda")
+    idx = torch.empty((0, k), dtype=torch.int32, device="cuda")
+    offsets, srt = torch.zeros(M + 1, dtype=torch.int32, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+    gate = torch.empty((0, k), device="cuda")
+    announce("expert_ffn and its backward pass, no tokens")
+    assert layer.expert_ffn(x, W1, W2, idx, offsets, srt, gate).shape == (0, h)
+    g = layer.expert_ffn_backward(x, W1, W2, idx, offsets, srt, gate, x)
+    torch.cuda.synchronize()
+    assert not g.dW1t.any() and not g.dW2t.any()
+
+
+def test_rows_past_32_bits():
+    """y and the weights hold more than 2^31 elements: entries at the end, experts at the end."""
+    torch = require_gpu()
+    from paper_2609_36301_amd import layer
+    T, h, s, M, k = 270000, 4096, 8, 16, 2
+    announce("expert_ffn with %d elements of y" % (T * k * h))
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    normal = lambda *n, scale=1.0: torch.empty(n, dtype=torch.bfloat16, device="cuda").normal_(0, scale, generator=gen)  # noqa: E731
+    x, W1, W2 = normal(T, h), normal(M, 2 * s, h, scale=h ** -0.5), normal(M, h, s, scale=s ** -0.5)
+    idx = torch.randint(0, M, (T, k), dtype=torch.int32, device="cuda", generator=gen)
+    from paper_2609_36301_amd import router
+    y = layer.expert_ffn(x, W1, W2, idx, *router.dispatch_sort(idx, M), None)
+    rows = [0, 1, T - 2, T - 1, 2 ** 31 // (k * h) + 1]
+    want, bound = ref.ffn(x[rows].double().cpu().numpy(), W1.double().cpu().numpy(), W2.double().cpu().numpy(),
+                          idx[rows].cpu().numpy(), None)
+    got = y.view(T, k, h)[rows].reshape(-1, h).float().cpu().numpy()
+    check("y", got, want, bound, "past 32 bits")
+    del x, y, idx
+    M, T = 66000, 3
+    announce("expert_ffn with %d elements of W1t" % (M * 2 * s * h))
+    x, W1, W2 = normal(T, h), normal(M, 2 * s, h, scale=h ** -0.5), normal(M, h, s, scale=s ** -0.5)
+    idx = torch.tensor([[M - 1, 0], [M - 2, 5], [M - 1, M - 3]], dtype=torch.int32, device="cuda")
+    y = layer.expert_ffn(x, W1, W2, idx, *router.dispatch_sort(idx, M), None)
+    used = sorted(set(idx.flatten().tolist()))
+    small = np.searchsorted(used, idx.cpu().numpy()).astype(np.int32)
+    want, bound = ref.ffn(x.double().cpu().numpy(), W1[used].double().cpu().numpy(), W2[used].double().cpu().numpy(),
+                          small, None)
+    check("y", y.float().cpu().numpy(), want, bound, "weights past 32 bits")
+
+
+def test_same_bits_on_every_run_and_another_stream():
+    torch = require_gpu()
+    from paper_2609_36301_amd import layer
+    kw = dict(T=500, h=272, s=72, M=12, k=4, drop=0.05)
+    idx, bits, gate, _ = make(**kw)
+    d, i, o, s, g = on_device(idx, bits, gate, kw["M"])
+    announce("expert_ffn twice, the second time on another stream")
+    run = lambda: (layer.expert_ffn(d["x"], d["W1t"], d["W2t"], i, o, s, g),  # noqa: E731
+                   layer.expert_ffn_backward(d["x"], d["W1t"], d["W2t"], i, o, s, g, d["du"]))
+    y, b = run()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        y2, b2 = run()
+    side.synchronize()
+    for u, v in ((y, y2), (b.dx, b2.dx), (b.dW1t, b2.dW1t), (b.dW2t, b2.dW2t), (b.dgate, b2.dgate)):
+        assert torch.equal(u.view(torch.int16 if u.dtype == torch.bfloat16 else torch.int32),
+                           v.view(torch.int16 if v.dtype == torch.bfloat16 else torch.int32))
+
+
+def test_binding_refuses():
+    torch = require_gpu()
+    from paper_2609_36301_amd import layer
+    idx, bits, gate, _ = make(T=8, h=32, s=8, M=4, k=2)
+    d, i, o, s, g = on_device(idx, bits, gate, 4)
+    call = layer.ExpertFFN(8, 32, 8, 4, 2)
+    with pytest.raises(TypeError, match="x must be torch.bfloat16"):
+        call(d["x"].float(), d["W1t"], d["W2t"], i, o, s, g)
+    with pytest.raises(ValueError, match="W1t must be a contiguous"):
+        call(d["x"], d["W1t"].transpose(1, 2), d["W2t"], i, o, s, g)
+    with pytest.raises(ValueError, match="offsets"):
+        call(d["x"], d["W1t"], d["W2t"], i, o[:-1], s, g)
+    with pytest.raises(ValueError, match="must be on"):
+        call(d["x"], d["W1t"], d["W2t"], i.cpu(), o, s, g)
+    with pytest.raises(TypeError, match="sorted"):
+        call(d["x"], d["W1t"], d["W2t"], i, o, s.long(), g)
+    with pytest.raises(layer._lib.MoreError):
+        layer.ExpertFFN(8, 40, 8, 4, 2)

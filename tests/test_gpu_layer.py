@@ -1,0 +1,152 @@
+"""A layer's training step as a program runs it: norm, router, Sort + Count, experts, block end, and back
+through all of them to clipped gradients; against the same layer in 64 bits with the same selection
+(marked `gpu`).
+
+Tolerance of the whole chain.  Between the loss and a gradient lie at most twelve roundings to bf16 (xn,
+the hidden units, y, u, xn of the next layer, and in the backward pass du, the two hidden gradients, dx,
+the balance-free router's operands, dW), each at most 2^-8 of a value, and no stage here enlarges a
+relative error (unit-variance inputs, norms between the stages): 12 * 2^-8 = 4.7% of the gradient's
+2-norm.  The stages' own tests hold the tight bounds.
+"""
+import numpy as np
+import pytest
+
+from gpu_util import announce, require_gpu
+
+pytestmark = pytest.mark.gpu
+
+T, H, S, M, K, R = 384, 256, 40, 24, 4, 16
+ALPHA, EPS, MAX_NORM = 0.8, 1e-5, 0.5
+
+
+def _inputs(torch, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    normal = lambda *n, scale=1.0, dtype=torch.bfloat16: torch.empty(n, device="cuda").normal_(0, scale, generator=gen).to(dtype)  # noqa: E731
+    f32 = torch.float32
+    return {"r": normal(T, H, scale=2.0, dtype=f32), "R1t": normal(R, H, scale=H ** -0.5), "R2t": normal(M, R, scale=R ** -0.5),
+            "W1t": normal(M, 2 * S, H, scale=H ** -0.5), "W2t": normal(M, H, S, scale=S ** -0.5),
+            "w0": normal(H, scale=0.1, dtype=f32) + 1, "w1": normal(H, scale=0.1, dtype=f32) + 1,
+            "w2": normal(H, scale=0.1, dtype=f32) + 1, "c_r": normal(T, H, dtype=f32), "c_x": normal(T, H)}
+
+
+class Step:
+    """The layer's training step on handles that it keeps."""
+
+    def __init__(self):
+        from paper_2609_36301_amd import layer, router
+        import torch
+        kw = {"resid_dtype": torch.float32, "alpha": ALPHA, "eps": EPS}
+        self.first = layer.BlockNorm(T, H, 0, **kw)
+        self.route = router.LowrankTrainRouter(T, H, R, M, K)
+        self.sort = router.DispatchSorter(T, K, M)
+        self.ffn = layer.ExpertFFN(T, H, S, M, K)
+        self.end = layer.BlockNorm(T, H, K, save_u=True, **kw)
+        self.end_back = layer.BlockNormBackward(T, H, **kw)
+        self.ffn_back = layer.ExpertFFNBackward(T, H, S, M, K)
+        self.route_back = router.LowrankBackward(T, H, R, M, K, balance=False)
+        self.first_back = layer.BlockNormBackward(T, H, **kw)
+        grads = [self.end_back.dw_after, self.end_back.dw_before, self.ffn_back.dW1t, self.ffn_back.dW2t,
+                 self.route_back.out.dR1t, self.route_back.out.dR2t, self.first_back.dw_before]
+        self.clip = layer.GradClipper(grads, MAX_NORM)
+
+    def __call__(self, p):
+        xn = self.first(p["r"], w_before=p["w0"]).xn
+        sel = self.route(xn, p["R1t"], p["R2t"])
+        offsets, srt = self.sort(sel.idx)
+        y = self.ffn(xn, p["W1t"], p["W2t"], sel.idx, offsets, srt, sel.gate)
+        end = self.end(p["r"], y, w_after=p["w1"], w_before=p["w2"])
+        # loss = <r', c_r> + <xn', c_x>
+        eb = self.end_back(end.u, end.r, p["c_r"], p["c_x"], w_after=p["w1"], w_before=p["w2"])
+        fb = self.ffn_back(xn, p["W1t"], p["W2t"], sel.idx, offsets, srt, sel.gate, eb.du)
+        dtop = sel.gate * (fb.dgate - (sel.gate * fb.dgate).sum(1, keepdim=True))  # the gates' softmax
+        rb = self.route_back(xn, p["R1t"], p["R2t"], sel.idx, dtop)
+        nb = self.first_back(None, p["r"], eb.dr, fb.dx, dxn32=rb.dx, w_before=p["w0"])
+        norm, grads = self.clip()
+        return {"r": end.r, "xn": end.xn, "dr": nb.dr, "norm": norm, "idx": sel.idx} | {
+            n: g for n, g in zip(("dw1", "dw2", "dW1t", "dW2t", "dR1t", "dR2t", "dw0"), grads)}
+
+
+def _reference(torch, p, idx):
+    """The same in float64 with autograd, on the CPU, with the given selection."""
+    q = {n: v.double().cpu().requires_grad_(not n.startswith("c_")) for n, v in p.items()}
+    norm = lambda v: v * torch.rsqrt(v.square().mean(1, keepdim=True) + EPS)  # noqa: E731
+    xn = norm(q["r"]) * q["w0"]
+    idx = idx.long().cpu()
+    gate = torch.softmax((xn @ q["R1t"].t() @ q["R2t"].t()).gather(1, idx), dim=1)
+    u = 0
+    for j in range(K):
+        gu = torch.einsum("th,tch->tc", xn, q["W1t"][idx[:, j]])
+        a = torch.nn.functional.silu(gu[:, :S]) * gu[:, S:]
+        u = u + gate[:, j:j + 1] * torch.einsum("ts,ths->th", a, q["W2t"][idx[:, j]])
+    r = ALPHA * q["r"] + q["w1"] * norm(u)
+    xn2 = norm(r) * q["w2"]
+    ((r * q["c_r"]).sum() + (xn2 * q["c_x"]).sum()).backward()
+    grads = {"dw1": q["w1"].grad, "dw2": q["w2"].grad, "dW1t": q["W1t"].grad, "dW2t": q["W2t"].grad,
+             "dR1t": q["R1t"].grad, "dR2t": q["R2t"].grad, "dw0": q["w0"].grad}
+    total = torch.sqrt(sum(g.square().sum() for g in grads.values()))
+    scale = torch.clamp(MAX_NORM / (total + 1e-6), max=1.0)
+    return {"r": r.detach(), "xn": xn2.detach(), "dr": q["r"].grad, "norm": total} | {n: g * scale for n, g in grads.items()}
+
+
+def test_training_step():
+    torch = require_gpu()
+    announce("a layer's training step T=%d h=%d s=%d M=%d k=%d" % (T, H, S, M, K))
+    p = _inputs(torch, 1)
+    out = Step()(p)
+    torch.cuda.synchronize()
+    want = _reference(torch, p, out["idx"])
+    for name, w in want.items():
+        got = out[name].double().cpu()
+        off = float((got - w).norm() / w.norm())
+        print("[layer] %s off by %.2g" % (name, off), flush=True)
+        assert off <= 12 * 2.0 ** -8, name
+    # the scaled gradients have the largest norm allowed (their bf16 members rounded once more)
+    after = torch.sqrt(sum(out[n].double().square().sum() for n in want if n.startswith("d") and n != "dr"))
+    assert abs(float(after) / MAX_NORM - 1) <= 2.0 ** -8
+
+
+def test_training_step_in_a_graph():
+    """Captured once and replayed with other inputs in the same buffers, eager work between the replays."""
+    torch = require_gpu()
+    announce("a layer's training step in a graph")
+    step, eager = Step(), Step()
+    p = _inputs(torch, 2)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(p)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(p)
+    for seed in (2, 3, 4, 2):
+        for n, v in _inputs(torch, seed).items():
+            p[n].copy_(v)
+        graph.replay()
+        want = eager(p)
+        torch.cuda.synchronize()
+        for n, v in want.items():
+            assert torch.equal(out[n], v), (seed, n)
+
+
+def test_serving_one_token():
+    """The layer's forward pass for one token equals that token's row of a batch to bf16 rounding of the
+    hidden units and rows: their sums run in another order (2^-8 of each of three roundings)."""
+    torch = require_gpu()
+    from paper_2609_36301_amd import block_norm, dispatch_sort, expert_ffn, route_lowrank
+    p = _inputs(torch, 5)
+    announce("a layer's forward pass, a batch and its tokens one by one")
+
+    def forward(r):
+        xn = block_norm(r, w_before=p["w0"], eps=EPS).xn
+        sel = route_lowrank(xn, p["R1t"], p["R2t"], K)
+        y = expert_ffn(xn, p["W1t"], p["W2t"], sel.idx, *dispatch_sort(sel.idx, M), sel.gate)
+        return sel.idx, block_norm(r, y, w_after=p["w1"], w_before=p["w2"], alpha=ALPHA, eps=EPS)
+
+    idx, end = forward(p["r"])
+    for t in (0, 17, T - 1):
+        i, one = forward(p["r"][t:t + 1].contiguous())
+        assert torch.equal(i[0], idx[t])
+        for a, b in ((one.r, end.r), (one.xn, end.xn)):
+            off = float((a[0].double() - b[t].double()).norm() / b[t].double().norm())
+            assert off <= 3 * 2.0 ** -8
