@@ -37,6 +37,13 @@ void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t 
 hipError_t ffn_launch(const FfnPlan& p, const FfnArgs& a, uint16_t* y, void* workspace, hipStream_t stream);
 hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspace, hipStream_t stream);
 
+// Columns that a workgroup takes, in steps of `step`, of a product whose contraction is `len` long: a
+// single step where the contraction alone fills the pipeline, or where the groups of rows are too few to
+// fill the chip eight times over with more; else up to 512.
+inline int32_t ffn_span(int32_t len, int32_t step, int64_t groups, int32_t cols) {
+    return len >= 256 || groups * ((cols + 511) / 512) < 2048 ? step : 512;
+}
+
 // Lists the tiles (shared by both directions).
 hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* tiles, hipStream_t stream);
 

@@ -94,21 +94,25 @@ __global__ __launch_bounds__(kTileThreads) void ffn_tiles_kernel(const int32_t* 
 }
 
 // ------------------------------------------------------------------------------ up
-// A workgroup computes A of one tile and 64 hidden units: the 64 gate rows and 64 up rows of W1t are the
-// M side of the matrix product, the tile's token rows the N side.  A wave holds WS hidden units (both
-// projections) times WN tokens, so the activation meets both its factors in the same lane.
+// A workgroup computes A of one tile and kUnits hidden units: the gate rows and up rows of W1t are the
+// M side of the matrix product, the tile's token rows the N side.  A wave holds kS times 16 hidden units
+// (both projections) and kN times 16 tokens, so the activation meets both its factors in the same lane.
 template <int BM>
 struct UpShape {
-    static constexpr int kWavesS = BM >= 64 ? 2 : 4;  // waves along the hidden units
-    static constexpr int kS = 64 / kWavesS / 16;      // 16-unit tiles per wave
-    static constexpr int kN = BM / (4 / kWavesS) / 16;
+    static constexpr int kWaves = BM == 256 ? 8 : 4;
+    static constexpr int kThreads = 64 * kWaves;
+    static constexpr int kWavesS = BM >= 64 ? 2 : 4;      // waves along the hidden units
+    static constexpr int kUnits = BM == 256 ? 128 : 64;
+    static constexpr int kS = kUnits / kWavesS / 16;      // 16-unit tiles per wave
+    static constexpr int kN = BM / (kWaves / kWavesS) / 16;
     static constexpr int kStages = BM >= 128 ? 2 : 3;
-    static constexpr int kStageBytes = (128 + BM) * 128;
-    static constexpr int kLoads = 4 + BM / 32;
+    static constexpr int kRowsAt = 2 * kUnits * 128;      // the token rows' place in a stage
+    static constexpr int kStageBytes = kRowsAt + BM * 128;
+    static constexpr int kLoads = (2 * kUnits + BM) / kWaves / 8;
 };
 
 template <int BM>
-__global__ __launch_bounds__(kFfnThreads, 2) void ffn_up_kernel(FfnArgs a, const void* __restrict__ list,
+__global__ __launch_bounds__(UpShape<BM>::kThreads, 2) void ffn_up_kernel(FfnArgs a, const void* __restrict__ list,
                                                              uint16_t* __restrict__ hidden) {
     using S = UpShape<BM>;
     __shared__ __attribute__((aligned(1024))) char smem_raw[S::kStages * S::kStageBytes];
@@ -116,21 +120,21 @@ __global__ __launch_bounds__(kFfnThreads, 2) void ffn_up_kernel(FfnArgs a, const
     const FfnTile* tiles = ffn_tile_list(list);
     const int32_t s = a.s, h = a.h;
     const int32_t n = a.T * a.k;
-    const int32_t cols = (s + 63) / 64;
+    const int32_t cols = (s + S::kUnits - 1) / S::kUnits;
     const int wave = ffn_wave(), lane = ffn_lane();
     const int ws = wave % S::kWavesS, wn = wave / S::kWavesS;
     const int64_t total = (int64_t)*static_cast<const int32_t*>(list) * cols;
     ffn_for_each(total, [&](int64_t item) {
         const FfnTile tile = tiles[item / cols];
         if (tile.expert < 0) return;
-        const int32_t s0 = (int32_t)(item % cols) * 64;
-        RowTileLoader<128> weights;
+        const int32_t s0 = (int32_t)(item % cols) * S::kUnits;
+        RowTileLoader<2 * S::kUnits, S::kWaves> weights;
         const uint16_t* W = a.W1t + (int64_t)tile.expert * 2 * s * h;
         weights.init([&](int i) {
-            const int32_t u = min(s0 + (i & 63), s - 1);
-            return W + (int64_t)((i >> 6) * s + u) * h;
+            const int32_t u = min(s0 + i % S::kUnits, s - 1);
+            return W + (int64_t)(i / S::kUnits * s + u) * h;
         });
-        RowTileLoader<BM> tokens;
+        RowTileLoader<BM, S::kWaves> tokens;
         tokens.init([&](int i) {
             const uint32_t p = a.sorted[tile.row0 + min(i, tile.rows - 1)];
             return a.x + (int64_t)(p < (uint32_t)n ? p / (uint32_t)a.k : 0) * h;
@@ -140,32 +144,38 @@ __global__ __launch_bounds__(kFfnThreads, 2) void ffn_up_kernel(FfnArgs a, const
         for (int i = 0; i < S::kS; ++i)
 #pragma unroll
             for (int j = 0; j < S::kN; ++j) g[i][j] = u[i][j] = zero_f32x4();
-        ffn_pipeline<S::kStages, S::kLoads>(
-            (h + kFfnBK - 1) / kFfnBK,
+        // the gate rows are one group of M-side fragments, the up rows the other
+        using M = FfnFragments<S::kS>;
+        using N = FfnFragments<S::kN>;
+        ffn_pipeline<S::kStages, S::kLoads, M, N>(
+            (h + kFfnBK - 1) / kFfnBK, 16 * wn * S::kN < tile.rows,
             [&](int step, int slot) {
                 LdsChar* at = smem + slot * S::kStageBytes;
                 weights.load(at, step * kFfnBK, h);
-                tokens.load(at + 128 * 128, step * kFfnBK, h);
+                tokens.load(at + S::kRowsAt, step * kFfnBK, h);
             },
-            [&](int step, int slot) {
-                LdsChar* at = smem + slot * S::kStageBytes;
+            ffn_work(
+                [&](int slot, int kk, int group, M& m) {
 #pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    bf16x8 b[S::kN];
+                    for (int i = 0; i < S::kS; ++i)
+                        m.v[i] = row_fragment(smem + slot * S::kStageBytes,
+                                              group * S::kUnits + 16 * (ws * S::kS + i), kk);
+                },
+                [&](int slot, int kk, N& f) {
 #pragma unroll
-                    for (int j = 0; j < S::kN; ++j) b[j] = row_fragment(at + 128 * 128, 16 * (wn * S::kN + j), kk);
+                    for (int j = 0; j < S::kN; ++j)
+                        f.v[j] = row_fragment(smem + slot * S::kStageBytes + S::kRowsAt, 16 * (wn * S::kN + j), kk);
+                },
+                [&](int group, const M& m, const N& f) {
 #pragma unroll
-                    for (int i = 0; i < S::kS; ++i) {
-                        const bf16x8 fg = row_fragment(at, 16 * (ws * S::kS + i), kk);
-                        const bf16x8 fu = row_fragment(at, 64 + 16 * (ws * S::kS + i), kk);
+                    for (int i = 0; i < S::kS; ++i)
 #pragma unroll
                         for (int j = 0; j < S::kN; ++j) {
-                            g[i][j] = mfma_16x16x32(fg, b[j], g[i][j]);
-                            u[i][j] = mfma_16x16x32(fu, b[j], u[i][j]);
+                            f32x4& c = group ? u[i][j] : g[i][j];
+                            c = mfma_16x16x32(m.v[i], f.v[j], c);
                         }
-                    }
-                }
-            });
+                },
+                [] {}));
         // lane l holds token l % 16 and hidden units 4 (l / 16) .. + 3 of each 16 x 16 tile
 #pragma unroll
         for (int j = 0; j < S::kN; ++j) {
@@ -186,21 +196,25 @@ __global__ __launch_bounds__(kFfnThreads, 2) void ffn_up_kernel(FfnArgs a, const
 }
 
 // ------------------------------------------------------------------------------ down
-// A workgroup computes y of one tile and `hspan` columns in steps of 128: the rows of W2t are the M
+// A workgroup computes y of one tile and `hspan` columns in steps of kCols: the rows of W2t are the M
 // side, the tile's rows of A the N side.  The pipeline runs over (column step, contraction step) pairs,
 // so that the short contraction of small experts (one step up to s = 64) does not drain it.
 template <int BM>
 struct DownShape {
+    static constexpr int kWaves = BM == 256 ? 8 : 4;
+    static constexpr int kThreads = 64 * kWaves;
+    static constexpr int kCols = BM == 256 ? 256 : 128;   // columns of a step
     static constexpr int kWavesM = BM >= 64 ? 2 : 4;
-    static constexpr int kM = 128 / kWavesM / 16;
-    static constexpr int kN = BM / (4 / kWavesM) / 16;
+    static constexpr int kM = kCols / kWavesM / 16;
+    static constexpr int kN = BM / (kWaves / kWavesM) / 16;
     static constexpr int kStages = BM >= 128 ? 2 : 3;
-    static constexpr int kStageBytes = (128 + BM) * 128;
-    static constexpr int kLoads = 4 + BM / 32;
+    static constexpr int kRowsAt = kCols * 128;
+    static constexpr int kStageBytes = kRowsAt + BM * 128;
+    static constexpr int kLoads = (kCols + BM) / kWaves / 8;
 };
 
 template <int BM>
-__global__ __launch_bounds__(kFfnThreads, 2) void ffn_down_kernel(FfnArgs a, const void* __restrict__ list,
+__global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(FfnArgs a, const void* __restrict__ list,
                                                                const uint16_t* __restrict__ hidden, int32_t hspan,
                                                                uint16_t* __restrict__ y) {
     using S = DownShape<BM>;
@@ -218,7 +232,7 @@ __global__ __launch_bounds__(kFfnThreads, 2) void ffn_down_kernel(FfnArgs a, con
         const int32_t h0 = (int32_t)(item % spans) * hspan, h1 = min(h, h0 + hspan);
         if (tile.expert < 0) {  // dropped entries: zero rows
             const int32_t pieces = (h1 - h0) / 8;
-            for (int32_t i = threadIdx.x; i < tile.rows * pieces; i += kFfnThreads) {
+            for (int32_t i = threadIdx.x; i < tile.rows * pieces; i += S::kThreads) {
                 const uint32_t p = a.sorted[tile.row0 + i / pieces];
                 if (p < (uint32_t)n)
                     *reinterpret_cast<u32x4*>(y + (int64_t)p * h + h0 + 8 * (i % pieces)) = u32x4{0u, 0u, 0u, 0u};
@@ -226,7 +240,8 @@ __global__ __launch_bounds__(kFfnThreads, 2) void ffn_down_kernel(FfnArgs a, con
             return;
         }
         const uint16_t* W = a.W2t + (int64_t)tile.expert * h * s;
-        RowTileLoader<BM> rows;
+        RowTileLoader<S::kCols, S::kWaves> weights;
+        RowTileLoader<BM, S::kWaves> rows;
         rows.init([&](int i) { return hidden + (int64_t)(tile.row0 + min(i, tile.rows - 1)) * s; });
         uint32_t place[S::kN];
         float gate[S::kN];
@@ -242,52 +257,63 @@ __global__ __launch_bounds__(kFfnThreads, 2) void ffn_down_kernel(FfnArgs a, con
 #pragma unroll
             for (int j = 0; j < S::kN; ++j) acc[i][j] = zero_f32x4();
         const int32_t ksteps = (s + kFfnBK - 1) / kFfnBK;
-        const int32_t hsteps = (h1 - h0 + 127) / 128;
+        const int32_t hsteps = (h1 - h0 + S::kCols - 1) / S::kCols;
         // (column step, contraction step) of the next load and of the next compute
         int32_t lh = h0, lk = 0, ch = h0, ck = 0;
-        ffn_pipeline<S::kStages, S::kLoads>(
-            ksteps * hsteps,
+        using G = FfnGroups<S::kM>;
+        using M = FfnFragments<G::kSize>;
+        using N = FfnFragments<S::kN>;
+        ffn_pipeline<S::kStages, S::kLoads, M, N>(
+            ksteps * hsteps, 16 * wn * S::kN < tile.rows,
             [&](int, int slot) {
                 LdsChar* at = smem + slot * S::kStageBytes;
-                RowTileLoader<128> weights;
-                weights.init([&](int i) { return W + (int64_t)min(lh + i, h - 1) * s; });
+                if (lk == 0) weights.init([&](int i) { return W + (int64_t)min(lh + i, h - 1) * s; });
                 weights.load(at, lk * kFfnBK, s);
-                rows.load(at + 128 * 128, lk * kFfnBK, s);
+                rows.load(at + S::kRowsAt, lk * kFfnBK, s);
                 if (++lk == ksteps) {
                     lk = 0;
-                    lh += 128;
+                    lh += S::kCols;
                 }
             },
-            [&](int, int slot) {
-                LdsChar* at = smem + slot * S::kStageBytes;
+            ffn_work(
+                [&](int slot, int kk, int group, M& m) {
 #pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    bf16x8 b[S::kN];
+                    for (int i = 0; i < G::kSize; ++i)
+                        if (G::tile(group, i) < S::kM)
+                            m.v[i] = row_fragment(smem + slot * S::kStageBytes, 16 * (wm * S::kM + G::tile(group, i)), kk);
+                },
+                [&](int slot, int kk, N& f) {
 #pragma unroll
-                    for (int j = 0; j < S::kN; ++j) b[j] = row_fragment(at + 128 * 128, 16 * (wn * S::kN + j), kk);
+                    for (int j = 0; j < S::kN; ++j)
+                        f.v[j] = row_fragment(smem + slot * S::kStageBytes + S::kRowsAt, 16 * (wn * S::kN + j), kk);
+                },
+                [&](int group, const M& m, const N& f) {
 #pragma unroll
-                    for (int i = 0; i < S::kM; ++i) {
-                        const bf16x8 f = row_fragment(at, 16 * (wm * S::kM + i), kk);
+                    for (int i = 0; i < G::kSize; ++i)
+                        if (G::tile(group, i) < S::kM)
 #pragma unroll
-                        for (int j = 0; j < S::kN; ++j) acc[i][j] = mfma_16x16x32(f, b[j], acc[i][j]);
+                            for (int j = 0; j < S::kN; ++j) {
+                                f32x4& c = acc[G::tile(group, i)][j];
+                                c = mfma_16x16x32(m.v[i], f.v[j], c);
+                            }
+                },
+                [&] {
+                    if (++ck < ksteps) return;
+#pragma unroll
+                    for (int j = 0; j < S::kN; ++j) {
+#pragma unroll
+                        for (int i = 0; i < S::kM; ++i) {
+                            const int32_t c = ch + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
+                            const f32x4 v = acc[i][j] * gate[j];
+                            if (place[j] < (uint32_t)n && c < h1)
+                                *reinterpret_cast<uint2*>(y + (int64_t)place[j] * h + c) =
+                                    pack_bf16x4(v[0], v[1], v[2], v[3]);
+                            acc[i][j] = zero_f32x4();
+                        }
                     }
-                }
-                if (++ck < ksteps) return;
-#pragma unroll
-                for (int j = 0; j < S::kN; ++j) {
-#pragma unroll
-                    for (int i = 0; i < S::kM; ++i) {
-                        const int32_t c = ch + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
-                        const f32x4 v = acc[i][j] * gate[j];
-                        if (place[j] < (uint32_t)n && c < h1)
-                            *reinterpret_cast<uint2*>(y + (int64_t)place[j] * h + c) =
-                                pack_bf16x4(v[0], v[1], v[2], v[3]);
-                        acc[i][j] = zero_f32x4();
-                    }
-                }
-                ck = 0;
-                ch += 128;
-            });
+                    ck = 0;
+                    ch += S::kCols;
+                }));
     });
 }
 
@@ -303,14 +329,15 @@ unsigned grid_of(int64_t items) {
 }
 
 // Rows of a tile: the mean number of rows of an expert decides.
-int32_t tile_rows(int64_t n, int32_t M) {
+int32_t tile_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
     const int64_t mean = n / std::max<int64_t>(1, std::min<int64_t>(n, M));
+    if (mean >= 512 && h >= 256 && s >= 128) return 256;
     return mean >= 96 ? 128 : mean >= 40 ? 64 : 32;
 }
 
-void tiles_plan(int64_t T, int32_t M, int32_t k, FfnPlan* p) {
+void tiles_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {
     p->n = T * k;
-    p->bm = tile_rows(p->n, M);
+    p->bm = tile_rows(p->n, h, s, M);
     p->tiles = p->n / p->bm + std::min<int64_t>(M, p->n) + 1;
     p->off_tiles = 0;
 }
@@ -318,18 +345,20 @@ void tiles_plan(int64_t T, int32_t M, int32_t k, FfnPlan* p) {
 template <int BM>
 hipError_t forward(const FfnPlan& p, const FfnArgs& a, uint16_t* y, char* ws, hipStream_t stream) {
     uint16_t* hidden = reinterpret_cast<uint16_t*>(ws + p.off_hidden);
-    ffn_up_kernel<BM><<<grid_of(p.tiles * ((a.s + 63) / 64)), kFfnThreads, 0, stream>>>(
+    using U = UpShape<BM>;
+    using D = DownShape<BM>;
+    ffn_up_kernel<BM><<<grid_of(p.tiles * ((a.s + U::kUnits - 1) / U::kUnits)), U::kThreads, 0, stream>>>(
         a, ws + p.off_tiles, hidden);
-    const int32_t hspan = 512;
-    ffn_down_kernel<BM><<<grid_of(p.tiles * ((a.h + hspan - 1) / hspan)), kFfnThreads, 0,
-                          stream>>>(a, ws + p.off_tiles, hidden, hspan, y);
+    const int32_t hspan = ffn_span(a.s, D::kCols, p.tiles, a.h);
+    ffn_down_kernel<BM><<<grid_of(p.tiles * ((a.h + hspan - 1) / hspan)), D::kThreads, 0, stream>>>(
+        a, ws + p.off_tiles, hidden, hspan, y);
     return hipGetLastError();
 }
 
 }  // namespace
 
 void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {
-    tiles_plan(T, M, k, p);
+    tiles_plan(T, h, s, M, k, p);
     p->off_hidden = align256(kFfnTileHeader + (size_t)p->tiles * sizeof(FfnTile));
     p->workspace_bytes = p->off_hidden + align256((size_t)p->n * s * 2);
 }
@@ -346,6 +375,7 @@ hipError_t ffn_launch(const FfnPlan& p, const FfnArgs& a, uint16_t* y, void* wor
     hipError_t e = ffn_tiles_launch(p, a, ws + p.off_tiles, stream);
     if (e != hipSuccess) return e;
     switch (p.bm) {
+        case 256: return forward<256>(p, a, y, ws, stream);
         case 128: return forward<128>(p, a, y, ws, stream);
         case 64: return forward<64>(p, a, y, ws, stream);
         default: return forward<32>(p, a, y, ws, stream);

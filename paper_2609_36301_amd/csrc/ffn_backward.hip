@@ -8,8 +8,8 @@
 //
 // Kernels of one call (entries in the order of Sort + Count, cut into tiles of one expert):
 //   ffn_tiles     lists the tiles
-//   ffn_bwd_up    G, U and dA0 of one tile and 64 hidden units, all three contracted over h in one loop:
-//                 [dG dU] and gate A (bf16, sorted order) and the partial sums of dgate
+//   ffn_bwd_up    G, U and dA0 of one tile and 64 (128) hidden units: [dG dU] and gate A (bf16, sorted
+//                 order) and the partial sums of dgate
 //   ffn_bwd_dx    [dG dU] W1t[e] per entry (fp32, entry order)
 //   ffn_bwd_sum   dx: the k entries of a token added in order; dgate: the partials added in order
 //   ffn_bwd_dw    dW1t and dW2t: contractions over the rows of an expert, one launch each; an expert
@@ -29,22 +29,27 @@
 namespace more {
 
 // ------------------------------------------------------------------------------ up
+// A workgroup computes one tile and kUnits hidden units: first G and U (x rows against the gate and up
+// rows of W1t), then dA0 (du rows against a column tile of W2t) into other accumulators.  In turn rather
+// than side by side: a stage is smaller by the second pair of operands, so twice as many workgroups fit
+// a CU (or a tile twice as large).
 template <int BM>
 struct BwdUpShape {
+    static constexpr int kWaves = BM == 256 ? 8 : 4;
+    static constexpr int kThreads = 64 * kWaves;
     static constexpr int kWavesS = BM >= 64 ? 2 : 4;
-    static constexpr int kS = 64 / kWavesS / 16;
-    static constexpr int kN = BM / (4 / kWavesS) / 16;
+    static constexpr int kUnits = BM == 256 ? 128 : 64;
+    static constexpr int kS = kUnits / kWavesS / 16;
+    static constexpr int kN = BM / (kWaves / kWavesS) / 16;
     static constexpr int kStages = 2;
-    // x rows, du rows, gate and up rows, a column tile of W2t
-    static constexpr int kOffDu = BM * 128, kOffW1 = 2 * BM * 128, kOffW2 = kOffW1 + 128 * 128;
-    static constexpr int kStageBytes = kOffW2 + 64 * 128;
-    static constexpr int kLoads = 2 * (BM / 32) + 4 + 2;
+    static constexpr int kRowsAt = 2 * kUnits * 128;
+    static constexpr int kStageBytes = kRowsAt + BM * 128;
 };
 
 template <int BM>
-__global__ __launch_bounds__(kFfnThreads) void ffn_bwd_up_kernel(FfnArgs a, const void* __restrict__ list,
-                                                              uint16_t* __restrict__ hidden,
-                                                              uint16_t* __restrict__ dgu, float* __restrict__ dgp) {
+__global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel(
+    FfnArgs a, const void* __restrict__ list, uint16_t* __restrict__ hidden, uint16_t* __restrict__ dgu,
+    float* __restrict__ dgp) {
     using S = BwdUpShape<BM>;
     __shared__ __attribute__((aligned(1024))) char smem_raw[S::kStages * S::kStageBytes];
     __shared__ float dsum[S::kWavesS][BM];
@@ -52,72 +57,110 @@ __global__ __launch_bounds__(kFfnThreads) void ffn_bwd_up_kernel(FfnArgs a, cons
     const FfnTile* tiles = ffn_tile_list(list);
     const int32_t s = a.s, h = a.h;
     const int32_t n = a.T * a.k;
-    const int32_t cols = (s + 63) / 64;
+    const int32_t cols = (s + S::kUnits - 1) / S::kUnits;
+    const int32_t hsteps = (h + kFfnBK - 1) / kFfnBK;
     const int wave = ffn_wave(), lane = ffn_lane();
     const int ws = wave % S::kWavesS, wn = wave / S::kWavesS;
     const int64_t total = (int64_t)*static_cast<const int32_t*>(list) * cols;
     ffn_for_each(total, [&](int64_t item) {
         const FfnTile tile = tiles[item / cols];
         if (tile.expert < 0) return;
-        const int32_t col = (int32_t)(item % cols), s0 = col * 64;
-        RowTileLoader<128> weights;
+        const int32_t col = (int32_t)(item % cols), s0 = col * S::kUnits;
+        RowTileLoader<2 * S::kUnits, S::kWaves> weights;
         const uint16_t* W1 = a.W1t + (int64_t)tile.expert * 2 * s * h;
         const uint16_t* W2 = a.W2t + (int64_t)tile.expert * h * s;
         weights.init([&](int i) {
-            const int32_t u = min(s0 + (i & 63), s - 1);
-            return W1 + (int64_t)((i >> 6) * s + u) * h;
+            const int32_t u = min(s0 + i % S::kUnits, s - 1);
+            return W1 + (int64_t)(i / S::kUnits * s + u) * h;
         });
-        ColTileLoader<64> down;
+        ColTileLoader<S::kUnits, S::kWaves> down;
         down.init();
-        RowTileLoader<BM> tokens, grads;
-        auto token_of = [&](int i) {
+        RowTileLoader<BM, S::kWaves> rows;
+        rows.init([&](int i) {
             const uint32_t p = a.sorted[tile.row0 + min(i, tile.rows - 1)];
-            return (int64_t)(p < (uint32_t)n ? p / (uint32_t)a.k : 0) * h;
-        };
-        tokens.init([&](int i) { return a.x + token_of(i); });
-        grads.init([&](int i) { return a.du + token_of(i); });
+            return a.x + (int64_t)(p < (uint32_t)n ? p / (uint32_t)a.k : 0) * h;
+        });
         f32x4 g[S::kS][S::kN], u[S::kS][S::kN], d[S::kS][S::kN];
 #pragma unroll
         for (int i = 0; i < S::kS; ++i)
 #pragma unroll
-            for (int j = 0; j < S::kN; ++j) g[i][j] = u[i][j] = d[i][j] = zero_f32x4();
-        ffn_pipeline<S::kStages, S::kLoads>(
-            (h + kFfnBK - 1) / kFfnBK,
+            for (int j = 0; j < S::kN; ++j) g[i][j] = u[i][j] = zero_f32x4();
+        const bool live = 16 * wn * S::kN < tile.rows;  // (per wave) some of its rows are wanted
+        // the gate rows are one group of M-side fragments, the up rows the other
+        using M = FfnFragments<S::kS>;
+        using N = FfnFragments<S::kN>;
+        ffn_pipeline<S::kStages, 0, M, N>(
+            (h + kFfnBK - 1) / kFfnBK, live,
+            [&](int step, int slot) {
+                LdsChar* at = smem + slot * S::kStageBytes;
+                rows.load(at + S::kRowsAt, step * kFfnBK, h);
+                weights.load(at, step * kFfnBK, h);
+            },
+            ffn_work(
+                [&](int slot, int kk, int group, M& m) {
+#pragma unroll
+                    for (int i = 0; i < S::kS; ++i)
+                        m.v[i] = row_fragment(smem + slot * S::kStageBytes,
+                                              group * S::kUnits + 16 * (ws * S::kS + i), kk);
+                },
+                [&](int slot, int kk, N& f) {
+#pragma unroll
+                    for (int j = 0; j < S::kN; ++j)
+                        f.v[j] = row_fragment(smem + slot * S::kStageBytes + S::kRowsAt, 16 * (wn * S::kN + j), kk);
+                },
+                [&](int group, const M& m, const N& f) {
+#pragma unroll
+                    for (int i = 0; i < S::kS; ++i)
+#pragma unroll
+                        for (int j = 0; j < S::kN; ++j) {
+                            f32x4& c = group ? u[i][j] : g[i][j];
+                            c = mfma_16x16x32(m.v[i], f.v[j], c);
+                        }
+                },
+                [] {}));
+#pragma unroll
+        for (int i = 0; i < S::kS; ++i)
+#pragma unroll
+            for (int j = 0; j < S::kN; ++j) d[i][j] = zero_f32x4();
+        const int64_t to_du = a.du - a.x;  // (elements; the same rows of the other tensor)
+#pragma unroll
+        for (int i = 0; i < rows.kLoads; ++i) rows.p[i] += to_du;
+        using G = FfnGroups<S::kS>;
+        using M2 = FfnFragments<G::kSize>;
+        ffn_pipeline<S::kStages, 0, M2, N>(
+            hsteps, live,
             [&](int step, int slot) {
                 LdsChar* at = smem + slot * S::kStageBytes;
                 const int32_t k0 = step * kFfnBK;
-                tokens.load(at, k0, h);
-                grads.load(at + S::kOffDu, k0, h);
-                weights.load(at + S::kOffW1, k0, h);
-                down.load(at + S::kOffW2, s - s0, [&](int, int kappa) {
-                    return k0 + kappa < h ? W2 + (int64_t)(k0 + kappa) * s + s0 : nullptr;
+                rows.load(at + S::kRowsAt, k0, h);
+                down.load(at, s - s0, [&](int i) {
+                    const int kappa = k0 + down.row(i);
+                    return kappa < h ? W2 + (int64_t)kappa * s + s0 : nullptr;
                 });
             },
-            [&](int, int slot) {
-                LdsChar* at = smem + slot * S::kStageBytes;
+            ffn_work(
+                [&](int slot, int kk, int group, M2& m) {
 #pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    bf16x8 b[S::kN], c[S::kN];
+                    for (int i = 0; i < G::kSize; ++i)
+                        if (G::tile(group, i) < S::kS)
+                            m.v[i] = col_fragment(smem + slot * S::kStageBytes, 16 * (ws * S::kS + G::tile(group, i)), kk);
+                },
+                [&](int slot, int kk, N& f) {
 #pragma unroll
-                    for (int j = 0; j < S::kN; ++j) {
-                        b[j] = row_fragment(at, 16 * (wn * S::kN + j), kk);
-                        c[j] = row_fragment(at + S::kOffDu, 16 * (wn * S::kN + j), kk);
-                    }
+                    for (int j = 0; j < S::kN; ++j)
+                        f.v[j] = row_fragment(smem + slot * S::kStageBytes + S::kRowsAt, 16 * (wn * S::kN + j), kk);
+                },
+                [&](int group, const M2& m, const N& f) {
 #pragma unroll
-                    for (int i = 0; i < S::kS; ++i) {
-                        const int row = 16 * (ws * S::kS + i);
-                        const bf16x8 fg = row_fragment(at + S::kOffW1, row, kk);
-                        const bf16x8 fu = row_fragment(at + S::kOffW1, 64 + row, kk);
-                        const bf16x8 fd = col_fragment<64>(at + S::kOffW2, row, kk);
+                    for (int i = 0; i < G::kSize; ++i)
+                        if (G::tile(group, i) < S::kS)
 #pragma unroll
-                        for (int j = 0; j < S::kN; ++j) {
-                            g[i][j] = mfma_16x16x32(fg, b[j], g[i][j]);
-                            u[i][j] = mfma_16x16x32(fu, b[j], u[i][j]);
-                            d[i][j] = mfma_16x16x32(fd, c[j], d[i][j]);
-                        }
-                    }
-                }
-            });
+                            for (int j = 0; j < S::kN; ++j) {
+                                f32x4& c = d[G::tile(group, i)][j];
+                                c = mfma_16x16x32(m.v[i], f.v[j], c);
+                            }
+                },
+                [] {}));
         // lane l holds token l % 16 and hidden units 4 (l / 16) .. + 3 of each 16 x 16 tile
 #pragma unroll
         for (int j = 0; j < S::kN; ++j) {
@@ -155,7 +198,7 @@ __global__ __launch_bounds__(kFfnThreads) void ffn_bwd_up_kernel(FfnArgs a, cons
         }
         if (a.dgate) {
             ffn_barrier<63>();
-            for (int32_t row = threadIdx.x; row < tile.rows; row += kFfnThreads) {
+            for (int32_t row = threadIdx.x; row < tile.rows; row += S::kThreads) {
                 float v = 0.0f;
 #pragma unroll
                 for (int w = 0; w < S::kWavesS; ++w) v += dsum[w][row];
@@ -169,16 +212,20 @@ __global__ __launch_bounds__(kFfnThreads) void ffn_bwd_up_kernel(FfnArgs a, cons
 // As ffn_down with [dG dU] as the rows and W1t[e] [2s][h] as a column tile (contraction over 2s).
 template <int BM>
 struct BwdDxShape {
+    static constexpr int kWaves = BM == 256 ? 8 : 4;
+    static constexpr int kThreads = 64 * kWaves;
+    static constexpr int kCols = BM == 256 ? 256 : 128;
     static constexpr int kWavesM = BM >= 64 ? 2 : 4;
-    static constexpr int kM = 128 / kWavesM / 16;
-    static constexpr int kN = BM / (4 / kWavesM) / 16;
+    static constexpr int kM = kCols / kWavesM / 16;
+    static constexpr int kN = BM / (kWaves / kWavesM) / 16;
     static constexpr int kStages = BM >= 128 ? 2 : 3;
-    static constexpr int kStageBytes = (128 + BM) * 128;
-    static constexpr int kLoads = 4 + BM / 32;
+    static constexpr int kRowsAt = kCols * 128;
+    static constexpr int kStageBytes = kRowsAt + BM * 128;
+    static constexpr int kLoads = (kCols + BM) / kWaves / 8;
 };
 
 template <int BM>
-__global__ __launch_bounds__(kFfnThreads, 2) void ffn_bwd_dx_kernel(FfnArgs a, const void* __restrict__ list,
+__global__ __launch_bounds__(BwdDxShape<BM>::kThreads, 2) void ffn_bwd_dx_kernel(FfnArgs a, const void* __restrict__ list,
                                                                  const uint16_t* __restrict__ dgu, int32_t hspan,
                                                                  float* __restrict__ dxs) {
     using S = BwdDxShape<BM>;
@@ -196,9 +243,9 @@ __global__ __launch_bounds__(kFfnThreads, 2) void ffn_bwd_dx_kernel(FfnArgs a, c
         if (tile.expert < 0) return;  // dropped entries have no share (ffn_bwd_sum leaves them out)
         const int32_t h0 = (int32_t)(item % spans) * hspan, h1 = min(h, h0 + hspan);
         const uint16_t* W = a.W1t + (int64_t)tile.expert * s2 * h;
-        RowTileLoader<BM> rows;
+        RowTileLoader<BM, S::kWaves> rows;
         rows.init([&](int i) { return dgu + (int64_t)(tile.row0 + min(i, tile.rows - 1)) * s2; });
-        ColTileLoader<128> weights;
+        ColTileLoader<S::kCols, S::kWaves> weights;
         weights.init();
         uint32_t place[S::kN];
 #pragma unroll
@@ -212,50 +259,63 @@ __global__ __launch_bounds__(kFfnThreads, 2) void ffn_bwd_dx_kernel(FfnArgs a, c
 #pragma unroll
             for (int j = 0; j < S::kN; ++j) acc[i][j] = zero_f32x4();
         const int32_t ksteps = (s2 + kFfnBK - 1) / kFfnBK;
-        const int32_t hsteps = (h1 - h0 + 127) / 128;
+        const int32_t hsteps = (h1 - h0 + S::kCols - 1) / S::kCols;
         int32_t lh = h0, lk = 0, ch = h0, ck = 0;
-        ffn_pipeline<S::kStages, S::kLoads>(
-            ksteps * hsteps,
+        using G = FfnGroups<S::kM>;
+        using M = FfnFragments<G::kSize>;
+        using N = FfnFragments<S::kN>;
+        ffn_pipeline<S::kStages, S::kLoads, M, N>(
+            ksteps * hsteps, 16 * wn * S::kN < tile.rows,
             [&](int, int slot) {
                 LdsChar* at = smem + slot * S::kStageBytes;
                 const int32_t k0 = lk * kFfnBK;
-                weights.load(at, h - lh, [&](int, int kappa) {
-                    return k0 + kappa < s2 ? W + (int64_t)(k0 + kappa) * h + lh : nullptr;
+                weights.load(at, h - lh, [&](int i) {
+                    const int kappa = k0 + weights.row(i);
+                    return kappa < s2 ? W + (int64_t)kappa * h + lh : nullptr;
                 });
-                rows.load(at + 128 * 128, k0, s2);
+                rows.load(at + S::kRowsAt, k0, s2);
                 if (++lk == ksteps) {
                     lk = 0;
-                    lh += 128;
+                    lh += S::kCols;
                 }
             },
-            [&](int, int slot) {
-                LdsChar* at = smem + slot * S::kStageBytes;
+            ffn_work(
+                [&](int slot, int kk, int group, M& m) {
 #pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    bf16x8 b[S::kN];
+                    for (int i = 0; i < G::kSize; ++i)
+                        if (G::tile(group, i) < S::kM)
+                            m.v[i] = col_fragment(smem + slot * S::kStageBytes, 16 * (wm * S::kM + G::tile(group, i)), kk);
+                },
+                [&](int slot, int kk, N& f) {
 #pragma unroll
-                    for (int j = 0; j < S::kN; ++j) b[j] = row_fragment(at + 128 * 128, 16 * (wn * S::kN + j), kk);
+                    for (int j = 0; j < S::kN; ++j)
+                        f.v[j] = row_fragment(smem + slot * S::kStageBytes + S::kRowsAt, 16 * (wn * S::kN + j), kk);
+                },
+                [&](int group, const M& m, const N& f) {
 #pragma unroll
-                    for (int i = 0; i < S::kM; ++i) {
-                        const bf16x8 f = col_fragment<128>(at, 16 * (wm * S::kM + i), kk);
+                    for (int i = 0; i < G::kSize; ++i)
+                        if (G::tile(group, i) < S::kM)
 #pragma unroll
-                        for (int j = 0; j < S::kN; ++j) acc[i][j] = mfma_16x16x32(f, b[j], acc[i][j]);
+                            for (int j = 0; j < S::kN; ++j) {
+                                f32x4& c = acc[G::tile(group, i)][j];
+                                c = mfma_16x16x32(m.v[i], f.v[j], c);
+                            }
+                },
+                [&] {
+                    if (++ck < ksteps) return;
+#pragma unroll
+                    for (int j = 0; j < S::kN; ++j) {
+#pragma unroll
+                        for (int i = 0; i < S::kM; ++i) {
+                            const int32_t c = ch + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
+                            if (place[j] < (uint32_t)n && c < h1)
+                                *reinterpret_cast<f32x4*>(dxs + (int64_t)place[j] * h + c) = acc[i][j];
+                            acc[i][j] = zero_f32x4();
+                        }
                     }
-                }
-                if (++ck < ksteps) return;
-#pragma unroll
-                for (int j = 0; j < S::kN; ++j) {
-#pragma unroll
-                    for (int i = 0; i < S::kM; ++i) {
-                        const int32_t c = ch + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
-                        if (place[j] < (uint32_t)n && c < h1)
-                            *reinterpret_cast<f32x4*>(dxs + (int64_t)place[j] * h + c) = acc[i][j];
-                        acc[i][j] = zero_f32x4();
-                    }
-                }
-                ck = 0;
-                ch += 128;
-            });
+                    ck = 0;
+                    ch += S::kCols;
+                }));
     });
 }
 
@@ -302,81 +362,132 @@ __global__ __launch_bounds__(256) void ffn_bwd_sum_kernel(const float* __restric
 // ------------------------------------------------------------------------------ weight gradients
 // out[e] [rows_out][cols_out] = sum over the entries i of expert e of Q[i][row] P[i][col], both operands
 // column tiles (the contraction runs over rows).  dW1t: P = x of the entry's token (cols h), Q = [dG dU]
-// (rows 2s).  dW2t: P = gate A (cols s), Q = du of the entry's token (rows h).
-template <int CT, int RT, bool GATHER_P, bool GATHER_Q>
-__global__ __launch_bounds__(kFfnThreads, 2) void ffn_bwd_dw_kernel(const uint16_t* __restrict__ P,
-                                                                 const uint16_t* __restrict__ Q,
-                                                                 const int32_t* __restrict__ offsets,
-                                                                 const int32_t* __restrict__ sorted, int32_t n,
-                                                                 int32_t k, int32_t M, int32_t rows_out,
-                                                                 int32_t cols_out, uint16_t* __restrict__ out) {
+// (rows 2s).  dW2t: P = gate A (cols s), Q = du of the entry's token (rows h).  A workgroup computes RT
+// rows and `cspan` columns in steps of CT; the pipeline runs over (column step, 64 entries) pairs, so
+// that the few rows of a small expert do not drain it.
+template <int CT, int RT, int WAVES, bool GATHER_P>
+__global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(const uint16_t* __restrict__ P,
+                                                                const uint16_t* __restrict__ Q,
+                                                                const int32_t* __restrict__ offsets,
+                                                                const int32_t* __restrict__ sorted, int32_t n,
+                                                                int32_t k, int32_t M, int32_t rows_out,
+                                                                int32_t cols_out, int32_t cspan,
+                                                                uint16_t* __restrict__ out) {
     constexpr int kStages = 2;
     constexpr int kStageBytes = (CT + RT) * 128;
-    constexpr int kM = CT / 32, kN = RT / 32;  // 16 x 16 tiles per wave (2 x 2 waves)
+    constexpr int kM = CT / 32, kN = RT / (WAVES / 2) / 16;  // 16 x 16 tiles per wave
+    using PLoader = ColTileLoader<CT, WAVES>;
+    using QLoader = ColTileLoader<RT, WAVES>;
+    constexpr int kGathered = PLoader::kGroups;  // rows per lane of either operand
     __shared__ __attribute__((aligned(1024))) char smem_raw[kStages * kStageBytes];
     LdsChar* smem = (LdsChar*)smem_raw;
     const int wave = ffn_wave(), lane = ffn_lane();
     const int wm = wave & 1, wn = wave >> 1;
-    const int32_t ct = (cols_out + CT - 1) / CT, rt = (rows_out + RT - 1) / RT;
-    ffn_for_each((int64_t)M * ct * rt, [&](int64_t item) {
-        const int32_t e = (int32_t)(item / (ct * rt)), q = (int32_t)(item % (ct * rt));
-        const int32_t c0 = (q % ct) * CT, r0 = (q / ct) * RT;
+    const int32_t spans = (cols_out + cspan - 1) / cspan, rt = (rows_out + RT - 1) / RT;
+    // Items in turn over the XCDs: the parts of an expert run on all of them, so that experts with many
+    // entries load them alike.
+    for (int64_t item = blockIdx.x; item < (int64_t)M * spans * rt; item += gridDim.x) {
+        const int32_t e = (int32_t)(item / (spans * rt)), q = (int32_t)(item % (spans * rt));
+        const int32_t c0 = (q % spans) * cspan, c1 = min(cols_out, c0 + cspan), r0 = (q / spans) * RT;
         const int32_t begin = min(max(offsets[e], 0), n), end = min(max(offsets[e + 1], begin), n);
-        ColTileLoader<CT> pl;
-        ColTileLoader<RT> ql;
+        PLoader pl;
+        QLoader ql;
         pl.init();
         ql.init();
-        auto token_of = [&](int32_t i) {
-            const uint32_t p = (uint32_t)sorted[i];
-            return p < (uint32_t)n ? p / (uint32_t)k : 0u;
+        const int32_t ksteps = (end - begin + kFfnBK - 1) / kFfnBK;
+        const int32_t csteps = (c1 - c0 + CT - 1) / CT;
+        // the gathered operand's entries of the next load (read one load ahead)
+        int32_t entry[kGathered];
+        auto fetch = [&](int32_t step) {
+#pragma unroll
+            for (int i = 0; i < kGathered; ++i) {
+                const int32_t at = begin + step * kFfnBK + pl.row(i);
+                entry[i] = at < end ? sorted[at] : -1;
+            }
+        };
+        auto gathered = [&](int i, const uint16_t* base, int32_t stride) -> const uint16_t* {
+            const uint32_t p = (uint32_t)entry[i];
+            return p < (uint32_t)n ? base + (int64_t)(p / (uint32_t)k) * stride : nullptr;
         };
         f32x4 acc[kM][kN];
 #pragma unroll
         for (int i = 0; i < kM; ++i)
 #pragma unroll
             for (int j = 0; j < kN; ++j) acc[i][j] = zero_f32x4();
-        ffn_pipeline<kStages, ColTileLoader<CT>::kLoads + ColTileLoader<RT>::kLoads>(
-            (end - begin + kFfnBK - 1) / kFfnBK,
-            [&](int step, int slot) {
-                LdsChar* at = smem + slot * kStageBytes;
-                const int32_t i0 = begin + step * kFfnBK;
-                pl.load(at, cols_out - c0, [&](int, int kappa) -> const uint16_t* {
-                    if (i0 + kappa >= end) return nullptr;
-                    return P + (int64_t)(GATHER_P ? token_of(i0 + kappa) : i0 + kappa) * cols_out + c0;
-                });
-                ql.load(at + CT * 128, rows_out - r0, [&](int, int kappa) -> const uint16_t* {
-                    if (i0 + kappa >= end) return nullptr;
-                    return Q + (int64_t)(GATHER_Q ? token_of(i0 + kappa) : i0 + kappa) * rows_out + r0;
-                });
-            },
+        int32_t lc = c0, lk = 0, cc = c0, ck = 0;
+        auto store = [&] {
+            uint16_t* o = out + (int64_t)e * rows_out * cols_out;
+#pragma unroll
+            for (int j = 0; j < kN; ++j) {
+                const int32_t r = r0 + 16 * (wn * kN + j) + (lane & 15);
+#pragma unroll
+                for (int i = 0; i < kM; ++i) {
+                    const int32_t c = cc + 16 * (wm * kM + i) + 4 * (lane >> 4);
+                    if (r < rows_out && c < c1)
+                        *reinterpret_cast<uint2*>(o + (int64_t)r * cols_out + c) =
+                            pack_bf16x4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+                    acc[i][j] = zero_f32x4();
+                }
+            }
+            cc += CT;
+        };
+        if (ksteps == 0) {  // no entries: zeros
+            for (int32_t step = 0; step < csteps; ++step) store();
+            continue;
+        }
+        using G = FfnGroups<kM>;
+        using MF = FfnFragments<G::kSize>;
+        using NF = FfnFragments<kN>;
+        fetch(0);
+        ffn_pipeline<kStages, 0, MF, NF>(
+            ksteps * csteps, true,
             [&](int, int slot) {
                 LdsChar* at = smem + slot * kStageBytes;
-#pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    bf16x8 b[kN];
-#pragma unroll
-                    for (int j = 0; j < kN; ++j) b[j] = col_fragment<RT>(at + CT * 128, 16 * (wn * kN + j), kk);
-#pragma unroll
-                    for (int i = 0; i < kM; ++i) {
-                        const bf16x8 f = col_fragment<CT>(at, 16 * (wm * kM + i), kk);
-#pragma unroll
-                        for (int j = 0; j < kN; ++j) acc[i][j] = mfma_16x16x32(f, b[j], acc[i][j]);
-                    }
+                const int32_t i0 = begin + lk * kFfnBK;
+                pl.load(at, c1 - lc, [&](int i) -> const uint16_t* {
+                    if constexpr (GATHER_P) return gathered(i, P + lc, cols_out);
+                    const int32_t row = i0 + pl.row(i);
+                    return row < end ? P + (int64_t)row * cols_out + lc : nullptr;
+                });
+                ql.load(at + CT * 128, rows_out - r0, [&](int i) -> const uint16_t* {
+                    if constexpr (!GATHER_P) return gathered(i, Q + r0, rows_out);
+                    const int32_t row = i0 + ql.row(i);
+                    return row < end ? Q + (int64_t)row * rows_out + r0 : nullptr;
+                });
+                if (++lk == ksteps) {
+                    lk = 0;
+                    lc += CT;
                 }
-            });
-        uint16_t* o = out + (int64_t)e * rows_out * cols_out;
+                if (ksteps > 1) fetch(lk);
+            },
+            ffn_work(
+                [&](int slot, int kk, int group, MF& m) {
 #pragma unroll
-        for (int j = 0; j < kN; ++j) {
-            const int32_t r = r0 + 16 * (wn * kN + j) + (lane & 15);
+                    for (int i = 0; i < G::kSize; ++i)
+                        if (G::tile(group, i) < kM)
+                            m.v[i] = col_fragment(smem + slot * kStageBytes, 16 * (wm * kM + G::tile(group, i)), kk);
+                },
+                [&](int slot, int kk, NF& f) {
 #pragma unroll
-            for (int i = 0; i < kM; ++i) {
-                const int32_t c = c0 + 16 * (wm * kM + i) + 4 * (lane >> 4);
-                if (r < rows_out && c < cols_out)
-                    *reinterpret_cast<uint2*>(o + (int64_t)r * cols_out + c) =
-                        pack_bf16x4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
-            }
-        }
-    });
+                    for (int j = 0; j < kN; ++j)
+                        f.v[j] = col_fragment(smem + slot * kStageBytes + CT * 128, 16 * (wn * kN + j), kk);
+                },
+                [&](int group, const MF& m, const NF& f) {
+#pragma unroll
+                    for (int i = 0; i < G::kSize; ++i)
+                        if (G::tile(group, i) < kM)
+#pragma unroll
+                            for (int j = 0; j < kN; ++j) {
+                                f32x4& c = acc[G::tile(group, i)][j];
+                                c = mfma_16x16x32(m.v[i], f.v[j], c);
+                            }
+                },
+                [&] {
+                    if (++ck < ksteps) return;
+                    ck = 0;
+                    store();
+                }));
+    }
 }
 
 // ------------------------------------------------------------------------------ host
@@ -388,15 +499,33 @@ unsigned grid_of(int64_t items) {
     return (unsigned)(std::min<int64_t>((items + 7) / 8, kMaxBlocks / 8) * 8);
 }
 
+// Workgroups along the hidden units of ffn_bwd_up: a partial sum of dgate each.
+int32_t dgate_parts(const FfnPlan& p, int32_t s) {
+    const int32_t units = p.bm == 256 ? BwdUpShape<256>::kUnits : 64;
+    return (s + units - 1) / units;
+}
+
 template <int BM>
 void rows_launch(const FfnPlan& p, const FfnArgs& a, char* ws, hipStream_t stream) {
     uint16_t* hidden = reinterpret_cast<uint16_t*>(ws + p.off_hidden);
     uint16_t* dgu = reinterpret_cast<uint16_t*>(ws + p.off_dgu);
-    ffn_bwd_up_kernel<BM><<<grid_of(p.tiles * ((a.s + 63) / 64)), kFfnThreads, 0, stream>>>(
+    using U = BwdUpShape<BM>;
+    using D = BwdDxShape<BM>;
+    ffn_bwd_up_kernel<BM><<<grid_of(p.tiles * ((a.s + U::kUnits - 1) / U::kUnits)), U::kThreads, 0, stream>>>(
         a, ws + p.off_tiles, hidden, dgu, reinterpret_cast<float*>(ws + p.off_dgp));
-    const int32_t hspan = 512;
-    ffn_bwd_dx_kernel<BM><<<grid_of(p.tiles * ((a.h + hspan - 1) / hspan)), kFfnThreads, 0, stream>>>(
+    const int32_t hspan = ffn_span(2 * a.s, D::kCols, p.tiles, a.h);
+    ffn_bwd_dx_kernel<BM><<<grid_of(p.tiles * ((a.h + hspan - 1) / hspan)), D::kThreads, 0, stream>>>(
         a, ws + p.off_tiles, dgu, hspan, reinterpret_cast<float*>(ws + p.off_dxs));
+}
+
+template <int CT, int RT, int WAVES, bool GATHER_P>
+void dw_launch(const FfnPlan& p, const FfnArgs& a, const uint16_t* P, const uint16_t* Q, int32_t rows, int32_t cols,
+               uint16_t* out, hipStream_t stream) {
+    const int64_t groups = (int64_t)a.M * ((rows + RT - 1) / RT);
+    const int32_t cspan = ffn_span((int32_t)std::min<int64_t>(p.n / a.M, 1 << 20), CT, groups, cols);
+    const int64_t items = groups * ((cols + cspan - 1) / cspan);
+    ffn_bwd_dw_kernel<CT, RT, WAVES, GATHER_P><<<grid_of(items), 64 * WAVES, 0, stream>>>(
+        P, Q, a.offsets, a.sorted, (int32_t)p.n, a.k, a.M, rows, cols, cspan, out);
 }
 
 }  // namespace
@@ -409,7 +538,7 @@ void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t 
     p->off_dxs = at;
     at += align256((size_t)p->n * h * 4);
     p->off_dgp = at;
-    at += align256((size_t)p->n * ((s + 63) / 64) * 4);
+    at += align256((size_t)p->n * dgate_parts(*p, s) * 4);
     p->workspace_bytes = at;
 }
 
@@ -420,6 +549,7 @@ hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspa
         hipError_t e = ffn_tiles_launch(p, a, ws + p.off_tiles, stream);
         if (e != hipSuccess) return e;
         switch (p.bm) {
+                case 256: rows_launch<256>(p, a, ws, stream); break;
             case 128: rows_launch<128>(p, a, ws, stream); break;
             case 64: rows_launch<64>(p, a, ws, stream); break;
             default: rows_launch<32>(p, a, ws, stream);
@@ -428,17 +558,17 @@ hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspa
         const int64_t gateblocks = a.dgate ? std::min<int64_t>(((int64_t)n + 255) / 256, 1 << 14) : 0;
         ffn_bwd_sum_kernel<<<(unsigned)(colblocks + gateblocks), 256, 0, stream>>>(
             reinterpret_cast<const float*>(ws + p.off_dxs), a.idx, a.T, a.h, a.M, a.k, a.dx, colblocks,
-            reinterpret_cast<const float*>(ws + p.off_dgp), (a.s + 63) / 64, a.sorted, a.dgate);
+            reinterpret_cast<const float*>(ws + p.off_dgp), dgate_parts(p, a.s), a.sorted, a.dgate);
     }
     const uint16_t* hidden = reinterpret_cast<const uint16_t*>(ws + p.off_hidden);
     const uint16_t* dgu = reinterpret_cast<const uint16_t*>(ws + p.off_dgu);
-    auto tiles = [](int32_t v, int32_t t) { return (int64_t)((v + t - 1) / t); };
-    ffn_bwd_dw_kernel<128, 128, true, false>
-        <<<grid_of(a.M * tiles(a.h, 128) * tiles(2 * a.s, 128)), kFfnThreads, 0, stream>>>(
-            a.x, dgu, a.offsets, a.sorted, n, a.k, a.M, 2 * a.s, a.h, a.dW1t);
-    ffn_bwd_dw_kernel<64, 128, false, true>
-        <<<grid_of(a.M * tiles(a.s, 64) * tiles(a.h, 128)), kFfnThreads, 0, stream>>>(
-            hidden, a.du, a.offsets, a.sorted, n, a.k, a.M, a.h, a.s, a.dW2t);
+    if (p.bm == 256) {
+        dw_launch<256, 256, 8, true>(p, a, a.x, dgu, 2 * a.s, a.h, a.dW1t, stream);
+        dw_launch<128, 256, 8, false>(p, a, hidden, a.du, a.h, a.s, a.dW2t, stream);
+    } else {
+        dw_launch<128, 128, 4, true>(p, a, a.x, dgu, 2 * a.s, a.h, a.dW1t, stream);
+        dw_launch<64, 128, 4, false>(p, a, hidden, a.du, a.h, a.s, a.dW2t, stream);
+    }
     return hipGetLastError();
 }
 

@@ -1,10 +1,10 @@
 // Device helpers of the experts' feed-forward kernels (gfx950): the tile list, LDS tiles filled by
 // direct-to-LDS loads, their fragments for the 16x16x32 bf16 MFMA, and the work loop.
 //
-// A workgroup has four waves.  An operand tile is one of two kinds, 128 bytes of K per row or column:
+// A workgroup has four or eight waves.  An operand tile is one of two kinds, 128 bytes of K per row or column:
 //   row tile     ROWS x 64: row m or n holds 64 consecutive values of the contraction axis
-//   column tile  64 x COLS: row kappa holds COLS consecutive values of the other axis; its fragments are
-//                read with the transposing 8-byte LDS read (ds_read_b64_tr_b16)
+//   column tile  64 x COLS: row kappa holds consecutive values of the other axis; its fragments are read
+//                with the transposing 8-byte LDS read (ds_read_b64_tr_b16)
 // A direct-to-LDS load writes lane l's 16 bytes at 16 l, so the layout is permuted at the source: the
 // 16-byte piece (row tile) or 32-byte piece (column tile) that lies at a place is XORed with bits of the
 // row, which spreads the 16 rows that a fragment read touches over all banks.
@@ -17,7 +17,6 @@
 
 namespace more {
 
-constexpr int kFfnThreads = 256;
 constexpr int kFfnBK = 64;  // contraction values per stage
 
 // A tile: rows [row0, row0 + rows) of the sorted entries, all of expert `expert` (-1: dropped entries).
@@ -61,10 +60,11 @@ __device__ __forceinline__ int ffn_wave() { return __builtin_amdgcn_readfirstlan
 __device__ __forceinline__ int ffn_lane() { return threadIdx.x & 63; }
 
 // Fills a row tile.  Lane l of a load takes row l / 8 of eight and the piece (l % 8) ^ (l / 8) of its
-// 128 bytes; a wave fills ROWS / 4 rows.
-template <int ROWS>
+// 128 bytes; a wave fills ROWS / WAVES rows.
+template <int ROWS, int WAVES>
 struct RowTileLoader {
-    static constexpr int kLoads = ROWS / 32;
+    static constexpr int kPerWave = ROWS / WAVES;
+    static constexpr int kLoads = kPerWave / 8;
     static constexpr int kBytes = ROWS * 128;
     const uint16_t* p[kLoads];
     int piece;
@@ -75,12 +75,11 @@ struct RowTileLoader {
         const int l = ffn_lane(), w = ffn_wave();
         piece = ((l & 7) ^ (l >> 3)) * 8;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) p[i] = row_of(w * (ROWS / 4) + 8 * i + (l >> 3)) + piece;
+        for (int i = 0; i < kLoads; ++i) p[i] = row_of(w * kPerWave + 8 * i + (l >> 3)) + piece;
     }
     // contraction values [k0, k0 + 64) of K (a multiple of 8); past K: zeros
     __device__ __forceinline__ void load(LdsChar* lds, int k0, int K) const {
-        const int w = ffn_wave();
-        LdsChar* at = lds + w * (ROWS / 4) * 128;
+        LdsChar* at = lds + ffn_wave() * kPerWave * 128;
         if (k0 + kFfnBK <= K) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) ffn_dma16(p[i] + k0, at + i * 1024);
@@ -101,57 +100,64 @@ __device__ __forceinline__ bf16x8 row_fragment(const LdsChar* lds, int row0, int
         bf16x8, *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(lds + row * 128 + piece * 16));
 }
 
-// The 32-byte piece of a column tile's row kappa that holds columns 16 q .. 16 q + 15 lies at
-// q ^ column_swizzle(kappa): a transposing read takes rows 0-3, 8-11, 16-19 and 24-27 (or four on) of
-// 32, and these then meet every 32 bytes of the 256-byte bank row twice.
-template <int COLS>
-__device__ __forceinline__ int column_swizzle(int kappa) {
-    static_assert(COLS == 64 || COLS == 128, "128- or 256-byte rows");
-    return COLS == 128 ? ((kappa & 3) << 1) | ((kappa >> 3) & 1)
-                       : ((kappa >> 1) & 1) | (((kappa >> 3) & 1) << 1);
-}
+// A column tile lies in panels of 64 columns (64 rows of 128 bytes, 8 KiB).  The 32-byte piece of row
+// kappa that holds columns 16 q .. 16 q + 15 of its panel lies at q ^ column_swizzle(kappa): a
+// transposing read takes rows 0-3, 8-11, 16-19 and 24-27 (or four on) of 32, and these then meet every
+// 32 bytes of the 256-byte bank row twice.  (Panels, not rows of the whole tile: a fragment's address is
+// then one of four per lane plus a constant.)
+constexpr int kFfnPanel = 64 * 128;
+__device__ __forceinline__ int column_swizzle(int kappa) { return ((kappa >> 1) & 1) | (((kappa >> 3) & 1) << 1); }
 
-// Fills a column tile: a load takes 512 / COLS rows, a wave 16 rows.
-template <int COLS>
+// Fills a column tile: a load takes eight rows of a panel, a wave the same rows of every panel.
+template <int COLS, int WAVES>
 struct ColTileLoader {
-    static constexpr int kRows = 512 / COLS;      // rows per load
-    static constexpr int kLoads = 16 / kRows;     // per wave
-    static constexpr int kLanes = 64 / kRows;     // lanes per row
+    static constexpr int kPanels = COLS / 64;
+    static constexpr int kGroups = 8 / WAVES;             // groups of eight rows per wave
+    static constexpr int kLoads = kPanels * kGroups;      // per wave
     static constexpr int kBytes = COLS * 128;
-    int col[kLoads];   // first column of the lane's piece
+    int col[kGroups];   // first column in the panel of the lane's piece
 
-    __device__ __forceinline__ int row_in_tile(int i) const {
-        return ffn_wave() * 16 + i * kRows + ffn_lane() / kLanes;
-    }
+    // the lane's row in the wave's i-th group
+    __device__ __forceinline__ int row(int i) const { return 8 * (ffn_wave() + WAVES * i) + (ffn_lane() >> 3); }
     __device__ __forceinline__ void init() {
-        const int c = ffn_lane() % kLanes;  // 16-byte place in the row
+        const int c = ffn_lane() & 7;  // 16-byte place in the row
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            col[i] = 16 * ((c >> 1) ^ column_swizzle<COLS>(row_in_tile(i))) + 8 * (c & 1);
+        for (int i = 0; i < kGroups; ++i) col[i] = 16 * ((c >> 1) ^ column_swizzle(row(i))) + 8 * (c & 1);
     }
-    // row_of(i, kappa): the address of column 0 of tile row kappa (the lane's i-th), or NULL (zeros);
-    // columns from `cols` on (a multiple of 8) are zeros
+    // row_of(i): the address of column 0 of the lane's row in group i, or NULL (zeros); columns from
+    // `cols` on (a multiple of 8) are zeros
     template <typename F>
     __device__ __forceinline__ void load(LdsChar* lds, int cols, F row_of) const {
-        LdsChar* at = lds + ffn_wave() * 16 * (COLS * 2);
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const uint16_t* r = row_of(i, row_in_tile(i));
-            ffn_dma16(r && col[i] < cols ? r + col[i] : ffn_zeros, at + i * 1024);
+        for (int i = 0; i < kGroups; ++i) {
+            const uint16_t* r = row_of(i);
+            LdsChar* at = lds + (ffn_wave() + WAVES * i) * 1024;
+            if (cols >= COLS) {
+                const uint16_t* from = r ? r + col[i] : ffn_zeros;
+                const int step = r ? 64 : 0;
+#pragma unroll
+                for (int q = 0; q < kPanels; ++q) ffn_dma16(from + q * step, at + q * kFfnPanel);
+            } else {
+#pragma unroll
+                for (int q = 0; q < kPanels; ++q) {
+                    const int c = 64 * q + col[i];
+                    ffn_dma16(r && c < cols ? r + c : ffn_zeros, at + q * kFfnPanel);
+                }
+            }
         }
     }
 };
 // Fragment of columns col0 .. col0 + 15 (col0 a multiple of 16) and rows 32 kk .. 32 kk + 31: lane l
 // gets column l % 16, rows 8 (l / 16) .. + 7.
-template <int COLS>
 __device__ __forceinline__ bf16x8 col_fragment(LdsChar* lds, int col0, int kk) {
     const int l = ffn_lane();
-    const int kappa = 32 * kk + 8 * (l >> 4) + ((l & 15) >> 2);
-    LdsChar* a = lds + kappa * (COLS * 2) + (((col0 >> 4) ^ column_swizzle<COLS>(kappa)) << 5) + ((l & 3) << 3);
+    const int kappa = 8 * (l >> 4) + ((l & 15) >> 2);
+    LdsChar* a = lds + kappa * 128 + ((((col0 >> 4) & 3) ^ column_swizzle(kappa)) << 5) + ((l & 3) << 3) +
+                 (col0 >> 6) * kFfnPanel + kk * 32 * 128;
     // rows kappa + 4 have the same swizzle
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4*>(a));
     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        reinterpret_cast<__attribute__((address_space(3))) s16x4*>(a + 4 * (COLS * 2)));
+        reinterpret_cast<__attribute__((address_space(3))) s16x4*>(a + 4 * 128));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
@@ -167,29 +173,88 @@ __device__ __forceinline__ void ffn_for_each(int64_t total, F body) {
     }
 }
 
-// Software pipeline over `steps` stages of an LDS ring of STAGES: load(step, slot) issues LOADS
-// direct-to-LDS loads per wave, compute(step, slot) reads them.  The loads of a step are STAGES - 1
-// steps ahead; the barrier that lets a step's data be read also ends all reads of the slot that is
-// filled next.
-template <int STAGES, int LOADS, typename L, typename C>
-__device__ __forceinline__ void ffn_pipeline(int steps, L load, C compute) {
-    constexpr int kAhead = STAGES - 1;
+// Software pipeline over `steps` stages of an LDS ring of STAGES; load(step, slot) issues LOADS
+// direct-to-LDS loads per wave.  A stage's product runs in four parts: for each half kk of its contraction
+// values, the M-side fragments in two groups against the N-side fragments.  `w` gives read_m(slot, kk,
+// group, m) and read_n(slot, kk, n), which fill fragments of types M and N, multiply(group, m, n), and
+// done(), which follows the last product of a step.  The fragments of a part are read while the part
+// before is multiplied, across steps too, so that the LDS works while the matrix cores do; the one
+// barrier of a step stands before its last part, where the next stage has to have landed and the present
+// one has been read by every wave, so that its slot can be filled again, STAGES stages ahead.  A wave
+// that has no wanted rows (live = false) only loads.
+template <int STAGES, int LOADS, typename M, typename N, typename L, typename W>
+__device__ __forceinline__ void ffn_pipeline(int steps, bool live, L load, W w) {
     ffn_barrier<0>();  // the previous work item's reads are over
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i)
+    for (int i = 0; i < STAGES; ++i)
         if (i < steps) load(i, i);
-    int slot = 0;
-    for (int step = 0; step < steps; ++step) {
-        if (step + kAhead <= steps) {
-            ffn_barrier<(kAhead - 1) * LOADS>();
+    if (steps >= STAGES) {
+        ffn_barrier<(STAGES - 1) * LOADS>();
+    } else {
+        ffn_barrier<0>();
+    }
+    auto turn = [&](int step, int slot) {  // before the last part of a step that is not the last
+        if (step + STAGES <= steps) {
+            ffn_barrier<(STAGES - 2) * LOADS>();
         } else {
             ffn_barrier<0>();
         }
-        if (step + kAhead < steps) load(step + kAhead, slot == 0 ? STAGES - 1 : slot - 1);
-        compute(step, slot);
-        slot = slot + 1 == STAGES ? 0 : slot + 1;
+        if (step + STAGES < steps) load(step + STAGES, slot);
+    };
+    int slot = 0;
+    if (!live) {
+        for (int step = 0; step + 1 < steps; ++step) {
+            turn(step, slot);
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
+        }
+        return;
+    }
+    M m0, m1;
+    N n0, n1;
+    w.read_n(0, 0, n0);
+    w.read_m(0, 0, 0, m0);
+    for (int step = 0; step < steps; ++step) {
+        const int next = slot + 1 == STAGES ? 0 : slot + 1;
+        w.read_m(slot, 0, 1, m1);
+        w.multiply(0, m0, n0);
+        w.read_n(slot, 1, n1);
+        w.read_m(slot, 1, 0, m0);
+        w.multiply(1, m1, n0);
+        w.read_m(slot, 1, 1, m1);
+        w.multiply(0, m0, n1);
+        if (step + 1 < steps) {
+            turn(step, slot);
+            w.read_n(next, 0, n0);
+            w.read_m(next, 0, 0, m0);
+        }
+        w.multiply(1, m1, n1);
+        w.done();
+        slot = next;
     }
 }
+
+// The four functions of a pipeline as one argument.
+template <typename RM, typename RN, typename P, typename D>
+struct FfnWork {
+    RM read_m;
+    RN read_n;
+    P multiply;
+    D done;
+};
+template <typename RM, typename RN, typename P, typename D>
+__device__ __forceinline__ FfnWork<RM, RN, P, D> ffn_work(RM rm, RN rn, P p, D d) {
+    return FfnWork<RM, RN, P, D>{rm, rn, p, d};
+}
+template <int COUNT>
+struct FfnFragments {
+    bf16x8 v[COUNT];
+};
+// M-side tiles of group 0 (the first half, rounded up) and of the part in all
+template <int TILES>
+struct FfnGroups {
+    static constexpr int kSize = (TILES + 1) / 2;
+    __device__ static constexpr int tile(int group, int i) { return group * kSize + i; }
+};
 
 __device__ __forceinline__ f32x4 zero_f32x4() { return f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
 

@@ -61,6 +61,8 @@ CASES = {
     "tile128_ragged": dict(T=515, h=1040, s=200, M=3, k=2),
     "tile64": dict(T=100, h=272, s=64, M=4, k=2),
     "tile64_hot": dict(T=301, h=144, s=40, M=16, k=3, hot=0.6, drop=0.03),
+    "tile256": dict(T=1100, h=272, s=136, M=2, k=1),
+    "tile256_skewed": dict(T=2500, h=528, s=264, M=4, k=1, hot=0.5, drop=0.02),
     "hot_expert": dict(T=400, h=64, s=16, M=300, k=2, hot=0.9),
     "many_experts": dict(T=33, h=64, s=8, M=5000, k=4, drop=0.2),
     "repeated_ids": dict(T=50, h=80, s=32, M=6, k=4, repeat=True),
