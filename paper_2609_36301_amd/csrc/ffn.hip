@@ -10,6 +10,7 @@
 //   ffn_up      both projections, the activation and the product of one tile and 64 hidden units:
 //               A (bf16, sorted order) into the workspace
 //   ffn_down    A W2^T times the gate, to the entry's row of y
+// With few rows per expert (a decode step) ffn_few_up and ffn_few_down do the same without tiles.
 // Numerics: both contractions take bf16 operands with fp32 accumulation; A is rounded to bf16 once (the
 // matrix cores' operand type), the activation and the gate are applied in fp32.
 #include <hip/hip_runtime.h>
@@ -317,6 +318,180 @@ __global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(Ff
     });
 }
 
+// ------------------------------------------------------------------------------ few rows per expert
+// Where experts have one to a few rows, each of their weights is used for one product with up to 16
+// rows, and the weights' way from memory is all that counts: they go straight into the registers of the
+// 16x16x32 MFMA (16 weight rows against 16 tokens), with no LDS, no tile list and no barrier on the way.
+// Workgroups are laid over the sorted entries; the one whose entry is the first, 17th, ... of its expert
+// takes that and the next 15 entries, the others end at once.
+constexpr int kFewWaves = 8;
+constexpr int kFewRows = 16;
+constexpr int kFewUnits = 16;    // hidden units of an up workgroup
+constexpr int kFewCols = 32;     // columns of y per wave of a down workgroup
+
+// What the wave's lanes know of the sixteen sorted entries from i on: lane l has entry i + l % 16.
+struct FewRows {
+    uint32_t p;      // the lane's entry (t k + j)
+    int32_t expert;  // of entry i; -1: dropped
+    int32_t rows;    // of that expert (1 for a dropped entry); 0: entry i is not the first of its sixteen
+};
+// Two dependent reads (sorted, idx) for an expert that starts at i; offsets is read only where the entry
+// before i is of the same expert.
+__device__ __forceinline__ FewRows few_rows(const FfnArgs& a, int32_t n, int32_t i) {
+    const int32_t at = i + (ffn_lane() & 15);
+    FewRows f;
+    f.p = (uint32_t)a.sorted[min(at, n - 1)];
+    const uint32_t before = (uint32_t)a.sorted[max(i - 1, 0)];
+    const int32_t e = f.p < (uint32_t)n ? a.idx[f.p] : -1;
+    const int32_t eb = before < (uint32_t)n ? a.idx[before] : -1;
+    f.expert = __builtin_amdgcn_readfirstlane(e);
+    const uint32_t same = (uint32_t)__ballot(e == f.expert && at < n) & 0xFFFFu;
+    f.rows = __builtin_ctz(~same);
+    if ((uint32_t)f.expert >= (uint32_t)a.M) {
+        f.expert = -1;
+        f.rows = 1;
+    } else if (i > 0 && eb == f.expert && (i - a.offsets[f.expert]) % kFewRows != 0) {
+        f.rows = 0;
+    }
+    return f;
+}
+
+// 16 bytes at p, or zeros
+__device__ __forceinline__ bf16x8 few_load(const uint16_t* p, bool in) {
+    return load_bf16x8(in ? p : ffn_zeros);
+}
+
+// Waves take pieces of 64 contraction values in turn and their sums are added in wave order.
+__global__ __launch_bounds__(64 * kFewWaves) void ffn_few_up_kernel(FfnArgs a, uint16_t* __restrict__ hidden) {
+    constexpr int kAhead = 4;  // pieces in flight per wave
+    __shared__ f32x4 part[kFewWaves][2][64];
+    const int32_t s = a.s, h = a.h, n = a.T * a.k;
+    const int32_t groups = (s + kFewUnits - 1) / kFewUnits;
+    const int wave = ffn_wave(), lane = ffn_lane();
+    for (int64_t item = blockIdx.x; item < (int64_t)n * groups; item += gridDim.x) {
+        const int32_t i = (int32_t)(item / groups), s0 = (int32_t)(item % groups) * kFewUnits;
+        const FewRows f = few_rows(a, n, i);
+        const int32_t e = f.expert, rows = f.rows;
+        if (rows == 0 || e < 0) continue;
+        const int32_t at = 8 * (lane >> 4);
+        const uint16_t* wg = a.W1t + ((int64_t)e * 2 * s + min(s0 + (lane & 15), s - 1)) * h + at;
+        const uint16_t* wu = wg + (int64_t)s * h;
+        // (the columns of lanes past the rows are not stored)
+        const uint16_t* x = a.x + (int64_t)(f.p < (uint32_t)n ? f.p / (uint32_t)a.k : 0) * h + at;
+        f32x4 g = zero_f32x4(), u = zero_f32x4();
+        for (int32_t k0 = 64 * wave; k0 < h; k0 += 64 * kFewWaves * kAhead) {
+            bf16x8 fg[kAhead][2], fu[kAhead][2], fx[kAhead][2];
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int32_t k = k0 + 64 * kFewWaves * q + 32 * c;
+                    const bool in = k + at < h;
+                    fg[q][c] = few_load(wg + k, in);
+                    fu[q][c] = few_load(wu + k, in);
+                    fx[q][c] = few_load(x + k, in);
+                }
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    g = mfma_16x16x32(fg[q][c], fx[q][c], g);
+                    u = mfma_16x16x32(fu[q][c], fx[q][c], u);
+                }
+        }
+        __syncthreads();  // the item before has been read
+        part[wave][0][lane] = g;
+        part[wave][1][lane] = u;
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int w = 1; w < kFewWaves; ++w) {
+                g += part[w][0][lane];
+                u += part[w][1][lane];
+            }
+            const int32_t c = s0 + 4 * (lane >> 4);
+            if ((lane & 15) < rows && c < s) {
+                float v[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[q] = g[q] * ffn_sigmoid(g[q]) * u[q];
+                *reinterpret_cast<uint2*>(hidden + (int64_t)(i + (lane & 15)) * s + c) =
+                    pack_bf16x4(v[0], v[1], v[2], v[3]);
+            }
+        }
+    }
+}
+
+// A wave computes 32 columns (two groups of weight rows).  SPLIT: the waves share their 32 columns and take
+// pieces of 32 contraction values in turn, their sums added in wave order; else each has columns of its
+// own.  AHEAD pieces are in flight per wave.
+template <bool SPLIT, int AHEAD>
+__global__ __launch_bounds__(64 * kFewWaves) void ffn_few_down_kernel(FfnArgs a, const uint16_t* __restrict__ hidden,
+                                                                   uint16_t* __restrict__ y) {
+    constexpr int kSpan = SPLIT ? kFewCols : kFewWaves * kFewCols;
+    constexpr int kStep = SPLIT ? 32 * kFewWaves : 32;  // from a wave's piece to its next
+    __shared__ f32x4 part[SPLIT ? kFewWaves : 1][2][64];
+    const int32_t s = a.s, h = a.h, n = a.T * a.k;
+    const int32_t spans = (h + kSpan - 1) / kSpan;
+    const int wave = ffn_wave(), lane = ffn_lane();
+    for (int64_t item = blockIdx.x; item < (int64_t)n * spans; item += gridDim.x) {
+        const int32_t i = (int32_t)(item / spans);
+        const int32_t c0 = (int32_t)(item % spans) * kSpan + (SPLIT ? 0 : wave * kFewCols);
+        if (c0 >= h) continue;  // (SPLIT: never)
+        const FewRows f = few_rows(a, n, i);
+        const int32_t e = f.expert, rows = f.rows;
+        if (rows == 0) continue;
+        const uint32_t p = f.p;
+        const bool mine = (lane & 15) < rows && p < (uint32_t)n;
+        if (e < 0) {  // a dropped entry: zeros
+            if (mine && (!SPLIT || wave == 0) && c0 + 8 * (lane >> 4) < h)
+                *reinterpret_cast<u32x4*>(y + (int64_t)p * h + c0 + 8 * (lane >> 4)) = u32x4{0u, 0u, 0u, 0u};
+            continue;
+        }
+        const int32_t at = 8 * (lane >> 4);
+        const uint16_t* w[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+            w[r] = a.W2t + ((int64_t)e * h + min(c0 + 16 * r + (lane & 15), h - 1)) * s + at;
+        const uint16_t* hid = hidden + (int64_t)(i + min(lane & 15, rows - 1)) * s + at;
+        const float gate = a.gate && mine ? a.gate[p] : 1.0f;
+        f32x4 acc[2] = {zero_f32x4(), zero_f32x4()};
+        for (int32_t k0 = SPLIT ? 32 * wave : 0; k0 < s; k0 += kStep * AHEAD) {
+            bf16x8 fw[2][AHEAD], fh[AHEAD];
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q) {
+                const int32_t k = k0 + kStep * q;
+                const bool in = k + at < s;
+                fh[q] = few_load(hid + k, in);
+#pragma unroll
+                for (int r = 0; r < 2; ++r) fw[r][q] = few_load(w[r] + k, in);
+            }
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) acc[r] = mfma_16x16x32(fw[r][q], fh[q], acc[r]);
+        }
+        if constexpr (SPLIT) {
+            __syncthreads();  // the item before has been read
+            part[wave][0][lane] = acc[0];
+            part[wave][1][lane] = acc[1];
+            __syncthreads();
+            if (wave > 0) continue;
+#pragma unroll
+            for (int v = 1; v < kFewWaves; ++v) {
+                acc[0] += part[v][0][lane];
+                acc[1] += part[v][1][lane];
+            }
+        }
+        if (!mine) continue;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int32_t c = c0 + 16 * r + 4 * (lane >> 4);
+            const f32x4 v = acc[r] * gate;
+            if (c < h) *reinterpret_cast<uint2*>(y + (int64_t)p * h + c) = pack_bf16x4(v[0], v[1], v[2], v[3]);
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------ host
 namespace {
 
@@ -327,6 +502,8 @@ constexpr int64_t kMaxBlocks = 1 << 19;
 unsigned grid_of(int64_t items) {
     return (unsigned)(std::min<int64_t>((items + 7) / 8, kMaxBlocks / 8) * 8);
 }
+
+unsigned few_grid(int64_t items) { return (unsigned)std::min<int64_t>(items, 1 << 22); }
 
 // Rows of a tile: the mean number of rows of an expert decides.
 int32_t tile_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
@@ -357,6 +534,17 @@ hipError_t forward(const FfnPlan& p, const FfnArgs& a, uint16_t* y, char* ws, hi
 
 }  // namespace
 
+// Whether the kernels without tiles are taken: while ffn_few_up has at most two workgroups per CU with
+// work (and few that end at once).  They wait for three dependent reads where the tiled kernels wait for
+// the list, but stream at 4 TB/s where those reach 6.  Measured, few against tiles, us: h = 2048, s = 64,
+// one row per expert, 8 entries 10.3 : 19.2, 128 entries 24.3 : 29.8, 512 entries 96 : 81; s = 1024, 8
+// entries 16.3 : 20.4, 16 entries 26.2 : 23.7; dense, s = 1024, 1 row 11.5 : 23.9, 64 rows 30.3 : 29.5.
+static bool few(const FfnPlan& p, int32_t s, int32_t M) {
+    const int64_t groups = (s + kFewUnits - 1) / kFewUnits;
+    const int64_t starts = std::min<int64_t>(p.n, std::min<int64_t>(p.n, M) + p.n / kFewRows);
+    return starts * groups <= 512 && p.n * groups <= 2048;
+}
+
 void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {
     tiles_plan(T, h, s, M, k, p);
     p->off_hidden = align256(kFfnTileHeader + (size_t)p->tiles * sizeof(FfnTile));
@@ -372,6 +560,18 @@ hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* tiles, hip
 
 hipError_t ffn_launch(const FfnPlan& p, const FfnArgs& a, uint16_t* y, void* workspace, hipStream_t stream) {
     char* ws = static_cast<char*>(workspace);
+    if (few(p, a.s, a.M)) {
+        uint16_t* hidden = reinterpret_cast<uint16_t*>(ws + p.off_hidden);
+        ffn_few_up_kernel<<<few_grid(p.n * ((a.s + kFewUnits - 1) / kFewUnits)), 64 * kFewWaves, 0, stream>>>(a, hidden);
+        const bool split = a.s > 128;  // a wave of its own would have the whole contraction to itself
+        const int32_t span = split ? kFewCols : kFewWaves * kFewCols;
+        const unsigned blocks = few_grid(p.n * ((a.h + span - 1) / span));
+        if (split)
+            ffn_few_down_kernel<true, 4><<<blocks, 64 * kFewWaves, 0, stream>>>(a, hidden, y);
+        else
+            ffn_few_down_kernel<false, 2><<<blocks, 64 * kFewWaves, 0, stream>>>(a, hidden, y);
+        return hipGetLastError();
+    }
     hipError_t e = ffn_tiles_launch(p, a, ws + p.off_tiles, stream);
     if (e != hipSuccess) return e;
     switch (p.bm) {

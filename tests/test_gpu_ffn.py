@@ -51,6 +51,9 @@ CASES = {
     "one_token": dict(T=1, h=512, s=64, M=64, k=8),
     "one_value": dict(T=1, h=16, s=8, M=1, k=1),
     "three_tokens": dict(T=3, h=48, s=24, M=5, k=2),
+    "token_of_wide_experts": dict(T=2, h=1040, s=520, M=7, k=3, drop=0.2),
+    "few_rows": dict(T=40, h=528, s=24, M=11, k=2, drop=0.1),
+    "few_rows_dense": dict(T=31, h=256, s=72, M=1, k=1),
     "all_experts": dict(T=7, h=128, s=64, M=3, k=3),
     "more_slots_than_experts": dict(T=5, h=64, s=16, M=2, k=32, repeat=True),
     "dense": dict(T=64, h=64, s=72, M=1, k=1, gated=False),
