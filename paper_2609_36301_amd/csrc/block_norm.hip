@@ -24,14 +24,15 @@ namespace more {
 
 namespace {
 
-constexpr int kNormThreads = 256;
+// A workgroup holds four rows of one wave each, or one row of W waves.
+constexpr int norm_threads(int W) { return W == 1 ? 256 : 64 * W; }
+constexpr int norm_rows(int W) { return W == 1 ? 4 : 1; }
 
 struct V8 {
     float v[8];
 };
 
-__device__ __forceinline__ V8 load8(const uint16_t* p) {
-    const u32x4 b = *reinterpret_cast<const u32x4*>(p);
+__device__ __forceinline__ V8 unpack8(u32x4 b) {
     V8 o;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -40,6 +41,7 @@ __device__ __forceinline__ V8 load8(const uint16_t* p) {
     }
     return o;
 }
+__device__ __forceinline__ V8 load8(const uint16_t* p) { return unpack8(*reinterpret_cast<const u32x4*>(p)); }
 __device__ __forceinline__ V8 load8(const float* p) {
     const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
     return V8{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
@@ -100,9 +102,9 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* red) {
 
 // ------------------------------------------------------------------------------ forward
 template <int W, int CH, bool WIDE>
-__global__ __launch_bounds__(kNormThreads) void block_norm_kernel(NormArgs a) {
-    constexpr int kRows = 4 / W;  // rows per workgroup
-    __shared__ float red[2][4];
+__global__ __launch_bounds__(norm_threads(W)) void block_norm_kernel(NormArgs a) {
+    constexpr int kRows = norm_rows(W);  // rows per workgroup
+    __shared__ float red[2][W];
     const int lane = threadIdx.x & (64 * W - 1);
     const int64_t t = (int64_t)blockIdx.x * kRows + (W == 1 ? threadIdx.x >> 6 : 0);
     if (t >= a.T) return;  // W > 1: uniform over the workgroup
@@ -121,22 +123,25 @@ __global__ __launch_bounds__(kNormThreads) void block_norm_kernel(NormArgs a) {
     }
     if (a.k > 0) {
         const uint16_t* y = a.y + t * a.k * h;
-        for (int32_t j = 0; j < a.k; j += 4) {
-            // four rows are in flight before they are added, in order
-            V8 v[4][CH];
+        constexpr int kAhead = 8;  // rows in flight, added in order
+        for (int32_t j = 0; j < a.k; j += kAhead) {
+            u32x4 v[kAhead][CH];
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < kAhead; ++q)
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
-                    v[q][i] = V8{};
-                    if (in[i] && j + q < a.k) v[q][i] = load8(y + (int64_t)(j + q) * h + c[i]);
+                    v[q][i] = u32x4{0u, 0u, 0u, 0u};
+                    if (in[i] && j + q < a.k)
+                        v[q][i] = *reinterpret_cast<const u32x4*>(y + (int64_t)(j + q) * h + c[i]);
                 }
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < kAhead; ++q)
 #pragma unroll
-                for (int i = 0; i < CH; ++i)
+                for (int i = 0; i < CH; ++i) {
+                    const V8 x = unpack8(v[q][i]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) u[i].v[e] += v[q][i].v[e];
+                    for (int e = 0; e < 8; ++e) u[i].v[e] += x.v[e];
+                }
         }
         float scale = a.gate ? a.gate[t] : 1.0f;
         if (a.norm_after) {
@@ -186,9 +191,9 @@ __global__ __launch_bounds__(kNormThreads) void block_norm_kernel(NormArgs a) {
 // gradients are summed in its registers over the workgroup's rows and written as one partial row per
 // workgroup: parts [workgroup][2][h] (dw_after, dw_before).
 template <int W, int CH, bool WIDE>
-__global__ __launch_bounds__(kNormThreads) void block_norm_backward_kernel(NormArgs a, float* __restrict__ parts) {
-    constexpr int kRows = 4 / W;
-    __shared__ float red[2][4 * 4];
+__global__ __launch_bounds__(norm_threads(W)) void block_norm_backward_kernel(NormArgs a, float* __restrict__ parts) {
+    constexpr int kRows = norm_rows(W);
+    __shared__ float red[2][3 * W];
     __shared__ float fold[W == 1 ? 2 * 4 * 512 * CH : 1];
     const int lane = threadIdx.x & (64 * W - 1);
     const int32_t h = a.h;
@@ -293,7 +298,7 @@ __global__ __launch_bounds__(kNormThreads) void block_norm_backward_kernel(NormA
             store8(fold + (wave * 2 + 1) * 512 * CH + c[i], dwb[i]);
         }
         __syncthreads();
-        for (int32_t i = threadIdx.x; i < 2 * h; i += kNormThreads) {
+        for (int32_t i = threadIdx.x; i < 2 * h; i += norm_threads(W)) {
             const int32_t which = i / h, col = i - which * h;
             float v = 0.0f;
 #pragma unroll
@@ -341,21 +346,21 @@ int32_t backward_blocks(int64_t T, int32_t h) {
 
 template <int W, int CH>
 hipError_t forward(const NormArgs& a, hipStream_t stream) {
-    constexpr int kRows = 4 / W;
+    constexpr int kRows = norm_rows(W);
     const unsigned blocks = (unsigned)(((int64_t)a.T + kRows - 1) / kRows);
     if (a.wide)
-        block_norm_kernel<W, CH, true><<<blocks, kNormThreads, 0, stream>>>(a);
+        block_norm_kernel<W, CH, true><<<blocks, norm_threads(W), 0, stream>>>(a);
     else
-        block_norm_kernel<W, CH, false><<<blocks, kNormThreads, 0, stream>>>(a);
+        block_norm_kernel<W, CH, false><<<blocks, norm_threads(W), 0, stream>>>(a);
     return hipGetLastError();
 }
 
 template <int W, int CH>
 hipError_t backward(const NormArgs& a, float* parts, int32_t blocks, hipStream_t stream) {
     if (a.wide)
-        block_norm_backward_kernel<W, CH, true><<<blocks, kNormThreads, 0, stream>>>(a, parts);
+        block_norm_backward_kernel<W, CH, true><<<blocks, norm_threads(W), 0, stream>>>(a, parts);
     else
-        block_norm_backward_kernel<W, CH, false><<<blocks, kNormThreads, 0, stream>>>(a, parts);
+        block_norm_backward_kernel<W, CH, false><<<blocks, norm_threads(W), 0, stream>>>(a, parts);
     return hipGetLastError();
 }
 
@@ -365,8 +370,8 @@ hipError_t block_norm_launch(const NormArgs& a, hipStream_t stream) {
     if (a.h <= 512) return forward<1, 1>(a, stream);
     if (a.h <= 1024) return forward<1, 2>(a, stream);
     if (a.h <= 2048) return forward<4, 1>(a, stream);
-    if (a.h <= 4096) return forward<4, 2>(a, stream);
-    return forward<4, 4>(a, stream);
+    if (a.h <= 4096) return forward<8, 1>(a, stream);
+    return forward<8, 2>(a, stream);
 }
 
 size_t block_norm_backward_workspace(int64_t T, int32_t h) {
@@ -381,8 +386,8 @@ hipError_t block_norm_backward_launch(const NormArgs& a, void* workspace, hipStr
         if (a.h <= 512) e = backward<1, 1>(a, parts, blocks, stream);
         else if (a.h <= 1024) e = backward<1, 2>(a, parts, blocks, stream);
         else if (a.h <= 2048) e = backward<4, 1>(a, parts, blocks, stream);
-        else if (a.h <= 4096) e = backward<4, 2>(a, parts, blocks, stream);
-        else e = backward<4, 4>(a, parts, blocks, stream);
+        else if (a.h <= 4096) e = backward<8, 1>(a, parts, blocks, stream);
+        else e = backward<8, 2>(a, parts, blocks, stream);
         if (e != hipSuccess) return e;
     }
     if (!a.dw_after && !a.dw_before) return e;

@@ -24,12 +24,11 @@
 namespace more {
 
 // ------------------------------------------------------------------------------ tiles
-// A workgroup lists the tiles of 4096 experts, four per thread; it counts the tiles of all earlier
-// experts itself (one launch, no cross-workgroup sum).  The last workgroup adds the tiles of the dropped
-// entries.  Offsets that Sort + Count cannot have written are cut to [0, n], and tiles past the list's
-// end are not written, so that no call reads or writes outside its buffers.
+// A workgroup lists the tiles of 1024 experts, one per thread; it counts the tiles of all earlier experts
+// itself (one launch, no cross-workgroup sum).  The last workgroup adds the tiles of the dropped entries.
+// Offsets that Sort + Count cannot have written are cut to [0, n], and tiles past the list's end are not
+// written, so that no call reads or writes outside its buffers.
 constexpr int kTileThreads = 1024;
-constexpr int kTileExperts = 4 * kTileThreads;
 
 __device__ __forceinline__ int32_t ffn_cut(int32_t v, int32_t n) { return v < 0 ? 0 : v > n ? n : v; }
 
@@ -37,29 +36,21 @@ __global__ __launch_bounds__(kTileThreads) void ffn_tiles_kernel(const int32_t* 
                                                                  int32_t n, int32_t log_bm, int64_t bound,
                                                                  int32_t* __restrict__ list) {
     FfnTile* tiles = reinterpret_cast<FfnTile*>(reinterpret_cast<char*>(list) + kFfnTileHeader);
-    __shared__ int32_t part[kTileThreads / 64];
+    __shared__ int32_t part[2][kTileThreads / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int32_t bm1 = (1 << log_bm) - 1;
-    const int32_t e0 = (int32_t)blockIdx.x * kTileExperts;
+    const int32_t e0 = (int32_t)blockIdx.x * kTileThreads, e = e0 + tid;
+    const int32_t valid = ffn_cut(offsets[M], n);
+    const int32_t begin = ffn_cut(offsets[min(e, M)], n);
+    const int32_t len = max(ffn_cut(offsets[min(e + 1, M)], n) - begin, 0);
     int32_t before = 0;
 #pragma unroll 8
-    for (int32_t e = tid; e < e0; e += kTileThreads) {
-        const int32_t a = ffn_cut(offsets[e], n), b = ffn_cut(offsets[e + 1], n);
+    for (int32_t q = tid; q < e0; q += kTileThreads) {
+        const int32_t a = ffn_cut(offsets[q], n), b = ffn_cut(offsets[q + 1], n);
         before += b > a ? (b - a + bm1) >> log_bm : 0;
     }
-    int32_t start[4], len[4], mine = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int32_t e = e0 + 4 * tid + j;
-        start[j] = len[j] = 0;
-        if (e < M) {
-            start[j] = ffn_cut(offsets[e], n);
-            len[j] = ffn_cut(offsets[e + 1], n) - start[j];
-            len[j] = len[j] > 0 ? len[j] : 0;
-        }
-        mine += (len[j] + bm1) >> log_bm;
-    }
-    // inclusive scan of `mine` over the workgroup, and the sum of `before`
+    // inclusive scan of the threads' tiles over the workgroup, and the sum of `before`
+    const int32_t mine = (len + bm1) >> log_bm;
     int32_t scan = mine, sum = before;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -67,23 +58,19 @@ __global__ __launch_bounds__(kTileThreads) void ffn_tiles_kernel(const int32_t* 
         scan += lane >= d ? o : 0;
         sum += __shfl_xor(sum, d, 64);
     }
-    __shared__ int32_t part2[kTileThreads / 64];
-    if (lane == 63) part[wave] = scan;
-    if (lane == 0) part2[wave] = sum;
+    if (lane == 63) part[0][wave] = scan;
+    if (lane == 0) part[1][wave] = sum;
     __syncthreads();
     int32_t base = 0, total = 0;
+#pragma unroll
     for (int w = 0; w < kTileThreads / 64; ++w) {
-        total += part[w] + part2[w];
-        base += part2[w] + (w < wave ? part[w] : 0);
+        total += part[0][w] + part[1][w];
+        base += part[1][w] + (w < wave ? part[0][w] : 0);
     }
     int64_t at = (int64_t)base + scan - mine;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        for (int32_t r = 0; r < len[j]; r += bm1 + 1, ++at)
-            if (at < bound)
-                tiles[at] = FfnTile{e0 + 4 * tid + j, start[j] + r, min(len[j] - r, bm1 + 1), 0};
+    for (int32_t r = 0; r < len; r += bm1 + 1, ++at)
+        if (at < bound) tiles[at] = FfnTile{e, begin + r, min(len - r, bm1 + 1), 0};
     if (blockIdx.x == gridDim.x - 1) {
-        const int32_t valid = ffn_cut(offsets[M], n);
         const int32_t extra = (n - valid + bm1) >> log_bm;
         for (int32_t r = tid; r < extra; r += kTileThreads)
             if ((int64_t)total + r < bound) {
@@ -552,7 +539,7 @@ void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPla
 }
 
 hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* tiles, hipStream_t stream) {
-    const unsigned blocks = (unsigned)((a.M + kTileExperts - 1) / kTileExperts);
+    const unsigned blocks = (unsigned)(((int64_t)a.M + kTileThreads - 1) / kTileThreads);
     ffn_tiles_kernel<<<blocks, kTileThreads, 0, stream>>>(a.offsets, a.M, (int32_t)p.n, __builtin_ctz(p.bm), p.tiles,
                                                           static_cast<int32_t*>(tiles));
     return hipGetLastError();

@@ -53,12 +53,12 @@ __global__ __launch_bounds__(kClipThreads) void grad_sumsq_kernel(ClipBatch b, d
     double sum = 0.0;
     for (int64_t item = blockIdx.x; item < b.first[b.n]; item += gridDim.x) {
         const int i = clip_tensor(b, item);
-        const int64_t at = (item - b.first[i]) * kClipChunk;
-        const int32_t len = (int32_t)min((int64_t)kClipChunk, b.numel[i] - at);
+        const int64_t at = (item - b.first[i]) * b.chunk;
+        const int32_t len = (int32_t)min((int64_t)b.chunk, b.numel[i] - at);
         const int32_t vec = b.vec[i] ? (b.bits[i] == 32 ? len / 4 : len / 8) : 0;
         if (b.bits[i] == 32) {
             const float* g = static_cast<const float*>(b.in[i]) + at;
-#pragma unroll 4
+#pragma unroll 8
             for (int32_t q = threadIdx.x; q < vec; q += kClipThreads) {
                 const f32x4 v = reinterpret_cast<const f32x4*>(g)[q];
                 sum += (square(v[0]) + square(v[1])) + (square(v[2]) + square(v[3]));
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(kClipThreads) void grad_sumsq_kernel(ClipBatch b, d
             for (int32_t q = 4 * vec + threadIdx.x; q < len; q += kClipThreads) sum += square(g[q]);
         } else {
             const uint16_t* g = static_cast<const uint16_t*>(b.in[i]) + at;
-#pragma unroll 4
+#pragma unroll 8
             for (int32_t q = threadIdx.x; q < vec; q += kClipThreads) {
                 const u32x4 v = reinterpret_cast<const u32x4*>(g)[q];
 #pragma unroll
@@ -96,29 +96,30 @@ __global__ __launch_bounds__(kClipThreads) void grad_scale_kernel(ClipBatch b, c
     for (int64_t item = blockIdx.x; item < b.first[b.n]; item += gridDim.x) {
         const int i = clip_tensor(b, item);
         if (c == 1.0f && b.in[i] == b.out[i]) continue;
-        const int64_t at = (item - b.first[i]) * kClipChunk;
-        const int32_t len = (int32_t)min((int64_t)kClipChunk, b.numel[i] - at);
+        const int64_t at = (item - b.first[i]) * b.chunk;
+        const int32_t len = (int32_t)min((int64_t)b.chunk, b.numel[i] - at);
         const int32_t vec = b.vec[i] ? (b.bits[i] == 32 ? len / 4 : len / 8) : 0;
         if (b.bits[i] == 32) {
             const float* g = static_cast<const float*>(b.in[i]) + at;
             float* o = static_cast<float*>(b.out[i]) + at;
-#pragma unroll 4
+#pragma unroll 8
             for (int32_t q = threadIdx.x; q < vec; q += kClipThreads)
-                reinterpret_cast<f32x4*>(o)[q] = reinterpret_cast<const f32x4*>(g)[q] * c;
+                __builtin_nontemporal_store(__builtin_nontemporal_load(reinterpret_cast<const f32x4*>(g) + q) * c,
+                                            reinterpret_cast<f32x4*>(o) + q);
             for (int32_t q = 4 * vec + threadIdx.x; q < len; q += kClipThreads) o[q] = g[q] * c;
         } else {
             const uint16_t* g = static_cast<const uint16_t*>(b.in[i]) + at;
             uint16_t* o = static_cast<uint16_t*>(b.out[i]) + at;
-#pragma unroll 4
+#pragma unroll 8
             for (int32_t q = threadIdx.x; q < vec; q += kClipThreads) {
-                const u32x4 v = reinterpret_cast<const u32x4*>(g)[q];
+                const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(g) + q);
                 bf16x8 r;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     r[2 * e] = (__bf16)(__builtin_bit_cast(float, v[e] << 16) * c);
                     r[2 * e + 1] = (__bf16)(__builtin_bit_cast(float, v[e] & 0xFFFF0000u) * c);
                 }
-                reinterpret_cast<u32x4*>(o)[q] = __builtin_bit_cast(u32x4, r);
+                __builtin_nontemporal_store(__builtin_bit_cast(u32x4, r), reinterpret_cast<u32x4*>(o) + q);
             }
             for (int32_t q = 8 * vec + threadIdx.x; q < len; q += kClipThreads)
                 o[q] = __builtin_bit_cast(uint16_t, (__bf16)(bf16_bits_to_f32(g[q]) * c));
@@ -129,20 +130,33 @@ __global__ __launch_bounds__(kClipThreads) void grad_scale_kernel(ClipBatch b, c
 // ------------------------------------------------------------------------------ host
 namespace {
 
-int64_t batch_items(const int64_t* numel, int32_t first, int32_t count) {
+// Elements per work item: so many that kClipBlocks workgroups have about one item each, within 2048 (a
+// 16-byte load per thread) and 16384.
+int32_t clip_chunk(const int64_t* numel, int32_t n) {
+    int64_t total = 0;
+    for (int32_t i = 0; i < n; ++i) total += numel[i];
+    return (int32_t)std::min<int64_t>(16384, std::max<int64_t>(1, total / (2048 * kClipBlocks)) * 2048);
+}
+
+int64_t batch_items(const int64_t* numel, int32_t first, int32_t count, int32_t chunk) {
     int64_t items = 0;
-    for (int32_t i = 0; i < count; ++i) items += (numel[first + i] + kClipChunk - 1) / kClipChunk;
+    for (int32_t i = 0; i < count; ++i) items += (numel[first + i] + chunk - 1) / chunk;
     return items;
 }
 
-int64_t batch_blocks(int64_t items) { return std::max<int64_t>(1, std::min(items, kClipBlocks)); }
+// At most kClipBlocks workgroups with the same number of items each (but for the last ones).
+int64_t batch_blocks(int64_t items) {
+    const int64_t rounds = std::max<int64_t>(1, (items + kClipBlocks - 1) / kClipBlocks);
+    return std::max<int64_t>(1, (items + rounds - 1) / rounds);
+}
 
 }  // namespace
 
 size_t grad_clip_workspace(const int64_t* numel, int32_t n) {
     int64_t parts = 0;
+    const int32_t chunk = clip_chunk(numel, n);
     for (int32_t first = 0; first == 0 || first < n; first += kClipBatch)
-        parts += batch_blocks(batch_items(numel, first, std::min(kClipBatch, n - first)));
+        parts += batch_blocks(batch_items(numel, first, std::min(kClipBatch, n - first), chunk));
     return (size_t)parts * sizeof(double);
 }
 
@@ -150,18 +164,20 @@ hipError_t grad_clip_launch(const void* const* in, void* const* out, const int64
                             float max_norm, float eps, float* norm, void* workspace, hipStream_t stream) {
     double* parts = static_cast<double*>(workspace);
     int64_t nparts = 0;
+    const int32_t chunk = clip_chunk(numel, n);
     for (int pass = 0; pass < 2; ++pass) {
         int64_t at = 0;
         for (int32_t first = 0; first == 0 || first < n; first += kClipBatch) {
             ClipBatch b = {};
             b.n = std::min(kClipBatch, n - first);
+            b.chunk = chunk;
             for (int32_t i = 0; i < b.n; ++i) {
                 b.in[i] = in[first + i];
                 b.out[i] = out[first + i];
                 b.numel[i] = numel[first + i];
                 b.bits[i] = (uint8_t)bits[first + i];
                 b.vec[i] = ((reinterpret_cast<uintptr_t>(b.in[i]) | reinterpret_cast<uintptr_t>(b.out[i])) & 15) == 0;
-                b.first[i + 1] = b.first[i] + (b.numel[i] + kClipChunk - 1) / kClipChunk;
+                b.first[i + 1] = b.first[i] + (b.numel[i] + chunk - 1) / chunk;
             }
             const unsigned blocks = (unsigned)batch_blocks(b.first[b.n]);
             if (pass == 0)

@@ -7,7 +7,7 @@
 
 namespace more {
 
-// Longest row of the norms: four waves with four chunks of eight columns per lane.
+// Longest row of the norms: eight waves with two chunks of eight columns per lane.
 constexpr int32_t kNormMaxH = 8192;
 
 struct NormArgs {
@@ -40,7 +40,6 @@ hipError_t block_norm_backward_launch(const NormArgs& a, void* workspace, hipStr
 
 // Tensors of one launch: the descriptors travel in the kernel's arguments.
 constexpr int kClipBatch = 48;
-constexpr int64_t kClipChunk = 16384;  // elements per work item
 struct ClipBatch {
     const void* in[kClipBatch];
     void* out[kClipBatch];
@@ -49,6 +48,7 @@ struct ClipBatch {
     uint8_t bits[kClipBatch];
     uint8_t vec[kClipBatch];        // in and out are 16-byte aligned
     int32_t n;
+    int32_t chunk;                  // elements per work item
 };
 size_t grad_clip_workspace(const int64_t* numel, int32_t n);
 hipError_t grad_clip_launch(const void* const* in, void* const* out, const int64_t* numel, const int32_t* bits, int32_t n,

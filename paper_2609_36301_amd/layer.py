@@ -24,7 +24,10 @@ from typing import Optional, Sequence
 import torch
 
 from . import _lib
-from .router import _ptr
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
 
 
 def _device(device) -> torch.device:
@@ -46,9 +49,17 @@ def _check(name: str, t, dtype, shape, device):
         raise ValueError("%s must be on %s, got %s" % (name, device, t.device))
 
 
+def _check_all(device, *wanted):
+    """_check of each (name, tensor, dtype, shape)."""
+    for name, t, dtype, shape in wanted:
+        if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.shape == shape and t.device == device
+                and t.is_contiguous()):
+            _check(name, t, dtype, shape, device)
+
+
 def _call(name: str, device: torch.device, *args):
     """The library call `name` on the device's current stream (the library works on the current device)."""
-    stream = ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+    stream = torch.cuda.current_stream(device).cuda_stream
     fn = getattr(_lib.load(), name)
     if torch.cuda.current_device() == device.index:
         st = fn(*args, stream)
@@ -80,14 +91,10 @@ def expert_ffn_backward_workspace_size(T: int, h: int, s: int, M: int, k: int) -
 def _check_ffn(shape, device, x, W1t, W2t, idx, offsets, srt, gate):
     T, h, s, M, k = shape
     bf16, i32 = torch.bfloat16, torch.int32
-    _check("x", x, bf16, (T, h), device)
-    _check("W1t", W1t, bf16, (M, 2 * s, h), device)
-    _check("W2t", W2t, bf16, (M, h, s), device)
-    _check("idx", idx, i32, (T, k), device)
-    _check("offsets", offsets, i32, (M + 1,), device)
-    _check("sorted", srt, i32, (T * k,), device)
+    _check_all(device, ("x", x, bf16, (T, h)), ("W1t", W1t, bf16, (M, 2 * s, h)), ("W2t", W2t, bf16, (M, h, s)),
+               ("idx", idx, i32, (T, k)), ("offsets", offsets, i32, (M + 1,)), ("sorted", srt, i32, (T * k,)))
     if gate is not None:
-        _check("gate", gate, torch.float32, (T, k), device)
+        _check_all(device, ("gate", gate, torch.float32, (T, k)))
 
 
 def _ffn_shape(x, W1t, W2t, idx):
@@ -202,14 +209,15 @@ class BlockNorm:
     def __call__(self, r, y=None, *, w_after=None, w_before=None, gate=None) -> BlockEnd:
         T, h, k = self.shape
         dev, f32 = self.device, torch.float32
-        _check("r", r, self.resid_dtype, (T, h), dev)
         if (y is not None) != (k > 0):
             raise ValueError("y must be given exactly when the norm was set up with k > 0")
+        wanted = [("r", r, self.resid_dtype, (T, h))]
         if y is not None:
-            _check("y", y, torch.bfloat16, (T * k, h) if y.dim() == 2 else (T, k, h), dev)
+            wanted.append(("y", y, torch.bfloat16, (T * k, h) if y.dim() == 2 else (T, k, h)))
         for name, t, shape in (("w_after", w_after, (h,)), ("w_before", w_before, (h,)), ("gate", gate, (T,))):
             if t is not None:
-                _check(name, t, f32, shape, dev)
+                wanted.append((name, t, f32, shape))
+        _check_all(dev, *wanted)
         out = None if k == 0 else r if self.inplace else self.r
         xn = None if w_before is None else self.xn
         _call("more_block_norm", dev, _ptr(r), self.resid_bits, _ptr(y), T, h, k, _ptr(w_after), _ptr(w_before),
@@ -268,13 +276,14 @@ class BlockNormBackward:
         dev, f32, bf16 = self.device, torch.float32, torch.bfloat16
         if (gate is not None) != self.gated:
             raise ValueError("gate must be given exactly when the backward was set up with gated=True")
-        _check("r_out", r_out, self.resid_dtype, (T, h), dev)
+        wanted = [("r_out", r_out, self.resid_dtype, (T, h))]
         for name, t, dtype, shape in (("u", u, bf16, (T, h)), ("dr_out", dr_out, self.resid_dtype, (T, h)),
                                       ("dxn", dxn, bf16, (T, h)), ("dxn32", dxn32, f32, (T, h)),
                                       ("w_after", w_after, f32, (h,)), ("w_before", w_before, f32, (h,)),
                                       ("gate", gate, f32, (T,))):
             if t is not None:
-                _check(name, t, dtype, shape, dev)
+                wanted.append((name, t, dtype, shape))
+        _check_all(dev, *wanted)
         block = u is not None
         du = self.du if block else None
         dwa = self.dw_after if w_after is not None else None
