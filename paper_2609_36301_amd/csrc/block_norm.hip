@@ -132,7 +132,8 @@ __global__ __launch_bounds__(norm_threads(W)) void block_norm_kernel(NormArgs a)
                 for (int i = 0; i < CH; ++i) {
                     v[q][i] = u32x4{0u, 0u, 0u, 0u};
                     if (in[i] && j + q < a.k)
-                        v[q][i] = *reinterpret_cast<const u32x4*>(y + (int64_t)(j + q) * h + c[i]);
+                        v[q][i] = __builtin_nontemporal_load(
+                            reinterpret_cast<const u32x4*>(y + (int64_t)(j + q) * h + c[i]));  // not read again
                 }
 #pragma unroll
             for (int q = 0; q < kAhead; ++q)

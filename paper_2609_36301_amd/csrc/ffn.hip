@@ -89,6 +89,7 @@ template <int BM>
 struct UpShape {
     static constexpr int kWaves = BM == 256 ? 8 : 4;
     static constexpr int kThreads = 64 * kWaves;
+    static constexpr bool kOnce = BM == 32;               // an expert has one tile, mostly
     static constexpr int kWavesS = BM >= 64 ? 2 : 4;      // waves along the hidden units
     static constexpr int kUnits = BM == 256 ? 128 : 64;
     static constexpr int kS = kUnits / kWavesS / 16;      // 16-unit tiles per wave
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(UpShape<BM>::kThreads, 2) void ffn_up_kernel(FfnArg
         const FfnTile tile = tiles[item / cols];
         if (tile.expert < 0) return;
         const int32_t s0 = (int32_t)(item % cols) * S::kUnits;
-        RowTileLoader<2 * S::kUnits, S::kWaves> weights;
+        RowTileLoader<2 * S::kUnits, S::kWaves, S::kOnce> weights;
         const uint16_t* W = a.W1t + (int64_t)tile.expert * 2 * s * h;
         weights.init([&](int i) {
             const int32_t u = min(s0 + i % S::kUnits, s - 1);
@@ -135,7 +136,7 @@ __global__ __launch_bounds__(UpShape<BM>::kThreads, 2) void ffn_up_kernel(FfnArg
         // the gate rows are one group of M-side fragments, the up rows the other
         using M = FfnFragments<S::kS>;
         using N = FfnFragments<S::kN>;
-        ffn_pipeline<S::kStages, S::kLoads, M, N>(
+        ffn_pipeline<S::kStages, S::kLoads, 0, M, N>(
             (h + kFfnBK - 1) / kFfnBK, 16 * wn * S::kN < tile.rows,
             [&](int step, int slot) {
                 LdsChar* at = smem + slot * S::kStageBytes;
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(UpShape<BM>::kThreads, 2) void ffn_up_kernel(FfnArg
                             c = mfma_16x16x32(m.v[i], f.v[j], c);
                         }
                 },
-                [] {}));
+                [] { return false; }));
         // lane l holds token l % 16 and hidden units 4 (l / 16) .. + 3 of each 16 x 16 tile
 #pragma unroll
         for (int j = 0; j < S::kN; ++j) {
@@ -191,6 +192,7 @@ template <int BM>
 struct DownShape {
     static constexpr int kWaves = BM == 256 ? 8 : 4;
     static constexpr int kThreads = 64 * kWaves;
+    static constexpr bool kOnce = BM == 32;               // an expert has one tile, mostly
     static constexpr int kCols = BM == 256 ? 256 : 128;   // columns of a step
     static constexpr int kWavesM = BM >= 64 ? 2 : 4;
     static constexpr int kM = kCols / kWavesM / 16;
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(Ff
             return;
         }
         const uint16_t* W = a.W2t + (int64_t)tile.expert * h * s;
-        RowTileLoader<S::kCols, S::kWaves> weights;
+        RowTileLoader<S::kCols, S::kWaves, S::kOnce> weights;
         RowTileLoader<BM, S::kWaves> rows;
         rows.init([&](int i) { return hidden + (int64_t)(tile.row0 + min(i, tile.rows - 1)) * s; });
         uint32_t place[S::kN];
@@ -239,6 +241,9 @@ __global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(Ff
             place[j] = row < tile.rows ? (uint32_t)a.sorted[tile.row0 + row] : 0xFFFFFFFFu;
             gate[j] = a.gate && place[j] < (uint32_t)n ? a.gate[place[j]] : 1.0f;
         }
+        bool full = true;  // (per wave) every lane stores all its rows
+#pragma unroll
+        for (int j = 0; j < S::kN; ++j) full = full && __all(place[j] < (uint32_t)n);
         f32x4 acc[S::kM][S::kN];
 #pragma unroll
         for (int i = 0; i < S::kM; ++i)
@@ -251,7 +256,7 @@ __global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(Ff
         using G = FfnGroups<S::kM>;
         using M = FfnFragments<G::kSize>;
         using N = FfnFragments<S::kN>;
-        ffn_pipeline<S::kStages, S::kLoads, M, N>(
+        ffn_pipeline<S::kStages, S::kLoads, S::kM * S::kN, M, N>(
             ksteps * hsteps, 16 * wn * S::kN < tile.rows,
             [&](int, int slot) {
                 LdsChar* at = smem + slot * S::kStageBytes;
@@ -286,14 +291,15 @@ __global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(Ff
                             }
                 },
                 [&] {
-                    if (++ck < ksteps) return;
+                    if (++ck < ksteps) return false;
+                    const bool whole = full && ch + S::kCols <= h1;
 #pragma unroll
                     for (int j = 0; j < S::kN; ++j) {
 #pragma unroll
                         for (int i = 0; i < S::kM; ++i) {
                             const int32_t c = ch + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
                             const f32x4 v = acc[i][j] * gate[j];
-                            if (place[j] < (uint32_t)n && c < h1)
+                            if (whole || (place[j] < (uint32_t)n && c < h1))
                                 *reinterpret_cast<uint2*>(y + (int64_t)place[j] * h + c) =
                                     pack_bf16x4(v[0], v[1], v[2], v[3]);
                             acc[i][j] = zero_f32x4();
@@ -301,6 +307,7 @@ __global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(Ff
                     }
                     ck = 0;
                     ch += S::kCols;
+                    return whole;
                 }));
     });
 }
@@ -496,7 +503,7 @@ unsigned few_grid(int64_t items) { return (unsigned)std::min<int64_t>(items, 1 <
 int32_t tile_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
     const int64_t mean = n / std::max<int64_t>(1, std::min<int64_t>(n, M));
     if (mean >= 512 && h >= 256 && s >= 128) return 256;
-    return mean >= 96 ? 128 : mean >= 40 ? 64 : 32;
+    return mean >= 96 ? 128 : mean >= 24 ? 64 : 32;
 }
 
 void tiles_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {

@@ -8,7 +8,7 @@
 //
 // Kernels of one call (entries in the order of Sort + Count, cut into tiles of one expert):
 //   ffn_tiles     lists the tiles
-//   ffn_bwd_up    G, U and dA0 of one tile and 64 (128) hidden units: [dG dU] and gate A (bf16, sorted
+//   ffn_bwd_up    G, U and dA0 of one tile and 64 hidden units: [dG dU] and gate A (bf16, sorted
 //                 order) and the partial sums of dgate
 //   ffn_bwd_dx    [dG dU] W1t[e] per entry (fp32, entry order)
 //   ffn_bwd_sum   dx: the k entries of a token added in order; dgate: the partials added in order
@@ -38,7 +38,7 @@ struct BwdUpShape {
     static constexpr int kWaves = BM == 256 ? 8 : 4;
     static constexpr int kThreads = 64 * kWaves;
     static constexpr int kWavesS = BM >= 64 ? 2 : 4;
-    static constexpr int kUnits = BM == 256 ? 128 : 64;
+    static constexpr int kUnits = 64;
     static constexpr int kS = kUnits / kWavesS / 16;
     static constexpr int kN = BM / (kWaves / kWavesS) / 16;
     static constexpr int kStages = 2;
@@ -52,8 +52,8 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
     float* __restrict__ dgp) {
     using S = BwdUpShape<BM>;
     __shared__ __attribute__((aligned(1024))) char smem_raw[S::kStages * S::kStageBytes];
-    __shared__ float dsum[S::kWavesS][BM];
     LdsChar* smem = (LdsChar*)smem_raw;
+    __shared__ float dsum[S::kWavesS][BM];
     const FfnTile* tiles = ffn_tile_list(list);
     const int32_t s = a.s, h = a.h;
     const int32_t n = a.T * a.k;
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
         // the gate rows are one group of M-side fragments, the up rows the other
         using M = FfnFragments<S::kS>;
         using N = FfnFragments<S::kN>;
-        ffn_pipeline<S::kStages, 0, M, N>(
+        ffn_pipeline<S::kStages, 0, 0, M, N>(
             (h + kFfnBK - 1) / kFfnBK, live,
             [&](int step, int slot) {
                 LdsChar* at = smem + slot * S::kStageBytes;
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
                             c = mfma_16x16x32(m.v[i], f.v[j], c);
                         }
                 },
-                [] {}));
+                [] { return false; }));
 #pragma unroll
         for (int i = 0; i < S::kS; ++i)
 #pragma unroll
@@ -127,16 +127,20 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
         for (int i = 0; i < rows.kLoads; ++i) rows.p[i] += to_du;
         using G = FfnGroups<S::kS>;
         using M2 = FfnFragments<G::kSize>;
-        ffn_pipeline<S::kStages, 0, M2, N>(
+        using Stage = StagePair<decltype(rows), decltype(down)>;
+        ffn_pipeline_staged<Stage, M2, N>(
             hsteps, live,
-            [&](int step, int slot) {
-                LdsChar* at = smem + slot * S::kStageBytes;
+            [&](int step, Stage& st) {
                 const int32_t k0 = step * kFfnBK;
-                rows.load(at + S::kRowsAt, k0, h);
-                down.load(at, s - s0, [&](int i) {
+                rows.fetch(st.a, k0, h);
+                down.fetch(st.b, s - s0, [&](int i) {
                     const int kappa = k0 + down.row(i);
                     return kappa < h ? W2 + (int64_t)kappa * s + s0 : nullptr;
                 });
+            },
+            [&](int slot, const Stage& st) {
+                rows.put(smem + slot * S::kStageBytes + S::kRowsAt, st.a);
+                down.put(smem + slot * S::kStageBytes, st.b);
             },
             ffn_work(
                 [&](int slot, int kk, int group, M2& m) {
@@ -160,7 +164,7 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
                                 c = mfma_16x16x32(m.v[i], f.v[j], c);
                             }
                 },
-                [] {}));
+                [] { return false; }));
         // lane l holds token l % 16 and hidden units 4 (l / 16) .. + 3 of each 16 x 16 tile
 #pragma unroll
         for (int j = 0; j < S::kN; ++j) {
@@ -214,14 +218,13 @@ template <int BM>
 struct BwdDxShape {
     static constexpr int kWaves = BM == 256 ? 8 : 4;
     static constexpr int kThreads = 64 * kWaves;
-    static constexpr int kCols = BM == 256 ? 256 : 128;
+    static constexpr int kCols = 128;
     static constexpr int kWavesM = BM >= 64 ? 2 : 4;
     static constexpr int kM = kCols / kWavesM / 16;
     static constexpr int kN = BM / (kWaves / kWavesM) / 16;
-    static constexpr int kStages = BM >= 128 ? 2 : 3;
+    static constexpr int kStages = 2;
     static constexpr int kRowsAt = kCols * 128;
     static constexpr int kStageBytes = kRowsAt + BM * 128;
-    static constexpr int kLoads = (kCols + BM) / kWaves / 8;
 };
 
 template <int BM>
@@ -264,20 +267,24 @@ __global__ __launch_bounds__(BwdDxShape<BM>::kThreads, 2) void ffn_bwd_dx_kernel
         using G = FfnGroups<S::kM>;
         using M = FfnFragments<G::kSize>;
         using N = FfnFragments<S::kN>;
-        ffn_pipeline<S::kStages, S::kLoads, M, N>(
+        using Stage = StagePair<decltype(weights), decltype(rows)>;
+        ffn_pipeline_staged<Stage, M, N>(
             ksteps * hsteps, 16 * wn * S::kN < tile.rows,
-            [&](int, int slot) {
-                LdsChar* at = smem + slot * S::kStageBytes;
+            [&](int, Stage& st) {
                 const int32_t k0 = lk * kFfnBK;
-                weights.load(at, h - lh, [&](int i) {
+                weights.fetch(st.a, h - lh, [&](int i) {
                     const int kappa = k0 + weights.row(i);
                     return kappa < s2 ? W + (int64_t)kappa * h + lh : nullptr;
                 });
-                rows.load(at + S::kRowsAt, k0, s2);
+                rows.fetch(st.b, k0, s2);
                 if (++lk == ksteps) {
                     lk = 0;
                     lh += S::kCols;
                 }
+            },
+            [&](int slot, const Stage& st) {
+                weights.put(smem + slot * S::kStageBytes, st.a);
+                rows.put(smem + slot * S::kStageBytes + S::kRowsAt, st.b);
             },
             ffn_work(
                 [&](int slot, int kk, int group, M& m) {
@@ -302,7 +309,7 @@ __global__ __launch_bounds__(BwdDxShape<BM>::kThreads, 2) void ffn_bwd_dx_kernel
                             }
                 },
                 [&] {
-                    if (++ck < ksteps) return;
+                    if (++ck < ksteps) return false;
 #pragma unroll
                     for (int j = 0; j < S::kN; ++j) {
 #pragma unroll
@@ -315,6 +322,7 @@ __global__ __launch_bounds__(BwdDxShape<BM>::kThreads, 2) void ffn_bwd_dx_kernel
                     }
                     ck = 0;
                     ch += S::kCols;
+                    return false;
                 }));
     });
 }
@@ -438,18 +446,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(const uint16_
         using G = FfnGroups<kM>;
         using MF = FfnFragments<G::kSize>;
         using NF = FfnFragments<kN>;
+        using Stage = StagePair<PLoader, QLoader>;
         fetch(0);
-        ffn_pipeline<kStages, 0, MF, NF>(
+        ffn_pipeline_staged<Stage, MF, NF>(
             ksteps * csteps, true,
-            [&](int, int slot) {
-                LdsChar* at = smem + slot * kStageBytes;
+            [&](int, Stage& st) {
                 const int32_t i0 = begin + lk * kFfnBK;
-                pl.load(at, c1 - lc, [&](int i) -> const uint16_t* {
+                pl.fetch(st.a, c1 - lc, [&](int i) -> const uint16_t* {
                     if constexpr (GATHER_P) return gathered(i, P + lc, cols_out);
                     const int32_t row = i0 + pl.row(i);
                     return row < end ? P + (int64_t)row * cols_out + lc : nullptr;
                 });
-                ql.load(at + CT * 128, rows_out - r0, [&](int i) -> const uint16_t* {
+                ql.fetch(st.b, rows_out - r0, [&](int i) -> const uint16_t* {
                     if constexpr (!GATHER_P) return gathered(i, Q + r0, rows_out);
                     const int32_t row = i0 + ql.row(i);
                     return row < end ? Q + (int64_t)row * rows_out + r0 : nullptr;
@@ -459,6 +467,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(const uint16_
                     lc += CT;
                 }
                 if (ksteps > 1) fetch(lk);
+            },
+            [&](int slot, const Stage& st) {
+                pl.put(smem + slot * kStageBytes, st.a);
+                ql.put(smem + slot * kStageBytes + CT * 128, st.b);
             },
             ffn_work(
                 [&](int slot, int kk, int group, MF& m) {
@@ -483,9 +495,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(const uint16_
                             }
                 },
                 [&] {
-                    if (++ck < ksteps) return;
+                    if (++ck < ksteps) return false;
                     ck = 0;
                     store();
+                    return false;
                 }));
     }
 }
@@ -500,9 +513,8 @@ unsigned grid_of(int64_t items) {
 }
 
 // Workgroups along the hidden units of ffn_bwd_up: a partial sum of dgate each.
-int32_t dgate_parts(const FfnPlan& p, int32_t s) {
-    const int32_t units = p.bm == 256 ? BwdUpShape<256>::kUnits : 64;
-    return (s + units - 1) / units;
+int32_t dgate_parts(int32_t s) {
+    return (s + BwdUpShape<256>::kUnits - 1) / BwdUpShape<256>::kUnits;
 }
 
 template <int BM>
@@ -538,7 +550,7 @@ void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t 
     p->off_dxs = at;
     at += align256((size_t)p->n * h * 4);
     p->off_dgp = at;
-    at += align256((size_t)p->n * dgate_parts(*p, s) * 4);
+    at += align256((size_t)p->n * dgate_parts(s) * 4);
     p->workspace_bytes = at;
 }
 
@@ -558,12 +570,12 @@ hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspa
         const int64_t gateblocks = a.dgate ? std::min<int64_t>(((int64_t)n + 255) / 256, 1 << 14) : 0;
         ffn_bwd_sum_kernel<<<(unsigned)(colblocks + gateblocks), 256, 0, stream>>>(
             reinterpret_cast<const float*>(ws + p.off_dxs), a.idx, a.T, a.h, a.M, a.k, a.dx, colblocks,
-            reinterpret_cast<const float*>(ws + p.off_dgp), dgate_parts(p, a.s), a.sorted, a.dgate);
+            reinterpret_cast<const float*>(ws + p.off_dgp), dgate_parts(a.s), a.sorted, a.dgate);
     }
     const uint16_t* hidden = reinterpret_cast<const uint16_t*>(ws + p.off_hidden);
     const uint16_t* dgu = reinterpret_cast<const uint16_t*>(ws + p.off_dgu);
     if (p.bm == 256) {
-        dw_launch<256, 256, 8, true>(p, a, a.x, dgu, 2 * a.s, a.h, a.dW1t, stream);
+        dw_launch<128, 256, 8, true>(p, a, a.x, dgu, 2 * a.s, a.h, a.dW1t, stream);
         dw_launch<128, 256, 8, false>(p, a, hidden, a.du, a.h, a.s, a.dW2t, stream);
     } else {
         dw_launch<128, 128, 4, true>(p, a, a.x, dgu, 2 * a.s, a.h, a.dW1t, stream);

@@ -44,9 +44,12 @@ __host__ __device__ constexpr int ffn_wait_imm(int n) {
     return (n & 15) | ((n >> 4) << 14) | (7 << 4);
 }
 // Direct-to-LDS load of 16 bytes per lane: lane l of the wave writes lds + 16 l (lds wave-uniform).
+// ONCE marks data that no other workgroup wants (nontemporal).
+template <bool ONCE = false>
 __device__ __forceinline__ void ffn_dma16(const uint16_t* g, LdsChar* lds) {
-    __builtin_amdgcn_global_load_lds(g, lds, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds(g, lds, 16, 0, ONCE ? 2 : 0);
 }
+__host__ __device__ constexpr int ffn_most(int n) { return n < 63 ? n : 63; }
 // Workgroup barrier that leaves at most VM of the wave's own vector memory operations outstanding.
 template <int VM>
 __device__ __forceinline__ void ffn_barrier() {
@@ -59,9 +62,17 @@ __device__ __forceinline__ void ffn_barrier() {
 __device__ __forceinline__ int ffn_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 __device__ __forceinline__ int ffn_lane() { return threadIdx.x & 63; }
 
+// How a tile's 16-byte pieces get to LDS: straight (load: direct-to-LDS loads), or by way of registers
+// (fetch, then put).  The compiler lets a transposing LDS read wait for every direct-to-LDS load before it, so
+// the kernels that read column tiles take the second way.
+template <int LOADS>
+struct Staged {
+    u32x4 v[LOADS];
+};
+
 // Fills a row tile.  Lane l of a load takes row l / 8 of eight and the piece (l % 8) ^ (l / 8) of its
 // 128 bytes; a wave fills ROWS / WAVES rows.
-template <int ROWS, int WAVES>
+template <int ROWS, int WAVES, bool ONCE = false>
 struct RowTileLoader {
     static constexpr int kPerWave = ROWS / WAVES;
     static constexpr int kLoads = kPerWave / 8;
@@ -78,16 +89,30 @@ struct RowTileLoader {
         for (int i = 0; i < kLoads; ++i) p[i] = row_of(w * kPerWave + 8 * i + (l >> 3)) + piece;
     }
     // contraction values [k0, k0 + 64) of K (a multiple of 8); past K: zeros
-    __device__ __forceinline__ void load(LdsChar* lds, int k0, int K) const {
-        LdsChar* at = lds + ffn_wave() * kPerWave * 128;
+    template <typename F>
+    __device__ __forceinline__ void each(int k0, int K, F f) const {
         if (k0 + kFfnBK <= K) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) ffn_dma16(p[i] + k0, at + i * 1024);
+            for (int i = 0; i < kLoads; ++i) f(i, p[i] + k0);
         } else {
             const bool in = k0 + piece < K;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) ffn_dma16(in ? p[i] + k0 : ffn_zeros, at + i * 1024);
+            for (int i = 0; i < kLoads; ++i) f(i, in ? p[i] + k0 : ffn_zeros);
         }
+    }
+    __device__ __forceinline__ void load(LdsChar* lds, int k0, int K) const {
+        LdsChar* at = lds + ffn_wave() * kPerWave * 128;
+        each(k0, K, [&](int i, const uint16_t* g) { ffn_dma16<ONCE>(g, at + i * 1024); });
+    }
+    using Stage = Staged<kLoads>;
+    __device__ __forceinline__ void fetch(Stage& s, int k0, int K) const {
+        each(k0, K, [&](int i, const uint16_t* g) { s.v[i] = *reinterpret_cast<const u32x4*>(g); });
+    }
+    __device__ __forceinline__ void put(LdsChar* lds, const Stage& s) const {
+        LdsChar* at = lds + ffn_wave() * kPerWave * 128 + ffn_lane() * 16;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(at + i * 1024) = s.v[i];
     }
 };
 // Fragment of 16 rows and contraction values 32 kk .. 32 kk + 31: lane l gets row l % 16, values
@@ -126,24 +151,26 @@ struct ColTileLoader {
     }
     // row_of(i): the address of column 0 of the lane's row in group i, or NULL (zeros); columns from
     // `cols` on (a multiple of 8) are zeros
+    using Stage = Staged<kLoads>;
     template <typename F>
-    __device__ __forceinline__ void load(LdsChar* lds, int cols, F row_of) const {
+    __device__ __forceinline__ void fetch(Stage& s, int cols, F row_of) const {
 #pragma unroll
         for (int i = 0; i < kGroups; ++i) {
             const uint16_t* r = row_of(i);
-            LdsChar* at = lds + (ffn_wave() + WAVES * i) * 1024;
-            if (cols >= COLS) {
-                const uint16_t* from = r ? r + col[i] : ffn_zeros;
-                const int step = r ? 64 : 0;
 #pragma unroll
-                for (int q = 0; q < kPanels; ++q) ffn_dma16(from + q * step, at + q * kFfnPanel);
-            } else {
-#pragma unroll
-                for (int q = 0; q < kPanels; ++q) {
-                    const int c = 64 * q + col[i];
-                    ffn_dma16(r && c < cols ? r + c : ffn_zeros, at + q * kFfnPanel);
-                }
+            for (int q = 0; q < kPanels; ++q) {
+                const int c = 64 * q + col[i];
+                s.v[i * kPanels + q] = *reinterpret_cast<const u32x4*>(r && c < cols ? r + c : ffn_zeros);
             }
+        }
+    }
+    __device__ __forceinline__ void put(LdsChar* lds, const Stage& s) const {
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+            LdsChar* at = lds + (ffn_wave() + WAVES * i) * 1024 + ffn_lane() * 16;
+#pragma unroll
+            for (int q = 0; q < kPanels; ++q)
+                *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(at + q * kFfnPanel) = s.v[i * kPanels + q];
         }
     }
 };
@@ -173,17 +200,50 @@ __device__ __forceinline__ void ffn_for_each(int64_t total, F body) {
     }
 }
 
-// Software pipeline over `steps` stages of an LDS ring of STAGES; load(step, slot) issues LOADS
-// direct-to-LDS loads per wave.  A stage's product runs in four parts: for each half kk of its contraction
-// values, the M-side fragments in two groups against the N-side fragments.  `w` gives read_m(slot, kk,
-// group, m) and read_n(slot, kk, n), which fill fragments of types M and N, multiply(group, m, n), and
-// done(), which follows the last product of a step.  The fragments of a part are read while the part
-// before is multiplied, across steps too, so that the LDS works while the matrix cores do; the one
-// barrier of a step stands before its last part, where the next stage has to have landed and the present
-// one has been read by every wave, so that its slot can be filled again, STAGES stages ahead.  A wave
-// that has no wanted rows (live = false) only loads.
-template <int STAGES, int LOADS, typename M, typename N, typename L, typename W>
+// The products of `steps` stages of an LDS ring of `stages`.  A stage's product runs in four parts: for
+// each half kk of its contraction values, the M-side fragments in two groups against the N-side fragments.
+// `w` gives read_m(slot, kk, group, m) and read_n(slot, kk, n), which fill fragments of types M and N,
+// multiply(group, m, n), and done(), which follows the last product of a step.  The fragments of a part
+// are read while the part before is multiplied, across steps too, so that the LDS works while the matrix
+// cores do.  turn(step, slot, stored) stands before the last part of every step but the last: there the
+// next stage has to become readable, and the present one has been read and can be filled again.
+// `stored` holds what done() returned after the step before (bit 0) and the one before that (bit 1).
+template <typename M, typename N, typename T, typename W>
+__device__ __forceinline__ void ffn_steps(int steps, int stages, T turn, W w) {
+    M m0, m1;
+    N n0, n1;
+    w.read_n(0, 0, n0);
+    w.read_m(0, 0, 0, m0);
+    int slot = 0, stored = 0;
+    for (int step = 0; step < steps; ++step) {
+        const int next = slot + 1 == stages ? 0 : slot + 1;
+        w.read_m(slot, 0, 1, m1);
+        w.multiply(0, m0, n0);
+        w.read_n(slot, 1, n1);
+        w.read_m(slot, 1, 0, m0);
+        w.multiply(1, m1, n0);
+        w.read_m(slot, 1, 1, m1);
+        w.multiply(0, m0, n1);
+        if (step + 1 < steps) {
+            turn(step, slot, stored);
+            w.read_n(next, 0, n0);
+            w.read_m(next, 0, 0, m0);
+        }
+        w.multiply(1, m1, n1);
+        stored = (stored << 1 | (w.done() ? 1 : 0)) & 3;
+        slot = next;
+    }
+}
+
+// The pipeline with direct-to-LDS loads: load(step, slot) issues LOADS of them per wave, STAGES stages
+// ahead.  A wave's own vector memory operations complete in the order in which they were issued, loads
+// and stores alike, so the next stage's loads are known to have landed while younger operations are
+// outstanding: the loads of later stages, and STORES stores where done() says that it issued exactly so
+// many.  A wave that has no wanted rows (live = false) only loads.
+template <int STAGES, int LOADS, int STORES, typename M, typename N, typename L, typename W>
 __device__ __forceinline__ void ffn_pipeline(int steps, bool live, L load, W w) {
+    static_assert(STAGES == 2 || STAGES == 3, "");
+    constexpr int kLeft = (STAGES - 2) * LOADS;  // loads younger than the next stage's
     ffn_barrier<0>();  // the previous work item's reads are over
 #pragma unroll
     for (int i = 0; i < STAGES; ++i)
@@ -193,43 +253,63 @@ __device__ __forceinline__ void ffn_pipeline(int steps, bool live, L load, W w) 
     } else {
         ffn_barrier<0>();
     }
-    auto turn = [&](int step, int slot) {  // before the last part of a step that is not the last
-        if (step + STAGES <= steps) {
-            ffn_barrier<(STAGES - 2) * LOADS>();
-        } else {
+    auto turn = [&](int step, int slot, int stored) {
+        if (step + STAGES > steps) {
             ffn_barrier<0>();
+        } else if (STORES > 0 && STAGES == 3 && stored == 3) {
+            ffn_barrier<ffn_most(kLeft + 2 * STORES)>();
+        } else if (STORES > 0 && (stored & 1)) {
+            ffn_barrier<ffn_most(kLeft + STORES)>();
+        } else {
+            ffn_barrier<kLeft>();
         }
         if (step + STAGES < steps) load(step + STAGES, slot);
+        asm volatile("" ::: "memory");  // (the stores that follow stay younger than these loads)
     };
-    int slot = 0;
-    if (!live) {
+    if (live) {
+        ffn_steps<M, N>(steps, STAGES, turn, w);
+    } else {
+        int slot = 0;
         for (int step = 0; step + 1 < steps; ++step) {
-            turn(step, slot);
+            turn(step, slot, 0);
             slot = slot + 1 == STAGES ? 0 : slot + 1;
         }
-        return;
     }
-    M m0, m1;
-    N n0, n1;
-    w.read_n(0, 0, n0);
-    w.read_m(0, 0, 0, m0);
-    for (int step = 0; step < steps; ++step) {
-        const int next = slot + 1 == STAGES ? 0 : slot + 1;
-        w.read_m(slot, 0, 1, m1);
-        w.multiply(0, m0, n0);
-        w.read_n(slot, 1, n1);
-        w.read_m(slot, 1, 0, m0);
-        w.multiply(1, m1, n0);
-        w.read_m(slot, 1, 1, m1);
-        w.multiply(0, m0, n1);
-        if (step + 1 < steps) {
-            turn(step, slot);
-            w.read_n(next, 0, n0);
-            w.read_m(next, 0, 0, m0);
-        }
-        w.multiply(1, m1, n1);
-        w.done();
-        slot = next;
+}
+
+// A stage of both operands on its way through registers.
+template <typename A, typename B>
+struct StagePair {
+    typename A::Stage a;
+    typename B::Stage b;
+};
+
+// The pipeline by way of registers, two stages in LDS: fetch(step, s) reads a stage into registers,
+// put(slot, s) writes it to LDS a step later, and another step later it is multiplied.
+template <typename S, typename M, typename N, typename F, typename P, typename W>
+__device__ __forceinline__ void ffn_pipeline_staged(int steps, bool live, F fetch, P put, W w) {
+    S s;
+    ffn_barrier<63>();  // the previous work item's reads are over
+    fetch(0, s);
+    if (steps > 1) {
+        S s1;
+        fetch(1, s1);
+        put(0, s);
+        put(1, s1);
+    } else {
+        put(0, s);
+    }
+    if (steps > 2) fetch(2, s);
+    ffn_barrier<63>();
+    auto turn = [&](int step, int slot, int) {
+        ffn_barrier<63>();
+        if (step + 2 < steps) put(slot, s);
+        if (step + 3 < steps) fetch(step + 3, s);
+    };
+    if (live) {
+        ffn_steps<M, N>(steps, 2, turn, w);
+    } else {
+        for (int step = 0; step + 1 < steps; ++step) turn(step, step & 1, 0);
     }
 }
 
