@@ -370,40 +370,46 @@ __global__ __launch_bounds__(256) void ffn_bwd_sum_kernel(const float* __restric
 // ------------------------------------------------------------------------------ weight gradients
 // out[e] [rows_out][cols_out] = sum over the entries i of expert e of Q[i][row] P[i][col], both operands
 // column tiles (the contraction runs over rows).  dW1t: P = x of the entry's token (cols h), Q = [dG dU]
-// (rows 2s).  dW2t: P = gate A (cols s), Q = du of the entry's token (rows h).  A workgroup computes RT
-// rows and `cspan` columns in steps of CT; the pipeline runs over (column step, 64 entries) pairs, so
-// that the few rows of a small expert do not drain it.
+// (rows 2s).  dW2t: P = gate A (cols s), Q = du of the entry's token (rows h).  The gathered operand is the
+// one along h; a workgroup computes a tile of RT rows and CT columns after the other over `hspan` of h, and
+// the pipeline runs over (tile, 64 entries) pairs, so that the few rows of a small expert do not drain it.
 template <int CT, int RT, int WAVES, bool GATHER_P>
 __global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(const uint16_t* __restrict__ P,
                                                                 const uint16_t* __restrict__ Q,
                                                                 const int32_t* __restrict__ offsets,
                                                                 const int32_t* __restrict__ sorted, int32_t n,
                                                                 int32_t k, int32_t M, int32_t rows_out,
-                                                                int32_t cols_out, int32_t cspan,
+                                                                int32_t cols_out, int32_t hspan,
                                                                 uint16_t* __restrict__ out) {
     constexpr int kStages = 2;
     constexpr int kStageBytes = (CT + RT) * 128;
-    constexpr int kM = CT / 32, kN = RT / (WAVES / 2) / 16;  // 16 x 16 tiles per wave
+    constexpr int kWavesM = CT / 64, kWavesN = WAVES / kWavesM;
+    constexpr int kM = 4, kN = RT / kWavesN / 16;  // 16 x 16 tiles per wave: 64 columns, a line of out
     using PLoader = ColTileLoader<CT, WAVES>;
     using QLoader = ColTileLoader<RT, WAVES>;
     constexpr int kGathered = PLoader::kGroups;  // rows per lane of either operand
     __shared__ __attribute__((aligned(1024))) char smem_raw[kStages * kStageBytes];
+    __shared__ __attribute__((aligned(16))) char scratch_raw[WAVES * kFfnScratch];
     LdsChar* smem = (LdsChar*)smem_raw;
-    const int wave = ffn_wave(), lane = ffn_lane();
-    const int wm = wave & 1, wn = wave >> 1;
-    const int32_t spans = (cols_out + cspan - 1) / cspan, rt = (rows_out + RT - 1) / RT;
+    LdsChar* scratch = (LdsChar*)scratch_raw + ffn_wave() * kFfnScratch;
+    const int wm = ffn_wave() % kWavesM, wn = ffn_wave() / kWavesM;
+    constexpr int kStep = GATHER_P ? CT : RT;  // of h
+    const int32_t h = GATHER_P ? cols_out : rows_out;
+    const int32_t spans = (h + hspan - 1) / hspan;
+    const int32_t others = GATHER_P ? (rows_out + RT - 1) / RT : (cols_out + CT - 1) / CT;
     // Items in turn over the XCDs: the parts of an expert run on all of them, so that experts with many
     // entries load them alike.
-    for (int64_t item = blockIdx.x; item < (int64_t)M * spans * rt; item += gridDim.x) {
-        const int32_t e = (int32_t)(item / (spans * rt)), q = (int32_t)(item % (spans * rt));
-        const int32_t c0 = (q % spans) * cspan, c1 = min(cols_out, c0 + cspan), r0 = (q / spans) * RT;
+    for (int64_t item = blockIdx.x; item < (int64_t)M * spans * others; item += gridDim.x) {
+        const int32_t e = (int32_t)(item / (spans * others)), q = (int32_t)(item % (spans * others));
+        const int32_t h0 = (q % spans) * hspan, h1 = min(h, h0 + hspan);
+        const int32_t other = (q / spans) * (GATHER_P ? RT : CT);  // first row (column) of the other side
         const int32_t begin = min(max(offsets[e], 0), n), end = min(max(offsets[e + 1], begin), n);
         PLoader pl;
         QLoader ql;
         pl.init();
         ql.init();
         const int32_t ksteps = (end - begin + kFfnBK - 1) / kFfnBK;
-        const int32_t csteps = (c1 - c0 + CT - 1) / CT;
+        const int32_t hsteps = (h1 - h0 + kStep - 1) / kStep;
         // the gathered operand's entries of the next load (read one load ahead)
         int32_t entry[kGathered];
         auto fetch = [&](int32_t step) {
@@ -422,25 +428,26 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(const uint16_
         for (int i = 0; i < kM; ++i)
 #pragma unroll
             for (int j = 0; j < kN; ++j) acc[i][j] = zero_f32x4();
-        int32_t lc = c0, lk = 0, cc = c0, ck = 0;
+        int32_t lh = h0, lk = 0, ch = h0, ck = 0;
         auto store = [&] {
             uint16_t* o = out + (int64_t)e * rows_out * cols_out;
 #pragma unroll
             for (int j = 0; j < kN; ++j) {
-                const int32_t r = r0 + 16 * (wn * kN + j) + (lane & 15);
 #pragma unroll
                 for (int i = 0; i < kM; ++i) {
-                    const int32_t c = cc + 16 * (wm * kM + i) + 4 * (lane >> 4);
-                    if (r < rows_out && c < c1)
-                        *reinterpret_cast<uint2*>(o + (int64_t)r * cols_out + c) =
-                            pack_bf16x4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+                    place_bf16(scratch, i, acc[i][j]);
                     acc[i][j] = zero_f32x4();
                 }
+                const int32_t c = (GATHER_P ? ch : other) + 64 * wm;
+                const int32_t r = (GATHER_P ? other : ch) + 16 * (wn * kN + j);
+                flush_rows(scratch, ((GATHER_P ? h1 : cols_out) - c) * 2, [&](int row) {
+                    return r + row < (GATHER_P ? rows_out : h1) ? o + (int64_t)(r + row) * cols_out + c : nullptr;
+                });
             }
-            cc += CT;
+            ch += kStep;
         };
         if (ksteps == 0) {  // no entries: zeros
-            for (int32_t step = 0; step < csteps; ++step) store();
+            for (int32_t step = 0; step < hsteps; ++step) store();
             continue;
         }
         using G = FfnGroups<kM>;
@@ -449,22 +456,23 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(const uint16_
         using Stage = StagePair<PLoader, QLoader>;
         fetch(0);
         ffn_pipeline_staged<Stage, MF, NF>(
-            ksteps * csteps, true,
+            ksteps * hsteps, true,
             [&](int, Stage& st) {
                 const int32_t i0 = begin + lk * kFfnBK;
-                pl.fetch(st.a, c1 - lc, [&](int i) -> const uint16_t* {
-                    if constexpr (GATHER_P) return gathered(i, P + lc, cols_out);
+                const int32_t c = GATHER_P ? lh : other, r = GATHER_P ? other : lh;
+                pl.fetch(st.a, cols_out - c, [&](int i) -> const uint16_t* {
+                    if constexpr (GATHER_P) return gathered(i, P + c, cols_out);
                     const int32_t row = i0 + pl.row(i);
-                    return row < end ? P + (int64_t)row * cols_out + lc : nullptr;
+                    return row < end ? P + (int64_t)row * cols_out + c : nullptr;
                 });
-                ql.fetch(st.b, rows_out - r0, [&](int i) -> const uint16_t* {
-                    if constexpr (!GATHER_P) return gathered(i, Q + r0, rows_out);
+                ql.fetch(st.b, rows_out - r, [&](int i) -> const uint16_t* {
+                    if constexpr (!GATHER_P) return gathered(i, Q + r, rows_out);
                     const int32_t row = i0 + ql.row(i);
-                    return row < end ? Q + (int64_t)row * rows_out + r0 : nullptr;
+                    return row < end ? Q + (int64_t)row * rows_out + r : nullptr;
                 });
                 if (++lk == ksteps) {
                     lk = 0;
-                    lc += CT;
+                    lh += kStep;
                 }
                 if (ksteps > 1) fetch(lk);
             },
@@ -533,11 +541,11 @@ void rows_launch(const FfnPlan& p, const FfnArgs& a, char* ws, hipStream_t strea
 template <int CT, int RT, int WAVES, bool GATHER_P>
 void dw_launch(const FfnPlan& p, const FfnArgs& a, const uint16_t* P, const uint16_t* Q, int32_t rows, int32_t cols,
                uint16_t* out, hipStream_t stream) {
-    const int64_t groups = (int64_t)a.M * ((rows + RT - 1) / RT);
-    const int32_t cspan = ffn_span((int32_t)std::min<int64_t>(p.n / a.M, 1 << 20), CT, groups, cols);
-    const int64_t items = groups * ((cols + cspan - 1) / cspan);
+    const int64_t groups = (int64_t)a.M * (GATHER_P ? (rows + RT - 1) / RT : (cols + CT - 1) / CT);
+    const int32_t hspan = ffn_span((int32_t)std::min<int64_t>(p.n / a.M, 1 << 20), GATHER_P ? CT : RT, groups, a.h);
+    const int64_t items = groups * ((a.h + hspan - 1) / hspan);
     ffn_bwd_dw_kernel<CT, RT, WAVES, GATHER_P><<<grid_of(items), 64 * WAVES, 0, stream>>>(
-        P, Q, a.offsets, a.sorted, (int32_t)p.n, a.k, a.M, rows, cols, cspan, out);
+        P, Q, a.offsets, a.sorted, (int32_t)p.n, a.k, a.M, rows, cols, hspan, out);
 }
 
 }  // namespace
