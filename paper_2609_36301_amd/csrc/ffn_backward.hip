@@ -12,8 +12,8 @@
 //                 order) and the partial sums of dgate
 //   ffn_bwd_dx    [dG dU] W1t[e] per entry (fp32, entry order)
 //   ffn_bwd_sum   dx: the k entries of a token added in order; dgate: the partials added in order
-//   ffn_bwd_dw    dW1t and dW2t: contractions over the rows of an expert, one launch each; an expert
-//                 without rows gets zeros
+//   ffn_bwd_dw    dW1t and dW2t: contractions over the rows of an expert; an expert without rows gets
+//                 zeros
 // Every sum runs in a fixed order: nothing is added atomically, and a call gives the same bits on every
 // run.  Numerics: bf16 operands with fp32 accumulation; [dG dU] and gate A are rounded to bf16 once (the
 // matrix cores' operand type), the entries' shares of dx stay in fp32 until they are summed, dgate comes
@@ -373,25 +373,25 @@ __global__ __launch_bounds__(256) void ffn_bwd_sum_kernel(const float* __restric
 // (rows 2s).  dW2t: P = gate A (cols s), Q = du of the entry's token (rows h).  The gathered operand is the
 // one along h; a workgroup computes a tile of RT rows and CT columns after the other over `hspan` of h, and
 // the pipeline runs over (tile, 64 entries) pairs, so that the few rows of a small expert do not drain it.
+struct DwArgs {
+    const uint16_t *P, *Q;
+    int32_t rows_out, cols_out, hspan, blocks;  // workgroups of this product
+    uint16_t* out;
+};
+
 template <int CT, int RT, int WAVES, bool GATHER_P>
-__global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(const uint16_t* __restrict__ P,
-                                                                const uint16_t* __restrict__ Q,
-                                                                const int32_t* __restrict__ offsets,
-                                                                const int32_t* __restrict__ sorted, int32_t n,
-                                                                int32_t k, int32_t M, int32_t rows_out,
-                                                                int32_t cols_out, int32_t hspan,
-                                                                uint16_t* __restrict__ out) {
-    constexpr int kStages = 2;
+__device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __restrict__ offsets,
+                                           const int32_t* __restrict__ sorted, int32_t n, int32_t k, int32_t M,
+                                           LdsChar* smem, LdsChar* scratch, int32_t block) {
+    const uint16_t *P = d.P, *Q = d.Q;
+    const int32_t rows_out = d.rows_out, cols_out = d.cols_out, hspan = d.hspan;
+    uint16_t* out = d.out;
     constexpr int kStageBytes = (CT + RT) * 128;
     constexpr int kWavesM = CT / 64, kWavesN = WAVES / kWavesM;
     constexpr int kM = 4, kN = RT / kWavesN / 16;  // 16 x 16 tiles per wave: 64 columns, a line of out
     using PLoader = ColTileLoader<CT, WAVES>;
     using QLoader = ColTileLoader<RT, WAVES>;
     constexpr int kGathered = PLoader::kGroups;  // rows per lane of either operand
-    __shared__ __attribute__((aligned(1024))) char smem_raw[kStages * kStageBytes];
-    __shared__ __attribute__((aligned(16))) char scratch_raw[WAVES * kFfnScratch];
-    LdsChar* smem = (LdsChar*)smem_raw;
-    LdsChar* scratch = (LdsChar*)scratch_raw + ffn_wave() * kFfnScratch;
     const int wm = ffn_wave() % kWavesM, wn = ffn_wave() / kWavesM;
     constexpr int kStep = GATHER_P ? CT : RT;  // of h
     const int32_t h = GATHER_P ? cols_out : rows_out;
@@ -399,7 +399,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(const uint16_
     const int32_t others = GATHER_P ? (rows_out + RT - 1) / RT : (cols_out + CT - 1) / CT;
     // Items in turn over the XCDs: the parts of an expert run on all of them, so that experts with many
     // entries load them alike.
-    for (int64_t item = blockIdx.x; item < (int64_t)M * spans * others; item += gridDim.x) {
+    for (int64_t item = block; item < (int64_t)M * spans * others; item += d.blocks) {
         const int32_t e = (int32_t)(item / (spans * others)), q = (int32_t)(item % (spans * others));
         const int32_t h0 = (q % spans) * hspan, h1 = min(h, h0 + hspan);
         const int32_t other = (q / spans) * (GATHER_P ? RT : CT);  // first row (column) of the other side
@@ -511,6 +511,24 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(const uint16_
     }
 }
 
+// Both products in one launch (the second one's workgroups follow the first one's, so that the last of one
+// and the first of the other share the chip).
+template <int CT2, int RT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(DwArgs w1, DwArgs w2,
+                                                                const int32_t* __restrict__ offsets,
+                                                                const int32_t* __restrict__ sorted, int32_t n,
+                                                                int32_t k, int32_t M) {
+    __shared__ __attribute__((aligned(1024))) char smem_raw[2 * (128 + RT) * 128];
+    __shared__ __attribute__((aligned(16))) char scratch_raw[WAVES * kFfnScratch];
+    LdsChar* smem = (LdsChar*)smem_raw;
+    LdsChar* scratch = (LdsChar*)scratch_raw + ffn_wave() * kFfnScratch;
+    const int32_t block = (int32_t)blockIdx.x;
+    if (block < w1.blocks)
+        ffn_bwd_dw<128, RT, WAVES, true>(w1, offsets, sorted, n, k, M, smem, scratch, block);
+    else
+        ffn_bwd_dw<CT2, RT, WAVES, false>(w2, offsets, sorted, n, k, M, smem, scratch, block - w1.blocks);
+}
+
 // ------------------------------------------------------------------------------ host
 namespace {
 
@@ -538,14 +556,27 @@ void rows_launch(const FfnPlan& p, const FfnArgs& a, char* ws, hipStream_t strea
         a, ws + p.off_tiles, dgu, hspan, reinterpret_cast<float*>(ws + p.off_dxs));
 }
 
-template <int CT, int RT, int WAVES, bool GATHER_P>
-void dw_launch(const FfnPlan& p, const FfnArgs& a, const uint16_t* P, const uint16_t* Q, int32_t rows, int32_t cols,
-               uint16_t* out, hipStream_t stream) {
-    const int64_t groups = (int64_t)a.M * (GATHER_P ? (rows + RT - 1) / RT : (cols + CT - 1) / CT);
-    const int32_t hspan = ffn_span((int32_t)std::min<int64_t>(p.n / a.M, 1 << 20), GATHER_P ? CT : RT, groups, a.h);
-    const int64_t items = groups * ((a.h + hspan - 1) / hspan);
-    ffn_bwd_dw_kernel<CT, RT, WAVES, GATHER_P><<<grid_of(items), 64 * WAVES, 0, stream>>>(
-        P, Q, a.offsets, a.sorted, (int32_t)p.n, a.k, a.M, rows, cols, hspan, out);
+// One weight gradient: tiles of rt x ct, `other` of them across h.
+DwArgs dw_args(const FfnPlan& p, const FfnArgs& a, const uint16_t* P, const uint16_t* Q, int32_t rows, int32_t cols,
+               int32_t others, int32_t step, uint16_t* out) {
+    DwArgs d;
+    d.P = P;
+    d.Q = Q;
+    d.rows_out = rows;
+    d.cols_out = cols;
+    const int64_t groups = (int64_t)a.M * others;
+    d.hspan = ffn_span((int32_t)std::min<int64_t>(p.n / a.M, 1 << 20), step, groups, a.h);
+    d.blocks = (int32_t)grid_of(groups * ((a.h + d.hspan - 1) / d.hspan));
+    d.out = out;
+    return d;
+}
+
+template <int CT2, int RT, int WAVES>
+void dw_launch(const FfnPlan& p, const FfnArgs& a, const uint16_t* hidden, const uint16_t* dgu, hipStream_t stream) {
+    const DwArgs w1 = dw_args(p, a, a.x, dgu, 2 * a.s, a.h, (2 * a.s + RT - 1) / RT, 128, a.dW1t);
+    const DwArgs w2 = dw_args(p, a, hidden, a.du, a.h, a.s, (a.s + CT2 - 1) / CT2, RT, a.dW2t);
+    ffn_bwd_dw_kernel<CT2, RT, WAVES><<<(unsigned)(w1.blocks + w2.blocks), 64 * WAVES, 0, stream>>>(
+        w1, w2, a.offsets, a.sorted, (int32_t)p.n, a.k, a.M);
 }
 
 }  // namespace
@@ -582,13 +613,10 @@ hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspa
     }
     const uint16_t* hidden = reinterpret_cast<const uint16_t*>(ws + p.off_hidden);
     const uint16_t* dgu = reinterpret_cast<const uint16_t*>(ws + p.off_dgu);
-    if (p.bm == 256) {
-        dw_launch<128, 256, 8, true>(p, a, a.x, dgu, 2 * a.s, a.h, a.dW1t, stream);
-        dw_launch<128, 256, 8, false>(p, a, hidden, a.du, a.h, a.s, a.dW2t, stream);
-    } else {
-        dw_launch<128, 128, 4, true>(p, a, a.x, dgu, 2 * a.s, a.h, a.dW1t, stream);
-        dw_launch<64, 128, 4, false>(p, a, hidden, a.du, a.h, a.s, a.dW2t, stream);
-    }
+    if (p.bm == 256)
+        dw_launch<128, 256, 8>(p, a, hidden, dgu, stream);
+    else
+        dw_launch<64, 128, 4>(p, a, hidden, dgu, stream);
     return hipGetLastError();
 }
 
