@@ -28,7 +28,7 @@ struct FfnPlan {
     int64_t n;        // T k entries
     int32_t bm;       // rows of a tile (all of one expert)
     int64_t tiles;    // bound on the number of tiles
-    size_t off_tiles, off_hidden, off_dgu, off_dxs, off_dgp;
+    size_t off_tiles, off_hidden, off_dgu, off_da0, off_dxs, off_dgp;
     size_t workspace_bytes;
 };
 

@@ -20,6 +20,7 @@
 
 #include "ffn.h"
 #include "ffn_device.h"
+#include "ffn_up.h"
 
 namespace more {
 
@@ -79,109 +80,6 @@ __global__ __launch_bounds__(kTileThreads) void ffn_tiles_kernel(const int32_t* 
             }
         if (tid == 0) *list = (int32_t)std::min<int64_t>((int64_t)total + extra, bound);
     }
-}
-
-// ------------------------------------------------------------------------------ up
-// A workgroup computes A of one tile and kUnits hidden units: the gate rows and up rows of W1t are the
-// M side of the matrix product, the tile's token rows the N side.  A wave holds kS times 16 hidden units
-// (both projections) and kN times 16 tokens, so the activation meets both its factors in the same lane.
-template <int BM>
-struct UpShape {
-    static constexpr int kWaves = BM == 256 ? 8 : 4;
-    static constexpr int kThreads = 64 * kWaves;
-    static constexpr bool kOnce = BM == 32;               // an expert has one tile, mostly
-    static constexpr int kWavesS = BM >= 64 ? 2 : 4;      // waves along the hidden units
-    static constexpr int kUnits = BM == 256 ? 128 : 64;
-    static constexpr int kS = kUnits / kWavesS / 16;      // 16-unit tiles per wave
-    static constexpr int kN = BM / (kWaves / kWavesS) / 16;
-    static constexpr int kStages = BM >= 128 ? 2 : 3;
-    static constexpr int kRowsAt = 2 * kUnits * 128;      // the token rows' place in a stage
-    static constexpr int kStageBytes = kRowsAt + BM * 128;
-    static constexpr int kLoads = (2 * kUnits + BM) / kWaves / 8;
-};
-
-template <int BM>
-__global__ __launch_bounds__(UpShape<BM>::kThreads, 2) void ffn_up_kernel(FfnArgs a, const void* __restrict__ list,
-                                                             uint16_t* __restrict__ hidden) {
-    using S = UpShape<BM>;
-    __shared__ __attribute__((aligned(1024))) char smem_raw[S::kStages * S::kStageBytes];
-    LdsChar* smem = (LdsChar*)smem_raw;
-    const FfnTile* tiles = ffn_tile_list(list);
-    const int32_t s = a.s, h = a.h;
-    const int32_t n = a.T * a.k;
-    const int32_t cols = (s + S::kUnits - 1) / S::kUnits;
-    const int wave = ffn_wave(), lane = ffn_lane();
-    const int ws = wave % S::kWavesS, wn = wave / S::kWavesS;
-    const int64_t total = (int64_t)*static_cast<const int32_t*>(list) * cols;
-    ffn_for_each(total, [&](int64_t item) {
-        const FfnTile tile = tiles[item / cols];
-        if (tile.expert < 0) return;
-        const int32_t s0 = (int32_t)(item % cols) * S::kUnits;
-        RowTileLoader<2 * S::kUnits, S::kWaves, S::kOnce> weights;
-        const uint16_t* W = a.W1t + (int64_t)tile.expert * 2 * s * h;
-        weights.init([&](int i) {
-            const int32_t u = min(s0 + i % S::kUnits, s - 1);
-            return W + (int64_t)(i / S::kUnits * s + u) * h;
-        });
-        RowTileLoader<BM, S::kWaves> tokens;
-        tokens.init([&](int i) {
-            const uint32_t p = a.sorted[tile.row0 + min(i, tile.rows - 1)];
-            return a.x + (int64_t)(p < (uint32_t)n ? p / (uint32_t)a.k : 0) * h;
-        });
-        f32x4 g[S::kS][S::kN], u[S::kS][S::kN];
-#pragma unroll
-        for (int i = 0; i < S::kS; ++i)
-#pragma unroll
-            for (int j = 0; j < S::kN; ++j) g[i][j] = u[i][j] = zero_f32x4();
-        // the gate rows are one group of M-side fragments, the up rows the other
-        using M = FfnFragments<S::kS>;
-        using N = FfnFragments<S::kN>;
-        ffn_pipeline<S::kStages, S::kLoads, 0, M, N>(
-            (h + kFfnBK - 1) / kFfnBK, 16 * wn * S::kN < tile.rows,
-            [&](int step, int slot) {
-                LdsChar* at = smem + slot * S::kStageBytes;
-                weights.load(at, step * kFfnBK, h);
-                tokens.load(at + S::kRowsAt, step * kFfnBK, h);
-            },
-            ffn_work(
-                [&](int slot, int kk, int group, M& m) {
-#pragma unroll
-                    for (int i = 0; i < S::kS; ++i)
-                        m.v[i] = row_fragment(smem + slot * S::kStageBytes,
-                                              group * S::kUnits + 16 * (ws * S::kS + i), kk);
-                },
-                [&](int slot, int kk, N& f) {
-#pragma unroll
-                    for (int j = 0; j < S::kN; ++j)
-                        f.v[j] = row_fragment(smem + slot * S::kStageBytes + S::kRowsAt, 16 * (wn * S::kN + j), kk);
-                },
-                [&](int group, const M& m, const N& f) {
-#pragma unroll
-                    for (int i = 0; i < S::kS; ++i)
-#pragma unroll
-                        for (int j = 0; j < S::kN; ++j) {
-                            f32x4& c = group ? u[i][j] : g[i][j];
-                            c = mfma_16x16x32(m.v[i], f.v[j], c);
-                        }
-                },
-                [] { return false; }));
-        // lane l holds token l % 16 and hidden units 4 (l / 16) .. + 3 of each 16 x 16 tile
-#pragma unroll
-        for (int j = 0; j < S::kN; ++j) {
-            const int32_t row = 16 * (wn * S::kN + j) + (lane & 15);
-            if (row >= tile.rows) continue;
-            uint16_t* out = hidden + (int64_t)(tile.row0 + row) * s;
-#pragma unroll
-            for (int i = 0; i < S::kS; ++i) {
-                const int32_t c = s0 + 16 * (ws * S::kS + i) + 4 * (lane >> 4);
-                if (c >= s) continue;
-                float v[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] = g[i][j][q] * ffn_sigmoid(g[i][j][q]) * u[i][j][q];
-                *reinterpret_cast<uint2*>(out + c) = pack_bf16x4(v[0], v[1], v[2], v[3]);
-            }
-        }
-    });
 }
 
 // ------------------------------------------------------------------------------ down
@@ -518,8 +416,8 @@ hipError_t forward(const FfnPlan& p, const FfnArgs& a, uint16_t* y, char* ws, hi
     uint16_t* hidden = reinterpret_cast<uint16_t*>(ws + p.off_hidden);
     using U = UpShape<BM>;
     using D = DownShape<BM>;
-    ffn_up_kernel<BM><<<grid_of(p.tiles * ((a.s + U::kUnits - 1) / U::kUnits)), U::kThreads, 0, stream>>>(
-        a, ws + p.off_tiles, hidden);
+    ffn_up_kernel<BM, false><<<grid_of(p.tiles * ((a.s + U::kUnits - 1) / U::kUnits)), U::kThreads, 0, stream>>>(
+        a, ws + p.off_tiles, hidden, UpBackward{});
     const int32_t hspan = ffn_span(a.s, D::kCols, p.tiles, a.h);
     ffn_down_kernel<BM><<<grid_of(p.tiles * ((a.h + hspan - 1) / hspan)), D::kThreads, 0, stream>>>(
         a, ws + p.off_tiles, hidden, hspan, y);

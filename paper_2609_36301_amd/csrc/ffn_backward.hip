@@ -8,9 +8,11 @@
 //
 // Kernels of one call (entries in the order of Sort + Count, cut into tiles of one expert):
 //   ffn_tiles     lists the tiles
-//   ffn_bwd_up    G, U and dA0 of one tile and 64 hidden units: [dG dU] and gate A (bf16, sorted
-//                 order) and the partial sums of dgate
-//   ffn_bwd_dx    [dG dU] W1t[e] per entry (fp32, entry order)
+//   ffn_bwd_up    G, U and dA0 of one tile and 64 hidden units: [dG dU] and gate A (bf16, sorted order) and
+//                 the partial sums of dgate; tiles of 256 rows take two kernels instead,
+//   ffn_bwd_rows  dA0 = du_t W2t[e] (fp32, sorted order), and
+//   ffn_up        G and U, with the same results from them and dA0
+//   ffn_bwd_rows  [dG dU] W1t[e] per entry (fp32, entry order)
 //   ffn_bwd_sum   dx: the k entries of a token added in order; dgate: the partials added in order
 //   ffn_bwd_dw    dW1t and dW2t: contractions over the rows of an expert; an expert without rows gets
 //                 zeros
@@ -25,17 +27,22 @@
 
 #include "ffn.h"
 #include "ffn_device.h"
+#include "ffn_up.h"
 
 namespace more {
 
-// ------------------------------------------------------------------------------ up
+// ------------------------------------------------------------------------------ up, tiles of up to 128 rows
+// (Two kernels for tiles of 256 rows: there the matrix products count, a tile of 128 hidden units halves
+// what the caches deliver, and three sets of accumulators do not fit; 32 experts of s = 1024, h = 2048
+// 654 us against 820.  For the 4096 experts of s = 64, h = 512 this one kernel takes 213 us against 235.)
 // A workgroup computes one tile and kUnits hidden units: first G and U (x rows against the gate and up
 // rows of W1t), then dA0 (du rows against a column tile of W2t) into other accumulators.  In turn rather
 // than side by side: a stage is smaller by the second pair of operands, so twice as many workgroups fit
 // a CU (or a tile twice as large).
 template <int BM>
 struct BwdUpShape {
-    static constexpr int kWaves = BM == 256 ? 8 : 4;
+    static_assert(BM <= 128, "");
+    static constexpr int kWaves = 4;
     static constexpr int kThreads = 64 * kWaves;
     static constexpr int kWavesS = BM >= 64 ? 2 : 4;
     static constexpr int kUnits = 64;
@@ -200,7 +207,7 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
             dot += __shfl_xor(dot, 32, 64);
             if (lane < 16) dsum[ws][row] = dot;
         }
-        if (a.dgate) {
+        if (dgp) {
             ffn_barrier<63>();
             for (int32_t row = threadIdx.x; row < tile.rows; row += S::kThreads) {
                 float v = 0.0f;
@@ -212,74 +219,87 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
     });
 }
 
-// ------------------------------------------------------------------------------ dx of the entries
-// As ffn_down with [dG dU] as the rows and W1t[e] [2s][h] as a column tile (contraction over 2s).
+// ------------------------------------------------------------------------------ rows times weights
+// out = rows W[e] with fp32 results, for the two products whose weights lie with the contraction axis
+// slowest: dA0 = du W2t[e] (the token's row of du, contraction over h, results in sorted order) and the
+// entries' shares of dx = [dG dU] W1t[e] (contraction over 2s, results in entry order).  The weights are a
+// column tile (M side), the rows a row tile (N side).  A workgroup computes `span` columns in steps of
+// kCols; the pipeline runs over (column step, contraction step) pairs.
+constexpr int rows_threads(int bm) { return bm == 256 ? 512 : 256; }
 template <int BM>
-struct BwdDxShape {
-    static constexpr int kWaves = BM == 256 ? 8 : 4;
-    static constexpr int kThreads = 64 * kWaves;
+struct RowsShape {
+    static constexpr int kThreads = rows_threads(BM);
+    static constexpr int kWaves = kThreads / 64;
     static constexpr int kCols = 128;
     static constexpr int kWavesM = BM >= 64 ? 2 : 4;
     static constexpr int kM = kCols / kWavesM / 16;
     static constexpr int kN = BM / (kWaves / kWavesM) / 16;
-    static constexpr int kStages = 2;
     static constexpr int kRowsAt = kCols * 128;
     static constexpr int kStageBytes = kRowsAt + BM * 128;
 };
 
-template <int BM>
-__global__ __launch_bounds__(BwdDxShape<BM>::kThreads, 2) void ffn_bwd_dx_kernel(FfnArgs a, const void* __restrict__ list,
-                                                                 const uint16_t* __restrict__ dgu, int32_t hspan,
-                                                                 float* __restrict__ dxs) {
-    using S = BwdDxShape<BM>;
-    __shared__ __attribute__((aligned(1024))) char smem_raw[S::kStages * S::kStageBytes];
+template <int BM, bool TOKENS>
+__global__ __launch_bounds__(rows_threads(BM), 2) void ffn_bwd_rows_kernel(
+    FfnArgs a, const void* __restrict__ list, const uint16_t* __restrict__ rows_in, const uint16_t* __restrict__ W,
+    int32_t len, int32_t cols, int32_t span, float* __restrict__ out) {
+    using S = RowsShape<BM>;
+    __shared__ __attribute__((aligned(1024))) char smem_raw[2 * S::kStageBytes];
     LdsChar* smem = (LdsChar*)smem_raw;
     const FfnTile* tiles = ffn_tile_list(list);
-    const int32_t h = a.h, s2 = 2 * a.s;
     const int32_t n = a.T * a.k;
-    const int32_t spans = (h + hspan - 1) / hspan;
+    const int32_t spans = (cols + span - 1) / span;
     const int wave = ffn_wave(), lane = ffn_lane();
     const int wm = wave % S::kWavesM, wn = wave / S::kWavesM;
     const int64_t total = (int64_t)*static_cast<const int32_t*>(list) * spans;
     ffn_for_each(total, [&](int64_t item) {
         const FfnTile tile = tiles[item / spans];
         if (tile.expert < 0) return;  // dropped entries have no share (ffn_bwd_sum leaves them out)
-        const int32_t h0 = (int32_t)(item % spans) * hspan, h1 = min(h, h0 + hspan);
-        const uint16_t* W = a.W1t + (int64_t)tile.expert * s2 * h;
+        const int32_t c0 = (int32_t)(item % spans) * span, c1 = min(cols, c0 + span);
+        const uint16_t* We = W + (int64_t)tile.expert * len * cols;
         RowTileLoader<BM, S::kWaves> rows;
-        rows.init([&](int i) { return dgu + (int64_t)(tile.row0 + min(i, tile.rows - 1)) * s2; });
+        rows.init([&](int i) {
+            const int32_t at = tile.row0 + min(i, tile.rows - 1);
+            if constexpr (!TOKENS) return rows_in + (int64_t)at * len;
+            const uint32_t p = a.sorted[at];
+            return rows_in + (int64_t)(p < (uint32_t)n ? p / (uint32_t)a.k : 0) * len;
+        });
         ColTileLoader<S::kCols, S::kWaves> weights;
         weights.init();
-        uint32_t place[S::kN];
+        int64_t place[S::kN];  // of the lane's rows in out; -1: not wanted
 #pragma unroll
         for (int j = 0; j < S::kN; ++j) {
             const int32_t row = 16 * (wn * S::kN + j) + (lane & 15);
-            place[j] = row < tile.rows ? (uint32_t)a.sorted[tile.row0 + row] : 0xFFFFFFFFu;
+            place[j] = row < tile.rows ? tile.row0 + row : -1;
+            if (!TOKENS && row < tile.rows) {
+                const uint32_t p = (uint32_t)a.sorted[tile.row0 + row];
+                place[j] = p < (uint32_t)n ? (int64_t)p : -1;
+            }
         }
         f32x4 acc[S::kM][S::kN];
 #pragma unroll
         for (int i = 0; i < S::kM; ++i)
 #pragma unroll
             for (int j = 0; j < S::kN; ++j) acc[i][j] = zero_f32x4();
-        const int32_t ksteps = (s2 + kFfnBK - 1) / kFfnBK;
-        const int32_t hsteps = (h1 - h0 + S::kCols - 1) / S::kCols;
-        int32_t lh = h0, lk = 0, ch = h0, ck = 0;
+        const int32_t ksteps = (len + kFfnBK - 1) / kFfnBK;
+        const int32_t csteps = (c1 - c0 + S::kCols - 1) / S::kCols;
+        // (column step, contraction step) of the next load and of the next product
+        int32_t lc = c0, lk = 0, cc = c0, ck = 0;
         using G = FfnGroups<S::kM>;
         using M = FfnFragments<G::kSize>;
         using N = FfnFragments<S::kN>;
         using Stage = StagePair<decltype(weights), decltype(rows)>;
         ffn_pipeline_staged<Stage, M, N>(
-            ksteps * hsteps, 16 * wn * S::kN < tile.rows,
+            ksteps * csteps, 16 * wn * S::kN < tile.rows,
             [&](int, Stage& st) {
                 const int32_t k0 = lk * kFfnBK;
-                weights.fetch(st.a, h - lh, [&](int i) {
+                weights.fetch(st.a, cols - lc, [&](int i) {
                     const int kappa = k0 + weights.row(i);
-                    return kappa < s2 ? W + (int64_t)kappa * h + lh : nullptr;
+                    return kappa < len ? We + (int64_t)kappa * cols + lc : nullptr;
                 });
-                rows.fetch(st.b, k0, s2);
+                rows.fetch(st.b, k0, len);
                 if (++lk == ksteps) {
                     lk = 0;
-                    lh += S::kCols;
+                    lc += S::kCols;
                 }
             },
             [&](int slot, const Stage& st) {
@@ -314,14 +334,14 @@ __global__ __launch_bounds__(BwdDxShape<BM>::kThreads, 2) void ffn_bwd_dx_kernel
                     for (int j = 0; j < S::kN; ++j) {
 #pragma unroll
                         for (int i = 0; i < S::kM; ++i) {
-                            const int32_t c = ch + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
-                            if (place[j] < (uint32_t)n && c < h1)
-                                *reinterpret_cast<f32x4*>(dxs + (int64_t)place[j] * h + c) = acc[i][j];
+                            const int32_t c = cc + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
+                            if (place[j] >= 0 && c < c1)
+                                *reinterpret_cast<f32x4*>(out + place[j] * cols + c) = acc[i][j];
                             acc[i][j] = zero_f32x4();
                         }
                     }
                     ck = 0;
-                    ch += S::kCols;
+                    cc += S::kCols;
                     return false;
                 }));
     });
@@ -440,7 +460,7 @@ __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __res
                 }
                 const int32_t c = (GATHER_P ? ch : other) + 64 * wm;
                 const int32_t r = (GATHER_P ? other : ch) + 16 * (wn * kN + j);
-                flush_rows(scratch, ((GATHER_P ? h1 : cols_out) - c) * 2, [&](int row) {
+                flush_rows<true>(scratch, ((GATHER_P ? h1 : cols_out) - c) * 2, [&](int row) {
                     return r + row < (GATHER_P ? rows_out : h1) ? o + (int64_t)(r + row) * cols_out + c : nullptr;
                 });
             }
@@ -538,22 +558,33 @@ unsigned grid_of(int64_t items) {
     return (unsigned)(std::min<int64_t>((items + 7) / 8, kMaxBlocks / 8) * 8);
 }
 
-// Workgroups along the hidden units of ffn_bwd_up: a partial sum of dgate each.
-int32_t dgate_parts(int32_t s) {
-    return (s + BwdUpShape<256>::kUnits - 1) / BwdUpShape<256>::kUnits;
+// Workgroups along the hidden units: a partial sum of dgate each.
+int32_t dgate_parts(const FfnPlan& p, int32_t s) {
+    const int32_t units = p.bm == 256 ? UpShape<256>::kUnits : BwdUpShape<128>::kUnits;
+    return (s + units - 1) / units;
 }
 
 template <int BM>
 void rows_launch(const FfnPlan& p, const FfnArgs& a, char* ws, hipStream_t stream) {
+    using R = RowsShape<BM>;
+    const void* list = ws + p.off_tiles;
     uint16_t* hidden = reinterpret_cast<uint16_t*>(ws + p.off_hidden);
     uint16_t* dgu = reinterpret_cast<uint16_t*>(ws + p.off_dgu);
-    using U = BwdUpShape<BM>;
-    using D = BwdDxShape<BM>;
-    ffn_bwd_up_kernel<BM><<<grid_of(p.tiles * ((a.s + U::kUnits - 1) / U::kUnits)), U::kThreads, 0, stream>>>(
-        a, ws + p.off_tiles, hidden, dgu, reinterpret_cast<float*>(ws + p.off_dgp));
-    const int32_t hspan = ffn_span(2 * a.s, D::kCols, p.tiles, a.h);
-    ffn_bwd_dx_kernel<BM><<<grid_of(p.tiles * ((a.h + hspan - 1) / hspan)), D::kThreads, 0, stream>>>(
-        a, ws + p.off_tiles, dgu, hspan, reinterpret_cast<float*>(ws + p.off_dxs));
+    float* dgp = a.dgate ? reinterpret_cast<float*>(ws + p.off_dgp) : nullptr;
+    const unsigned up_blocks = grid_of(p.tiles * dgate_parts(p, a.s));
+    if constexpr (BM == 256) {
+        float* dA0 = reinterpret_cast<float*>(ws + p.off_da0);
+        const int32_t span = ffn_span(a.h, R::kCols, p.tiles, a.s);
+        ffn_bwd_rows_kernel<BM, true><<<grid_of(p.tiles * ((a.s + span - 1) / span)), R::kThreads, 0, stream>>>(
+            a, list, a.du, a.W2t, a.h, a.s, span, dA0);
+        ffn_up_kernel<BM, true><<<up_blocks, UpShape<BM>::kThreads, 0, stream>>>(a, list, hidden,
+                                                                              UpBackward{dA0, dgu, dgp});
+    } else {
+        ffn_bwd_up_kernel<BM><<<up_blocks, BwdUpShape<BM>::kThreads, 0, stream>>>(a, list, hidden, dgu, dgp);
+    }
+    const int32_t span = ffn_span(2 * a.s, R::kCols, p.tiles, a.h);
+    ffn_bwd_rows_kernel<BM, false><<<grid_of(p.tiles * ((a.h + span - 1) / span)), R::kThreads, 0, stream>>>(
+        a, list, dgu, a.W1t, 2 * a.s, a.h, span, reinterpret_cast<float*>(ws + p.off_dxs));
 }
 
 // One weight gradient: tiles of rt x ct, `other` of them across h.
@@ -586,10 +617,12 @@ void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t 
     size_t at = p->workspace_bytes;
     p->off_dgu = at;
     at += align256((size_t)p->n * 2 * s * 2);
+    p->off_da0 = at;
+    at += p->bm == 256 ? align256((size_t)p->n * s * 4) : 0;
     p->off_dxs = at;
     at += align256((size_t)p->n * h * 4);
     p->off_dgp = at;
-    at += align256((size_t)p->n * dgate_parts(s) * 4);
+    at += align256((size_t)p->n * dgate_parts(*p, s) * 4);
     p->workspace_bytes = at;
 }
 
@@ -609,7 +642,7 @@ hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspa
         const int64_t gateblocks = a.dgate ? std::min<int64_t>(((int64_t)n + 255) / 256, 1 << 14) : 0;
         ffn_bwd_sum_kernel<<<(unsigned)(colblocks + gateblocks), 256, 0, stream>>>(
             reinterpret_cast<const float*>(ws + p.off_dxs), a.idx, a.T, a.h, a.M, a.k, a.dx, colblocks,
-            reinterpret_cast<const float*>(ws + p.off_dgp), dgate_parts(a.s), a.sorted, a.dgate);
+            reinterpret_cast<const float*>(ws + p.off_dgp), dgate_parts(p, a.s), a.sorted, a.dgate);
     }
     const uint16_t* hidden = reinterpret_cast<const uint16_t*>(ws + p.off_hidden);
     const uint16_t* dgu = reinterpret_cast<const uint16_t*>(ws + p.off_dgu);
