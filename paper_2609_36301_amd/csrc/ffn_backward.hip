@@ -135,7 +135,7 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
         using G = FfnGroups<S::kS>;
         using M2 = FfnFragments<G::kSize>;
         using Stage = StagePair<decltype(rows), decltype(down)>;
-        ffn_pipeline_staged<Stage, M2, N>(
+        ffn_pipeline_staged<Stage, 2, M2, N>(
             hsteps, live,
             [&](int step, Stage& st) {
                 const int32_t k0 = step * kFfnBK;
@@ -230,7 +230,7 @@ template <int BM>
 struct RowsShape {
     static constexpr int kThreads = rows_threads(BM);
     static constexpr int kWaves = kThreads / 64;
-    static constexpr int kCols = 128;
+    static constexpr int kCols = BM == 256 ? 256 : 128;
     static constexpr int kWavesM = BM >= 64 ? 2 : 4;
     static constexpr int kM = kCols / kWavesM / 16;
     static constexpr int kN = BM / (kWaves / kWavesM) / 16;
@@ -284,11 +284,11 @@ __global__ __launch_bounds__(rows_threads(BM), 2) void ffn_bwd_rows_kernel(
         const int32_t csteps = (c1 - c0 + S::kCols - 1) / S::kCols;
         // (column step, contraction step) of the next load and of the next product
         int32_t lc = c0, lk = 0, cc = c0, ck = 0;
-        using G = FfnGroups<S::kM>;
+        using G = FfnGroups<S::kM, S::kM == 8 ? 4 : 2>;
         using M = FfnFragments<G::kSize>;
         using N = FfnFragments<S::kN>;
         using Stage = StagePair<decltype(weights), decltype(rows)>;
-        ffn_pipeline_staged<Stage, M, N>(
+        ffn_pipeline_staged<Stage, G::kGroups, M, N>(
             ksteps * csteps, 16 * wn * S::kN < tile.rows,
             [&](int, Stage& st) {
                 const int32_t k0 = lk * kFfnBK;
@@ -407,8 +407,9 @@ __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __res
     const int32_t rows_out = d.rows_out, cols_out = d.cols_out, hspan = d.hspan;
     uint16_t* out = d.out;
     constexpr int kStageBytes = (CT + RT) * 128;
-    constexpr int kWavesM = CT / 64, kWavesN = WAVES / kWavesM;
-    constexpr int kM = 4, kN = RT / kWavesN / 16;  // 16 x 16 tiles per wave: 64 columns, a line of out
+    constexpr int kWavesM = CT >= 128 ? 2 : 1, kWavesN = WAVES / kWavesM;
+    constexpr int kM = CT / kWavesM / 16, kN = RT / kWavesN / 16;  // 16 x 16 tiles per wave
+    static_assert(kM % 4 == 0, "whole lines of out: 64 columns");
     using PLoader = ColTileLoader<CT, WAVES>;
     using QLoader = ColTileLoader<RT, WAVES>;
     constexpr int kGathered = PLoader::kGroups;  // rows per lane of either operand
@@ -452,30 +453,32 @@ __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __res
         auto store = [&] {
             uint16_t* o = out + (int64_t)e * rows_out * cols_out;
 #pragma unroll
-            for (int j = 0; j < kN; ++j) {
+            for (int j = 0; j < kN; ++j)
 #pragma unroll
-                for (int i = 0; i < kM; ++i) {
-                    place_bf16(scratch, i, acc[i][j]);
-                    acc[i][j] = zero_f32x4();
+                for (int i0 = 0; i0 < kM; i0 += 4) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        place_bf16(scratch, i, acc[i0 + i][j]);
+                        acc[i0 + i][j] = zero_f32x4();
+                    }
+                    const int32_t c = (GATHER_P ? ch : other) + 16 * (wm * kM + i0);
+                    const int32_t r = (GATHER_P ? other : ch) + 16 * (wn * kN + j);
+                    flush_rows<true>(scratch, ((GATHER_P ? h1 : cols_out) - c) * 2, [&](int row) {
+                        return r + row < (GATHER_P ? rows_out : h1) ? o + (int64_t)(r + row) * cols_out + c : nullptr;
+                    });
                 }
-                const int32_t c = (GATHER_P ? ch : other) + 64 * wm;
-                const int32_t r = (GATHER_P ? other : ch) + 16 * (wn * kN + j);
-                flush_rows<true>(scratch, ((GATHER_P ? h1 : cols_out) - c) * 2, [&](int row) {
-                    return r + row < (GATHER_P ? rows_out : h1) ? o + (int64_t)(r + row) * cols_out + c : nullptr;
-                });
-            }
             ch += kStep;
         };
         if (ksteps == 0) {  // no entries: zeros
             for (int32_t step = 0; step < hsteps; ++step) store();
             continue;
         }
-        using G = FfnGroups<kM>;
+        using G = FfnGroups<kM, kM == 8 ? 4 : 2>;
         using MF = FfnFragments<G::kSize>;
         using NF = FfnFragments<kN>;
         using Stage = StagePair<PLoader, QLoader>;
         fetch(0);
-        ffn_pipeline_staged<Stage, MF, NF>(
+        ffn_pipeline_staged<Stage, G::kGroups, MF, NF>(
             ksteps * hsteps, true,
             [&](int, Stage& st) {
                 const int32_t i0 = begin + lk * kFfnBK;
@@ -533,18 +536,18 @@ __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __res
 
 // Both products in one launch (the second one's workgroups follow the first one's, so that the last of one
 // and the first of the other share the chip).
-template <int CT2, int RT, int WAVES>
+template <int CT1, int CT2, int RT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(DwArgs w1, DwArgs w2,
                                                                 const int32_t* __restrict__ offsets,
                                                                 const int32_t* __restrict__ sorted, int32_t n,
                                                                 int32_t k, int32_t M) {
-    __shared__ __attribute__((aligned(1024))) char smem_raw[2 * (128 + RT) * 128];
+    __shared__ __attribute__((aligned(1024))) char smem_raw[2 * (CT1 + RT) * 128];
     __shared__ __attribute__((aligned(16))) char scratch_raw[WAVES * kFfnScratch];
     LdsChar* smem = (LdsChar*)smem_raw;
     LdsChar* scratch = (LdsChar*)scratch_raw + ffn_wave() * kFfnScratch;
     const int32_t block = (int32_t)blockIdx.x;
     if (block < w1.blocks)
-        ffn_bwd_dw<128, RT, WAVES, true>(w1, offsets, sorted, n, k, M, smem, scratch, block);
+        ffn_bwd_dw<CT1, RT, WAVES, true>(w1, offsets, sorted, n, k, M, smem, scratch, block);
     else
         ffn_bwd_dw<CT2, RT, WAVES, false>(w2, offsets, sorted, n, k, M, smem, scratch, block - w1.blocks);
 }
@@ -602,11 +605,11 @@ DwArgs dw_args(const FfnPlan& p, const FfnArgs& a, const uint16_t* P, const uint
     return d;
 }
 
-template <int CT2, int RT, int WAVES>
+template <int CT1, int CT2, int RT, int WAVES>
 void dw_launch(const FfnPlan& p, const FfnArgs& a, const uint16_t* hidden, const uint16_t* dgu, hipStream_t stream) {
-    const DwArgs w1 = dw_args(p, a, a.x, dgu, 2 * a.s, a.h, (2 * a.s + RT - 1) / RT, 128, a.dW1t);
+    const DwArgs w1 = dw_args(p, a, a.x, dgu, 2 * a.s, a.h, (2 * a.s + RT - 1) / RT, CT1, a.dW1t);
     const DwArgs w2 = dw_args(p, a, hidden, a.du, a.h, a.s, (a.s + CT2 - 1) / CT2, RT, a.dW2t);
-    ffn_bwd_dw_kernel<CT2, RT, WAVES><<<(unsigned)(w1.blocks + w2.blocks), 64 * WAVES, 0, stream>>>(
+    ffn_bwd_dw_kernel<CT1, CT2, RT, WAVES><<<(unsigned)(w1.blocks + w2.blocks), 64 * WAVES, 0, stream>>>(
         w1, w2, a.offsets, a.sorted, (int32_t)p.n, a.k, a.M);
 }
 
@@ -647,9 +650,9 @@ hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspa
     const uint16_t* hidden = reinterpret_cast<const uint16_t*>(ws + p.off_hidden);
     const uint16_t* dgu = reinterpret_cast<const uint16_t*>(ws + p.off_dgu);
     if (p.bm == 256)
-        dw_launch<128, 256, 8>(p, a, hidden, dgu, stream);
+        dw_launch<256, 256, 256, 8>(p, a, hidden, dgu, stream);
     else
-        dw_launch<64, 128, 4>(p, a, hidden, dgu, stream);
+        dw_launch<128, 64, 128, 4>(p, a, hidden, dgu, stream);
     return hipGetLastError();
 }
 

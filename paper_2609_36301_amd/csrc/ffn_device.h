@@ -237,36 +237,37 @@ __device__ __forceinline__ void ffn_for_each(int64_t total, F body) {
     }
 }
 
-// The products of `steps` stages of an LDS ring of `stages`.  A stage's product runs in four parts: for
-// each half kk of its contraction values, the M-side fragments in two groups against the N-side fragments.
+// The products of `steps` stages of an LDS ring of `stages`.  A stage's product runs in parts: for each
+// half kk of its contraction values, the M-side fragments in GROUPS groups against the N-side fragments.
 // `w` gives read_m(slot, kk, group, m) and read_n(slot, kk, n), which fill fragments of types M and N,
 // multiply(group, m, n), and done(), which follows the last product of a step.  The fragments of a part
 // are read while the part before is multiplied, across steps too, so that the LDS works while the matrix
 // cores do.  turn(step, slot, stored) stands before the last part of every step but the last: there the
 // next stage has to become readable, and the present one has been read and can be filled again.
 // `stored` holds what done() returned after the step before (bit 0) and the one before that (bit 1).
-template <typename M, typename N, typename T, typename W>
+template <int GROUPS, typename M, typename N, typename T, typename W>
 __device__ __forceinline__ void ffn_steps(int steps, int stages, T turn, W w) {
-    M m0, m1;
-    N n0, n1;
-    w.read_n(0, 0, n0);
-    w.read_m(0, 0, 0, m0);
+    constexpr int kParts = 2 * GROUPS;
+    M m[2];
+    N n[2];
+    w.read_n(0, 0, n[0]);
+    w.read_m(0, 0, 0, m[0]);
     int slot = 0, stored = 0;
     for (int step = 0; step < steps; ++step) {
         const int next = slot + 1 == stages ? 0 : slot + 1;
-        w.read_m(slot, 0, 1, m1);
-        w.multiply(0, m0, n0);
-        w.read_n(slot, 1, n1);
-        w.read_m(slot, 1, 0, m0);
-        w.multiply(1, m1, n0);
-        w.read_m(slot, 1, 1, m1);
-        w.multiply(0, m0, n1);
-        if (step + 1 < steps) {
-            turn(step, slot, stored);
-            w.read_n(next, 0, n0);
-            w.read_m(next, 0, 0, m0);
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+            const int then = part + 1;
+            if (then < kParts) {
+                if (then == GROUPS) w.read_n(slot, 1, n[1]);
+                w.read_m(slot, then / GROUPS, then % GROUPS, m[then & 1]);
+            } else if (step + 1 < steps) {
+                turn(step, slot, stored);
+                w.read_n(next, 0, n[0]);
+                w.read_m(next, 0, 0, m[0]);
+            }
+            w.multiply(part % GROUPS, m[part & 1], n[part / GROUPS]);
         }
-        w.multiply(1, m1, n1);
         stored = (stored << 1 | (w.done() ? 1 : 0)) & 3;
         slot = next;
     }
@@ -304,7 +305,7 @@ __device__ __forceinline__ void ffn_pipeline(int steps, bool live, L load, W w) 
         asm volatile("" ::: "memory");  // (the stores that follow stay younger than these loads)
     };
     if (live) {
-        ffn_steps<M, N>(steps, STAGES, turn, w);
+        ffn_steps<2, M, N>(steps, STAGES, turn, w);
     } else {
         int slot = 0;
         for (int step = 0; step + 1 < steps; ++step) {
@@ -323,7 +324,7 @@ struct StagePair {
 
 // The pipeline by way of registers, two stages in LDS: fetch(step, s) reads a stage into registers,
 // put(slot, s) writes it to LDS a step later, and another step later it is multiplied.
-template <typename S, typename M, typename N, typename F, typename P, typename W>
+template <typename S, int GROUPS, typename M, typename N, typename F, typename P, typename W>
 __device__ __forceinline__ void ffn_pipeline_staged(int steps, bool live, F fetch, P put, W w) {
     S s;
     ffn_barrier<63>();  // the previous work item's reads are over
@@ -344,7 +345,7 @@ __device__ __forceinline__ void ffn_pipeline_staged(int steps, bool live, F fetc
         if (step + 3 < steps) fetch(step + 3, s);
     };
     if (live) {
-        ffn_steps<M, N>(steps, 2, turn, w);
+        ffn_steps<GROUPS, M, N>(steps, 2, turn, w);
     } else {
         for (int step = 0; step + 1 < steps; ++step) turn(step, step & 1, 0);
     }
@@ -366,10 +367,11 @@ template <int COUNT>
 struct FfnFragments {
     bf16x8 v[COUNT];
 };
-// M-side tiles of group 0 (the first half, rounded up) and of the part in all
-template <int TILES>
+// TILES M-side tiles in GROUPS groups (the last ones may be short).
+template <int TILES, int GROUPS = 2>
 struct FfnGroups {
-    static constexpr int kSize = (TILES + 1) / 2;
+    static constexpr int kGroups = GROUPS;
+    static constexpr int kSize = (TILES + GROUPS - 1) / GROUPS;
     __device__ static constexpr int tile(int group, int i) { return group * kSize + i; }
 };
 
