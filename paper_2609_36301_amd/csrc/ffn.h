@@ -28,7 +28,8 @@ struct FfnPlan {
     int64_t n;        // T k entries
     int32_t bm;       // rows of a tile (all of one expert)
     int64_t tiles;    // bound on the number of tiles
-    size_t off_tiles, off_hidden, off_dgu, off_da0, off_dxs, off_dgp;
+    int32_t sums;     // workgroups that count tiles ahead of the list (0: none)
+    size_t off_tiles, off_sums, off_hidden, off_dgu, off_da0, off_dxs, off_dgp;
     size_t workspace_bytes;
 };
 
@@ -45,6 +46,6 @@ inline int32_t ffn_span(int32_t len, int32_t step, int64_t groups, int32_t cols)
 }
 
 // Lists the tiles (shared by both directions).
-hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* tiles, hipStream_t stream);
+hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* workspace, hipStream_t stream);
 
 }  // namespace more

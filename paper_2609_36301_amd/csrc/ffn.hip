@@ -25,16 +25,41 @@
 namespace more {
 
 // ------------------------------------------------------------------------------ tiles
-// A workgroup lists the tiles of 1024 experts, one per thread; it counts the tiles of all earlier experts
-// itself (one launch, no cross-workgroup sum).  The last workgroup adds the tiles of the dropped entries.
+// A workgroup lists the tiles of 1024 experts, one per thread; up to kTileAlone experts it counts the tiles
+// of all earlier experts itself (one launch), beyond it adds their workgroups' counts, which
+// ffn_tile_sums_kernel has made (counting 2^20 experts' offsets in every workgroup would be 2^29 reads).
+// The last workgroup adds the tiles of the dropped entries.
 // Offsets that Sort + Count cannot have written are cut to [0, n], and tiles past the list's end are not
 // written, so that no call reads or writes outside its buffers.
 constexpr int kTileThreads = 1024;
+constexpr int32_t kTileAlone = 1 << 16;
 
 __device__ __forceinline__ int32_t ffn_cut(int32_t v, int32_t n) { return v < 0 ? 0 : v > n ? n : v; }
 
+// The tiles of expert e, from its offsets.
+__device__ __forceinline__ int32_t ffn_tile_count(const int32_t* offsets, int32_t e, int32_t n, int32_t log_bm) {
+    const int32_t len = ffn_cut(offsets[e + 1], n) - ffn_cut(offsets[e], n);
+    return len > 0 ? (len + (1 << log_bm) - 1) >> log_bm : 0;
+}
+
+__global__ __launch_bounds__(kTileThreads) void ffn_tile_sums_kernel(const int32_t* __restrict__ offsets, int32_t M,
+                                                                     int32_t n, int32_t log_bm,
+                                                                     int32_t* __restrict__ sums) {
+    __shared__ int32_t part[kTileThreads / 64];
+    const int32_t e = (int32_t)blockIdx.x * kTileThreads + threadIdx.x;
+    int32_t v = e < M ? ffn_tile_count(offsets, e, n, log_bm) : 0;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < kTileThreads / 64; ++w) v += part[w];
+    sums[blockIdx.x] = v;
+}
+
 __global__ __launch_bounds__(kTileThreads) void ffn_tiles_kernel(const int32_t* __restrict__ offsets, int32_t M,
                                                                  int32_t n, int32_t log_bm, int64_t bound,
+                                                                 const int32_t* __restrict__ sums,
                                                                  int32_t* __restrict__ list) {
     FfnTile* tiles = reinterpret_cast<FfnTile*>(reinterpret_cast<char*>(list) + kFfnTileHeader);
     __shared__ int32_t part[2][kTileThreads / 64];
@@ -46,10 +71,8 @@ __global__ __launch_bounds__(kTileThreads) void ffn_tiles_kernel(const int32_t* 
     const int32_t len = max(ffn_cut(offsets[min(e + 1, M)], n) - begin, 0);
     int32_t before = 0;
 #pragma unroll 8
-    for (int32_t q = tid; q < e0; q += kTileThreads) {
-        const int32_t a = ffn_cut(offsets[q], n), b = ffn_cut(offsets[q + 1], n);
-        before += b > a ? (b - a + bm1) >> log_bm : 0;
-    }
+    for (int32_t q = tid; q < (sums ? (int32_t)blockIdx.x : e0); q += kTileThreads)
+        before += sums ? sums[q] : ffn_tile_count(offsets, q, n, log_bm);
     // inclusive scan of the threads' tiles over the workgroup, and the sum of `before`
     const int32_t mine = (len + bm1) >> log_bm;
     int32_t scan = mine, sum = before;
@@ -139,9 +162,6 @@ __global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(Ff
             place[j] = row < tile.rows ? (uint32_t)a.sorted[tile.row0 + row] : 0xFFFFFFFFu;
             gate[j] = a.gate && place[j] < (uint32_t)n ? a.gate[place[j]] : 1.0f;
         }
-        bool full = true;  // (per wave) every lane stores all its rows
-#pragma unroll
-        for (int j = 0; j < S::kN; ++j) full = full && __all(place[j] < (uint32_t)n);
         f32x4 acc[S::kM][S::kN];
 #pragma unroll
         for (int i = 0; i < S::kM; ++i)
@@ -154,7 +174,7 @@ __global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(Ff
         using G = FfnGroups<S::kM>;
         using M = FfnFragments<G::kSize>;
         using N = FfnFragments<S::kN>;
-        ffn_pipeline<S::kStages, S::kLoads, S::kM * S::kN, M, N>(
+        ffn_pipeline<S::kStages, S::kLoads, M, N>(
             ksteps * hsteps, 16 * wn * S::kN < tile.rows,
             [&](int, int slot) {
                 LdsChar* at = smem + slot * S::kStageBytes;
@@ -189,15 +209,14 @@ __global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(Ff
                             }
                 },
                 [&] {
-                    if (++ck < ksteps) return false;
-                    const bool whole = full && ch + S::kCols <= h1;
+                    if (++ck < ksteps) return;
 #pragma unroll
                     for (int j = 0; j < S::kN; ++j) {
 #pragma unroll
                         for (int i = 0; i < S::kM; ++i) {
                             const int32_t c = ch + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
                             const f32x4 v = acc[i][j] * gate[j];
-                            if (whole || (place[j] < (uint32_t)n && c < h1))
+                            if (place[j] < (uint32_t)n && c < h1)
                                 *reinterpret_cast<uint2*>(y + (int64_t)place[j] * h + c) =
                                     pack_bf16x4(v[0], v[1], v[2], v[3]);
                             acc[i][j] = zero_f32x4();
@@ -205,7 +224,6 @@ __global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(Ff
                     }
                     ck = 0;
                     ch += S::kCols;
-                    return whole;
                 }));
     });
 }
@@ -409,6 +427,8 @@ void tiles_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* 
     p->bm = tile_rows(p->n, h, s, M);
     p->tiles = p->n / p->bm + std::min<int64_t>(M, p->n) + 1;
     p->off_tiles = 0;
+    p->off_sums = align256(kFfnTileHeader + (size_t)p->tiles * sizeof(FfnTile));
+    p->sums = M > kTileAlone ? (M + kTileThreads - 1) / kTileThreads : 0;
 }
 
 template <int BM>
@@ -439,14 +459,18 @@ static bool few(const FfnPlan& p, int32_t s, int32_t M) {
 
 void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {
     tiles_plan(T, h, s, M, k, p);
-    p->off_hidden = align256(kFfnTileHeader + (size_t)p->tiles * sizeof(FfnTile));
+    p->off_hidden = p->off_sums + align256((size_t)p->sums * 4);
     p->workspace_bytes = p->off_hidden + align256((size_t)p->n * s * 2);
 }
 
-hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* tiles, hipStream_t stream) {
+hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* workspace, hipStream_t stream) {
+    char* ws = static_cast<char*>(workspace);
     const unsigned blocks = (unsigned)(((int64_t)a.M + kTileThreads - 1) / kTileThreads);
-    ffn_tiles_kernel<<<blocks, kTileThreads, 0, stream>>>(a.offsets, a.M, (int32_t)p.n, __builtin_ctz(p.bm), p.tiles,
-                                                          static_cast<int32_t*>(tiles));
+    const int32_t log_bm = __builtin_ctz(p.bm);
+    int32_t* sums = p.sums ? reinterpret_cast<int32_t*>(ws + p.off_sums) : nullptr;
+    if (sums) ffn_tile_sums_kernel<<<blocks, kTileThreads, 0, stream>>>(a.offsets, a.M, (int32_t)p.n, log_bm, sums);
+    ffn_tiles_kernel<<<blocks, kTileThreads, 0, stream>>>(a.offsets, a.M, (int32_t)p.n, log_bm, p.tiles, sums,
+                                                          reinterpret_cast<int32_t*>(ws + p.off_tiles));
     return hipGetLastError();
 }
 
@@ -464,7 +488,7 @@ hipError_t ffn_launch(const FfnPlan& p, const FfnArgs& a, uint16_t* y, void* wor
             ffn_few_down_kernel<false, 2><<<blocks, 64 * kFewWaves, 0, stream>>>(a, hidden, y);
         return hipGetLastError();
     }
-    hipError_t e = ffn_tiles_launch(p, a, ws + p.off_tiles, stream);
+    hipError_t e = ffn_tiles_launch(p, a, ws, stream);
     if (e != hipSuccess) return e;
     switch (p.bm) {
         case 256: return forward<256>(p, a, y, ws, stream);

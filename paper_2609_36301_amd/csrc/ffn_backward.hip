@@ -96,7 +96,7 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
         // the gate rows are one group of M-side fragments, the up rows the other
         using M = FfnFragments<S::kS>;
         using N = FfnFragments<S::kN>;
-        ffn_pipeline<S::kStages, 0, 0, M, N>(
+        ffn_pipeline<S::kStages, 0, M, N>(
             (h + kFfnBK - 1) / kFfnBK, live,
             [&](int step, int slot) {
                 LdsChar* at = smem + slot * S::kStageBytes;
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
                             c = mfma_16x16x32(m.v[i], f.v[j], c);
                         }
                 },
-                [] { return false; }));
+                [] {}));
 #pragma unroll
         for (int i = 0; i < S::kS; ++i)
 #pragma unroll
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
                                 c = mfma_16x16x32(m.v[i], f.v[j], c);
                             }
                 },
-                [] { return false; }));
+                [] {}));
         // lane l holds token l % 16 and hidden units 4 (l / 16) .. + 3 of each 16 x 16 tile
 #pragma unroll
         for (int j = 0; j < S::kN; ++j) {
@@ -329,7 +329,7 @@ __global__ __launch_bounds__(rows_threads(BM), 2) void ffn_bwd_rows_kernel(
                             }
                 },
                 [&] {
-                    if (++ck < ksteps) return false;
+                    if (++ck < ksteps) return;
 #pragma unroll
                     for (int j = 0; j < S::kN; ++j) {
 #pragma unroll
@@ -342,7 +342,6 @@ __global__ __launch_bounds__(rows_threads(BM), 2) void ffn_bwd_rows_kernel(
                     }
                     ck = 0;
                     cc += S::kCols;
-                    return false;
                 }));
     });
 }
@@ -526,10 +525,9 @@ __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __res
                             }
                 },
                 [&] {
-                    if (++ck < ksteps) return false;
+                    if (++ck < ksteps) return;
                     ck = 0;
                     store();
-                    return false;
                 }));
     }
 }
@@ -633,7 +631,7 @@ hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspa
     char* ws = static_cast<char*>(workspace);
     const int32_t n = (int32_t)p.n;
     if (n > 0) {
-        hipError_t e = ffn_tiles_launch(p, a, ws + p.off_tiles, stream);
+        hipError_t e = ffn_tiles_launch(p, a, ws, stream);
         if (e != hipSuccess) return e;
         switch (p.bm) {
                 case 256: rows_launch<256>(p, a, ws, stream); break;

@@ -49,7 +49,6 @@ template <bool ONCE = false>
 __device__ __forceinline__ void ffn_dma16(const uint16_t* g, LdsChar* lds) {
     __builtin_amdgcn_global_load_lds(g, lds, 16, 0, ONCE ? 2 : 0);
 }
-__host__ __device__ constexpr int ffn_most(int n) { return n < 63 ? n : 63; }
 // Workgroup barrier that leaves at most VM of the wave's own vector memory operations outstanding.
 template <int VM>
 __device__ __forceinline__ void ffn_barrier() {
@@ -242,9 +241,8 @@ __device__ __forceinline__ void ffn_for_each(int64_t total, F body) {
 // `w` gives read_m(slot, kk, group, m) and read_n(slot, kk, n), which fill fragments of types M and N,
 // multiply(group, m, n), and done(), which follows the last product of a step.  The fragments of a part
 // are read while the part before is multiplied, across steps too, so that the LDS works while the matrix
-// cores do.  turn(step, slot, stored) stands before the last part of every step but the last: there the
-// next stage has to become readable, and the present one has been read and can be filled again.
-// `stored` holds what done() returned after the step before (bit 0) and the one before that (bit 1).
+// cores do.  turn(step, slot) stands before the last part of every step but the last: there the next stage
+// has to become readable, and the present one has been read and can be filled again.
 template <int GROUPS, typename M, typename N, typename T, typename W>
 __device__ __forceinline__ void ffn_steps(int steps, int stages, T turn, W w) {
     constexpr int kParts = 2 * GROUPS;
@@ -252,7 +250,7 @@ __device__ __forceinline__ void ffn_steps(int steps, int stages, T turn, W w) {
     N n[2];
     w.read_n(0, 0, n[0]);
     w.read_m(0, 0, 0, m[0]);
-    int slot = 0, stored = 0;
+    int slot = 0;
     for (int step = 0; step < steps; ++step) {
         const int next = slot + 1 == stages ? 0 : slot + 1;
 #pragma unroll
@@ -262,26 +260,23 @@ __device__ __forceinline__ void ffn_steps(int steps, int stages, T turn, W w) {
                 if (then == GROUPS) w.read_n(slot, 1, n[1]);
                 w.read_m(slot, then / GROUPS, then % GROUPS, m[then & 1]);
             } else if (step + 1 < steps) {
-                turn(step, slot, stored);
+                turn(step, slot);
                 w.read_n(next, 0, n[0]);
                 w.read_m(next, 0, 0, m[0]);
             }
             w.multiply(part % GROUPS, m[part & 1], n[part / GROUPS]);
         }
-        stored = (stored << 1 | (w.done() ? 1 : 0)) & 3;
+        w.done();
         slot = next;
     }
 }
 
 // The pipeline with direct-to-LDS loads: load(step, slot) issues LOADS of them per wave, STAGES stages
-// ahead.  A wave's own vector memory operations complete in the order in which they were issued, loads
-// and stores alike, so the next stage's loads are known to have landed while younger operations are
-// outstanding: the loads of later stages, and STORES stores where done() says that it issued exactly so
-// many.  A wave that has no wanted rows (live = false) only loads.
-template <int STAGES, int LOADS, int STORES, typename M, typename N, typename L, typename W>
+// ahead.  A wave's own vector memory operations complete in the order in which they were issued, so the
+// next stage's loads are known to have landed while those of later stages are outstanding.  A wave that
+// has no wanted rows (live = false) only loads.
+template <int STAGES, int LOADS, typename M, typename N, typename L, typename W>
 __device__ __forceinline__ void ffn_pipeline(int steps, bool live, L load, W w) {
-    static_assert(STAGES == 2 || STAGES == 3, "");
-    constexpr int kLeft = (STAGES - 2) * LOADS;  // loads younger than the next stage's
     ffn_barrier<0>();  // the previous work item's reads are over
 #pragma unroll
     for (int i = 0; i < STAGES; ++i)
@@ -291,25 +286,20 @@ __device__ __forceinline__ void ffn_pipeline(int steps, bool live, L load, W w) 
     } else {
         ffn_barrier<0>();
     }
-    auto turn = [&](int step, int slot, int stored) {
-        if (step + STAGES > steps) {
-            ffn_barrier<0>();
-        } else if (STORES > 0 && STAGES == 3 && stored == 3) {
-            ffn_barrier<ffn_most(kLeft + 2 * STORES)>();
-        } else if (STORES > 0 && (stored & 1)) {
-            ffn_barrier<ffn_most(kLeft + STORES)>();
+    auto turn = [&](int step, int slot) {
+        if (step + STAGES <= steps) {
+            ffn_barrier<(STAGES - 2) * LOADS>();
         } else {
-            ffn_barrier<kLeft>();
+            ffn_barrier<0>();
         }
         if (step + STAGES < steps) load(step + STAGES, slot);
-        asm volatile("" ::: "memory");  // (the stores that follow stay younger than these loads)
     };
     if (live) {
         ffn_steps<2, M, N>(steps, STAGES, turn, w);
     } else {
         int slot = 0;
         for (int step = 0; step + 1 < steps; ++step) {
-            turn(step, slot, 0);
+            turn(step, slot);
             slot = slot + 1 == STAGES ? 0 : slot + 1;
         }
     }
@@ -339,7 +329,7 @@ __device__ __forceinline__ void ffn_pipeline_staged(int steps, bool live, F fetc
     }
     if (steps > 2) fetch(2, s);
     ffn_barrier<63>();
-    auto turn = [&](int step, int slot, int) {
+    auto turn = [&](int step, int slot) {
         ffn_barrier<63>();
         if (step + 2 < steps) put(slot, s);
         if (step + 3 < steps) fetch(step + 3, s);
@@ -347,7 +337,7 @@ __device__ __forceinline__ void ffn_pipeline_staged(int steps, bool live, F fetc
     if (live) {
         ffn_steps<GROUPS, M, N>(steps, 2, turn, w);
     } else {
-        for (int step = 0; step + 1 < steps; ++step) turn(step, step & 1, 0);
+        for (int step = 0; step + 1 < steps; ++step) turn(step, step & 1);
     }
 }
 

@@ -72,7 +72,7 @@ __global__ __launch_bounds__(UpShape<BM>::kThreads, 2) void ffn_up_kernel(FfnArg
         // the gate rows are one group of M-side fragments, the up rows the other
         using M = FfnFragments<S::kS>;
         using N = FfnFragments<S::kN>;
-        ffn_pipeline<S::kStages, S::kLoads, 0, M, N>(
+        ffn_pipeline<S::kStages, S::kLoads, M, N>(
             (h + kFfnBK - 1) / kFfnBK, 16 * wn * S::kN < tile.rows,
             [&](int step, int slot) {
                 LdsChar* at = smem + slot * S::kStageBytes;
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(UpShape<BM>::kThreads, 2) void ffn_up_kernel(FfnArg
                             c = mfma_16x16x32(m.v[i], f.v[j], c);
                         }
                 },
-                [] { return false; }));
+                [] {}));
         // lane l holds token l % 16 and hidden units 4 (l / 16) .. + 3 of each 16 x 16 tile
         if constexpr (!BACKWARD) {
 #pragma unroll
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(UpShape<BM>::kThreads, 2) void ffn_up_kernel(FfnArg
 #pragma unroll
                 for (int i = 0; i < S::kS; ++i) {
                     const int32_t c = s0 + 16 * (ws * S::kS + i) + 4 * (lane >> 4);
-                    ahead[i] = zero_f32x4();  // (no share of dgate)
+                    ahead[i] = zero_f32x4();
                     if (in && c < s)
                         ahead[i] = *reinterpret_cast<const f32x4*>(back.dA0 + (int64_t)(tile.row0 + row) * s + c);
                 }
@@ -151,7 +151,8 @@ __global__ __launch_bounds__(UpShape<BM>::kThreads, 2) void ffn_up_kernel(FfnArg
                         const float sig = ffn_sigmoid(g[i][j][q]);
                         const float silu = g[i][j][q] * sig;
                         const float A = silu * u[i][j][q];
-                        dot = __builtin_fmaf(A, d[i][q], dot);
+                        // units past s repeat unit s - 1 and have no share
+                        dot = c0 + 16 * i + 4 * (lane >> 4) < s ? __builtin_fmaf(A, d[i][q], dot) : dot;
                         const float dA = gate * d[i][q];
                         g[i][j][q] = dA * u[i][j][q] * (sig + silu * (1.0f - sig));
                         u[i][j][q] = dA * silu;

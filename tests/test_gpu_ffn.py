@@ -68,6 +68,7 @@ CASES = {
     "tile256_skewed": dict(T=2500, h=528, s=264, M=4, k=1, hot=0.5, drop=0.02),
     "hot_expert": dict(T=400, h=64, s=16, M=300, k=2, hot=0.9),
     "many_experts": dict(T=33, h=64, s=8, M=5000, k=4, drop=0.2),
+    "past_2_16_experts": dict(T=400, h=32, s=40, M=70000, k=3, drop=0.05),
     "repeated_ids": dict(T=50, h=80, s=32, M=6, k=4, repeat=True),
     "many_rows": dict(T=3000, h=64, s=16, M=5, k=3, drop=0.01),
 }
