@@ -345,15 +345,29 @@ int32_t backward_blocks(int64_t T, int32_t h) {
     return (int32_t)std::min<int64_t>(rows, 1024);
 }
 
+// In launches of at most 2^22 workgroups (a launch may not have 2^32 threads along an axis).
 template <int W, int CH>
-hipError_t forward(const NormArgs& a, hipStream_t stream) {
-    constexpr int kRows = norm_rows(W);
-    const unsigned blocks = (unsigned)(((int64_t)a.T + kRows - 1) / kRows);
-    if (a.wide)
-        block_norm_kernel<W, CH, true><<<blocks, norm_threads(W), 0, stream>>>(a);
-    else
-        block_norm_kernel<W, CH, false><<<blocks, norm_threads(W), 0, stream>>>(a);
-    return hipGetLastError();
+hipError_t forward(NormArgs a, hipStream_t stream) {
+    constexpr int64_t kMaxRows = (int64_t)norm_rows(W) << 22;
+    const int64_t T = a.T, resid = a.wide ? 4 : 2;
+    for (int64_t t = 0; t < T; t += kMaxRows) {
+        a.T = (int32_t)std::min(T - t, kMaxRows);
+        const unsigned blocks = (unsigned)((a.T + norm_rows(W) - 1) / norm_rows(W));
+        if (a.wide)
+            block_norm_kernel<W, CH, true><<<blocks, norm_threads(W), 0, stream>>>(a);
+        else
+            block_norm_kernel<W, CH, false><<<blocks, norm_threads(W), 0, stream>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        const int64_t step = a.T * (int64_t)a.h;
+        a.r = static_cast<const char*>(a.r) + step * resid;
+        if (a.r_out) a.r_out = static_cast<char*>(a.r_out) + step * resid;
+        if (a.y) a.y += step * a.k;
+        if (a.u) a.u += step;
+        if (a.xn) a.xn += step;
+        if (a.gate) a.gate += a.T;
+    }
+    return hipSuccess;
 }
 
 template <int W, int CH>

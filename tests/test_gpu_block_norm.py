@@ -139,6 +139,25 @@ def test_backward_of_the_norm_alone_and_no_tokens(T, h):
     assert layer.block_norm(empty, w_before=d["w_before"]).xn.shape == (0, h)
 
 
+def test_more_rows_than_a_launch_takes():
+    """2^26 rows of 16 columns and a few more: the last rows, and those at the seam."""
+    torch = require_gpu()
+    from paper_2609_36301_amd import layer
+    T, h = (1 << 26) + 5, 16
+    announce("block_norm T=%d h=%d" % (T, h))
+    r = torch.empty((T, h), dtype=torch.bfloat16, device="cuda").normal_()
+    y = torch.empty((T, h), dtype=torch.bfloat16, device="cuda").normal_()
+    gate = torch.rand(T, device="cuda")
+    w = torch.rand(h, device="cuda") + 0.5
+    out = layer.block_norm(r, y, w_after=w, w_before=w, gate=gate, save_u=True)
+    for rows in (slice(0, 3), slice((1 << 24) - 2, (1 << 24) + 2), slice((1 << 25) - 1, (1 << 25) + 1), slice(T - 7, T)):
+        e = lambda t: t[rows].double().cpu().numpy()  # noqa: E731
+        wd = w.double().cpu().numpy()
+        want, bound = ref.block_norm(e(r), e(y)[:, None], wd, wd, e(gate), 1.0, np.float32(1e-6).item(), True, 16)
+        for name, v, b in zip(("r", "xn", "u"), want, bound):
+            check(name, getattr(out, name)[rows].float().cpu().numpy(), v, b, str(rows))
+
+
 def test_binding_refuses():
     torch = require_gpu()
     from paper_2609_36301_amd import layer
