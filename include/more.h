@@ -338,7 +338,7 @@ more_status more_route_lowrank_noalloc(const uint16_t* x, const uint16_t* R1t, c
  *   workspace / workspace_bytes   at least more_expert_ffn_workspace_size() bytes, 256-byte aligned
  *                              (NULL allowed when T == 0)
  * Limits: h a positive multiple of 16, s a positive multiple of 8, both at most 65536;
- * 1 <= k <= MORE_K_MAX (k may exceed M: an id may occur more than once in a token); T k <= 2^31 - 1,
+ * 1 <= k <= MORE_K_MAX (k may exceed M: an id may occur more than once in a token); T k <= 2^31 - 2^16,
  * M < 2^30.  T == 0 writes nothing.  offsets and sorted that are not those of idx give undefined values
  * in y (no access outside the buffers).
  * Numerics: fp32 accumulation of exact bf16 products; A is rounded to bf16 once, between the two

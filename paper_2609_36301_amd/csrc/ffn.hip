@@ -29,8 +29,9 @@ namespace more {
 // of all earlier experts itself (one launch), beyond it adds their workgroups' counts, which
 // ffn_tile_sums_kernel has made (counting 2^20 experts' offsets in every workgroup would be 2^29 reads).
 // The last workgroup adds the tiles of the dropped entries.
-// Offsets that Sort + Count cannot have written are cut to [0, n], and tiles past the list's end are not
-// written, so that no call reads or writes outside its buffers.
+// Offsets that Sort + Count cannot have written are cut to [0, n], tiles past the list's end are not written
+// and counts are 64 bits wide (offsets that go up and down can ask for n / bm tiles per expert), so that no
+// call reads or writes outside its buffers.
 constexpr int kTileThreads = 1024;
 constexpr int32_t kTileAlone = 1 << 16;
 
@@ -44,10 +45,10 @@ __device__ __forceinline__ int32_t ffn_tile_count(const int32_t* offsets, int32_
 
 __global__ __launch_bounds__(kTileThreads) void ffn_tile_sums_kernel(const int32_t* __restrict__ offsets, int32_t M,
                                                                      int32_t n, int32_t log_bm,
-                                                                     int32_t* __restrict__ sums) {
-    __shared__ int32_t part[kTileThreads / 64];
+                                                                     int64_t* __restrict__ sums) {
+    __shared__ int64_t part[kTileThreads / 64];
     const int32_t e = (int32_t)blockIdx.x * kTileThreads + threadIdx.x;
-    int32_t v = e < M ? ffn_tile_count(offsets, e, n, log_bm) : 0;
+    int64_t v = e < M ? ffn_tile_count(offsets, e, n, log_bm) : 0;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
@@ -59,49 +60,49 @@ __global__ __launch_bounds__(kTileThreads) void ffn_tile_sums_kernel(const int32
 
 __global__ __launch_bounds__(kTileThreads) void ffn_tiles_kernel(const int32_t* __restrict__ offsets, int32_t M,
                                                                  int32_t n, int32_t log_bm, int64_t bound,
-                                                                 const int32_t* __restrict__ sums,
+                                                                 const int64_t* __restrict__ sums,
                                                                  int32_t* __restrict__ list) {
     FfnTile* tiles = reinterpret_cast<FfnTile*>(reinterpret_cast<char*>(list) + kFfnTileHeader);
-    __shared__ int32_t part[2][kTileThreads / 64];
+    __shared__ int64_t part[2][kTileThreads / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int32_t bm1 = (1 << log_bm) - 1;
     const int32_t e0 = (int32_t)blockIdx.x * kTileThreads, e = e0 + tid;
     const int32_t valid = ffn_cut(offsets[M], n);
     const int32_t begin = ffn_cut(offsets[min(e, M)], n);
     const int32_t len = max(ffn_cut(offsets[min(e + 1, M)], n) - begin, 0);
-    int32_t before = 0;
+    int64_t before = 0;
 #pragma unroll 8
     for (int32_t q = tid; q < (sums ? (int32_t)blockIdx.x : e0); q += kTileThreads)
-        before += sums ? sums[q] : ffn_tile_count(offsets, q, n, log_bm);
+        before += sums ? sums[q] : (int64_t)ffn_tile_count(offsets, q, n, log_bm);
     // inclusive scan of the threads' tiles over the workgroup, and the sum of `before`
     const int32_t mine = (len + bm1) >> log_bm;
-    int32_t scan = mine, sum = before;
+    int64_t scan = mine, sum = before;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const int32_t o = __shfl_up(scan, d, 64);
+        const int64_t o = __shfl_up(scan, d, 64);
         scan += lane >= d ? o : 0;
         sum += __shfl_xor(sum, d, 64);
     }
     if (lane == 63) part[0][wave] = scan;
     if (lane == 0) part[1][wave] = sum;
     __syncthreads();
-    int32_t base = 0, total = 0;
+    int64_t base = 0, total = 0;
 #pragma unroll
     for (int w = 0; w < kTileThreads / 64; ++w) {
         total += part[0][w] + part[1][w];
         base += part[1][w] + (w < wave ? part[0][w] : 0);
     }
-    int64_t at = (int64_t)base + scan - mine;
-    for (int32_t r = 0; r < len; r += bm1 + 1, ++at)
-        if (at < bound) tiles[at] = FfnTile{e, begin + r, min(len - r, bm1 + 1), 0};
+    int64_t at = base + scan - mine;
+    for (int32_t r = 0; r < len && at < bound; r += bm1 + 1, ++at)
+        tiles[at] = FfnTile{e, begin + r, min(len - r, bm1 + 1), 0};
     if (blockIdx.x == gridDim.x - 1) {
         const int32_t extra = (n - valid + bm1) >> log_bm;
         for (int32_t r = tid; r < extra; r += kTileThreads)
-            if ((int64_t)total + r < bound) {
+            if (total + r < bound) {
                 const int32_t row = valid + (r << log_bm);
-                tiles[(int64_t)total + r] = FfnTile{-1, row, min(n - row, bm1 + 1), 0};
+                tiles[total + r] = FfnTile{-1, row, min(n - row, bm1 + 1), 0};
             }
-        if (tid == 0) *list = (int32_t)std::min<int64_t>((int64_t)total + extra, bound);
+        if (tid == 0) *list = (int32_t)std::min<int64_t>(total + extra, bound);
     }
 }
 
@@ -459,7 +460,7 @@ static bool few(const FfnPlan& p, int32_t s, int32_t M) {
 
 void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {
     tiles_plan(T, h, s, M, k, p);
-    p->off_hidden = p->off_sums + align256((size_t)p->sums * 4);
+    p->off_hidden = p->off_sums + align256((size_t)p->sums * sizeof(int64_t));
     p->workspace_bytes = p->off_hidden + align256((size_t)p->n * s * 2);
 }
 
@@ -467,7 +468,7 @@ hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* workspace,
     char* ws = static_cast<char*>(workspace);
     const unsigned blocks = (unsigned)(((int64_t)a.M + kTileThreads - 1) / kTileThreads);
     const int32_t log_bm = __builtin_ctz(p.bm);
-    int32_t* sums = p.sums ? reinterpret_cast<int32_t*>(ws + p.off_sums) : nullptr;
+    int64_t* sums = p.sums ? reinterpret_cast<int64_t*>(ws + p.off_sums) : nullptr;
     if (sums) ffn_tile_sums_kernel<<<blocks, kTileThreads, 0, stream>>>(a.offsets, a.M, (int32_t)p.n, log_bm, sums);
     ffn_tiles_kernel<<<blocks, kTileThreads, 0, stream>>>(a.offsets, a.M, (int32_t)p.n, log_bm, p.tiles, sums,
                                                           reinterpret_cast<int32_t*>(ws + p.off_tiles));

@@ -634,7 +634,7 @@ hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspa
         hipError_t e = ffn_tiles_launch(p, a, ws, stream);
         if (e != hipSuccess) return e;
         switch (p.bm) {
-                case 256: rows_launch<256>(p, a, ws, stream); break;
+            case 256: rows_launch<256>(p, a, ws, stream); break;
             case 128: rows_launch<128>(p, a, ws, stream); break;
             case 64: rows_launch<64>(p, a, ws, stream); break;
             default: rows_launch<32>(p, a, ws, stream);

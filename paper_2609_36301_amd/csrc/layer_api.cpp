@@ -11,6 +11,7 @@
 namespace {
 
 constexpr int64_t kMaxEntries = 0x7FFFFFFF;
+constexpr int64_t kMaxFfnEntries = kMaxEntries - 0xFFFF;  // (the kernels add a tile's rows to an entry in 32 bits)
 constexpr int32_t kMaxM = 1 << 30;
 constexpr int32_t kMaxWidth = 65536;
 
@@ -23,7 +24,7 @@ more_status from_hip(hipError_t e) { return e == hipSuccess ? MORE_OK : MORE_ERR
 more_status check_ffn(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k) {
     if (T < 0 || h <= 0 || s <= 0 || M <= 0 || k < 1) return MORE_ERR_INVALID_ARG;
     if (h % 16 != 0 || s % 8 != 0 || h > kMaxWidth || s > kMaxWidth || k > MORE_K_MAX || M >= kMaxM ||
-        T > kMaxEntries || T * (int64_t)k > kMaxEntries)
+        T > kMaxFfnEntries || T * (int64_t)k > kMaxFfnEntries)
         return MORE_ERR_UNSUPPORTED;
     return MORE_OK;
 }

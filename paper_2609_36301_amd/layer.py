@@ -37,7 +37,14 @@ def _device(device) -> torch.device:
     return dev if dev.index is not None else torch.device("cuda", torch.cuda.current_device())
 
 
+def _good(t, dtype, shape, device) -> bool:
+    return (isinstance(t, torch.Tensor) and t.dtype == dtype and t.shape == shape and t.device == device
+            and t.is_contiguous())
+
+
 def _check(name: str, t, dtype, shape, device):
+    if _good(t, dtype, shape, device):
+        return
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
     if t.dtype != dtype:
@@ -45,16 +52,7 @@ def _check(name: str, t, dtype, shape, device):
     if t.shape != shape or not t.is_contiguous():
         raise ValueError("%s must be a contiguous tensor of shape %s, got %s"
                          % (name, tuple(shape), tuple(t.shape)))
-    if t.device != device:
-        raise ValueError("%s must be on %s, got %s" % (name, device, t.device))
-
-
-def _check_all(device, *wanted):
-    """_check of each (name, tensor, dtype, shape)."""
-    for name, t, dtype, shape in wanted:
-        if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.shape == shape and t.device == device
-                and t.is_contiguous()):
-            _check(name, t, dtype, shape, device)
+    raise ValueError("%s must be on %s, got %s" % (name, device, t.device))
 
 
 def _call(name: str, device: torch.device, *args):
@@ -88,13 +86,17 @@ def expert_ffn_backward_workspace_size(T: int, h: int, s: int, M: int, k: int) -
     return _size("more_expert_ffn_backward_workspace_size", T, h, s, M, k)
 
 
-def _check_ffn(shape, device, x, W1t, W2t, idx, offsets, srt, gate):
-    T, h, s, M, k = shape
+def _ffn_spec(T, h, s, M, k):
     bf16, i32 = torch.bfloat16, torch.int32
-    _check_all(device, ("x", x, bf16, (T, h)), ("W1t", W1t, bf16, (M, 2 * s, h)), ("W2t", W2t, bf16, (M, h, s)),
-               ("idx", idx, i32, (T, k)), ("offsets", offsets, i32, (M + 1,)), ("sorted", srt, i32, (T * k,)))
-    if gate is not None:
-        _check_all(device, ("gate", gate, torch.float32, (T, k)))
+    return (("x", bf16, (T, h)), ("W1t", bf16, (M, 2 * s, h)), ("W2t", bf16, (M, h, s)), ("idx", i32, (T, k)),
+            ("offsets", i32, (M + 1,)), ("sorted", i32, (T * k,)), ("gate", torch.float32, (T, k)),
+            ("du", bf16, (T, h)))
+
+
+def _check_ffn(spec, device, *tensors):
+    for (name, dtype, shape), t in zip(spec, tensors):
+        if not (t is None and name == "gate"):
+            _check(name, t, dtype, shape, device)
 
 
 def _ffn_shape(x, W1t, W2t, idx):
@@ -110,14 +112,14 @@ class ExpertFFN:
     """Pre-allocated output and workspace for repeated expert_ffn calls with one shape."""
 
     def __init__(self, T: int, h: int, s: int, M: int, k: int, *, device=None):
-        self.shape = (T, h, s, M, k)
+        self.shape, self.spec = (T, h, s, M, k), _ffn_spec(T, h, s, M, k)
         self.device = _device(device)
         self.workspace_bytes = expert_ffn_workspace_size(T, h, s, M, k)
         self.workspace = _workspace(self.workspace_bytes, self.device)
         self.y = torch.empty((T * k, h), dtype=torch.bfloat16, device=self.device)
 
     def __call__(self, x, W1t, W2t, idx, offsets, sorted, gate=None) -> torch.Tensor:
-        _check_ffn(self.shape, self.device, x, W1t, W2t, idx, offsets, sorted, gate)
+        _check_ffn(self.spec, self.device, x, W1t, W2t, idx, offsets, sorted, gate)
         _call("more_expert_ffn", self.device, _ptr(x), _ptr(W1t), _ptr(W2t), *self.shape, _ptr(idx),
               _ptr(offsets), _ptr(sorted), _ptr(gate), _ptr(self.y), _ptr(self.workspace),
               self.workspace_bytes)
@@ -145,7 +147,7 @@ class ExpertFFNBackward:
     """Pre-allocated gradients and workspace for repeated expert_ffn_backward calls with one shape."""
 
     def __init__(self, T: int, h: int, s: int, M: int, k: int, *, device=None):
-        self.shape = (T, h, s, M, k)
+        self.shape, self.spec = (T, h, s, M, k), _ffn_spec(T, h, s, M, k)
         self.device = dev = _device(device)
         self.workspace_bytes = expert_ffn_backward_workspace_size(T, h, s, M, k)
         self.workspace = _workspace(self.workspace_bytes, dev)
@@ -156,8 +158,7 @@ class ExpertFFNBackward:
         self.dgate = torch.empty((T, k), dtype=torch.float32, device=dev)
 
     def __call__(self, x, W1t, W2t, idx, offsets, sorted, gate, du) -> ExpertGradients:
-        _check_ffn(self.shape, self.device, x, W1t, W2t, idx, offsets, sorted, gate)
-        _check("du", du, torch.bfloat16, self.shape[:2], self.device)
+        _check_ffn(self.spec, self.device, x, W1t, W2t, idx, offsets, sorted, gate, du)
         dgate = None if gate is None else self.dgate
         _call("more_expert_ffn_backward", self.device, _ptr(x), _ptr(W1t), _ptr(W2t), *self.shape,
               _ptr(idx), _ptr(offsets), _ptr(sorted), _ptr(gate), _ptr(du), _ptr(self.dx),
@@ -211,13 +212,16 @@ class BlockNorm:
         dev, f32 = self.device, torch.float32
         if (y is not None) != (k > 0):
             raise ValueError("y must be given exactly when the norm was set up with k > 0")
-        wanted = [("r", r, self.resid_dtype, (T, h))]
+        _check("r", r, self.resid_dtype, (T, h), dev)
         if y is not None:
-            wanted.append(("y", y, torch.bfloat16, (T * k, h) if y.dim() == 2 else (T, k, h)))
-        for name, t, shape in (("w_after", w_after, (h,)), ("w_before", w_before, (h,)), ("gate", gate, (T,))):
-            if t is not None:
-                wanted.append((name, t, f32, shape))
-        _check_all(dev, *wanted)
+            flat = isinstance(y, torch.Tensor) and y.dim() == 2
+            _check("y", y, torch.bfloat16, (T * k, h) if flat else (T, k, h), dev)
+        if w_after is not None:
+            _check("w_after", w_after, f32, (h,), dev)
+        if w_before is not None:
+            _check("w_before", w_before, f32, (h,), dev)
+        if gate is not None:
+            _check("gate", gate, f32, (T,), dev)
         out = None if k == 0 else r if self.inplace else self.r
         xn = None if w_before is None else self.xn
         _call("more_block_norm", dev, _ptr(r), self.resid_bits, _ptr(y), T, h, k, _ptr(w_after), _ptr(w_before),
@@ -232,6 +236,8 @@ def block_norm(r, y=None, *, w_after=None, w_before=None, gate=None, norm_after:
     xn = w_before r'/rms(r').  Without y only the norm; without w_before no xn (more_block_norm)."""
     if not isinstance(r, torch.Tensor) or r.dim() != 2:
         raise ValueError("r must be a 2-D tensor")
+    if y is not None and (not isinstance(y, torch.Tensor) or y.dim() not in (2, 3)):
+        raise ValueError("y must be a 2-D or 3-D tensor")
     T, h = r.shape
     k = 0 if y is None else y.shape[1] if y.dim() == 3 else y.shape[0] // max(T, 1) if T else 1
     call = BlockNorm(T, h, k, resid_dtype=r.dtype, norm_after=norm_after, alpha=alpha, eps=eps, save_u=save_u,
@@ -276,14 +282,13 @@ class BlockNormBackward:
         dev, f32, bf16 = self.device, torch.float32, torch.bfloat16
         if (gate is not None) != self.gated:
             raise ValueError("gate must be given exactly when the backward was set up with gated=True")
-        wanted = [("r_out", r_out, self.resid_dtype, (T, h))]
+        _check("r_out", r_out, self.resid_dtype, (T, h), dev)
         for name, t, dtype, shape in (("u", u, bf16, (T, h)), ("dr_out", dr_out, self.resid_dtype, (T, h)),
                                       ("dxn", dxn, bf16, (T, h)), ("dxn32", dxn32, f32, (T, h)),
                                       ("w_after", w_after, f32, (h,)), ("w_before", w_before, f32, (h,)),
                                       ("gate", gate, f32, (T,))):
             if t is not None:
-                wanted.append((name, t, dtype, shape))
-        _check_all(dev, *wanted)
+                _check(name, t, dtype, shape, dev)
         block = u is not None
         du = self.du if block else None
         dwa = self.dw_after if w_after is not None else None
@@ -311,7 +316,8 @@ def block_norm_backward(u, r_out, dr_out=None, dxn=None, *, dxn32=None, w_after=
 class GradClipper:
     """Scales a fixed set of gradients (float32 or bfloat16) to a common 2-norm of at most max_norm:
     by min(1, max_norm / (N + eps)) with N their norm.  In place unless `out` names other tensors.
-    `__call__` reads the tensors as they are then and returns (N, the scaled tensors)."""
+    `__call__` reads the tensors as they are then and returns (N, the scaled tensors); tensors that have
+    been given other storage since are refused."""
 
     def __init__(self, grads: Sequence[torch.Tensor], max_norm: float, *, eps: float = 1e-6,
                  out: Optional[Sequence[torch.Tensor]] = None):
@@ -348,15 +354,22 @@ class GradClipper:
         self.max_norm, self.eps = float(max_norm), float(eps)
         self.device = grads[0].device
         n = len(grads)
-        self._in = (ctypes.c_void_p * n)(*[g.data_ptr() for g in grads])
-        self._out = (ctypes.c_void_p * n)(*[o.data_ptr() for o in out])
+        self._places = self._where()
+        self._in = (ctypes.c_void_p * n)(*self._places[:n])
+        self._out = (ctypes.c_void_p * n)(*self._places[n:])
         self._numel = (ctypes.c_int64 * n)(*[g.numel() for g in grads])
         self._bits = (ctypes.c_int32 * n)(*[_RESID_BITS[g.dtype] for g in grads])
         self.workspace_bytes = _size("more_grad_clip_workspace_size", self._numel, n)
         self.workspace = _workspace(self.workspace_bytes, self.device)
         self.norm = torch.empty((), dtype=torch.float32, device=self.device)
 
+    def _where(self):
+        """The tensors' addresses and, behind them, the outputs'."""
+        return [t.data_ptr() for t in self.grads] + [t.data_ptr() for t in self.out]
+
     def __call__(self):
+        if self._where() != self._places:
+            raise ValueError("a tensor's storage has changed since the clipper was set up")
         _call("more_grad_clip", self.device, self._in, self._out, self._numel, self._bits, len(self.grads),
               self.max_norm, self.eps, _ptr(self.norm), _ptr(self.workspace), self.workspace_bytes)
         return self.norm, self.out

@@ -70,6 +70,9 @@ CASES = {
     "many_experts": dict(T=33, h=64, s=8, M=5000, k=4, drop=0.2),
     "past_2_16_experts": dict(T=400, h=32, s=40, M=70000, k=3, drop=0.05),
     "repeated_ids": dict(T=50, h=80, s=32, M=6, k=4, repeat=True),
+    "long_rows": dict(T=3, h=9008, s=520, M=2, k=1),
+    "long_rows_on_tiles": dict(T=70, h=8208, s=136, M=2, k=1),
+    "wide_units": dict(T=2, h=32, s=8200, M=3, k=2),
     "many_rows": dict(T=3000, h=64, s=16, M=5, k=3, drop=0.01),
 }
 
@@ -179,6 +182,69 @@ def test_same_bits_on_every_run_and_another_stream():
     for u, v in ((y, y2), (b.dx, b2.dx), (b.dW1t, b2.dW1t), (b.dW2t, b2.dW2t), (b.dgate, b2.dgate)):
         assert torch.equal(u.view(torch.int16 if u.dtype == torch.bfloat16 else torch.int32),
                            v.view(torch.int16 if v.dtype == torch.bfloat16 else torch.int32))
+
+
+@pytest.mark.parametrize("T,k", [(6, 2), (300, 4)])
+def test_nothing_of_dropped_entries_is_read(T, k):
+    """NaN and infinities in the gates of dropped entries and in x and du of tokens without entries (the
+    padding of a batch): the results are those of zeros in their places, bit for bit."""
+    torch = require_gpu()
+    from paper_2609_36301_amd import layer
+    h, s, M = 144, 40, 5
+    idx, bits, gate, _ = make(T, h, s, M, k, drop=0.2, seed=3)
+    idx[-2:] = -1
+    idx[0] = M
+    dropped = (idx < 0) | (idx >= M)
+    none = dropped.all(1)
+    results = []
+    for fill, fill_bits in ((0.0, 0), (np.nan, 0x7FC0), (np.inf, 0x7F80)):
+        gate[dropped] = fill
+        bits["x"][none] = bits["du"][none] = fill_bits
+        d, i, o, srt, g = on_device(idx, bits, gate, M)
+        announce("expert_ffn with %r in dropped entries, T=%d" % (fill, T))
+        b = layer.expert_ffn_backward(d["x"], d["W1t"], d["W2t"], i, o, srt, g, d["du"])
+        results.append((layer.expert_ffn(d["x"], d["W1t"], d["W2t"], i, o, srt, g), b.dx, b.dW1t, b.dW2t, b.dgate))
+        torch.cuda.synchronize()
+    for other in results[1:]:
+        for a, b in zip(results[0], other):
+            assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T,M,form", [(1 << 22, 1 << 17, "up and down"), (1 << 16, 5000, "up and down"),
+                                      (5000, 300, "backwards"), (6, 9, "beyond")])
+def test_offsets_of_another_selection_stay_in_bounds(T, M, form):
+    """Offsets that no Sort + Count writes: the values are undefined, but nothing around the buffers is
+    written (the rows before and after the outputs and the workspace keep what they held)."""
+    torch = require_gpu()
+    from paper_2609_36301_amd import layer
+    h, s = 16, 8
+    zeros = lambda *n: torch.zeros(n, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    offsets = {"up and down": torch.arange(M + 1) % 2 * T, "backwards": T - torch.arange(M + 1) * T // M,
+               "beyond": (torch.arange(M + 1) - 3) * (2 ** 28)}[form].to(torch.int32).cuda()
+    idx = torch.randint(-1, M + 1, (T, 1), dtype=torch.int32, device="cuda")
+    srt = torch.randint(-5, T + 5, (T,), dtype=torch.int32, device="cuda")
+    announce("expert_ffn with offsets going %s, T=%d M=%d" % (form, T, M))
+    x, W1, W2 = zeros(T, h), zeros(M, 2 * s, h), zeros(M, h, s)
+    guards = []
+
+    def guarded(t):
+        """t's place inside a buffer with 4096 bytes of 0x5A around it."""
+        n = t.numel() * t.element_size()
+        buffer = torch.full((n + 8192,), 0x5A, dtype=torch.uint8, device="cuda")
+        guards.append((buffer, n))
+        return buffer[4096:4096 + n].view(t.dtype).view(t.shape)
+
+    call, back = layer.ExpertFFN(T, h, s, M, 1), layer.ExpertFFNBackward(T, h, s, M, 1)
+    for obj, names in ((call, ("y", "workspace")), (back, ("dx", "dW1t", "dW2t", "dgate", "workspace"))):
+        for name in names:
+            setattr(obj, name, guarded(getattr(obj, name)))
+    call(x, W1, W2, idx, offsets, srt, None)
+    torch.cuda.synchronize()
+    if T <= 1 << 16:  # (every expert's weight gradients run over the entries that its offsets claim)
+        back(x, W1, W2, idx, offsets, srt, torch.ones((T, 1), device="cuda"), x)
+        torch.cuda.synchronize()
+    for buffer, n in guards:
+        assert bool((buffer[:4096] == 0x5A).all()) and bool((buffer[4096 + n:] == 0x5A).all())
 
 
 def test_binding_refuses():

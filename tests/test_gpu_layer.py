@@ -150,3 +150,22 @@ def test_serving_one_token():
         for a, b in ((one.r, end.r), (one.xn, end.xn)):
             off = float((a[0].double() - b[t].double()).norm() / b[t].double().norm())
             assert off <= 3 * 2.0 ** -8
+
+
+def test_two_steps_at_once():
+    """Two training steps on handles of their own, side by side on two streams, give what each gives alone."""
+    torch = require_gpu()
+    announce("two training steps on two streams")
+    steps, inputs = [Step(), Step()], [_inputs(torch, 6), _inputs(torch, 7)]
+    alone = [{n: v.clone() for n, v in step(p).items()} for step, p in zip(steps, inputs)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        out = []
+        for step, p, stream in zip(steps, inputs, streams):
+            with torch.cuda.stream(stream):
+                out.append(step(p))
+        torch.cuda.synchronize()
+        for got, want in zip(out, alone):
+            for n, v in want.items():
+                assert torch.equal(got[n], v), n

@@ -150,3 +150,22 @@ def test_binding_refuses_what_is_not_on_a_gpu():
         layer.GradClipper([torch.zeros(4, dtype=torch.float64)], 1.0)
     with pytest.raises(TypeError, match="residual"):
         layer.BlockNorm(4, 64, 1, resid_dtype=torch.float16)
+
+
+def test_ffn_most_entries(lib):
+    """The kernels add up to a tile's rows to an entry in 32 bits, so 2^16 entries are kept free."""
+    n = ctypes.c_size_t(0)
+    most = (1 << 31) - (1 << 16)
+    for f in (lib.more_expert_ffn_workspace_size, lib.more_expert_ffn_backward_workspace_size):
+        assert f(most, 16, 8, 2, 1, ctypes.byref(n)) == _lib.OK and n.value >= most * 16
+        assert f(most + 1, 16, 8, 2, 1, ctypes.byref(n)) == UNSUPPORTED
+        assert f(most // 32 + 1, 16, 8, 2, 32, ctypes.byref(n)) == UNSUPPORTED
+
+
+def test_block_norm_refuses_before_the_gpu():
+    torch = pytest.importorskip("torch")
+    from paper_2609_36301_amd import block_norm
+    r = torch.zeros((4, 64))
+    for y in (torch.zeros(64), torch.zeros((1, 4, 2, 64)), [[0.0] * 64]):
+        with pytest.raises(ValueError, match="y must be a 2-D or 3-D tensor"):
+            block_norm(r, y)
