@@ -29,7 +29,9 @@ struct FfnPlan {
     int32_t bm;       // rows of a tile (all of one expert)
     int64_t tiles;    // bound on the number of tiles
     int32_t sums;     // workgroups that count tiles ahead of the list (0: none)
-    size_t off_tiles, off_sums, off_hidden, off_dgu, off_da0, off_dxs, off_dgp;
+    int32_t dw_tile;  // rows and columns of a tile of the weight gradients (128 or 256)
+    int32_t dw_parts; // parts of an expert's entries whose weight gradients are summed apart
+    size_t off_tiles, off_sums, off_hidden, off_dgu, off_da0, off_dxs, off_dgp, off_dwp;
     size_t workspace_bytes;
 };
 
@@ -39,11 +41,24 @@ hipError_t ffn_launch(const FfnPlan& p, const FfnArgs& a, uint16_t* y, void* wor
 hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspace, hipStream_t stream);
 
 // Columns that a workgroup takes, in steps of `step`, of a product whose contraction is `len` long: a
-// single step where the contraction alone fills the pipeline, or where the groups of rows are too few to
-// fill the chip eight times over with more; else up to 512.
+// single step where the contraction alone fills the pipeline (eight stages), or where the groups of rows are
+// too few to fill the chip four times over with more; else up to 512.
 inline int32_t ffn_span(int32_t len, int32_t step, int64_t groups, int32_t cols) {
-    return len >= 256 || groups * ((cols + 511) / 512) < 2048 ? step : 512;
+    return len > 512 || groups * ((cols + 511) / 512) < 1024 ? step : 512;
 }
+
+// What `items` workgroups with tiles of `bm` rows cost that run `steps` stages each: the rounds in which they
+// fill the chip (two of up to 128 rows to a CU, one of 256) times the stages times the time of a stage.
+inline int64_t ffn_cost(int64_t items, int64_t steps, int32_t bm) {
+    const int64_t slots = bm == 256 ? 256 : 512;
+    const int64_t stage = bm == 256 ? 34 : bm == 128 ? (items <= 256 ? 16 : 20) : 15;
+    return (items + slots - 1) / slots * steps * stage;
+}
+// Twice the expected number of tiles of n entries over M experts whose rows scatter by their mean's root.
+int64_t ffn_expected_tiles2(int64_t n, int32_t M, int32_t bm);
+
+// The part of a plan that concerns the tile list.
+void ffn_tiles_plan(int64_t n, int32_t M, int32_t bm, FfnPlan* p);
 
 // Lists the tiles (shared by both directions).
 hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* workspace, hipStream_t stream);

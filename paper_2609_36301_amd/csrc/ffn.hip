@@ -17,6 +17,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "ffn.h"
 #include "ffn_device.h"
@@ -416,20 +417,23 @@ unsigned grid_of(int64_t items) {
 
 unsigned few_grid(int64_t items) { return (unsigned)std::min<int64_t>(items, 1 << 22); }
 
-// Rows of a tile: the mean number of rows of an expert decides.
+// Rows of a tile.
 int32_t tile_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
-    const int64_t mean = n / std::max<int64_t>(1, std::min<int64_t>(n, M));
-    if (mean >= 512 && h >= 256 && s >= 128) return 256;
-    return mean >= 96 ? 128 : mean >= 24 ? 64 : 32;
-}
-
-void tiles_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {
-    p->n = T * k;
-    p->bm = tile_rows(p->n, h, s, M);
-    p->tiles = p->n / p->bm + std::min<int64_t>(M, p->n) + 1;
-    p->off_tiles = 0;
-    p->off_sums = align256(kFfnTileHeader + (size_t)p->tiles * sizeof(FfnTile));
-    p->sums = M > kTileAlone ? (M + kTileThreads - 1) / kTileThreads : 0;
+    if (n / std::max<int64_t>(1, std::min<int64_t>(n, M)) < 24) return 32;
+    int32_t best = 64;
+    int64_t least = INT64_MAX;
+    for (int32_t bm = 64; bm <= 256; bm *= 2) {
+        const int64_t tiles2 = ffn_expected_tiles2(n, M, bm);
+        const int32_t units = bm == 256 ? UpShape<256>::kUnits : UpShape<128>::kUnits;
+        const int32_t cols = bm == 256 ? DownShape<256>::kCols : DownShape<128>::kCols;
+        const int64_t cost = ffn_cost(tiles2 * ((s + units - 1) / units) / 2, (h + kFfnBK - 1) / kFfnBK, bm) +
+                             ffn_cost(tiles2 * ((h + cols - 1) / cols) / 2, (s + kFfnBK - 1) / kFfnBK, bm);
+        if (cost < least) {
+            least = cost;
+            best = bm;
+        }
+    }
+    return best;
 }
 
 template <int BM>
@@ -447,21 +451,45 @@ hipError_t forward(const FfnPlan& p, const FfnArgs& a, uint16_t* y, char* ws, hi
 
 }  // namespace
 
-// Whether the kernels without tiles are taken: while ffn_few_up has at most two workgroups per CU with
-// work (and few that end at once).  They wait for three dependent reads where the tiled kernels wait for
-// the list, but stream at 4 TB/s where those reach 6.  Measured, few against tiles, us: h = 2048, s = 64,
-// one row per expert, 8 entries 10.3 : 19.2, 128 entries 24.3 : 29.8, 512 entries 96 : 81; s = 1024, 8
-// entries 16.3 : 20.4, 16 entries 26.2 : 23.7; dense, s = 1024, 1 row 11.5 : 23.9, 64 rows 30.3 : 29.5.
-static bool few(const FfnPlan& p, int32_t s, int32_t M) {
+int64_t ffn_expected_tiles2(int64_t n, int32_t M, int32_t bm) {
+    const int64_t groups = std::max<int64_t>(1, std::min<int64_t>(n, M));
+    const double mean = (double)n / (double)groups, sd = M == 1 ? 0.0 : std::sqrt(mean);
+    const int64_t lo = (int64_t)std::ceil(std::max(mean - sd, 1.0) / bm), hi = (int64_t)std::ceil((mean + sd) / bm);
+    return groups * (lo + hi);
+}
+
+void ffn_tiles_plan(int64_t n, int32_t M, int32_t bm, FfnPlan* p) {
+    *p = FfnPlan{};
+    p->n = n;
+    p->bm = bm;
+    p->tiles = n / bm + std::min<int64_t>(M, n) + 1;
+    p->off_tiles = 0;
+    p->off_sums = align256(kFfnTileHeader + (size_t)p->tiles * sizeof(FfnTile));
+    p->sums = M > kTileAlone ? (M + kTileThreads - 1) / kTileThreads : 0;
+    p->workspace_bytes = p->off_sums + align256((size_t)p->sums * sizeof(int64_t));
+}
+
+// Upper bound on the workgroups along the entries that have work in the kernels without tiles.
+static int64_t few_starts(const FfnPlan& p, int32_t M) { return std::min<int64_t>(p.n, std::min<int64_t>(p.n, M) + p.n / kFewRows); }
+
+// Whether the kernels without tiles are taken: while the weights that they read (once for every 16 rows) are
+// few bytes and few workgroups end at once.  They save a launch and the latency of the stages (16 MB + 40 KB
+// for every column and hidden unit that the stages run over, at what their bandwidth is worse).
+static bool few(const FfnPlan& p, int32_t h, int32_t s, int32_t M) {
     const int64_t groups = (s + kFewUnits - 1) / kFewUnits;
-    const int64_t starts = std::min<int64_t>(p.n, std::min<int64_t>(p.n, M) + p.n / kFewRows);
-    return starts * groups <= 512 && p.n * groups <= 2048;
+    return few_starts(p, M) * 6 * h * s <= ((int64_t)16 << 20) + (int64_t)40960 * (h + s) && p.n * groups <= 4096;
+}
+
+// Whether a workgroup of ffn_few_down shares columns: while the workgroups that have the whole contraction
+// per wave would be few against its length.
+static bool few_split(const FfnPlan& p, int32_t h, int32_t s, int32_t M) {
+    return 4 * few_starts(p, M) * ((h + kFewWaves * kFewCols - 1) / (kFewWaves * kFewCols)) <= s;
 }
 
 void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {
-    tiles_plan(T, h, s, M, k, p);
-    p->off_hidden = p->off_sums + align256((size_t)p->sums * sizeof(int64_t));
-    p->workspace_bytes = p->off_hidden + align256((size_t)p->n * s * 2);
+    ffn_tiles_plan(T * k, M, tile_rows(T * k, h, s, M), p);
+    p->off_hidden = p->workspace_bytes;
+    p->workspace_bytes += align256((size_t)p->n * s * 2);
 }
 
 hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* workspace, hipStream_t stream) {
@@ -477,10 +505,10 @@ hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* workspace,
 
 hipError_t ffn_launch(const FfnPlan& p, const FfnArgs& a, uint16_t* y, void* workspace, hipStream_t stream) {
     char* ws = static_cast<char*>(workspace);
-    if (few(p, a.s, a.M)) {
+    if (few(p, a.h, a.s, a.M)) {
         uint16_t* hidden = reinterpret_cast<uint16_t*>(ws + p.off_hidden);
         ffn_few_up_kernel<<<few_grid(p.n * ((a.s + kFewUnits - 1) / kFewUnits)), 64 * kFewWaves, 0, stream>>>(a, hidden);
-        const bool split = a.s > 128;  // a wave of its own would have the whole contraction to itself
+        const bool split = few_split(p, a.h, a.s, a.M);
         const int32_t span = split ? kFewCols : kFewWaves * kFewCols;
         const unsigned blocks = few_grid(p.n * ((a.h + span - 1) / span));
         if (split)

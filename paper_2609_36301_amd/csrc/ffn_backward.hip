@@ -24,6 +24,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "ffn.h"
 #include "ffn_device.h"
@@ -392,13 +393,18 @@ __global__ __launch_bounds__(256) void ffn_bwd_sum_kernel(const float* __restric
 // (rows 2s).  dW2t: P = gate A (cols s), Q = du of the entry's token (rows h).  The gathered operand is the
 // one along h; a workgroup computes a tile of RT rows and CT columns after the other over `hspan` of h, and
 // the pipeline runs over (tile, 64 entries) pairs, so that the few rows of a small expert do not drain it.
+// PARTS: the entries of an expert are cut into `parts` runs and a workgroup takes one tile and one run; the
+// fp32 results of run i go to parts_out + i part_stride, and ffn_bwd_dw_sum adds them.
 struct DwArgs {
     const uint16_t *P, *Q;
     int32_t rows_out, cols_out, hspan, blocks;  // workgroups of this product
     uint16_t* out;
+    int32_t parts;
+    float* parts_out;
+    int64_t part_stride;
 };
 
-template <int CT, int RT, int WAVES, bool GATHER_P>
+template <int CT, int RT, int WAVES, bool GATHER_P, bool PARTS>
 __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __restrict__ offsets,
                                            const int32_t* __restrict__ sorted, int32_t n, int32_t k, int32_t M,
                                            LdsChar* smem, LdsChar* scratch, int32_t block) {
@@ -419,11 +425,19 @@ __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __res
     const int32_t others = GATHER_P ? (rows_out + RT - 1) / RT : (cols_out + CT - 1) / CT;
     // Items in turn over the XCDs: the parts of an expert run on all of them, so that experts with many
     // entries load them alike.
-    for (int64_t item = block; item < (int64_t)M * spans * others; item += d.blocks) {
+    const int32_t runs = PARTS ? d.parts : 1;
+    for (int64_t work = block; work < (int64_t)M * spans * others * runs; work += d.blocks) {
+        const int32_t run = PARTS ? (int32_t)(work % runs) : 0;
+        const int64_t item = PARTS ? work / runs : work;
         const int32_t e = (int32_t)(item / (spans * others)), q = (int32_t)(item % (spans * others));
         const int32_t h0 = (q % spans) * hspan, h1 = min(h, h0 + hspan);
         const int32_t other = (q / spans) * (GATHER_P ? RT : CT);  // first row (column) of the other side
-        const int32_t begin = min(max(offsets[e], 0), n), end = min(max(offsets[e + 1], begin), n);
+        int32_t begin = min(max(offsets[e], 0), n), end = min(max(offsets[e + 1], begin), n);
+        if constexpr (PARTS) {  // whole stages
+            const int32_t len = ((end - begin + runs - 1) / runs + kFfnBK - 1) / kFfnBK * kFfnBK;
+            begin = (int32_t)min((int64_t)begin + (int64_t)run * len, (int64_t)end);
+            end = (int32_t)min((int64_t)begin + len, (int64_t)end);
+        }
         PLoader pl;
         QLoader ql;
         pl.init();
@@ -450,6 +464,21 @@ __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __res
             for (int j = 0; j < kN; ++j) acc[i][j] = zero_f32x4();
         int32_t lh = h0, lk = 0, ch = h0, ck = 0;
         auto store = [&] {
+            if constexpr (PARTS) {
+                float* o = d.parts_out + run * d.part_stride + (int64_t)e * rows_out * cols_out;
+#pragma unroll
+                for (int j = 0; j < kN; ++j)
+#pragma unroll
+                    for (int i = 0; i < kM; ++i) {
+                        const int32_t c = (GATHER_P ? ch : other) + 16 * (wm * kM + i) + 4 * (ffn_lane() >> 4);
+                        const int32_t r = (GATHER_P ? other : ch) + 16 * (wn * kN + j) + (ffn_lane() & 15);
+                        if (c < (GATHER_P ? h1 : cols_out) && r < (GATHER_P ? rows_out : h1))
+                            *reinterpret_cast<f32x4*>(o + (int64_t)r * cols_out + c) = acc[i][j];
+                        acc[i][j] = zero_f32x4();
+                    }
+                ch += kStep;
+                return;
+            }
             uint16_t* o = out + (int64_t)e * rows_out * cols_out;
 #pragma unroll
             for (int j = 0; j < kN; ++j)
@@ -534,7 +563,7 @@ __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __res
 
 // Both products in one launch (the second one's workgroups follow the first one's, so that the last of one
 // and the first of the other share the chip).
-template <int CT1, int CT2, int RT, int WAVES>
+template <int CT1, int CT2, int RT, int WAVES, bool PARTS>
 __global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(DwArgs w1, DwArgs w2,
                                                                 const int32_t* __restrict__ offsets,
                                                                 const int32_t* __restrict__ sorted, int32_t n,
@@ -545,9 +574,26 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(DwArgs w1, Dw
     LdsChar* scratch = (LdsChar*)scratch_raw + ffn_wave() * kFfnScratch;
     const int32_t block = (int32_t)blockIdx.x;
     if (block < w1.blocks)
-        ffn_bwd_dw<CT1, RT, WAVES, true>(w1, offsets, sorted, n, k, M, smem, scratch, block);
+        ffn_bwd_dw<CT1, RT, WAVES, true, PARTS>(w1, offsets, sorted, n, k, M, smem, scratch, block);
     else
-        ffn_bwd_dw<CT2, RT, WAVES, false>(w2, offsets, sorted, n, k, M, smem, scratch, block - w1.blocks);
+        ffn_bwd_dw<CT2, RT, WAVES, false, PARTS>(w2, offsets, sorted, n, k, M, smem, scratch, block - w1.blocks);
+}
+
+// Adds the runs' partial gradients in order: a thread takes eight values, of dW1t and behind them of dW2t.
+__global__ __launch_bounds__(256) void ffn_bwd_dw_sum_kernel(const float* __restrict__ parts, int32_t count,
+                                                          int64_t stride, int64_t size1, uint16_t* __restrict__ dW1t,
+                                                          uint16_t* __restrict__ dW2t) {
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < stride; i += (int64_t)gridDim.x * 256 * 8) {
+        f32x4 a = zero_f32x4(), b = zero_f32x4();
+#pragma unroll 4
+        for (int32_t q = 0; q < count; ++q) {
+            const f32x4* v = reinterpret_cast<const f32x4*>(parts + q * stride + i);
+            a += v[0];
+            b += v[1];
+        }
+        const uint2 lo = pack_bf16x4(a[0], a[1], a[2], a[3]), hi = pack_bf16x4(b[0], b[1], b[2], b[3]);
+        *reinterpret_cast<u32x4*>(i < size1 ? dW1t + i : dW2t + (i - size1)) = u32x4{lo.x, lo.y, hi.x, hi.y};
+    }
 }
 
 // ------------------------------------------------------------------------------ host
@@ -558,6 +604,9 @@ constexpr int64_t kMaxBlocks = 1 << 19;
 unsigned grid_of(int64_t items) {
     return (unsigned)(std::min<int64_t>((items + 7) / 8, kMaxBlocks / 8) * 8);
 }
+
+// Elements of both weight gradients.
+int64_t dw_size(int32_t h, int32_t s, int32_t M) { return (int64_t)M * 3 * s * h; }
 
 // Workgroups along the hidden units: a partial sum of dgate each.
 int32_t dgate_parts(const FfnPlan& p, int32_t s) {
@@ -590,32 +639,84 @@ void rows_launch(const FfnPlan& p, const FfnArgs& a, char* ws, hipStream_t strea
 
 // One weight gradient: tiles of rt x ct, `other` of them across h.
 DwArgs dw_args(const FfnPlan& p, const FfnArgs& a, const uint16_t* P, const uint16_t* Q, int32_t rows, int32_t cols,
-               int32_t others, int32_t step, uint16_t* out) {
+               int32_t others, int32_t step, uint16_t* out, float* parts_out) {
     DwArgs d;
     d.P = P;
     d.Q = Q;
     d.rows_out = rows;
     d.cols_out = cols;
+    d.parts = p.dw_parts;
+    d.parts_out = parts_out;
+    d.part_stride = dw_size(a.h, a.s, a.M);
     const int64_t groups = (int64_t)a.M * others;
-    d.hspan = ffn_span((int32_t)std::min<int64_t>(p.n / a.M, 1 << 20), step, groups, a.h);
-    d.blocks = (int32_t)grid_of(groups * ((a.h + d.hspan - 1) / d.hspan));
+    d.hspan = d.parts > 1 ? step : ffn_span((int32_t)std::min<int64_t>(p.n / a.M, 1 << 20), step, groups, a.h);
+    d.blocks = (int32_t)grid_of(groups * ((a.h + d.hspan - 1) / d.hspan) * d.parts);
     d.out = out;
     return d;
 }
 
-template <int CT1, int CT2, int RT, int WAVES>
-void dw_launch(const FfnPlan& p, const FfnArgs& a, const uint16_t* hidden, const uint16_t* dgu, hipStream_t stream) {
-    const DwArgs w1 = dw_args(p, a, a.x, dgu, 2 * a.s, a.h, (2 * a.s + RT - 1) / RT, CT1, a.dW1t);
-    const DwArgs w2 = dw_args(p, a, hidden, a.du, a.h, a.s, (a.s + CT2 - 1) / CT2, RT, a.dW2t);
-    ffn_bwd_dw_kernel<CT1, CT2, RT, WAVES><<<(unsigned)(w1.blocks + w2.blocks), 64 * WAVES, 0, stream>>>(
+template <int CT1, int CT2, int RT, int WAVES, bool PARTS>
+void dw_launch(const FfnPlan& p, const FfnArgs& a, char* ws, hipStream_t stream) {
+    const uint16_t* hidden = reinterpret_cast<const uint16_t*>(ws + p.off_hidden);
+    const uint16_t* dgu = reinterpret_cast<const uint16_t*>(ws + p.off_dgu);
+    float* parts = reinterpret_cast<float*>(ws + p.off_dwp);
+    const int64_t size1 = (int64_t)a.M * 2 * a.s * a.h;
+    const DwArgs w1 = dw_args(p, a, a.x, dgu, 2 * a.s, a.h, (2 * a.s + RT - 1) / RT, CT1, a.dW1t, parts);
+    const DwArgs w2 = dw_args(p, a, hidden, a.du, a.h, a.s, (a.s + CT2 - 1) / CT2, RT, a.dW2t, parts + size1);
+    ffn_bwd_dw_kernel<CT1, CT2, RT, WAVES, PARTS><<<(unsigned)(w1.blocks + w2.blocks), 64 * WAVES, 0, stream>>>(
         w1, w2, a.offsets, a.sorted, (int32_t)p.n, a.k, a.M);
+    if (PARTS) {
+        const int64_t size = dw_size(a.h, a.s, a.M);
+        ffn_bwd_dw_sum_kernel<<<(unsigned)std::min<int64_t>((size / 8 + 255) / 256, 1 << 14), 256, 0, stream>>>(
+            parts, p.dw_parts, size, size1, a.dW1t, a.dW2t);
+    }
+}
+
+// Tile size of the weight gradients, and the runs into which an expert's entries are cut.
+void dw_plan(int64_t n, int32_t h, int32_t s, int32_t M, FfnPlan* p) {
+    const int64_t steps = std::max<int64_t>(1, n / M / kFfnBK);
+    auto tiles = [&](int32_t a, int32_t b) { return (int64_t)((a + b - 1) / b); };
+    const int64_t large = M * tiles(h, 256) * (tiles(2 * s, 256) + tiles(s, 256));
+    const int64_t small = M * tiles(h, 128) * (tiles(2 * s, 128) + (tiles(s, 64) + 1) / 2);
+    p->dw_tile = ffn_cost(large, steps, 256) < ffn_cost(small, steps, 128) ? 256 : 128;
+    p->dw_parts = 1;
+    if (p->dw_tile == 128) p->dw_parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(256 / small, steps / 4));
+}
+
+// Rows of a tile, as in the forward pass.
+int32_t backward_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
+    if (n / std::max<int64_t>(1, std::min<int64_t>(n, M)) < 24) return 32;
+    int32_t best = 64;
+    int64_t least = INT64_MAX;
+    const int64_t hsteps = (h + kFfnBK - 1) / kFfnBK, ssteps = (2 * s + kFfnBK - 1) / kFfnBK;
+    auto parts = [](int32_t v, int32_t size) { return (int64_t)((v + size - 1) / size); };
+    for (int32_t bm = 64; bm <= 256; bm *= 2) {
+        const int64_t tiles2 = ffn_expected_tiles2(n, M, bm);
+        int64_t cost;
+        if (bm == 256) {
+            cost = ffn_cost(tiles2 * parts(s, RowsShape<256>::kCols) / 2, hsteps, bm) +
+                   ffn_cost(tiles2 * parts(s, UpShape<256>::kUnits) / 2, hsteps, bm) +
+                   ffn_cost(tiles2 * parts(h, RowsShape<256>::kCols) / 2, ssteps, bm);
+        } else {
+            cost = ffn_cost(tiles2 * parts(s, BwdUpShape<128>::kUnits) / 2, 2 * hsteps, bm) +
+                   ffn_cost(tiles2 * parts(h, RowsShape<128>::kCols) / 2, ssteps, bm);
+        }
+        if (cost < least) {
+            least = cost;
+            best = bm;
+        }
+    }
+    return best;
 }
 
 }  // namespace
 
 void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {
-    ffn_make_plan(T, h, s, M, k, p);
+    ffn_tiles_plan(T * k, M, backward_rows(T * k, h, s, M), p);
+    dw_plan(p->n, h, s, M, p);
     size_t at = p->workspace_bytes;
+    p->off_hidden = at;
+    at += align256((size_t)p->n * s * 2);
     p->off_dgu = at;
     at += align256((size_t)p->n * 2 * s * 2);
     p->off_da0 = at;
@@ -624,6 +725,8 @@ void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t 
     at += align256((size_t)p->n * h * 4);
     p->off_dgp = at;
     at += align256((size_t)p->n * dgate_parts(*p, s) * 4);
+    p->off_dwp = at;
+    at += p->dw_parts > 1 ? align256((size_t)p->dw_parts * dw_size(h, s, M) * 4) : 0;
     p->workspace_bytes = at;
 }
 
@@ -645,12 +748,12 @@ hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspa
             reinterpret_cast<const float*>(ws + p.off_dxs), a.idx, a.T, a.h, a.M, a.k, a.dx, colblocks,
             reinterpret_cast<const float*>(ws + p.off_dgp), dgate_parts(p, a.s), a.sorted, a.dgate);
     }
-    const uint16_t* hidden = reinterpret_cast<const uint16_t*>(ws + p.off_hidden);
-    const uint16_t* dgu = reinterpret_cast<const uint16_t*>(ws + p.off_dgu);
-    if (p.bm == 256)
-        dw_launch<256, 256, 256, 8>(p, a, hidden, dgu, stream);
+    if (p.dw_tile == 256)
+        dw_launch<256, 256, 256, 8, false>(p, a, ws, stream);
+    else if (p.dw_parts > 1)
+        dw_launch<128, 64, 128, 4, true>(p, a, ws, stream);
     else
-        dw_launch<128, 64, 128, 4>(p, a, hidden, dgu, stream);
+        dw_launch<128, 64, 128, 4, false>(p, a, ws, stream);
     return hipGetLastError();
 }
 

@@ -354,21 +354,18 @@ class GradClipper:
         self.max_norm, self.eps = float(max_norm), float(eps)
         self.device = grads[0].device
         n = len(grads)
-        self._places = self._where()
+        self._tensors = grads if all(g is o for g, o in zip(grads, out)) else grads + out
+        self._places = list(map(torch.Tensor.data_ptr, self._tensors))
         self._in = (ctypes.c_void_p * n)(*self._places[:n])
-        self._out = (ctypes.c_void_p * n)(*self._places[n:])
+        self._out = (ctypes.c_void_p * n)(*self._places[-n:])
         self._numel = (ctypes.c_int64 * n)(*[g.numel() for g in grads])
         self._bits = (ctypes.c_int32 * n)(*[_RESID_BITS[g.dtype] for g in grads])
         self.workspace_bytes = _size("more_grad_clip_workspace_size", self._numel, n)
         self.workspace = _workspace(self.workspace_bytes, self.device)
         self.norm = torch.empty((), dtype=torch.float32, device=self.device)
 
-    def _where(self):
-        """The tensors' addresses and, behind them, the outputs'."""
-        return [t.data_ptr() for t in self.grads] + [t.data_ptr() for t in self.out]
-
     def __call__(self):
-        if self._where() != self._places:
+        if list(map(torch.Tensor.data_ptr, self._tensors)) != self._places:
             raise ValueError("a tensor's storage has changed since the clipper was set up")
         _call("more_grad_clip", self.device, self._in, self._out, self._numel, self._bits, len(self.grads),
               self.max_norm, self.eps, _ptr(self.norm), _ptr(self.workspace), self.workspace_bytes)

@@ -73,6 +73,13 @@ CASES = {
     "long_rows": dict(T=3, h=9008, s=520, M=2, k=1),
     "long_rows_on_tiles": dict(T=70, h=8208, s=136, M=2, k=1),
     "wide_units": dict(T=2, h=32, s=8200, M=3, k=2),
+    "runs_of_the_dense_block": dict(T=1100, h=80, s=40, M=1, k=1),
+    "runs_skewed": dict(T=2100, h=144, s=72, M=3, k=1, hot=0.9, drop=0.02),
+    "runs_without_rows": dict(T=1300, h=64, s=136, M=2, k=1, hot=1.1),
+    "tiles_of_128": dict(T=8000, h=48, s=136, M=128, k=1, drop=0.01),
+    "tiles_of_128_wide": dict(T=6000, h=272, s=136, M=5, k=2, hot=0.3),
+    "tiles_of_256": dict(T=8000, h=496, s=200, M=32, k=2, drop=0.01),
+    "tiles_of_256_skewed": dict(T=16000, h=496, s=200, M=32, k=1, hot=0.4),
     "many_rows": dict(T=3000, h=64, s=16, M=5, k=3, drop=0.01),
 }
 
