@@ -93,9 +93,22 @@ __global__ __launch_bounds__(kTileThreads) void ffn_tiles_kernel(const int32_t* 
         total += part[0][w] + part[1][w];
         base += part[1][w] + (w < wave ? part[0][w] : 0);
     }
-    int64_t at = base + scan - mine;
-    for (int32_t r = 0; r < len && at < bound; r += bm1 + 1, ++at)
-        tiles[at] = FfnTile{e, begin + r, min(len - r, bm1 + 1), 0};
+    const int64_t at = base + scan - mine;
+    if (mine <= 16)
+        for (int32_t r = 0; r < len && at + (r >> log_bm) < bound; r += bm1 + 1)
+            tiles[at + (r >> log_bm)] = FfnTile{e, begin + r, min(len - r, bm1 + 1), 0};
+    // experts with more tiles: the wave's lanes write them together
+    for (uint64_t left = __ballot(mine > 16); left; left &= left - 1) {
+        const int l = __builtin_ctzll(left);
+        const int32_t len1 = __builtin_amdgcn_readlane(len, l), begin1 = __builtin_amdgcn_readlane(begin, l);
+        const int32_t mine1 = (len1 + bm1) >> log_bm;
+        const int64_t at1 = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int32_t)(at >> 32), l) << 32 |
+                                      (uint32_t)__builtin_amdgcn_readlane((int32_t)at, l));
+        for (int32_t q = lane; q < mine1 && at1 + q < bound; q += 64) {
+            const int32_t r = q << log_bm;
+            tiles[at1 + q] = FfnTile{e - lane + l, begin1 + r, min(len1 - r, bm1 + 1), 0};
+        }
+    }
     if (blockIdx.x == gridDim.x - 1) {
         const int32_t extra = (n - valid + bm1) >> log_bm;
         for (int32_t r = tid; r < extra; r += kTileThreads)
@@ -476,7 +489,7 @@ static int64_t few_starts(const FfnPlan& p, int32_t M) { return std::min<int64_t
 // few bytes and few workgroups end at once.  They save a launch and the latency of the stages (16 MB + 40 KB
 // for every column and hidden unit that the stages run over, at what their bandwidth is worse).
 static bool few(const FfnPlan& p, int32_t h, int32_t s, int32_t M) {
-    const int64_t groups = (s + kFewUnits - 1) / kFewUnits;
+    const int64_t groups = std::max((s + kFewUnits - 1) / kFewUnits, (h + kFewWaves * kFewCols - 1) / (kFewWaves * kFewCols));
     return few_starts(p, M) * 6 * h * s <= ((int64_t)16 << 20) + (int64_t)40960 * (h + s) && p.n * groups <= 4096;
 }
 

@@ -394,7 +394,8 @@ __global__ __launch_bounds__(256) void ffn_bwd_sum_kernel(const float* __restric
 // one along h; a workgroup computes a tile of RT rows and CT columns after the other over `hspan` of h, and
 // the pipeline runs over (tile, 64 entries) pairs, so that the few rows of a small expert do not drain it.
 // PARTS: the entries of an expert are cut into `parts` runs and a workgroup takes one tile and one run; the
-// fp32 results of run i go to parts_out + i part_stride, and ffn_bwd_dw_sum adds them.
+// fp32 results of run i go to parts_out + i part_stride, and ffn_bwd_dw_sum adds them.  ONCE: nontemporal
+// stores.
 struct DwArgs {
     const uint16_t *P, *Q;
     int32_t rows_out, cols_out, hspan, blocks;  // workgroups of this product
@@ -404,7 +405,7 @@ struct DwArgs {
     int64_t part_stride;
 };
 
-template <int CT, int RT, int WAVES, bool GATHER_P, bool PARTS>
+template <int CT, int RT, int WAVES, bool GATHER_P, bool PARTS, bool ONCE>
 __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __restrict__ offsets,
                                            const int32_t* __restrict__ sorted, int32_t n, int32_t k, int32_t M,
                                            LdsChar* smem, LdsChar* scratch, int32_t block) {
@@ -491,14 +492,23 @@ __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __res
                     }
                     const int32_t c = (GATHER_P ? ch : other) + 16 * (wm * kM + i0);
                     const int32_t r = (GATHER_P ? other : ch) + 16 * (wn * kN + j);
-                    flush_rows<true>(scratch, ((GATHER_P ? h1 : cols_out) - c) * 2, [&](int row) {
+                    flush_rows<ONCE>(scratch, ((GATHER_P ? h1 : cols_out) - c) * 2, [&](int row) {
                         return r + row < (GATHER_P ? rows_out : h1) ? o + (int64_t)(r + row) * cols_out + c : nullptr;
                     });
                 }
             ch += kStep;
         };
         if (ksteps == 0) {  // no entries: zeros
-            for (int32_t step = 0; step < hsteps; ++step) store();
+            if constexpr (PARTS) {
+                for (int32_t step = 0; step < hsteps; ++step) store();
+            } else {  // the expert's items share its matrix in runs of whole lines
+                const int64_t pieces = (int64_t)rows_out * cols_out / 8;
+                const int64_t share = (pieces / (spans * others) + 8) / 8 * 8;
+                u32x4* o = reinterpret_cast<u32x4*>(out + (int64_t)e * rows_out * cols_out);
+                const int64_t last = min(pieces, (q + 1) * share);
+                for (int64_t i = q * share + threadIdx.x; i < last; i += 64 * WAVES)
+                    __builtin_nontemporal_store(u32x4{0u, 0u, 0u, 0u}, o + i);
+            }
             continue;
         }
         using G = FfnGroups<kM, kM == 8 ? 4 : 2>;
@@ -563,7 +573,7 @@ __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __res
 
 // Both products in one launch (the second one's workgroups follow the first one's, so that the last of one
 // and the first of the other share the chip).
-template <int CT1, int CT2, int RT, int WAVES, bool PARTS>
+template <int CT1, int CT2, int RT, int WAVES, bool PARTS, bool ONCE2>
 __global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(DwArgs w1, DwArgs w2,
                                                                 const int32_t* __restrict__ offsets,
                                                                 const int32_t* __restrict__ sorted, int32_t n,
@@ -574,9 +584,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ffn_bwd_dw_kernel(DwArgs w1, Dw
     LdsChar* scratch = (LdsChar*)scratch_raw + ffn_wave() * kFfnScratch;
     const int32_t block = (int32_t)blockIdx.x;
     if (block < w1.blocks)
-        ffn_bwd_dw<CT1, RT, WAVES, true, PARTS>(w1, offsets, sorted, n, k, M, smem, scratch, block);
+        ffn_bwd_dw<CT1, RT, WAVES, true, PARTS, true>(w1, offsets, sorted, n, k, M, smem, scratch, block);
     else
-        ffn_bwd_dw<CT2, RT, WAVES, false, PARTS>(w2, offsets, sorted, n, k, M, smem, scratch, block - w1.blocks);
+        ffn_bwd_dw<CT2, RT, WAVES, false, PARTS, ONCE2>(w2, offsets, sorted, n, k, M, smem, scratch, block - w1.blocks);
 }
 
 // Adds the runs' partial gradients in order: a thread takes eight values, of dW1t and behind them of dW2t.
@@ -655,7 +665,7 @@ DwArgs dw_args(const FfnPlan& p, const FfnArgs& a, const uint16_t* P, const uint
     return d;
 }
 
-template <int CT1, int CT2, int RT, int WAVES, bool PARTS>
+template <int CT1, int CT2, int RT, int WAVES, bool PARTS, bool ONCE2>
 void dw_launch(const FfnPlan& p, const FfnArgs& a, char* ws, hipStream_t stream) {
     const uint16_t* hidden = reinterpret_cast<const uint16_t*>(ws + p.off_hidden);
     const uint16_t* dgu = reinterpret_cast<const uint16_t*>(ws + p.off_dgu);
@@ -663,7 +673,7 @@ void dw_launch(const FfnPlan& p, const FfnArgs& a, char* ws, hipStream_t stream)
     const int64_t size1 = (int64_t)a.M * 2 * a.s * a.h;
     const DwArgs w1 = dw_args(p, a, a.x, dgu, 2 * a.s, a.h, (2 * a.s + RT - 1) / RT, CT1, a.dW1t, parts);
     const DwArgs w2 = dw_args(p, a, hidden, a.du, a.h, a.s, (a.s + CT2 - 1) / CT2, RT, a.dW2t, parts + size1);
-    ffn_bwd_dw_kernel<CT1, CT2, RT, WAVES, PARTS><<<(unsigned)(w1.blocks + w2.blocks), 64 * WAVES, 0, stream>>>(
+    ffn_bwd_dw_kernel<CT1, CT2, RT, WAVES, PARTS, ONCE2><<<(unsigned)(w1.blocks + w2.blocks), 64 * WAVES, 0, stream>>>(
         w1, w2, a.offsets, a.sorted, (int32_t)p.n, a.k, a.M);
     if (PARTS) {
         const int64_t size = dw_size(a.h, a.s, a.M);
@@ -748,12 +758,17 @@ hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspa
             reinterpret_cast<const float*>(ws + p.off_dxs), a.idx, a.T, a.h, a.M, a.k, a.dx, colblocks,
             reinterpret_cast<const float*>(ws + p.off_dgp), dgate_parts(p, a.s), a.sorted, a.dgate);
     }
+    // Nontemporal stores keep what the next kernels read in the caches (h = 512, s = 64, 4096 experts of 32
+    // rows: 623 us for the call against 651; s = 72, 1024 experts of 16 rows: 180 with dW1t alone against 209).
+    // Not for dW2t where a row takes several tiles of 64 columns that split a line (s = 72: 188 with both).
     if (p.dw_tile == 256)
-        dw_launch<256, 256, 256, 8, false>(p, a, ws, stream);
+        dw_launch<256, 256, 256, 8, false, true>(p, a, ws, stream);
     else if (p.dw_parts > 1)
-        dw_launch<128, 64, 128, 4, true>(p, a, ws, stream);
+        dw_launch<128, 64, 128, 4, true, false>(p, a, ws, stream);
+    else if (a.s <= 64 || a.s % 64 == 0)
+        dw_launch<128, 64, 128, 4, false, true>(p, a, ws, stream);
     else
-        dw_launch<128, 64, 128, 4, false>(p, a, ws, stream);
+        dw_launch<128, 64, 128, 4, false, false>(p, a, ws, stream);
     return hipGetLastError();
 }
 

@@ -207,8 +207,8 @@ __device__ __forceinline__ void place_bf16(LdsChar* scratch, int i, f32x4 v) {
     *reinterpret_cast<__attribute__((address_space(3))) u32x2*>(scratch + (l & 15) * 144 + i * 32 + (l >> 4) * 8) =
         u32x2{b.x, b.y};
 }
-// LAST marks rows that this call does not read again (nontemporal).
-template <bool LAST = false, typename F>
+// ONCE marks rows that this call does not read again (nontemporal).
+template <bool ONCE = false, typename F>
 __device__ __forceinline__ void flush_rows(LdsChar* scratch, int left, F row_of) {
     const int l = ffn_lane(), at = (l & 7) * 16;
 #pragma unroll
@@ -217,7 +217,7 @@ __device__ __forceinline__ void flush_rows(LdsChar* scratch, int left, F row_of)
         char* p = reinterpret_cast<char*>(row_of(row));
         const u32x4 v = *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(scratch + row * 144 + at);
         if (!p || at >= left) continue;
-        if constexpr (LAST)
+        if constexpr (ONCE)
             __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p + at));
         else
             *reinterpret_cast<u32x4*>(p + at) = v;
