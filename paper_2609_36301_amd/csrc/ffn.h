@@ -42,13 +42,17 @@ hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspa
 
 // Columns that a workgroup takes, in steps of `step`, of a product whose contraction is `len` long: a
 // single step where the contraction alone fills the pipeline (eight stages), or where the groups of rows are
-// too few to fill the chip four times over with more; else up to 512.
+// too few to fill the chip four times over with more; else up to 512.  us, forward and backward, single step :
+// up to 512: 4096 experts of h = 512, s = 64, 32 rows 256 + 680 : 215 + 621; 128 experts of h = 2048, s = 320,
+// 256 rows 276 + 886 : 264 + 844; 200 experts of h = 528, s = 72, 9 rows 24 + 61 : 26 + 74.
 inline int32_t ffn_span(int32_t len, int32_t step, int64_t groups, int32_t cols) {
     return len > 512 || groups * ((cols + 511) / 512) < 1024 ? step : 512;
 }
 
 // What `items` workgroups with tiles of `bm` rows cost that run `steps` stages each: the rounds in which they
-// fill the chip (two of up to 128 rows to a CU, one of 256) times the stages times the time of a stage.
+// fill the chip (two of up to 128 rows to a CU, one of 256) times the stages times the time of a stage.  The
+// stages' times were fitted to 196 measured shapes: against one of 128-row tiles, two to a CU, 0.8 with one to
+// a CU, 0.75 with 64 rows (half the work) and 1.7 with 256 (four times the work, one to a CU).
 inline int64_t ffn_cost(int64_t items, int64_t steps, int32_t bm) {
     const int64_t slots = bm == 256 ? 256 : 512;
     const int64_t stage = bm == 256 ? 34 : bm == 128 ? (items <= 256 ? 16 : 20) : 15;

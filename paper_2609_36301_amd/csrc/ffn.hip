@@ -123,7 +123,11 @@ __global__ __launch_bounds__(kTileThreads) void ffn_tiles_kernel(const int32_t* 
 // ------------------------------------------------------------------------------ down
 // A workgroup computes y of one tile and `hspan` columns in steps of kCols: the rows of W2t are the M
 // side, the tile's rows of A the N side.  The pipeline runs over (column step, contraction step) pairs,
-// so that the short contraction of small experts (one step up to s = 64) does not drain it.
+// so that the short contraction of small experts (one step up to s = 64) does not drain it.  Bound like
+// ffn_up: 4096 experts of h = 512, s = 64 with 32 rows 100 us, 4.2 TB/s (a third of it y); 32 experts of
+// h = 2048, s = 1024 with 1024 rows 222 us, 619 TFLOP/s (256 x 256 tiles, half as many rounds over the chip
+// as ffn_up, and the rest of the last one idle).  y is stored 8 bytes a lane, 32 bytes of a row, and L2 joins
+// the lines (stored by way of LDS in whole lines it was slower here).
 template <int BM>
 struct DownShape {
     static constexpr int kWaves = BM == 256 ? 8 : 4;
@@ -248,7 +252,8 @@ __global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(Ff
 // rows, and the weights' way from memory is all that counts: they go straight into the registers of the
 // 16x16x32 MFMA (16 weight rows against 16 tokens), with no LDS, no tile list and no barrier on the way.
 // Workgroups are laid over the sorted entries; the one whose entry is the first, 17th, ... of its expert
-// takes that and the next 15 entries, the others end at once.
+// takes that and the next 15 entries, the others end at once.  One token, 8 experts of h = 2048, s = 64: 7.5 us
+// up and 4.1 us down, most of it the three dependent reads (sorted, idx, weights) and the launch.
 constexpr int kFewWaves = 8;
 constexpr int kFewRows = 16;
 constexpr int kFewUnits = 16;    // hidden units of an up workgroup
@@ -430,7 +435,16 @@ unsigned grid_of(int64_t items) {
 
 unsigned few_grid(int64_t items) { return (unsigned)std::min<int64_t>(items, 1 << 22); }
 
-// Rows of a tile.
+// Rows of a tile: 32 where experts have less than 24 rows (then mostly one tile, whose weights are not read
+// again; us, 32 : 64 rows, 4096 experts of h = 512, s = 64 with 12 rows 164 : 185, with 24 185 : 205, with 32
+// 222 : 215; 64 experts of h = 1024, s = 256 with 24 rows 32 : 27), else what costs least by ffn_cost.  Large
+// tiles need less from the caches, small ones fill the chip: us for 64 : 128 : 256 rows,
+//   32 experts of h = 2048, s = 1024, 48 rows 98 : 107 : 119, 384 rows 292 : 236 : 206, 1024 rows - : 608 : 560
+//   64 experts of h = 1024, s = 512, 192 rows - : 73 : 66, 256 rows - : 90 : 114 (the 256-row tiles take one and
+//   a half rounds), 2048 rows - : 581 : 539
+//   a dense block of h = 2048, s = 1024, 1024 rows 35 : 46 : 88, 4096 rows 80 : 65 : 92, 8192 rows 149 : 115 : 100
+// Over 196 shapes (1 to 4096 experts, 12 to 16384 rows each) the choice is 1.3% off the best on geometric
+// mean and 21% at most; one by the mean number of rows alone was 11% off, and 2.6 times at most.
 int32_t tile_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
     if (n / std::max<int64_t>(1, std::min<int64_t>(n, M)) < 24) return 32;
     int32_t best = 64;
@@ -483,18 +497,26 @@ void ffn_tiles_plan(int64_t n, int32_t M, int32_t bm, FfnPlan* p) {
 }
 
 // Upper bound on the workgroups along the entries that have work in the kernels without tiles.
-static int64_t few_starts(const FfnPlan& p, int32_t M) { return std::min<int64_t>(p.n, std::min<int64_t>(p.n, M) + p.n / kFewRows); }
+static int64_t few_starts(const FfnPlan& p, int32_t M) {
+    return std::min<int64_t>(p.n, std::min<int64_t>(p.n, M) + p.n / kFewRows);
+}
 
 // Whether the kernels without tiles are taken: while the weights that they read (once for every 16 rows) are
-// few bytes and few workgroups end at once.  They save a launch and the latency of the stages (16 MB + 40 KB
-// for every column and hidden unit that the stages run over, at what their bandwidth is worse).
+// few bytes and few workgroups end at once.  They save a launch and the latency of the stages, but stream at
+// 4 TB/s where the tiled kernels reach 6: 16 MB even out the launch, and 40 KB every column and hidden unit that
+// the stages run over.  us, without tiles : with, one row per expert: h = 2048, s = 64, 8 entries 10.8 : 20.8, 128
+// entries 24 : 34, 512 entries 98 : 73; h = 1024, s = 512, 16 entries 16 : 19, 32 entries 30 : 22; h = 4096,
+// s = 1024, 4 entries 27 : 43, 16 entries 78 : 61; a dense block of s = 1024, h = 2048, 32 rows 18 : 29, 128
+// rows 52 : 40; s = 8, h = 3408, 1430 entries (20020 workgroups) 54 : 46.
 static bool few(const FfnPlan& p, int32_t h, int32_t s, int32_t M) {
-    const int64_t groups = std::max((s + kFewUnits - 1) / kFewUnits, (h + kFewWaves * kFewCols - 1) / (kFewWaves * kFewCols));
+    const int64_t groups =
+        std::max((s + kFewUnits - 1) / kFewUnits, (h + kFewWaves * kFewCols - 1) / (kFewWaves * kFewCols));
     return few_starts(p, M) * 6 * h * s <= ((int64_t)16 << 20) + (int64_t)40960 * (h + s) && p.n * groups <= 4096;
 }
 
 // Whether a workgroup of ffn_few_down shares columns: while the workgroups that have the whole contraction
-// per wave would be few against its length.
+// per wave would be few against its length.  us, sharing : not, h = 1024, s = 4096, 1 row 17 : 77; h = 4096,
+// s = 1024, 4 entries 27 : 40, 16 entries 78.5 : 81; s = 256, 4 entries 17.0 : 18.6, 16 entries 31.5 : 24.5.
 static bool few_split(const FfnPlan& p, int32_t h, int32_t s, int32_t M) {
     return 4 * few_starts(p, M) * ((h + kFewWaves * kFewCols - 1) / (kFewWaves * kFewCols)) <= s;
 }

@@ -34,8 +34,9 @@ namespace more {
 
 // ------------------------------------------------------------------------------ up, tiles of up to 128 rows
 // (Two kernels for tiles of 256 rows: there the matrix products count, a tile of 128 hidden units halves
-// what the caches deliver, and three sets of accumulators do not fit; 32 experts of s = 1024, h = 2048
-// 654 us against 820.  For the 4096 experts of s = 64, h = 512 this one kernel takes 213 us against 235.)
+// what the caches deliver, and three sets of accumulators do not fit; 32 experts of s = 1024, h = 2048 with
+// 1024 rows 654 us against 820.  For 4096 experts of s = 64, h = 512 with 32 rows, where the weights' way from
+// memory counts, this one kernel takes 213 us (805 MB of weights: 4.1 TB/s) against 235.)
 // A workgroup computes one tile and kUnits hidden units: first G and U (x rows against the gate and up
 // rows of W1t), then dA0 (du rows against a column tile of W2t) into other accumulators.  In turn rather
 // than side by side: a stage is smaller by the second pair of operands, so twice as many workgroups fit
@@ -225,7 +226,11 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
 // slowest: dA0 = du W2t[e] (the token's row of du, contraction over h, results in sorted order) and the
 // entries' shares of dx = [dG dU] W1t[e] (contraction over 2s, results in entry order).  The weights are a
 // column tile (M side), the rows a row tile (N side).  A workgroup computes `span` columns in steps of
-// kCols; the pipeline runs over (column step, contraction step) pairs.
+// kCols; the pipeline runs over (column step, contraction step) pairs.  Bound like the forward pass: 32 experts
+// of h = 2048, s = 1024 with 1024 rows, dA0 225 us (610 TFLOP/s), dx 390 us (705 TFLOP/s) on tiles of 256 rows
+// and 476 us on tiles of 128; 4096 experts of h = 512, s = 64 with 32 rows, dx 164 us (840 MB, 5.1 TB/s).
+// The shares of dx go through memory in fp32, a third of that traffic: in bf16 dx would carry k + 1 roundings
+// for one.
 constexpr int rows_threads(int bm) { return bm == 256 ? 512 : 256; }
 template <int BM>
 struct RowsShape {
@@ -349,7 +354,8 @@ __global__ __launch_bounds__(rows_threads(BM), 2) void ffn_bwd_rows_kernel(
 
 // ------------------------------------------------------------------------------ sums over the entries
 // A thread adds eight columns of a token's k rows in order; dropped entries (id outside [0, M)) are left
-// out.  The threads past the columns add the partials of dgate.
+// out.  The threads past the columns add the partials of dgate.  Memory-bound: 302 MB (h = 2048, 32768 entries)
+// in 55 us, 5.5 TB/s.
 __global__ __launch_bounds__(256) void ffn_bwd_sum_kernel(const float* __restrict__ dxs, const int32_t* __restrict__ idx,
                                                        int32_t T, int32_t h, int32_t M, int32_t k,
                                                        uint16_t* __restrict__ dx, int64_t colblocks,
@@ -396,6 +402,9 @@ __global__ __launch_bounds__(256) void ffn_bwd_sum_kernel(const float* __restric
 // PARTS: the entries of an expert are cut into `parts` runs and a workgroup takes one tile and one run; the
 // fp32 results of run i go to parts_out + i part_stride, and ffn_bwd_dw_sum adds them.  ONCE: nontemporal
 // stores.
+// Bound by the gradients' way to memory where experts are small (4096 of h = 512, s = 64 with 32 rows 236 us, 805 MB
+// written, 134 read: 4.0 TB/s), by the operands' way from L2 where they are large (32 of h = 2048, s = 1024 with
+// 1024 rows 540 us, 763 TFLOP/s).
 struct DwArgs {
     const uint16_t *P, *Q;
     int32_t rows_out, cols_out, hspan, blocks;  // workgroups of this product
@@ -682,7 +691,11 @@ void dw_launch(const FfnPlan& p, const FfnArgs& a, char* ws, hipStream_t stream)
     }
 }
 
-// Tile size of the weight gradients, and the runs into which an expert's entries are cut.
+// Tile size of the weight gradients, by the same cost as the rows' tiles (call in us, 256 : 128, 32 experts of
+// h = 2048, s = 1024 with 1024 rows 1599 : 1803, a dense block of 16384 rows 1037 : 728, whose 96 large tiles leave
+// most CUs idle), and the runs into which an expert's entries are cut: as many as bring the tiles to 256, of
+// four stages at least (a dense block of h = 512, s = 128, runs : us, 16384 rows 1 : 341, 8 : 100, 32 : 80, 64 : 88;
+// 1024 rows 1 : 48, 4 : 39, 16 : 42; h = 2048, s = 1024 with 256 tiles and more, 1 : 728, 2 : 761).
 void dw_plan(int64_t n, int32_t h, int32_t s, int32_t M, FfnPlan* p) {
     const int64_t steps = std::max<int64_t>(1, n / M / kFfnBK);
     auto tiles = [&](int32_t a, int32_t b) { return (int64_t)((a + b - 1) / b); };
@@ -693,7 +706,9 @@ void dw_plan(int64_t n, int32_t h, int32_t s, int32_t M, FfnPlan* p) {
     if (p->dw_tile == 128) p->dw_parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(256 / small, steps / 4));
 }
 
-// Rows of a tile, as in the forward pass.
+// Rows of a tile, as in the forward pass (over the same 196 shapes 0.9% off the best on geometric mean, at
+// most 20%; us for 64 : 128 : 256 rows, 32 experts of h = 2048, s = 1024, 96 rows 377 : 315 : 339, 384 rows 884 :
+// 839 : 659; 4096 experts of h = 512, s = 64, 32 rows 623 : 662 : 1134).
 int32_t backward_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
     if (n / std::max<int64_t>(1, std::min<int64_t>(n, M)) < 24) return 32;
     int32_t best = 64;
