@@ -55,9 +55,15 @@ def _check(name: str, t, dtype, shape, device):
     raise ValueError("%s must be on %s, got %s" % (name, device, t.device))
 
 
+# The handle of a device's current stream, by the device's index (without a Stream object around it, which
+# takes 1.9 us, a quarter of a short call).
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _call(name: str, device: torch.device, *args):
     """The library call `name` on the device's current stream (the library works on the current device)."""
-    stream = torch.cuda.current_stream(device).cuda_stream
+    stream = _stream(device.index)
     fn = getattr(_lib.load(), name)
     if torch.cuda.current_device() == device.index:
         st = fn(*args, stream)
