@@ -341,8 +341,9 @@ more_status more_route_lowrank_noalloc(const uint16_t* x, const uint16_t* R1t, c
  * 1 <= k <= MORE_K_MAX (k may exceed M: an id may occur more than once in a token); T k <= 2^31 - 2^16,
  * M < 2^30.  T == 0 writes nothing.  offsets and sorted that are not those of idx give undefined values
  * in y (no access outside the buffers).
- * Numerics: fp32 accumulation of exact bf16 products; A is rounded to bf16 once, between the two
- * contractions; activation and gate in fp32.  The sums run in a fixed order.
+ * Numerics: fp32 accumulation of exact bf16 products; between the two contractions A is rounded to bf16
+ * once, or, where few values are (T k s <= 2^15, and in some decode steps), to a sum of two bf16;
+ * activation and gate in fp32.  The sums run in a fixed order.
  */
 more_status more_expert_ffn(const uint16_t* x, const uint16_t* W1t, const uint16_t* W2t, int64_t T,
                             int32_t h, int32_t s, int32_t M, int32_t k, const int32_t* idx,
@@ -363,7 +364,7 @@ more_status more_expert_ffn_workspace_size(int64_t T, int32_t h, int32_t s, int3
  *   workspace / workspace_bytes   at least more_expert_ffn_backward_workspace_size() bytes, 256-byte
  *                              aligned (NULL allowed when T == 0)
  * Limits as for more_expert_ffn.  Numerics: bf16 operands with fp32 accumulation; the gradients of the
- * pre-activations and gate A are rounded to bf16 once, the entries' shares of dx are added in fp32,
+ * pre-activations and gate A are rounded to bf16 once (to a sum of two bf16 where T k s <= 2^15), the entries' shares of dx are added in fp32,
  * dgate comes from unrounded fp32 values.  Nothing is added atomically: a call gives the same bits on
  * every run.
  */

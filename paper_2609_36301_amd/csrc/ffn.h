@@ -22,11 +22,19 @@ struct FfnArgs {
     uint16_t* dW1t;          // [M][2s][h]
     uint16_t* dW2t;          // [M][h][s]
     float* dgate;            // [T][k] or NULL
+    int32_t planes;          // of what the kernels hand on in bf16 (FfnPlan::planes)
 };
 
 struct FfnPlan {
     int64_t n;        // T k entries
     int32_t bm;       // rows of a tile (all of one expert)
+    int32_t few;      // (forward) the kernels without tiles
+    // The hidden units (and, backward, the gradients of the pre-activations) go from kernel to kernel in bf16,
+    // the matrix cores' operand type.  A rounding error of each then sits in all its products, as large as the
+    // results' own rounding (together 1.41 of it) on average over many; where few are rounded (n s <= 2^15;
+    // below it the factor scatters by 2% and more, at 512 values by 10%) and the products are small, they are
+    // carried as a sum of two bf16 (planes = 2), [planes][n][s] and [planes][n][2s].
+    int32_t planes;
     int64_t tiles;    // bound on the number of tiles
     int32_t sums;     // workgroups that count tiles ahead of the list (0: none)
     int32_t dw_tile;  // rows and columns of a tile of the weight gradients (128 or 256)
@@ -37,8 +45,8 @@ struct FfnPlan {
 
 void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p);
 void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p);
-hipError_t ffn_launch(const FfnPlan& p, const FfnArgs& a, uint16_t* y, void* workspace, hipStream_t stream);
-hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspace, hipStream_t stream);
+hipError_t ffn_launch(const FfnPlan& p, FfnArgs a, uint16_t* y, void* workspace, hipStream_t stream);
+hipError_t ffn_backward_launch(const FfnPlan& p, FfnArgs a, void* workspace, hipStream_t stream);
 
 // Columns that a workgroup takes, in steps of `step`, of a product whose contraction is `len` long: a
 // single step where the contraction alone fills the pipeline (eight stages), or where the groups of rows are
@@ -58,6 +66,8 @@ inline int64_t ffn_cost(int64_t items, int64_t steps, int32_t bm) {
     const int64_t stage = bm == 256 ? 34 : bm == 128 ? (items <= 256 ? 16 : 20) : 15;
     return (items + slots - 1) / slots * steps * stage;
 }
+constexpr int64_t kFfnTwoPlanes = 1 << 15;
+
 // Twice the expected number of tiles of n entries over M experts whose rows scatter by their mean's root.
 int64_t ffn_expected_tiles2(int64_t n, int32_t M, int32_t bm);
 

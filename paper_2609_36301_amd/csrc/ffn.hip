@@ -12,7 +12,8 @@
 //   ffn_down    A W2^T times the gate, to the entry's row of y
 // With few rows per expert (a decode step) ffn_few_up and ffn_few_down do the same without tiles.
 // Numerics: both contractions take bf16 operands with fp32 accumulation; A is rounded to bf16 once (the
-// matrix cores' operand type), the activation and the gate are applied in fp32.
+// matrix cores' operand type), or to two bf16 addends where few values are (FfnPlan::planes); the activation and
+// the gate are applied in fp32.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(Ff
         for (int i = 0; i < S::kM; ++i)
 #pragma unroll
             for (int j = 0; j < S::kN; ++j) acc[i][j] = zero_f32x4();
-        const int32_t ksteps = (s + kFfnBK - 1) / kFfnBK;
+        const int32_t ksteps = (s + kFfnBK - 1) / kFfnBK, kall = ksteps * a.planes;
         const int32_t hsteps = (h1 - h0 + S::kCols - 1) / S::kCols;
         // (column step, contraction step) of the next load and of the next compute
         int32_t lh = h0, lk = 0, ch = h0, ck = 0;
@@ -194,13 +195,14 @@ __global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(Ff
         using M = FfnFragments<G::kSize>;
         using N = FfnFragments<S::kN>;
         ffn_pipeline<S::kStages, S::kLoads, M, N>(
-            ksteps * hsteps, 16 * wn * S::kN < tile.rows,
+            kall * hsteps, 16 * wn * S::kN < tile.rows,
             [&](int, int slot) {
                 LdsChar* at = smem + slot * S::kStageBytes;
                 if (lk == 0) weights.init([&](int i) { return W + (int64_t)min(lh + i, h - 1) * s; });
-                weights.load(at, lk * kFfnBK, s);
-                rows.load(at + S::kRowsAt, lk * kFfnBK, s);
-                if (++lk == ksteps) {
+                const int32_t k0 = (lk < ksteps ? lk : lk - ksteps) * kFfnBK;
+                weights.load(at, k0, s);
+                rows.load(at + S::kRowsAt, k0, s, lk < ksteps ? 0 : (int64_t)n * s);
+                if (++lk == kall) {
                     lk = 0;
                     lh += S::kCols;
                 }
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(Ff
                             }
                 },
                 [&] {
-                    if (++ck < ksteps) return;
+                    if (++ck < kall) return;
 #pragma unroll
                     for (int j = 0; j < S::kN; ++j) {
 #pragma unroll
@@ -291,7 +293,8 @@ __device__ __forceinline__ bf16x8 few_load(const uint16_t* p, bool in) {
     return load_bf16x8(in ? p : ffn_zeros);
 }
 
-// Waves take pieces of 64 contraction values in turn and their sums are added in wave order.
+// Waves take pieces of 64 contraction values in turn and their sums are added in wave order.  (These kernels
+// always carry A as two planes.)
 __global__ __launch_bounds__(64 * kFewWaves) void ffn_few_up_kernel(FfnArgs a, uint16_t* __restrict__ hidden) {
     constexpr int kAhead = 4;  // pieces in flight per wave
     __shared__ f32x4 part[kFewWaves][2][64];
@@ -344,8 +347,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void ffn_few_up_kernel(FfnArgs a, u
                 float v[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) v[q] = g[q] * ffn_sigmoid(g[q]) * u[q];
-                *reinterpret_cast<uint2*>(hidden + (int64_t)(i + (lane & 15)) * s + c) =
-                    pack_bf16x4(v[0], v[1], v[2], v[3]);
+                uint16_t* out = hidden + (int64_t)(i + (lane & 15)) * s + c;
+                *reinterpret_cast<uint2*>(out) = pack_bf16x4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<uint2*>(out + (int64_t)n * s) = pack_bf16_rest(v[0], v[1], v[2], v[3]);
             }
         }
     }
@@ -386,19 +390,23 @@ __global__ __launch_bounds__(64 * kFewWaves) void ffn_few_down_kernel(FfnArgs a,
         const float gate = a.gate && mine ? a.gate[p] : 1.0f;
         f32x4 acc[2] = {zero_f32x4(), zero_f32x4()};
         for (int32_t k0 = SPLIT ? 32 * wave : 0; k0 < s; k0 += kStep * AHEAD) {
-            bf16x8 fw[2][AHEAD], fh[AHEAD];
+            bf16x8 fw[2][AHEAD], fh[2][AHEAD];
 #pragma unroll
             for (int q = 0; q < AHEAD; ++q) {
                 const int32_t k = k0 + kStep * q;
                 const bool in = k + at < s;
-                fh[q] = few_load(hid + k, in);
+                fh[0][q] = few_load(hid + k, in);
+                fh[1][q] = few_load(hid + (int64_t)n * s + k, in);
 #pragma unroll
                 for (int r = 0; r < 2; ++r) fw[r][q] = few_load(w[r] + k, in);
             }
 #pragma unroll
             for (int q = 0; q < AHEAD; ++q)
 #pragma unroll
-                for (int r = 0; r < 2; ++r) acc[r] = mfma_16x16x32(fw[r][q], fh[q], acc[r]);
+                for (int r = 0; r < 2; ++r) {
+                    acc[r] = mfma_16x16x32(fw[r][q], fh[0][q], acc[r]);
+                    acc[r] = mfma_16x16x32(fw[r][q], fh[1][q], acc[r]);
+                }
         }
         if constexpr (SPLIT) {
             __syncthreads();  // the item before has been read
@@ -523,8 +531,10 @@ static bool few_split(const FfnPlan& p, int32_t h, int32_t s, int32_t M) {
 
 void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {
     ffn_tiles_plan(T * k, M, tile_rows(T * k, h, s, M), p);
+    p->few = few(*p, h, s, M);
+    p->planes = p->few || p->n * s <= kFfnTwoPlanes ? 2 : 1;
     p->off_hidden = p->workspace_bytes;
-    p->workspace_bytes += align256((size_t)p->n * s * 2);
+    p->workspace_bytes += align256((size_t)p->n * s * 2 * p->planes);
 }
 
 hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* workspace, hipStream_t stream) {
@@ -538,9 +548,10 @@ hipError_t ffn_tiles_launch(const FfnPlan& p, const FfnArgs& a, void* workspace,
     return hipGetLastError();
 }
 
-hipError_t ffn_launch(const FfnPlan& p, const FfnArgs& a, uint16_t* y, void* workspace, hipStream_t stream) {
+hipError_t ffn_launch(const FfnPlan& p, FfnArgs a, uint16_t* y, void* workspace, hipStream_t stream) {
     char* ws = static_cast<char*>(workspace);
-    if (few(p, a.h, a.s, a.M)) {
+    a.planes = p.planes;
+    if (p.few) {
         uint16_t* hidden = reinterpret_cast<uint16_t*>(ws + p.off_hidden);
         ffn_few_up_kernel<<<few_grid(p.n * ((a.s + kFewUnits - 1) / kFewUnits)), 64 * kFewWaves, 0, stream>>>(a, hidden);
         const bool split = few_split(p, a.h, a.s, a.M);

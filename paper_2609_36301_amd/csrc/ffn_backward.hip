@@ -18,7 +18,7 @@
 //                 zeros
 // Every sum runs in a fixed order: nothing is added atomically, and a call gives the same bits on every
 // run.  Numerics: bf16 operands with fp32 accumulation; [dG dU] and gate A are rounded to bf16 once (the
-// matrix cores' operand type), the entries' shares of dx stay in fp32 until they are summed, dgate comes
+// matrix cores' operand type), or to two bf16 addends where few values are (FfnPlan::planes), the entries' shares of dx stay in fp32 until they are summed, dgate comes
 // from unrounded fp32 values.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -203,6 +203,12 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
                     *reinterpret_cast<uint2*>(hidden + at * s + c) = pack_bf16x4(A[0], A[1], A[2], A[3]);
                     *reinterpret_cast<uint2*>(dgu + at * 2 * s + c) = pack_bf16x4(dG[0], dG[1], dG[2], dG[3]);
                     *reinterpret_cast<uint2*>(dgu + at * 2 * s + s + c) = pack_bf16x4(dU[0], dU[1], dU[2], dU[3]);
+                    if (a.planes > 1) {
+                        uint16_t *h1 = hidden + (int64_t)n * s, *g1 = dgu + (int64_t)n * 2 * s;
+                        *reinterpret_cast<uint2*>(h1 + at * s + c) = pack_bf16_rest(A[0], A[1], A[2], A[3]);
+                        *reinterpret_cast<uint2*>(g1 + at * 2 * s + c) = pack_bf16_rest(dG[0], dG[1], dG[2], dG[3]);
+                        *reinterpret_cast<uint2*>(g1 + at * 2 * s + s + c) = pack_bf16_rest(dU[0], dU[1], dU[2], dU[3]);
+                    }
                 }
             }
             dot += __shfl_xor(dot, 16, 64);
@@ -286,7 +292,7 @@ __global__ __launch_bounds__(rows_threads(BM), 2) void ffn_bwd_rows_kernel(
         for (int i = 0; i < S::kM; ++i)
 #pragma unroll
             for (int j = 0; j < S::kN; ++j) acc[i][j] = zero_f32x4();
-        const int32_t ksteps = (len + kFfnBK - 1) / kFfnBK;
+        const int32_t ksteps = (len + kFfnBK - 1) / kFfnBK, kall = TOKENS ? ksteps : ksteps * a.planes;
         const int32_t csteps = (c1 - c0 + S::kCols - 1) / S::kCols;
         // (column step, contraction step) of the next load and of the next product
         int32_t lc = c0, lk = 0, cc = c0, ck = 0;
@@ -295,15 +301,15 @@ __global__ __launch_bounds__(rows_threads(BM), 2) void ffn_bwd_rows_kernel(
         using N = FfnFragments<S::kN>;
         using Stage = StagePair<decltype(weights), decltype(rows)>;
         ffn_pipeline_staged<Stage, G::kGroups, M, N>(
-            ksteps * csteps, 16 * wn * S::kN < tile.rows,
+            kall * csteps, 16 * wn * S::kN < tile.rows,
             [&](int, Stage& st) {
-                const int32_t k0 = lk * kFfnBK;
+                const int32_t k0 = (lk < ksteps ? lk : lk - ksteps) * kFfnBK;
                 weights.fetch(st.a, cols - lc, [&](int i) {
                     const int kappa = k0 + weights.row(i);
                     return kappa < len ? We + (int64_t)kappa * cols + lc : nullptr;
                 });
-                rows.fetch(st.b, k0, len);
-                if (++lk == ksteps) {
+                rows.fetch(st.b, k0, len, lk < ksteps ? 0 : (int64_t)n * len);
+                if (++lk == kall) {
                     lk = 0;
                     lc += S::kCols;
                 }
@@ -335,7 +341,7 @@ __global__ __launch_bounds__(rows_threads(BM), 2) void ffn_bwd_rows_kernel(
                             }
                 },
                 [&] {
-                    if (++ck < ksteps) return;
+                    if (++ck < kall) return;
 #pragma unroll
                     for (int j = 0; j < S::kN; ++j) {
 #pragma unroll
@@ -409,7 +415,7 @@ struct DwArgs {
     const uint16_t *P, *Q;
     int32_t rows_out, cols_out, hspan, blocks;  // workgroups of this product
     uint16_t* out;
-    int32_t parts;
+    int32_t planes, parts;
     float* parts_out;
     int64_t part_stride;
 };
@@ -452,7 +458,7 @@ __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __res
         QLoader ql;
         pl.init();
         ql.init();
-        const int32_t ksteps = (end - begin + kFfnBK - 1) / kFfnBK;
+        const int32_t ksteps = (end - begin + kFfnBK - 1) / kFfnBK, kall = ksteps * d.planes;
         const int32_t hsteps = (h1 - h0 + kStep - 1) / kStep;
         // the gathered operand's entries of the next load (read one load ahead)
         int32_t entry[kGathered];
@@ -526,25 +532,27 @@ __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __res
         using Stage = StagePair<PLoader, QLoader>;
         fetch(0);
         ffn_pipeline_staged<Stage, G::kGroups, MF, NF>(
-            ksteps * hsteps, true,
+            kall * hsteps, true,
             [&](int, Stage& st) {
-                const int32_t i0 = begin + lk * kFfnBK;
+                const bool rest = lk >= ksteps;  // the second plane of the operand that is not gathered
+                const int32_t i0 = begin + (rest ? lk - ksteps : lk) * kFfnBK;
+                const int64_t first = rest ? n : 0;
                 const int32_t c = GATHER_P ? lh : other, r = GATHER_P ? other : lh;
                 pl.fetch(st.a, cols_out - c, [&](int i) -> const uint16_t* {
                     if constexpr (GATHER_P) return gathered(i, P + c, cols_out);
                     const int32_t row = i0 + pl.row(i);
-                    return row < end ? P + (int64_t)row * cols_out + c : nullptr;
+                    return row < end ? P + (first + row) * cols_out + c : nullptr;
                 });
                 ql.fetch(st.b, rows_out - r, [&](int i) -> const uint16_t* {
                     if constexpr (!GATHER_P) return gathered(i, Q + r, rows_out);
                     const int32_t row = i0 + ql.row(i);
-                    return row < end ? Q + (int64_t)row * rows_out + r : nullptr;
+                    return row < end ? Q + (first + row) * rows_out + r : nullptr;
                 });
-                if (++lk == ksteps) {
+                if (++lk == kall) {
                     lk = 0;
                     lh += kStep;
                 }
-                if (ksteps > 1) fetch(lk);
+                if (ksteps > 1) fetch(lk < ksteps ? lk : lk - ksteps);
             },
             [&](int slot, const Stage& st) {
                 pl.put(smem + slot * kStageBytes, st.a);
@@ -573,7 +581,7 @@ __device__ __forceinline__ void ffn_bwd_dw(const DwArgs& d, const int32_t* __res
                             }
                 },
                 [&] {
-                    if (++ck < ksteps) return;
+                    if (++ck < kall) return;
                     ck = 0;
                     store();
                 }));
@@ -664,6 +672,7 @@ DwArgs dw_args(const FfnPlan& p, const FfnArgs& a, const uint16_t* P, const uint
     d.Q = Q;
     d.rows_out = rows;
     d.cols_out = cols;
+    d.planes = p.planes;
     d.parts = p.dw_parts;
     d.parts_out = parts_out;
     d.part_stride = dw_size(a.h, a.s, a.M);
@@ -711,11 +720,12 @@ void dw_plan(int64_t n, int32_t h, int32_t s, int32_t M, FfnPlan* p) {
 // 839 : 659; 4096 experts of h = 512, s = 64, 32 rows 623 : 662 : 1134).
 int32_t backward_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
     if (n / std::max<int64_t>(1, std::min<int64_t>(n, M)) < 24) return 32;
+    const int32_t most = n * s <= kFfnTwoPlanes ? 128 : 256;  // (the kernels of 256 rows write one plane)
     int32_t best = 64;
     int64_t least = INT64_MAX;
     const int64_t hsteps = (h + kFfnBK - 1) / kFfnBK, ssteps = (2 * s + kFfnBK - 1) / kFfnBK;
     auto parts = [](int32_t v, int32_t size) { return (int64_t)((v + size - 1) / size); };
-    for (int32_t bm = 64; bm <= 256; bm *= 2) {
+    for (int32_t bm = 64; bm <= most; bm *= 2) {
         const int64_t tiles2 = ffn_expected_tiles2(n, M, bm);
         int64_t cost;
         if (bm == 256) {
@@ -738,12 +748,13 @@ int32_t backward_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
 
 void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {
     ffn_tiles_plan(T * k, M, backward_rows(T * k, h, s, M), p);
+    p->planes = p->n * s <= kFfnTwoPlanes ? 2 : 1;
     dw_plan(p->n, h, s, M, p);
     size_t at = p->workspace_bytes;
     p->off_hidden = at;
-    at += align256((size_t)p->n * s * 2);
+    at += align256((size_t)p->n * s * 2 * p->planes);
     p->off_dgu = at;
-    at += align256((size_t)p->n * 2 * s * 2);
+    at += align256((size_t)p->n * 2 * s * 2 * p->planes);
     p->off_da0 = at;
     at += p->bm == 256 ? align256((size_t)p->n * s * 4) : 0;
     p->off_dxs = at;
@@ -755,8 +766,9 @@ void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t 
     p->workspace_bytes = at;
 }
 
-hipError_t ffn_backward_launch(const FfnPlan& p, const FfnArgs& a, void* workspace, hipStream_t stream) {
+hipError_t ffn_backward_launch(const FfnPlan& p, FfnArgs a, void* workspace, hipStream_t stream) {
     char* ws = static_cast<char*>(workspace);
+    a.planes = p.planes;
     const int32_t n = (int32_t)p.n;
     if (n > 0) {
         hipError_t e = ffn_tiles_launch(p, a, ws, stream);

@@ -87,25 +87,26 @@ struct RowTileLoader {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) p[i] = row_of(w * kPerWave + 8 * i + (l >> 3)) + piece;
     }
-    // contraction values [k0, k0 + 64) of K (a multiple of 8); past K: zeros
+    // contraction values [k0, k0 + 64) of K (a multiple of 8); past K: zeros.  `plane`: elements from the
+    // rows to those meant
     template <typename F>
-    __device__ __forceinline__ void each(int k0, int K, F f) const {
+    __device__ __forceinline__ void each(int k0, int K, int64_t plane, F f) const {
         if (k0 + kFfnBK <= K) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) f(i, p[i] + k0);
+            for (int i = 0; i < kLoads; ++i) f(i, p[i] + (plane + k0));
         } else {
             const bool in = k0 + piece < K;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) f(i, in ? p[i] + k0 : ffn_zeros);
+            for (int i = 0; i < kLoads; ++i) f(i, in ? p[i] + (plane + k0) : ffn_zeros);
         }
     }
-    __device__ __forceinline__ void load(LdsChar* lds, int k0, int K) const {
+    __device__ __forceinline__ void load(LdsChar* lds, int k0, int K, int64_t plane = 0) const {
         LdsChar* at = lds + ffn_wave() * kPerWave * 128;
-        each(k0, K, [&](int i, const uint16_t* g) { ffn_dma16<ONCE>(g, at + i * 1024); });
+        each(k0, K, plane, [&](int i, const uint16_t* g) { ffn_dma16<ONCE>(g, at + i * 1024); });
     }
     using Stage = Staged<kLoads>;
-    __device__ __forceinline__ void fetch(Stage& s, int k0, int K) const {
-        each(k0, K, [&](int i, const uint16_t* g) { s.v[i] = *reinterpret_cast<const u32x4*>(g); });
+    __device__ __forceinline__ void fetch(Stage& s, int k0, int K, int64_t plane = 0) const {
+        each(k0, K, plane, [&](int i, const uint16_t* g) { s.v[i] = *reinterpret_cast<const u32x4*>(g); });
     }
     __device__ __forceinline__ void put(LdsChar* lds, const Stage& s) const {
         LdsChar* at = lds + ffn_wave() * kPerWave * 128 + ffn_lane() * 16;
@@ -191,6 +192,15 @@ __device__ __forceinline__ bf16x8 col_fragment(LdsChar* lds, int col0, int kk) {
 __device__ __forceinline__ uint2 pack_bf16x4(float a, float b, float c, float d) {
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
     return __builtin_bit_cast(uint2, bf16x4{(__bf16)a, (__bf16)b, (__bf16)c, (__bf16)d});
+}
+
+// What bf16 leaves of v (0 where the rounded value is not finite: it stands alone then).
+__device__ __forceinline__ float bf16_rest(float v) {
+    const float hi = (float)(__bf16)v;
+    return __builtin_fabsf(hi) < __builtin_huge_valf() ? v - hi : 0.0f;
+}
+__device__ __forceinline__ uint2 pack_bf16_rest(float a, float b, float c, float d) {
+    return pack_bf16x4(bf16_rest(a), bf16_rest(b), bf16_rest(c), bf16_rest(d));
 }
 
 // Stores of 16 rows of 128 bytes each (64 bf16 columns) from accumulator tiles, by way of a wave's own

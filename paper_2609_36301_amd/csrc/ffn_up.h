@@ -39,7 +39,8 @@ struct UpBackward {
     float* dgp;        // [workgroups along s][n], or NULL
 };
 
-// Forward: hidden = A.  BACKWARD: hidden = gate A, dgu = [dG dU], dgp = this workgroup's share of dgate.
+// Forward: hidden = A.  BACKWARD (of one plane only): hidden = gate A, dgu = [dG dU], dgp = this workgroup's
+// share of dgate.
 template <int BM, bool BACKWARD>
 __global__ __launch_bounds__(UpShape<BM>::kThreads, 2) void ffn_up_kernel(FfnArgs a, const void* __restrict__ list,
                                                              uint16_t* __restrict__ hidden, UpBackward back) {
@@ -124,6 +125,8 @@ __global__ __launch_bounds__(UpShape<BM>::kThreads, 2) void ffn_up_kernel(FfnArg
 #pragma unroll
                     for (int q = 0; q < 4; ++q) v[q] = g[i][j][q] * ffn_sigmoid(g[i][j][q]) * u[i][j][q];
                     *reinterpret_cast<uint2*>(out + c) = pack_bf16x4(v[0], v[1], v[2], v[3]);
+                    if (a.planes > 1)
+                        *reinterpret_cast<uint2*>(out + (int64_t)n * s + c) = pack_bf16_rest(v[0], v[1], v[2], v[3]);
                 }
             }
         } else {

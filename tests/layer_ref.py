@@ -55,8 +55,10 @@ def experts(idx, M):
             yield int(e), np.flatnonzero(flat == e)
 
 
-def ffn(x, W1t, W2t, idx, gate):
-    """y [T k][h] and its bound."""
+def ffn(x, W1t, W2t, idx, gate, planes=1):
+    """y [T k][h] and its bound; planes: the bf16 addends that A is rounded to (the second one takes what the
+    first leaves, at most E16 of it, and is off by E16 of that)."""
+    kept = E16 ** planes
     T, k = idx.shape
     M, h, s = W2t.shape
     g = np.ones(T * k) if gate is None else gate.ravel()
@@ -67,13 +69,14 @@ def ffn(x, W1t, W2t, idx, gate):
         c = g[p][:, None]
         y[p] = c * (A @ W2)
         mag = np.abs(c) * (np.abs(A) @ np.abs(W2))
-        bound[p] = (np.abs(c) * ((eA + E16 * (np.abs(A) + eA)) @ np.abs(W2)) * (1 + 2 * E16)
-                    + (s + 4) * E32 * mag + E16 * np.abs(y[p]) * (1 + 2 * E16) + TINY)
+        bound[p] = (np.abs(c) * ((eA + kept * (np.abs(A) + eA)) @ np.abs(W2)) * (1 + 2 * E16)
+                    + (planes * s + 4) * E32 * mag + E16 * np.abs(y[p]) * (1 + 2 * E16) + TINY)
     return y, bound
 
 
-def ffn_backward(x, W1t, W2t, idx, gate, du):
-    """(dx, dW1t, dW2t, dgate) and the bound of each."""
+def ffn_backward(x, W1t, W2t, idx, gate, du, planes=1):
+    """(dx, dW1t, dW2t, dgate) and the bound of each; planes as for ffn, of [dG dU] and gate A."""
+    kept = E16 ** planes
     T, k = idx.shape
     M, h, s = W2t.shape
     g = np.ones(T * k) if gate is None else gate.ravel()
@@ -96,17 +99,17 @@ def ffn_backward(x, W1t, W2t, idx, gate, du):
         edG = ac * (ed * aU * np.abs(slope) + ad * eU * np.abs(slope) + ad * aU * e_slope) + 8 * E32 * np.abs(dG)
         edU = ac * (ed * np.abs(silu) + ad * (1.1 * eG + np.abs(G) * e_sig)) + 8 * E32 * np.abs(dU)
         dGU, eGU = np.concatenate([dG, dU], 1), np.concatenate([edG, edU], 1)
-        r = eGU + E16 * (np.abs(dGU) + eGU)  # with the rounding to bf16
+        r = eGU + kept * (np.abs(dGU) + eGU)  # with the rounding to bf16
         np.add.at(dx, t, dGU @ W1t[e])
         np.add.at(bx, t, r @ np.abs(W1t[e]))
         np.add.at(mx, t, np.abs(dGU) @ np.abs(W1t[e]))
         dW1[e] = dGU.T @ X
-        b1[e] = r.T @ np.abs(X) + (n + 2) * E32 * (np.abs(dGU).T @ np.abs(X))
+        b1[e] = r.T @ np.abs(X) + (planes * n + 2) * E32 * (np.abs(dGU).T @ np.abs(X))
         gA, egA = c * A, ac * eA + 2 * E32 * ac * aA
-        rA = egA + E16 * (np.abs(gA) + egA)
+        rA = egA + kept * (np.abs(gA) + egA)
         dW2[e] = Y.T @ gA
-        b2[e] = np.abs(Y).T @ rA + (n + 2) * E32 * (np.abs(Y).T @ np.abs(gA))
-    bx += (2 * s + k + 2) * E32 * mx
+        b2[e] = np.abs(Y).T @ rA + (planes * n + 2) * E32 * (np.abs(Y).T @ np.abs(gA))
+    bx += (2 * planes * s + k + 2) * E32 * mx
     out = [dx, dW1, dW2, dg.reshape(T, k)]
     bounds = [b * (1 + 2 * E16) + E16 * np.abs(v) + TINY for b, v in ((bx, dx), (b1, dW1), (b2, dW2))]
     return out, bounds + [bg.reshape(T, k)]

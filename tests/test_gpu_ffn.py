@@ -125,6 +125,60 @@ def test_backward(name):
         check(field, out.float().cpu().numpy(), v, b, name)
 
 
+# T k s <= 2^15, with and without tiles, on every tile size that such calls take
+FEW_VALUES = {name: CASES[name] for name in (
+    "one_token", "one_value", "three_tokens", "token_of_wide_experts", "few_rows", "few_rows_dense", "all_experts",
+    "more_slots_than_experts", "dense", "all_dropped", "long_rows", "long_rows_on_tiles", "repeated_ids", "hot_expert",
+    "many_experts")} | {
+    "tiles_of_32": dict(T=90, h=1552, s=24, M=40, k=5, drop=0.05),
+    "tiles_of_64": dict(T=400, h=1040, s=40, M=6, k=2),
+    "rows_in_runs": dict(T=1900, h=80, s=16, M=1, k=1),
+    "runs_of_two_experts": dict(T=2000, h=48, s=16, M=2, k=1, hot=0.3),
+    "long_row_of_y": dict(T=300, h=65536, s=8, M=1, k=1),
+    "units_of_no_tile": dict(T=2, h=16, s=8200, M=2, k=1),
+}
+
+
+@pytest.mark.parametrize("name", list(FEW_VALUES))
+def test_few_values_are_carried_as_two_addends(name):
+    """The bounds without the rounding of the hidden units and of their gradients to one bf16."""
+    kw = FEW_VALUES[name]
+    M = kw["M"]
+    assert kw["T"] * kw["k"] * kw["s"] <= 2 ** 15
+    idx, bits, gate, exact = make(**kw, seed=4)
+    torch = require_gpu()
+    from paper_2609_36301_amd import layer
+    announce("expert_ffn and its backward pass, few values, %s %s" % (name, kw))
+    d, i, o, s, g = on_device(idx, bits, gate, M)
+    y = layer.expert_ffn(d["x"], d["W1t"], d["W2t"], i, o, s, g)
+    got = layer.expert_ffn_backward(d["x"], d["W1t"], d["W2t"], i, o, s, g, d["du"])
+    torch.cuda.synchronize()
+    given = (exact["x"], exact["W1t"], exact["W2t"], idx, exact["gate"])
+    want, bound = ref.ffn(*given, planes=2)
+    check("y", y.float().cpu().numpy(), want, bound, name)
+    want, bound = ref.ffn_backward(*given, exact["du"], planes=2)
+    for field, v, b in zip(("dx", "dW1t", "dW2t", "dgate"), want, bound):
+        if getattr(got, field) is not None:
+            check(field, getattr(got, field).float().cpu().numpy(), v, b, name)
+
+
+def test_large_hidden_units_stay_what_one_bf16_gives():
+    """A hidden unit past bf16's range is an infinity in its first addend, and the second one is zero then."""
+    torch = require_gpu()
+    from paper_2609_36301_amd import layer
+    announce("expert_ffn with a hidden unit past bf16's range")
+    bf = torch.bfloat16
+    x = torch.full((1, 16), 2.0 ** 60, device="cuda", dtype=bf)
+    W1 = torch.zeros((1, 16, 16), device="cuda", dtype=bf)
+    W1[0, :, 0] = 16.0
+    W1[0, :8, 1] = -2.0 ** -6  # G = 2^64 (1 - 2^-10), U = 2^64: A is fp32's, past half a step over bf16's largest
+    W2 = torch.ones((1, 16, 8), device="cuda", dtype=bf)
+    idx = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    offsets, srt = torch.tensor([0, 1], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    y = layer.expert_ffn(x, W1, W2, idx, offsets, srt)
+    assert bool((y == torch.inf).all())
+
+
 def test_empty_batch():
     torch = require_gpu()
     from paper_2609_36301_amd import layer
