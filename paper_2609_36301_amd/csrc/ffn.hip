@@ -129,7 +129,10 @@ __global__ __launch_bounds__(kTileThreads) void ffn_tiles_kernel(const int32_t* 
 // h = 2048, s = 1024 with 1024 rows 222 us, 619 TFLOP/s (256 x 256 tiles, half as many rounds over the chip
 // as ffn_up, and the rest of the last one idle).  y is stored 8 bytes a lane, 32 bytes of a row, and L2 joins
 // the lines (stored by way of LDS in whole lines it was slower here).
-template <int BM>
+// STAGES: of tiles of 32 rows two leave room for four workgroups to a CU instead of two, so two are taken from
+// eight workgroups per CU on, else three (us, two : three, 16904 workgroups, 1800 experts of h = 4096, s = 64 with
+// one row 148 : 165; 2608, h = 1024, s = 128 14 : 18; 1328, h = 4096, s = 128 55 : 47).
+template <int BM, int STAGES>
 struct DownShape {
     static constexpr int kWaves = BM == 256 ? 8 : 4;
     static constexpr int kThreads = 64 * kWaves;
@@ -138,17 +141,19 @@ struct DownShape {
     static constexpr int kWavesM = BM >= 64 ? 2 : 4;
     static constexpr int kM = kCols / kWavesM / 16;
     static constexpr int kN = BM / (kWaves / kWavesM) / 16;
-    static constexpr int kStages = BM >= 128 ? 2 : 3;
+    static constexpr int kStages = STAGES;
     static constexpr int kRowsAt = kCols * 128;
     static constexpr int kStageBytes = kRowsAt + BM * 128;
     static constexpr int kLoads = (kCols + BM) / kWaves / 8;
 };
 
-template <int BM>
-__global__ __launch_bounds__(DownShape<BM>::kThreads, 2) void ffn_down_kernel(FfnArgs a, const void* __restrict__ list,
+constexpr int down_threads(int bm) { return bm == 256 ? 512 : 256; }
+template <int BM, int STAGES>
+__global__ __launch_bounds__(down_threads(BM), 2) void ffn_down_kernel(FfnArgs a, const void* __restrict__ list,
                                                                const uint16_t* __restrict__ hidden, int32_t hspan,
                                                                uint16_t* __restrict__ y) {
-    using S = DownShape<BM>;
+    using S = DownShape<BM, STAGES>;
+    static_assert(S::kThreads == down_threads(BM), "");
     __shared__ __attribute__((aligned(1024))) char smem_raw[S::kStages * S::kStageBytes];
     LdsChar* smem = (LdsChar*)smem_raw;
     const FfnTile* tiles = ffn_tile_list(list);
@@ -460,7 +465,7 @@ int32_t tile_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
     for (int32_t bm = 64; bm <= 256; bm *= 2) {
         const int64_t tiles2 = ffn_expected_tiles2(n, M, bm);
         const int32_t units = bm == 256 ? UpShape<256>::kUnits : UpShape<128>::kUnits;
-        const int32_t cols = bm == 256 ? DownShape<256>::kCols : DownShape<128>::kCols;
+        const int32_t cols = bm == 256 ? DownShape<256, 2>::kCols : DownShape<128, 2>::kCols;
         const int64_t cost = ffn_cost(tiles2 * ((s + units - 1) / units) / 2, (h + kFfnBK - 1) / kFfnBK, bm) +
                              ffn_cost(tiles2 * ((h + cols - 1) / cols) / 2, (s + kFfnBK - 1) / kFfnBK, bm);
         if (cost < least) {
@@ -471,15 +476,15 @@ int32_t tile_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
     return best;
 }
 
-template <int BM>
+template <int BM, int STAGES>
 hipError_t forward(const FfnPlan& p, const FfnArgs& a, uint16_t* y, char* ws, hipStream_t stream) {
     uint16_t* hidden = reinterpret_cast<uint16_t*>(ws + p.off_hidden);
     using U = UpShape<BM>;
-    using D = DownShape<BM>;
+    using D = DownShape<BM, STAGES>;
     ffn_up_kernel<BM, false><<<grid_of(p.tiles * ((a.s + U::kUnits - 1) / U::kUnits)), U::kThreads, 0, stream>>>(
         a, ws + p.off_tiles, hidden, UpBackward{});
     const int32_t hspan = ffn_span(a.s, D::kCols, p.tiles, a.h);
-    ffn_down_kernel<BM><<<grid_of(p.tiles * ((a.h + hspan - 1) / hspan)), D::kThreads, 0, stream>>>(
+    ffn_down_kernel<BM, STAGES><<<grid_of(p.tiles * ((a.h + hspan - 1) / hspan)), D::kThreads, 0, stream>>>(
         a, ws + p.off_tiles, hidden, hspan, y);
     return hipGetLastError();
 }
@@ -566,10 +571,14 @@ hipError_t ffn_launch(const FfnPlan& p, FfnArgs a, uint16_t* y, void* workspace,
     hipError_t e = ffn_tiles_launch(p, a, ws, stream);
     if (e != hipSuccess) return e;
     switch (p.bm) {
-        case 256: return forward<256>(p, a, y, ws, stream);
-        case 128: return forward<128>(p, a, y, ws, stream);
-        case 64: return forward<64>(p, a, y, ws, stream);
-        default: return forward<32>(p, a, y, ws, stream);
+        case 256: return forward<256, 2>(p, a, y, ws, stream);
+        case 128: return forward<128, 2>(p, a, y, ws, stream);
+        case 64: return forward<64, 3>(p, a, y, ws, stream);
+        default: {
+            const int32_t span = ffn_span(a.s, DownShape<32, 2>::kCols, p.tiles, a.h);
+            return p.tiles * ((a.h + span - 1) / span) >= 2048 ? forward<32, 2>(p, a, y, ws, stream)
+                                                               : forward<32, 3>(p, a, y, ws, stream);
+        }
     }
 }
 
