@@ -702,9 +702,11 @@ void dw_launch(const FfnPlan& p, const FfnArgs& a, char* ws, hipStream_t stream)
 
 // Tile size of the weight gradients, by the same cost as the rows' tiles (call in us, 256 : 128, 32 experts of
 // h = 2048, s = 1024 with 1024 rows 1599 : 1803, a dense block of 16384 rows 1037 : 728, whose 96 large tiles leave
-// most CUs idle), and the runs into which an expert's entries are cut: as many as bring the tiles to 256, of
-// four stages at least (a dense block of h = 512, s = 128, runs : us, 16384 rows 1 : 341, 8 : 100, 32 : 80, 64 : 88;
-// 1024 rows 1 : 48, 4 : 39, 16 : 42; h = 2048, s = 1024 with 256 tiles and more, 1 : 728, 2 : 761).
+// most CUs idle), and the runs into which an expert's entries are cut: as many as bring the tiles to 512, of
+// four stages at least, and at most 32 (runs : us of the call, a dense block of h = 512, s = 128, 16384 rows 1 : 341,
+// 8 : 95, 32 : 75, 64 : 88; 1024 rows 1 : 48, 4 : 39, 16 : 42; four experts of h = 2016, s = 8, 12000 rows 1 : 477,
+// 2 : 373, 4 : 322, 16 : 338; two of h = 1024, s = 512, 4096 rows 1 : 188, 2 : 166, 8 : 188; and where there are
+// 512 tiles and more, h = 2048, s = 1024, 16384 rows 1 : 728, 2 : 761).
 void dw_plan(int64_t n, int32_t h, int32_t s, int32_t M, FfnPlan* p) {
     const int64_t steps = std::max<int64_t>(1, n / M / kFfnBK);
     auto tiles = [&](int32_t a, int32_t b) { return (int64_t)((a + b - 1) / b); };
@@ -712,7 +714,7 @@ void dw_plan(int64_t n, int32_t h, int32_t s, int32_t M, FfnPlan* p) {
     const int64_t small = M * tiles(h, 128) * (tiles(2 * s, 128) + (tiles(s, 64) + 1) / 2);
     p->dw_tile = ffn_cost(large, steps, 256) < ffn_cost(small, steps, 128) ? 256 : 128;
     p->dw_parts = 1;
-    if (p->dw_tile == 128) p->dw_parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(256 / small, steps / 4));
+    if (p->dw_tile == 128) p->dw_parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({512 / small, steps / 4, 32}));
 }
 
 // Rows of a tile, as in the forward pass (over the same 196 shapes 0.9% off the best on geometric mean, at
