@@ -196,17 +196,19 @@ __global__ __launch_bounds__(down_threads(BM), 2) void ffn_down_kernel(FfnArgs a
         const int32_t hsteps = (h1 - h0 + S::kCols - 1) / S::kCols;
         // (column step, contraction step) of the next load and of the next compute
         int32_t lh = h0, lk = 0, ch = h0, ck = 0;
-        using G = FfnGroups<S::kM>;
+        using G = FfnGroups<S::kM, BM == 256 ? 4 : 2>;
         using M = FfnFragments<G::kSize>;
         using N = FfnFragments<S::kN>;
-        ffn_pipeline<S::kStages, S::kLoads, M, N>(
+        ffn_pipeline<S::kStages, S::kLoads, G::kGroups, BM == 256, M, N>(
             kall * hsteps, 16 * wn * S::kN < tile.rows,
             [&](int, int slot) {
-                LdsChar* at = smem + slot * S::kStageBytes;
                 if (lk == 0) weights.init([&](int i) { return W + (int64_t)min(lh + i, h - 1) * s; });
                 const int32_t k0 = (lk < ksteps ? lk : lk - ksteps) * kFfnBK;
-                weights.load(at, k0, s);
-                rows.load(at + S::kRowsAt, k0, s, lk < ksteps ? 0 : (int64_t)n * s);
+                weights.load(smem + slot * S::kStageBytes, k0, s);
+            },
+            [&](int, int slot) {
+                const int32_t k0 = (lk < ksteps ? lk : lk - ksteps) * kFfnBK;
+                rows.load(smem + slot * S::kStageBytes + S::kRowsAt, k0, s, lk < ksteps ? 0 : (int64_t)n * s);
                 if (++lk == kall) {
                     lk = 0;
                     lh += S::kCols;

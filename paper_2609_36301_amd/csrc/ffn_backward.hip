@@ -98,13 +98,10 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
         // the gate rows are one group of M-side fragments, the up rows the other
         using M = FfnFragments<S::kS>;
         using N = FfnFragments<S::kN>;
-        ffn_pipeline<S::kStages, 0, M, N>(
+        ffn_pipeline<S::kStages, 0, 2, false, M, N>(
             (h + kFfnBK - 1) / kFfnBK, live,
-            [&](int step, int slot) {
-                LdsChar* at = smem + slot * S::kStageBytes;
-                rows.load(at + S::kRowsAt, step * kFfnBK, h);
-                weights.load(at, step * kFfnBK, h);
-            },
+            [&](int step, int slot) { rows.load(smem + slot * S::kStageBytes + S::kRowsAt, step * kFfnBK, h); },
+            [&](int step, int slot) { weights.load(smem + slot * S::kStageBytes, step * kFfnBK, h); },
             ffn_work(
                 [&](int slot, int kk, int group, M& m) {
 #pragma unroll

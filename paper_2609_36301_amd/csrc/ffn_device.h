@@ -251,16 +251,18 @@ __device__ __forceinline__ void ffn_for_each(int64_t total, F body) {
 // `w` gives read_m(slot, kk, group, m) and read_n(slot, kk, n), which fill fragments of types M and N,
 // multiply(group, m, n), and done(), which follows the last product of a step.  The fragments of a part
 // are read while the part before is multiplied, across steps too, so that the LDS works while the matrix
-// cores do.  turn(step, slot) stands before the last part of every step but the last: there the next stage
-// has to become readable, and the present one has been read and can be filled again.
-template <int GROUPS, typename M, typename N, typename T, typename W>
-__device__ __forceinline__ void ffn_steps(int steps, int stages, T turn, W w) {
+// cores do.  turn() stands before the last part of every step but the last: there the next stage has to become
+// readable, and the present one has been read and can be filled again.  That is done in two halves, first(step,
+// slot) ahead of the last part's product and second(step, slot) ahead of the next step's first: issued at once, the
+// loads hold all waves up while the matrix cores run dry (256 x 256 tiles from L2: 1435 TFLOP/s against 1351).
+template <int GROUPS, typename M, typename N, typename T, typename F, typename G, typename W>
+__device__ __forceinline__ void ffn_steps(int steps, int stages, T turn, F first, G second, W w) {
     constexpr int kParts = 2 * GROUPS;
     M m[2];
     N n[2];
     w.read_n(0, 0, n[0]);
     w.read_m(0, 0, 0, m[0]);
-    int slot = 0;
+    int slot = 0, before = 0;
     for (int step = 0; step < steps; ++step) {
         const int next = slot + 1 == stages ? 0 : slot + 1;
 #pragma unroll
@@ -273,24 +275,41 @@ __device__ __forceinline__ void ffn_steps(int steps, int stages, T turn, W w) {
                 turn(step, slot);
                 w.read_n(next, 0, n[0]);
                 w.read_m(next, 0, 0, m[0]);
+                first(step, slot);
             }
+            if (part == 0 && step > 0) second(step - 1, before);
             w.multiply(part % GROUPS, m[part & 1], n[part / GROUPS]);
         }
         w.done();
+        before = slot;
         slot = next;
     }
 }
+// The same for a wave that has no wanted rows: it only loads.
+template <typename T, typename F, typename G>
+__device__ __forceinline__ void ffn_loads_only(int steps, int stages, T turn, F first, G second) {
+    int slot = 0;
+    for (int step = 0; step + 1 < steps; ++step) {
+        turn(step, slot);
+        first(step, slot);
+        second(step, slot);
+        slot = slot + 1 == stages ? 0 : slot + 1;
+    }
+}
 
-// The pipeline with direct-to-LDS loads: load(step, slot) issues LOADS of them per wave, STAGES stages
-// ahead.  A wave's own vector memory operations complete in the order in which they were issued, so the
-// next stage's loads are known to have landed while those of later stages are outstanding.  A wave that
-// has no wanted rows (live = false) only loads.
-template <int STAGES, int LOADS, typename M, typename N, typename L, typename W>
-__device__ __forceinline__ void ffn_pipeline(int steps, bool live, L load, W w) {
+// The pipeline with direct-to-LDS loads: load1(slot, step) and load2(slot, step) issue LOADS of them per wave
+// together, STAGES stages ahead.  A wave's own vector memory operations complete in the order in which they were
+// issued, so the next stage's loads are known to have landed while those of later stages are outstanding.
+// SPLIT: the two halves apart (tiles of 256 rows, with one workgroup to a CU; with more, others multiply meanwhile).
+template <int STAGES, int LOADS, int GROUPS, bool SPLIT, typename M, typename N, typename L1, typename L2, typename W>
+__device__ __forceinline__ void ffn_pipeline(int steps, bool live, L1 load1, L2 load2, W w) {
     ffn_barrier<0>();  // the previous work item's reads are over
 #pragma unroll
     for (int i = 0; i < STAGES; ++i)
-        if (i < steps) load(i, i);
+        if (i < steps) {
+            load1(i, i);
+            load2(i, i);
+        }
     if (steps >= STAGES) {
         ffn_barrier<(STAGES - 1) * LOADS>();
     } else {
@@ -302,17 +321,21 @@ __device__ __forceinline__ void ffn_pipeline(int steps, bool live, L load, W w) 
         } else {
             ffn_barrier<0>();
         }
-        if (step + STAGES < steps) load(step + STAGES, slot);
-    };
-    if (live) {
-        ffn_steps<2, M, N>(steps, STAGES, turn, w);
-    } else {
-        int slot = 0;
-        for (int step = 0; step + 1 < steps; ++step) {
-            turn(step, slot);
-            slot = slot + 1 == STAGES ? 0 : slot + 1;
+        if (!SPLIT && step + STAGES < steps) {
+            load1(step + STAGES, slot);
+            load2(step + STAGES, slot);
         }
-    }
+    };
+    auto first = [&](int step, int slot) {
+        if (SPLIT && step + STAGES < steps) load1(step + STAGES, slot);
+    };
+    auto second = [&](int step, int slot) {
+        if (SPLIT && step + STAGES < steps) load2(step + STAGES, slot);
+    };
+    if (live)
+        ffn_steps<GROUPS, M, N>(steps, STAGES, turn, first, second, w);
+    else
+        ffn_loads_only(steps, STAGES, turn, first, second);
 }
 
 // A stage of both operands on its way through registers.
@@ -323,7 +346,8 @@ struct StagePair {
 };
 
 // The pipeline by way of registers, two stages in LDS: fetch(step, s) reads a stage into registers,
-// put(slot, s) writes it to LDS a step later, and another step later it is multiplied.
+// put(slot, s) writes it to LDS a step later, and another step later it is multiplied.  (Both at the turn: in
+// halves as above the products were 10% slower.)
 template <typename S, int GROUPS, typename M, typename N, typename F, typename P, typename W>
 __device__ __forceinline__ void ffn_pipeline_staged(int steps, bool live, F fetch, P put, W w) {
     S s;
@@ -344,11 +368,11 @@ __device__ __forceinline__ void ffn_pipeline_staged(int steps, bool live, F fetc
         if (step + 2 < steps) put(slot, s);
         if (step + 3 < steps) fetch(step + 3, s);
     };
-    if (live) {
-        ffn_steps<GROUPS, M, N>(steps, 2, turn, w);
-    } else {
-        for (int step = 0; step + 1 < steps; ++step) turn(step, step & 1);
-    }
+    auto none = [](int, int) {};
+    if (live)
+        ffn_steps<GROUPS, M, N>(steps, 2, turn, none, none, w);
+    else
+        ffn_loads_only(steps, 2, turn, none, none);
 }
 
 // The four functions of a pipeline as one argument.

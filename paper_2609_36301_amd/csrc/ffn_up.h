@@ -81,13 +81,10 @@ __global__ __launch_bounds__(UpShape<BM>::kThreads, 2) void ffn_up_kernel(FfnArg
         // the gate rows are one group of M-side fragments, the up rows the other
         using M = FfnFragments<S::kS>;
         using N = FfnFragments<S::kN>;
-        ffn_pipeline<S::kStages, S::kLoads, M, N>(
+        ffn_pipeline<S::kStages, S::kLoads, 2, BM == 256, M, N>(
             (h + kFfnBK - 1) / kFfnBK, 16 * wn * S::kN < tile.rows,
-            [&](int step, int slot) {
-                LdsChar* at = smem + slot * S::kStageBytes;
-                weights.load(at, step * kFfnBK, h);
-                tokens.load(at + S::kRowsAt, step * kFfnBK, h);
-            },
+            [&](int step, int slot) { weights.load(smem + slot * S::kStageBytes, step * kFfnBK, h); },
+            [&](int step, int slot) { tokens.load(smem + slot * S::kStageBytes + S::kRowsAt, step * kFfnBK, h); },
             ffn_work(
                 [&](int slot, int kk, int group, M& m) {
 #pragma unroll
