@@ -60,10 +60,10 @@ inline int32_t ffn_span(int32_t len, int32_t step, int64_t groups, int32_t cols)
 // What `items` workgroups with tiles of `bm` rows cost that run `steps` stages each: the rounds in which they
 // fill the chip (two of up to 128 rows to a CU, one of 256) times the stages times the time of a stage.  The
 // stages' times were fitted to 196 measured shapes: against one of 128-row tiles, two to a CU, 0.8 with one to
-// a CU, 0.75 with 64 rows (half the work) and 1.7 with 256 (four times the work, one to a CU).
+// a CU, 0.75 with 64 rows (half the work) and 1.6 with 256 (four times the work, one to a CU).
 inline int64_t ffn_cost(int64_t items, int64_t steps, int32_t bm) {
     const int64_t slots = bm == 256 ? 256 : 512;
-    const int64_t stage = bm == 256 ? 34 : bm == 128 ? (items <= 256 ? 16 : 20) : 15;
+    const int64_t stage = bm == 256 ? 32 : bm == 128 ? (items <= 256 ? 16 : 20) : 15;
     return (items + slots - 1) / slots * steps * stage;
 }
 constexpr int64_t kFfnTwoPlanes = 1 << 15;

@@ -126,7 +126,7 @@ __global__ __launch_bounds__(kTileThreads) void ffn_tiles_kernel(const int32_t* 
 // side, the tile's rows of A the N side.  The pipeline runs over (column step, contraction step) pairs,
 // so that the short contraction of small experts (one step up to s = 64) does not drain it.  Bound like
 // ffn_up: 4096 experts of h = 512, s = 64 with 32 rows 100 us, 4.2 TB/s (a third of it y); 32 experts of
-// h = 2048, s = 1024 with 1024 rows 222 us, 619 TFLOP/s (256 x 256 tiles, half as many rounds over the chip
+// h = 2048, s = 1024 with 1024 rows 225 us, 611 TFLOP/s (256 x 256 tiles, half as many rounds over the chip
 // as ffn_up, and the rest of the last one idle).  y is stored 8 bytes a lane, 32 bytes of a row, and L2 joins
 // the lines (stored by way of LDS in whole lines it was slower here).
 // STAGES: of tiles of 32 rows two leave room for four workgroups to a CU instead of two, so two are taken from
@@ -454,11 +454,11 @@ unsigned few_grid(int64_t items) { return (unsigned)std::min<int64_t>(items, 1 <
 // again; us, 32 : 64 rows, 4096 experts of h = 512, s = 64 with 12 rows 164 : 185, with 24 185 : 205, with 32
 // 222 : 215; 64 experts of h = 1024, s = 256 with 24 rows 32 : 27), else what costs least by ffn_cost.  Large
 // tiles need less from the caches, small ones fill the chip: us for 64 : 128 : 256 rows,
-//   32 experts of h = 2048, s = 1024, 48 rows 98 : 107 : 119, 384 rows 292 : 236 : 206, 1024 rows - : 608 : 560
-//   64 experts of h = 1024, s = 512, 192 rows - : 73 : 66, 256 rows - : 90 : 114 (the 256-row tiles take one and
-//   a half rounds), 2048 rows - : 581 : 539
-//   a dense block of h = 2048, s = 1024, 1024 rows 35 : 46 : 88, 4096 rows 80 : 65 : 92, 8192 rows 149 : 115 : 100
-// Over 196 shapes (1 to 4096 experts, 12 to 16384 rows each) the choice is 1.3% off the best on geometric
+//   32 experts of h = 2048, s = 1024, 48 rows 99 : 107 : 120, 384 rows 288 : 244 : 196, 1024 rows - : 528 : 453
+//   64 experts of h = 1024, s = 512, 192 rows 81 : 73 : 66, 256 rows 101 : 92 : 109 (the 256-row tiles take one and
+//   a half rounds), 1024 rows - : 310 : 276
+//   a dense block of h = 2048, s = 1024, 1024 rows 36 : 47 : 82, 4096 rows 78 : 65 : 87, 8192 rows 148 : 124 : 98
+// Over 196 shapes (1 to 4096 experts, 12 to 16384 rows each) the choice is 0.9% off the best on geometric
 // mean and 21% at most; one by the mean number of rows alone was 11% off, and 2.6 times at most.
 int32_t tile_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
     if (n / std::max<int64_t>(1, std::min<int64_t>(n, M)) < 24) return 32;

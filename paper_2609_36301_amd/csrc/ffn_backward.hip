@@ -35,7 +35,7 @@ namespace more {
 // ------------------------------------------------------------------------------ up, tiles of up to 128 rows
 // (Two kernels for tiles of 256 rows: there the matrix products count, a tile of 128 hidden units halves
 // what the caches deliver, and three sets of accumulators do not fit; 32 experts of s = 1024, h = 2048 with
-// 1024 rows 654 us against 820.  For 4096 experts of s = 64, h = 512 with 32 rows, where the weights' way from
+// 1024 rows 585 us against 820.  For 4096 experts of s = 64, h = 512 with 32 rows, where the weights' way from
 // memory counts, this one kernel takes 213 us (805 MB of weights: 4.1 TB/s) against 235.)
 // A workgroup computes one tile and kUnits hidden units: first G and U (x rows against the gate and up
 // rows of W1t), then dA0 (du rows against a column tile of W2t) into other accumulators.  In turn rather
@@ -714,9 +714,9 @@ void dw_plan(int64_t n, int32_t h, int32_t s, int32_t M, FfnPlan* p) {
     if (p->dw_tile == 128) p->dw_parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({512 / small, steps / 4, 32}));
 }
 
-// Rows of a tile, as in the forward pass (over the same 196 shapes 0.9% off the best on geometric mean, at
-// most 20%; us for 64 : 128 : 256 rows, 32 experts of h = 2048, s = 1024, 96 rows 377 : 315 : 339, 384 rows 884 :
-// 839 : 659; 4096 experts of h = 512, s = 64, 32 rows 623 : 662 : 1134).
+// Rows of a tile, as in the forward pass (over the same 196 shapes 0.6% off the best on geometric mean, at
+// most 18%; us for 64 : 128 : 256 rows, 32 experts of h = 2048, s = 1024, 96 rows 359 : 299 : 326, 384 rows 778 :
+// 712 : 607; 4096 experts of h = 512, s = 64, 32 rows 622 : 662 : 1051).
 int32_t backward_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
     if (n / std::max<int64_t>(1, std::min<int64_t>(n, M)) < 24) return 32;
     const int32_t most = n * s <= kFfnTwoPlanes ? 128 : 256;  // (the kernels of 256 rows write one plane)
