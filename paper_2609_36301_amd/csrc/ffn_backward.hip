@@ -406,7 +406,7 @@ __global__ __launch_bounds__(256) void ffn_bwd_sum_kernel(const float* __restric
 // fp32 results of run i go to parts_out + i part_stride, and ffn_bwd_dw_sum adds them.  ONCE: nontemporal
 // stores.
 // Bound by the gradients' way to memory where experts are small (4096 of h = 512, s = 64 with 32 rows 236 us, 805 MB
-// written, 134 read: 4.0 TB/s), by the operands' way from L2 where they are large (32 of h = 2048, s = 1024 with
+// written, 134 read: 4.0 TB/s), by the products' stages where they are large (32 of h = 2048, s = 1024 with
 // 1024 rows 540 us, 763 TFLOP/s).
 struct DwArgs {
     const uint16_t *P, *Q;

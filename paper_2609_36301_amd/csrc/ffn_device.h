@@ -251,10 +251,11 @@ __device__ __forceinline__ void ffn_for_each(int64_t total, F body) {
 // `w` gives read_m(slot, kk, group, m) and read_n(slot, kk, n), which fill fragments of types M and N,
 // multiply(group, m, n), and done(), which follows the last product of a step.  The fragments of a part
 // are read while the part before is multiplied, across steps too, so that the LDS works while the matrix
-// cores do.  turn() stands before the last part of every step but the last: there the next stage has to become
-// readable, and the present one has been read and can be filled again.  That is done in two halves, first(step,
-// slot) ahead of the last part's product and second(step, slot) ahead of the next step's first: issued at once, the
-// loads hold all waves up while the matrix cores run dry (256 x 256 tiles from L2: 1435 TFLOP/s against 1351).
+// cores do.  turn(step, slot) stands before the last part of every step but the last: there the
+// next stage has to become readable, and the present one has been read and can be filled again.  first(step, slot)
+// stands ahead of the last part's product and second(step, slot) ahead of the next step's first, for loads in two
+// halves: issued at once they hold all waves up while the matrix cores run dry (32 experts of h = 2048, s = 1024
+// with 1024 rows, up 317 us against 340, in the backward pass 358 against 442).
 template <int GROUPS, typename M, typename N, typename T, typename F, typename G, typename W>
 __device__ __forceinline__ void ffn_steps(int steps, int stages, T turn, F first, G second, W w) {
     constexpr int kParts = 2 * GROUPS;

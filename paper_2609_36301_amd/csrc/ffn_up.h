@@ -2,9 +2,10 @@
 //
 // What bounds it, and what it takes: with few rows per expert the weights' way from memory (4096 experts
 // of h = 512, s = 64 with 32 rows each: 118 us, 4.8 TB/s; 1800 experts of h = 4096 with one row: 280 us,
-// 6.8 TB/s); with many rows the operands' way from L2 to the CUs, about 7.5 TB/s (32 experts of h = 2048,
-// s = 1024 with 1024 rows: 317 us, 867 TFLOP/s, backward 358 us).  Hence tiles as large as the rows allow, and no tile
-// larger (256 x 256 of rows and hidden units would need 256 accumulators a lane for the two projections).
+// 6.8 TB/s); with many rows the stages of the matrix product (32 experts of h = 2048, s = 1024 with 1024 rows: 317
+// us, 867 TFLOP/s, backward 358 us): 1.14 us for 256 rows and 2 x 128 units with everything in LDS, 1.5 to 1.7 with
+// the loads, and by the card's power with both.  Hence tiles as large as the rows allow, and no tile larger
+// (256 x 256 of rows and hidden units would need 256 accumulators a lane for the two projections).
 #pragma once
 
 #include "ffn.h"
