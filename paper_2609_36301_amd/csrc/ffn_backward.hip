@@ -296,62 +296,85 @@ __global__ __launch_bounds__(rows_threads(BM), 2) void ffn_bwd_rows_kernel(
         using G = FfnGroups<S::kM, S::kM == 8 ? 4 : 2>;
         using M = FfnFragments<G::kSize>;
         using N = FfnFragments<S::kN>;
-        using Stage = StagePair<decltype(weights), decltype(rows)>;
-        ffn_pipeline_staged<Stage, G::kGroups, M, N>(
-            kall * csteps, 16 * wn * S::kN < tile.rows,
-            [&](int, Stage& st) {
-                const int32_t k0 = (lk < ksteps ? lk : lk - ksteps) * kFfnBK;
-                weights.fetch(st.a, cols - lc, [&](int i) {
-                    const int kappa = k0 + weights.row(i);
-                    return kappa < len ? We + (int64_t)kappa * cols + lc : nullptr;
-                });
-                rows.fetch(st.b, k0, len, lk < ksteps ? 0 : (int64_t)n * len);
-                if (++lk == kall) {
-                    lk = 0;
-                    lc += S::kCols;
-                }
-            },
-            [&](int slot, const Stage& st) {
-                weights.put(smem + slot * S::kStageBytes, st.a);
-                rows.put(smem + slot * S::kStageBytes + S::kRowsAt, st.b);
-            },
-            ffn_work(
-                [&](int slot, int kk, int group, M& m) {
+        auto weight_row = [&](int i) -> const uint16_t* {
+            const int kappa = (lk < ksteps ? lk : lk - ksteps) * kFfnBK + weights.row(i);
+            return kappa < len ? We + (int64_t)kappa * cols + lc : nullptr;
+        };
+        auto advance = [&] {
+            if (++lk < kall) return;
+            lk = 0;
+            lc += S::kCols;
+        };
+        auto read_n = [&](int slot, int kk, N& f) {
 #pragma unroll
-                    for (int i = 0; i < G::kSize; ++i)
-                        if (G::tile(group, i) < S::kM)
-                            m.v[i] = col_fragment(smem + slot * S::kStageBytes, 16 * (wm * S::kM + G::tile(group, i)), kk);
-                },
-                [&](int slot, int kk, N& f) {
+            for (int j = 0; j < S::kN; ++j)
+                f.v[j] = row_fragment(smem + slot * S::kStageBytes + S::kRowsAt, 16 * (wn * S::kN + j), kk);
+        };
+        auto multiply = [&](int group, const M& m, const N& f) {
 #pragma unroll
-                    for (int j = 0; j < S::kN; ++j)
-                        f.v[j] = row_fragment(smem + slot * S::kStageBytes + S::kRowsAt, 16 * (wn * S::kN + j), kk);
-                },
-                [&](int group, const M& m, const N& f) {
-#pragma unroll
-                    for (int i = 0; i < G::kSize; ++i)
-                        if (G::tile(group, i) < S::kM)
-#pragma unroll
-                            for (int j = 0; j < S::kN; ++j) {
-                                f32x4& c = acc[G::tile(group, i)][j];
-                                c = mfma_16x16x32(m.v[i], f.v[j], c);
-                            }
-                },
-                [&] {
-                    if (++ck < kall) return;
+            for (int i = 0; i < G::kSize; ++i)
+                if (G::tile(group, i) < S::kM)
 #pragma unroll
                     for (int j = 0; j < S::kN; ++j) {
-#pragma unroll
-                        for (int i = 0; i < S::kM; ++i) {
-                            const int32_t c = cc + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
-                            if (place[j] >= 0 && c < c1)
-                                *reinterpret_cast<f32x4*>(out + place[j] * cols + c) = acc[i][j];
-                            acc[i][j] = zero_f32x4();
-                        }
+                        f32x4& c = acc[G::tile(group, i)][j];
+                        c = mfma_16x16x32(m.v[i], f.v[j], c);
                     }
-                    ck = 0;
-                    cc += S::kCols;
-                }));
+        };
+        auto done = [&] {
+            if (++ck < kall) return;
+#pragma unroll
+            for (int j = 0; j < S::kN; ++j) {
+#pragma unroll
+                for (int i = 0; i < S::kM; ++i) {
+                    const int32_t c = cc + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
+                    if (place[j] >= 0 && c < c1)
+                        *reinterpret_cast<f32x4*>(out + place[j] * cols + c) = acc[i][j];
+                    acc[i][j] = zero_f32x4();
+                }
+            }
+            ck = 0;
+            cc += S::kCols;
+        };
+        if constexpr (BM == 256) {
+            constexpr int kLoads = weights.kLoads + rows.kLoads;
+            ffn_pipeline<2, kLoads, G::kGroups, true, M, N>(
+                kall * csteps, 16 * wn * S::kN < tile.rows,
+                [&](int, int slot) { weights.load(smem + slot * S::kStageBytes, cols - lc, weight_row); },
+                [&](int, int slot) {
+                    const int32_t k0 = (lk < ksteps ? lk : lk - ksteps) * kFfnBK;
+                    rows.load(smem + slot * S::kStageBytes + S::kRowsAt, k0, len, lk < ksteps ? 0 : (int64_t)n * len);
+                    advance();
+                },
+                ffn_work(
+                    [&](int slot, int kk, int group, M& m) {
+                        col_fragments2(smem + slot * S::kStageBytes, 16 * (wm * S::kM + G::tile(group, 0)), kk, m.v[0],
+                                       m.v[1]);
+                    },
+                    read_n, multiply, done));
+        } else {
+            using Stage = StagePair<decltype(weights), decltype(rows)>;
+            ffn_pipeline_staged<Stage, G::kGroups, M, N>(
+                kall * csteps, 16 * wn * S::kN < tile.rows,
+                [&](int, Stage& st) {
+                    weights.fetch(st.a, cols - lc, weight_row);
+                    const int32_t k0 = (lk < ksteps ? lk : lk - ksteps) * kFfnBK;
+                    rows.fetch(st.b, k0, len, lk < ksteps ? 0 : (int64_t)n * len);
+                    advance();
+                },
+                [&](int slot, const Stage& st) {
+                    weights.put(smem + slot * S::kStageBytes, st.a);
+                    rows.put(smem + slot * S::kStageBytes + S::kRowsAt, st.b);
+                },
+                ffn_work(
+                    [&](int slot, int kk, int group, M& m) {
+#pragma unroll
+                        for (int i = 0; i < G::kSize; ++i)
+                            if (G::tile(group, i) < S::kM)
+                                m.v[i] = col_fragment(smem + slot * S::kStageBytes,
+                                                      16 * (wm * S::kM + G::tile(group, i)), kk);
+                    },
+                    read_n, multiply, done));
+        }
     });
 }
 

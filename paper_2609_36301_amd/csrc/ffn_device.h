@@ -164,6 +164,19 @@ struct ColTileLoader {
             }
         }
     }
+    template <typename F>
+    __device__ __forceinline__ void load(LdsChar* lds, int cols, F row_of) const {
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+            const uint16_t* r = row_of(i);
+            LdsChar* at = lds + (ffn_wave() + WAVES * i) * 1024;
+#pragma unroll
+            for (int q = 0; q < kPanels; ++q) {
+                const int c = 64 * q + col[i];
+                ffn_dma16(r && c < cols ? r + c : ffn_zeros, at + q * kFfnPanel);
+            }
+        }
+    }
     __device__ __forceinline__ void put(LdsChar* lds, const Stage& s) const {
 #pragma unroll
         for (int i = 0; i < kGroups; ++i) {
@@ -186,6 +199,30 @@ __device__ __forceinline__ bf16x8 col_fragment(LdsChar* lds, int col0, int kk) {
     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
         reinterpret_cast<__attribute__((address_space(3))) s16x4*>(a + 4 * 128));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// The fragments of two neighbouring column tiles (col0 .. col0 + 31), read and waited for in one block: the
+// compiler lets the builtin's reads wait for all direct-to-LDS loads in flight, so tiles filled by those are read
+// this way.
+__device__ __forceinline__ void col_fragments2(LdsChar* lds, int col0, int kk, bf16x8& f0, bf16x8& f1) {
+    const int l = ffn_lane();
+    const int kappa = 8 * (l >> 4) + ((l & 15) >> 2);
+    LdsChar* row = lds + kappa * 128 + ((l & 3) << 3) + (col0 >> 6) * kFfnPanel + kk * 32 * 128;
+    const int q = (col0 >> 4) & 3, swizzle = column_swizzle(kappa);
+    const uint32_t a0 = (uint32_t)(uintptr_t)(row + ((q ^ swizzle) << 5));
+    const uint32_t a1 = (uint32_t)(uintptr_t)(row + (((q + 1) ^ swizzle) << 5));
+    s16x4 lo0, hi0, lo1, hi1;
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %4\n\t"
+        "ds_read_b64_tr_b16 %1, %4 offset:512\n\t"
+        "ds_read_b64_tr_b16 %2, %5\n\t"
+        "ds_read_b64_tr_b16 %3, %5 offset:512\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(lo0), "=&v"(hi0), "=&v"(lo1), "=&v"(hi1)
+        : "v"(a0), "v"(a1)
+        : "memory");
+    f0 = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo0, hi0, 0, 1, 2, 3, 4, 5, 6, 7));
+    f1 = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo1, hi1, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 // four fp32 -> four bf16 (round to nearest even)
