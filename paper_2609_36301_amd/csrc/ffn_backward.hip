@@ -35,7 +35,7 @@ namespace more {
 // ------------------------------------------------------------------------------ up, tiles of up to 128 rows
 // (Two kernels for tiles of 256 rows: there the matrix products count, a tile of 128 hidden units halves
 // what the caches deliver, and three sets of accumulators do not fit; 32 experts of s = 1024, h = 2048 with
-// 1024 rows 585 us against 820.  For 4096 experts of s = 64, h = 512 with 32 rows, where the weights' way from
+// 1024 rows 565 us against 820.  For 4096 experts of s = 64, h = 512 with 32 rows, where the weights' way from
 // memory counts, this one kernel takes 213 us (805 MB of weights: 4.1 TB/s) against 235.)
 // A workgroup computes one tile and kUnits hidden units: first G and U (x rows against the gate and up
 // rows of W1t), then dA0 (du rows against a column tile of W2t) into other accumulators.  In turn rather
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(BwdUpShape<BM>::kThreads, 2) void ffn_bwd_up_kernel
 // entries' shares of dx = [dG dU] W1t[e] (contraction over 2s, results in entry order).  The weights are a
 // column tile (M side), the rows a row tile (N side).  A workgroup computes `span` columns in steps of
 // kCols; the pipeline runs over (column step, contraction step) pairs.  Bound like the forward pass: 32 experts
-// of h = 2048, s = 1024 with 1024 rows, dA0 225 us (610 TFLOP/s), dx 390 us (705 TFLOP/s) on tiles of 256 rows
+// of h = 2048, s = 1024 with 1024 rows, dA0 213 us (645 TFLOP/s), dx 367 us (749 TFLOP/s) on tiles of 256 rows
 // and 476 us on tiles of 128; 4096 experts of h = 512, s = 64 with 32 rows, dx 164 us (840 MB, 5.1 TB/s).
 // The shares of dx go through memory in fp32, a third of that traffic: in bf16 dx would carry k + 1 roundings
 // for one.

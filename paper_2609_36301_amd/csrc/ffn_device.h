@@ -63,7 +63,7 @@ __device__ __forceinline__ int ffn_lane() { return threadIdx.x & 63; }
 
 // How a tile's 16-byte pieces get to LDS: straight (load: direct-to-LDS loads), or by way of registers
 // (fetch, then put).  The compiler lets a transposing LDS read wait for every direct-to-LDS load before it, so
-// the kernels that read column tiles take the second way.
+// the kernels that read column tiles take the second way (but for col_fragments2).
 template <int LOADS>
 struct Staged {
     u32x4 v[LOADS];
@@ -203,7 +203,8 @@ __device__ __forceinline__ bf16x8 col_fragment(LdsChar* lds, int col0, int kk) {
 
 // The fragments of two neighbouring column tiles (col0 .. col0 + 31), read and waited for in one block: the
 // compiler lets the builtin's reads wait for all direct-to-LDS loads in flight, so tiles filled by those are read
-// this way.
+// this way.  (256 x 256 tiles with one operand a column tile: 5% faster than by way of registers; with both, as in
+// the weight gradients, 14% slower.)
 __device__ __forceinline__ void col_fragments2(LdsChar* lds, int col0, int kk, bf16x8& f0, bf16x8& f1) {
     const int l = ffn_lane();
     const int kappa = 8 * (l >> 4) + ((l & 15) >> 2);
