@@ -4,11 +4,12 @@
 //   r'  = alpha r + gate[t] (w_after n)        (gate and residual scale)
 //   xn  = w_before r' / rms(r')
 // and its backward pass: with q = w_before dxn, D the gradient of r' and p = gate D w_after,
-//   D    = dr_out + q / rms(r') - r' mean(q r') / rms(r')^3
+//   D    = dr_out + (q - n' mean(q n')) / rms(r')   with n' = r' / rms(r')
 //   dr   = alpha D
-//   du   = p / rms(u) - u mean(p u) / rms(u)^3   (or p)
-//   dw_before = sum_t dxn r' / rms(r'),  dw_after = sum_t gate D n,  dgate = sum_c D w_after n
-// All sums are fp32; xn is normalised from the unrounded r'.
+//   du   = (p - n mean(p n)) / rms(u)   (or p)
+//   dw_before = sum_t dxn n',  dw_after = sum_t gate D n,  dgate = sum_c D w_after n
+// All sums are fp32; xn is normalised from the unrounded r'.  (1 / rms is never raised to its third power, which
+// leaves fp32 for rows of zeros with a small eps and for rows of large values.)
 //
 // Bound by memory: every row is read once and kept in registers, W waves to a row (a wave for short
 // rows), eight columns of 16 (bf16) or 32 bytes per lane and chunk, CH chunks per lane.  Measured: forward, 32768
@@ -248,13 +249,14 @@ __global__ __launch_bounds__(norm_threads(W)) void block_norm_backward_kernel(No
         row_sums<W, 3>(s1, red[0]);
         if (before) {
             const float rs = rsqrtf(__builtin_fmaf(s1[0], inv_h, a.eps));
-            const float m = rs * rs * rs * (s1[1] * inv_h);
+            const float m = rs * (s1[1] * inv_h);
 #pragma unroll
             for (int i = 0; i < CH; ++i)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    dwb[i].v[e] = __builtin_fmaf(dn[i].v[e], r[i].v[e] * rs, dwb[i].v[e]);
-                    D[i].v[e] += dn[i].v[e] * wb[i].v[e] * rs - r[i].v[e] * m;
+                    const float n = r[i].v[e] * rs;
+                    dwb[i].v[e] = __builtin_fmaf(dn[i].v[e], n, dwb[i].v[e]);
+                    D[i].v[e] += rs * (dn[i].v[e] * wb[i].v[e] - n * m);
                 }
         }
         const float alpha = block ? a.alpha : 1.0f;
@@ -278,7 +280,7 @@ __global__ __launch_bounds__(norm_threads(W)) void block_norm_backward_kernel(No
                     dwa[i].v[e] = __builtin_fmaf(gate * D[i].v[e], u[i].v[e] * ru, dwa[i].v[e]);
                 }
             row_sums<W, 1>(s2, red[1]);
-            const float m = a.norm_after ? gate * ru * ru * ru * (s2[0] * inv_h) : 0.0f;
+            const float m = a.norm_after ? ru * (s2[0] * inv_h) : 0.0f;
             if (a.dgate && lane == 0) a.dgate[t] = s2[0] * ru;
             const float p = gate * ru;
 #pragma unroll
@@ -286,7 +288,7 @@ __global__ __launch_bounds__(norm_threads(W)) void block_norm_backward_kernel(No
                 if (!in[i]) continue;
                 V8 o;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o.v[e] = p * (D[i].v[e] * wa[i].v[e]) - u[i].v[e] * m;
+                for (int e = 0; e < 8; ++e) o.v[e] = p * (D[i].v[e] * wa[i].v[e] - u[i].v[e] * ru * m);
                 store8(a.du + t * h + c[i], o);
             }
         }
