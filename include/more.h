@@ -352,6 +352,21 @@ more_status more_expert_ffn(const uint16_t* x, const uint16_t* W1t, const uint16
 more_status more_expert_ffn_workspace_size(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k,
                                            size_t* bytes);
 
+/* The form in which more_expert_ffn (backward == 0) or its backward pass runs this shape (written to *plan,
+ * host): for tests of every form and for a caller who wants to know how the hidden units are rounded. */
+typedef struct more_expert_plan {
+    int32_t tile_rows; /* rows of a tile: 32, 64, 128 or 256; 0: the kernels without tiles          */
+    int32_t addends;   /* bf16 addends as which A (backward: [dG dU] and gate A) is handed on: 1 or 2 */
+    int32_t span;      /* columns that a workgroup takes of y (backward: of the entries' shares of dx) */
+    int32_t stages;    /* of the LDS ring that feeds the second product (0 without tiles)            */
+    int32_t dw_tile;   /* (backward, else 0) rows and columns of a tile of the weight gradients      */
+    int32_t dw_runs;   /* (backward, else 0) runs of an expert's entries that are summed apart       */
+    int32_t dw1_span;  /* (backward, else 0) columns of h that a workgroup takes of dW1t ...         */
+    int32_t dw2_span;  /* ... and rows of h of dW2t                                                  */
+} more_expert_plan;
+more_status more_expert_ffn_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k,
+                                 int32_t backward, more_expert_plan* plan);
+
 /*
  * Backward pass of more_expert_ffn with recompute of the hidden units (nothing is kept from the forward
  * pass).  du is the gradient with respect to sum_j y[t k + j], the same for a token's k entries.

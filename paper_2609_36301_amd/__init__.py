@@ -19,7 +19,7 @@ __all__ = ["route_lowrank", "route_lowrank_train", "route_fullrank", "route_full
            "lowrank_backward_workspace_size", "Gradients", "lowrank_plan", "lowrank_route",
            "fullrank_workspace_size", "Routing", "TrainRouting"]
 _LAYER = ["expert_ffn", "expert_ffn_backward", "ExpertFFN", "ExpertFFNBackward", "ExpertGradients",
-          "expert_ffn_workspace_size", "expert_ffn_backward_workspace_size", "block_norm",
+          "expert_ffn_workspace_size", "expert_ffn_backward_workspace_size", "expert_ffn_plan", "block_norm",
           "block_norm_backward", "BlockNorm", "BlockNormBackward", "BlockEnd", "BlockEndGradients",
           "block_norm_backward_workspace_size", "clip_gradients", "GradClipper"]
 __all__ += _LAYER

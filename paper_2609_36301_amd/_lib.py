@@ -23,6 +23,14 @@ _P = ctypes.c_void_p
 _I64, _I32, _SZ, _F32 = ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t, ctypes.c_float
 _PSZ = ctypes.POINTER(ctypes.c_size_t)
 _PI32 = ctypes.POINTER(ctypes.c_int32)
+
+
+class ExpertPlan(ctypes.Structure):
+    """more_expert_plan."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("tile_rows", "addends", "span", "stages", "dw_tile", "dw_runs",
+                                                    "dw1_span", "dw2_span")]
+
+
 SIGNATURES = {
     "more_route_lowrank": (_I32, [_P, _P, _P, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _P,
                                   _SZ, _P]),
@@ -53,6 +61,7 @@ SIGNATURES = {
     "more_expert_ffn": (_I32, [_P, _P, _P, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _P, _P,
                                _SZ, _P]),
     "more_expert_ffn_workspace_size": (_I32, [_I64, _I32, _I32, _I32, _I32, _PSZ]),
+    "more_expert_ffn_plan": (_I32, [_I64, _I32, _I32, _I32, _I32, _I32, ctypes.POINTER(ExpertPlan)]),
     "more_expert_ffn_backward": (_I32, [_P, _P, _P, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _P,
                                         _P, _P, _P, _P, _P, _P, _SZ, _P]),
     "more_expert_ffn_backward_workspace_size": (_I32, [_I64, _I32, _I32, _I32, _I32, _PSZ]),

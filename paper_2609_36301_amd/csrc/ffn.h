@@ -29,6 +29,10 @@ struct FfnPlan {
     int64_t n;        // T k entries
     int32_t bm;       // rows of a tile (all of one expert)
     int32_t few;      // (forward) the kernels without tiles
+    int32_t split;    // (forward, without tiles) the waves of a down workgroup share columns
+    int32_t stages;   // (forward, tiles) of the down kernel's ring
+    int32_t span;     // columns of y (backward: of the shares of dx) that a workgroup takes
+    int32_t da0_span; // (backward, tiles of 256 rows) columns of dA0 that a workgroup takes
     // The hidden units (and, backward, the gradients of the pre-activations) go from kernel to kernel in bf16,
     // the matrix cores' operand type.  A rounding error of each then sits in all its products, as large as the
     // results' own rounding (together 1.41 of it) on average over many; where few are rounded (n s <= 2^15;
@@ -39,6 +43,7 @@ struct FfnPlan {
     int32_t sums;     // workgroups that count tiles ahead of the list (0: none)
     int32_t dw_tile;  // rows and columns of a tile of the weight gradients (128 or 256)
     int32_t dw_parts; // parts of an expert's entries whose weight gradients are summed apart
+    int32_t dw1_span, dw2_span;  // of h that a workgroup of dW1t and of dW2t takes
     size_t off_tiles, off_sums, off_hidden, off_dgu, off_da0, off_dxs, off_dgp, off_dwp;
     size_t workspace_bytes;
 };

@@ -485,9 +485,8 @@ hipError_t forward(const FfnPlan& p, const FfnArgs& a, uint16_t* y, char* ws, hi
     using D = DownShape<BM, STAGES>;
     ffn_up_kernel<BM, false><<<grid_of(p.tiles * ((a.s + U::kUnits - 1) / U::kUnits)), U::kThreads, 0, stream>>>(
         a, ws + p.off_tiles, hidden, UpBackward{});
-    const int32_t hspan = ffn_span(a.s, D::kCols, p.tiles, a.h);
-    ffn_down_kernel<BM, STAGES><<<grid_of(p.tiles * ((a.h + hspan - 1) / hspan)), D::kThreads, 0, stream>>>(
-        a, ws + p.off_tiles, hidden, hspan, y);
+    ffn_down_kernel<BM, STAGES><<<grid_of(p.tiles * ((a.h + p.span - 1) / p.span)), D::kThreads, 0, stream>>>(
+        a, ws + p.off_tiles, hidden, p.span, y);
     return hipGetLastError();
 }
 
@@ -539,6 +538,13 @@ static bool few_split(const FfnPlan& p, int32_t h, int32_t s, int32_t M) {
 void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {
     ffn_tiles_plan(T * k, M, tile_rows(T * k, h, s, M), p);
     p->few = few(*p, h, s, M);
+    if (p->few) {
+        p->split = few_split(*p, h, s, M);
+        p->span = p->split ? kFewCols : kFewWaves * kFewCols;
+    } else {
+        p->span = ffn_span(s, p->bm == 256 ? DownShape<256, 2>::kCols : DownShape<128, 2>::kCols, p->tiles, h);
+        p->stages = p->bm >= 128 ? 2 : p->bm == 64 ? 3 : p->tiles * ((h + p->span - 1) / p->span) >= 2048 ? 2 : 3;
+    }
     p->planes = p->few || p->n * s <= kFfnTwoPlanes ? 2 : 1;
     p->off_hidden = p->workspace_bytes;
     p->workspace_bytes += align256((size_t)p->n * s * 2 * p->planes);
@@ -561,10 +567,8 @@ hipError_t ffn_launch(const FfnPlan& p, FfnArgs a, uint16_t* y, void* workspace,
     if (p.few) {
         uint16_t* hidden = reinterpret_cast<uint16_t*>(ws + p.off_hidden);
         ffn_few_up_kernel<<<few_grid(p.n * ((a.s + kFewUnits - 1) / kFewUnits)), 64 * kFewWaves, 0, stream>>>(a, hidden);
-        const bool split = few_split(p, a.h, a.s, a.M);
-        const int32_t span = split ? kFewCols : kFewWaves * kFewCols;
-        const unsigned blocks = few_grid(p.n * ((a.h + span - 1) / span));
-        if (split)
+        const unsigned blocks = few_grid(p.n * ((a.h + p.span - 1) / p.span));
+        if (p.split)
             ffn_few_down_kernel<true, 4><<<blocks, 64 * kFewWaves, 0, stream>>>(a, hidden, y);
         else
             ffn_few_down_kernel<false, 2><<<blocks, 64 * kFewWaves, 0, stream>>>(a, hidden, y);
@@ -576,11 +580,7 @@ hipError_t ffn_launch(const FfnPlan& p, FfnArgs a, uint16_t* y, void* workspace,
         case 256: return forward<256, 2>(p, a, y, ws, stream);
         case 128: return forward<128, 2>(p, a, y, ws, stream);
         case 64: return forward<64, 3>(p, a, y, ws, stream);
-        default: {
-            const int32_t span = ffn_span(a.s, DownShape<32, 2>::kCols, p.tiles, a.h);
-            return p.tiles * ((a.h + span - 1) / span) >= 2048 ? forward<32, 2>(p, a, y, ws, stream)
-                                                               : forward<32, 3>(p, a, y, ws, stream);
-        }
+        default: return p.stages == 2 ? forward<32, 2>(p, a, y, ws, stream) : forward<32, 3>(p, a, y, ws, stream);
     }
 }
 

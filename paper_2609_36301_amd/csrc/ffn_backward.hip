@@ -671,7 +671,7 @@ void rows_launch(const FfnPlan& p, const FfnArgs& a, char* ws, hipStream_t strea
     const unsigned up_blocks = grid_of(p.tiles * dgate_parts(p, a.s));
     if constexpr (BM == 256) {
         float* dA0 = reinterpret_cast<float*>(ws + p.off_da0);
-        const int32_t span = ffn_span(a.h, R::kCols, p.tiles, a.s);
+        const int32_t span = p.da0_span;
         ffn_bwd_rows_kernel<BM, true><<<grid_of(p.tiles * ((a.s + span - 1) / span)), R::kThreads, 0, stream>>>(
             a, list, a.du, a.W2t, a.h, a.s, span, dA0);
         ffn_up_kernel<BM, true><<<up_blocks, UpShape<BM>::kThreads, 0, stream>>>(a, list, hidden,
@@ -679,14 +679,13 @@ void rows_launch(const FfnPlan& p, const FfnArgs& a, char* ws, hipStream_t strea
     } else {
         ffn_bwd_up_kernel<BM><<<up_blocks, BwdUpShape<BM>::kThreads, 0, stream>>>(a, list, hidden, dgu, dgp);
     }
-    const int32_t span = ffn_span(2 * a.s, R::kCols, p.tiles, a.h);
-    ffn_bwd_rows_kernel<BM, false><<<grid_of(p.tiles * ((a.h + span - 1) / span)), R::kThreads, 0, stream>>>(
-        a, list, dgu, a.W1t, 2 * a.s, a.h, span, reinterpret_cast<float*>(ws + p.off_dxs));
+    ffn_bwd_rows_kernel<BM, false><<<grid_of(p.tiles * ((a.h + p.span - 1) / p.span)), R::kThreads, 0, stream>>>(
+        a, list, dgu, a.W1t, 2 * a.s, a.h, p.span, reinterpret_cast<float*>(ws + p.off_dxs));
 }
 
-// One weight gradient: tiles of rt x ct, `other` of them across h.
+// One weight gradient: `others` tiles across h, `hspan` of h to a workgroup.
 DwArgs dw_args(const FfnPlan& p, const FfnArgs& a, const uint16_t* P, const uint16_t* Q, int32_t rows, int32_t cols,
-               int32_t others, int32_t step, uint16_t* out, float* parts_out) {
+               int32_t others, int32_t hspan, uint16_t* out, float* parts_out) {
     DwArgs d;
     d.P = P;
     d.Q = Q;
@@ -696,9 +695,8 @@ DwArgs dw_args(const FfnPlan& p, const FfnArgs& a, const uint16_t* P, const uint
     d.parts = p.dw_parts;
     d.parts_out = parts_out;
     d.part_stride = dw_size(a.h, a.s, a.M);
-    const int64_t groups = (int64_t)a.M * others;
-    d.hspan = d.parts > 1 ? step : ffn_span((int32_t)std::min<int64_t>(p.n / a.M, 1 << 20), step, groups, a.h);
-    d.blocks = (int32_t)grid_of(groups * ((a.h + d.hspan - 1) / d.hspan) * d.parts);
+    d.hspan = hspan;
+    d.blocks = (int32_t)grid_of((int64_t)a.M * others * ((a.h + hspan - 1) / hspan) * d.parts);
     d.out = out;
     return d;
 }
@@ -709,8 +707,8 @@ void dw_launch(const FfnPlan& p, const FfnArgs& a, char* ws, hipStream_t stream)
     const uint16_t* dgu = reinterpret_cast<const uint16_t*>(ws + p.off_dgu);
     float* parts = reinterpret_cast<float*>(ws + p.off_dwp);
     const int64_t size1 = (int64_t)a.M * 2 * a.s * a.h;
-    const DwArgs w1 = dw_args(p, a, a.x, dgu, 2 * a.s, a.h, (2 * a.s + RT - 1) / RT, CT1, a.dW1t, parts);
-    const DwArgs w2 = dw_args(p, a, hidden, a.du, a.h, a.s, (a.s + CT2 - 1) / CT2, RT, a.dW2t, parts + size1);
+    const DwArgs w1 = dw_args(p, a, a.x, dgu, 2 * a.s, a.h, (2 * a.s + RT - 1) / RT, p.dw1_span, a.dW1t, parts);
+    const DwArgs w2 = dw_args(p, a, hidden, a.du, a.h, a.s, (a.s + CT2 - 1) / CT2, p.dw2_span, a.dW2t, parts + size1);
     ffn_bwd_dw_kernel<CT1, CT2, RT, WAVES, PARTS, ONCE2><<<(unsigned)(w1.blocks + w2.blocks), 64 * WAVES, 0, stream>>>(
         w1, w2, a.offsets, a.sorted, (int32_t)p.n, a.k, a.M);
     if (PARTS) {
@@ -735,6 +733,10 @@ void dw_plan(int64_t n, int32_t h, int32_t s, int32_t M, FfnPlan* p) {
     p->dw_tile = ffn_cost(large, steps, 256) < ffn_cost(small, steps, 128) ? 256 : 128;
     p->dw_parts = 1;
     if (p->dw_tile == 128) p->dw_parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({512 / small, steps / 4, 32}));
+    const int32_t step = p->dw_tile, len = (int32_t)std::min<int64_t>(n / M, 1 << 20);
+    const int64_t groups1 = M * tiles(2 * s, step), groups2 = M * tiles(s, step == 256 ? 256 : 64);
+    p->dw1_span = p->dw_parts > 1 ? step : ffn_span(len, step, groups1, h);
+    p->dw2_span = p->dw_parts > 1 ? step : ffn_span(len, step, groups2, h);
 }
 
 // Rows of a tile, as in the forward pass (over the same 196 shapes 0.6% off the best on geometric mean, at
@@ -772,6 +774,9 @@ void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t 
     ffn_tiles_plan(T * k, M, backward_rows(T * k, h, s, M), p);
     p->planes = p->n * s <= kFfnTwoPlanes ? 2 : 1;
     dw_plan(p->n, h, s, M, p);
+    const int32_t cols = p->bm == 256 ? RowsShape<256>::kCols : RowsShape<128>::kCols;
+    p->span = ffn_span(2 * s, cols, p->tiles, h);
+    p->da0_span = ffn_span(h, cols, p->tiles, s);
     size_t at = p->workspace_bytes;
     p->off_hidden = at;
     at += align256((size_t)p->n * s * 2 * p->planes);

@@ -88,6 +88,31 @@ more_status more_expert_ffn(const uint16_t* x, const uint16_t* W1t, const uint16
                                      static_cast<hipStream_t>(stream)));
 }
 
+more_status more_expert_ffn_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, int32_t backward,
+                                 more_expert_plan* plan) {
+    if (!plan) return MORE_ERR_INVALID_ARG;
+    more_status st = check_ffn(T, h, s, M, k);
+    if (st != MORE_OK) return st;
+    more::FfnPlan p;
+    *plan = {};
+    if (backward) {
+        more::ffn_backward_make_plan(T, h, s, M, k, &p);
+        plan->tile_rows = p.bm;
+        plan->stages = 2;
+        plan->dw_tile = p.dw_tile;
+        plan->dw_runs = p.dw_parts;
+        plan->dw1_span = p.dw1_span;
+        plan->dw2_span = p.dw2_span;
+    } else {
+        more::ffn_make_plan(T, h, s, M, k, &p);
+        plan->tile_rows = p.few ? 0 : p.bm;
+        plan->stages = p.stages;
+    }
+    plan->addends = p.planes;
+    plan->span = p.span;
+    return MORE_OK;
+}
+
 more_status more_expert_ffn_backward_workspace_size(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k,
                                                     size_t* bytes) {
     if (!bytes) return MORE_ERR_INVALID_ARG;

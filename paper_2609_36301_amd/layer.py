@@ -92,6 +92,14 @@ def expert_ffn_backward_workspace_size(T: int, h: int, s: int, M: int, k: int) -
     return _size("more_expert_ffn_backward_workspace_size", T, h, s, M, k)
 
 
+def expert_ffn_plan(T: int, h: int, s: int, M: int, k: int, backward: bool = False) -> dict[str, int]:
+    """The form in which expert_ffn (or its backward pass) runs this shape: the fields of more_expert_plan."""
+    plan = _lib.ExpertPlan()
+    _lib.check(_lib.load().more_expert_ffn_plan(T, h, s, M, k, int(backward), ctypes.byref(plan)),
+               "more_expert_ffn_plan")
+    return {name: getattr(plan, name) for name, _ in plan._fields_}
+
+
 def _ffn_spec(T, h, s, M, k):
     bf16, i32 = torch.bfloat16, torch.int32
     return (("x", bf16, (T, h)), ("W1t", bf16, (M, 2 * s, h)), ("W2t", bf16, (M, h, s)), ("idx", i32, (T, k)),
