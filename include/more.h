@@ -341,9 +341,11 @@ more_status more_route_lowrank_noalloc(const uint16_t* x, const uint16_t* R1t, c
  * 1 <= k <= MORE_K_MAX (k may exceed M: an id may occur more than once in a token); T k <= 2^31 - 2^16,
  * M < 2^30.  T == 0 writes nothing.  offsets and sorted that are not those of idx give undefined values
  * in y (no access outside the buffers).
- * Numerics: fp32 accumulation of exact bf16 products; between the two contractions A is rounded to bf16
- * once, or, where few values are (T k s <= 2^15, and in some decode steps), to a sum of two bf16;
- * activation and gate in fp32.  The sums run in a fixed order.
+ * Numerics: fp32 accumulation of exact bf16 products; activation and gate in fp32.  Between the two
+ * contractions A is rounded to bf16 once (the matrix cores' operand type; with y's own rounding an error of
+ * 1.41 times the latter, on average), or to a sum of two bf16 (y's own rounding alone) where T k s <= 2^15 and
+ * in the kernels without tiles, where it costs little; more_expert_ffn_plan tells which for a shape, and
+ * more_expert_ffn_ex takes two addends at every size.  The sums run in a fixed order.
  */
 more_status more_expert_ffn(const uint16_t* x, const uint16_t* W1t, const uint16_t* W2t, int64_t T,
                             int32_t h, int32_t s, int32_t M, int32_t k, const int32_t* idx,
@@ -351,6 +353,20 @@ more_status more_expert_ffn(const uint16_t* x, const uint16_t* W1t, const uint16
                             uint16_t* y, void* workspace, size_t workspace_bytes, void* stream);
 more_status more_expert_ffn_workspace_size(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k,
                                            size_t* bytes);
+
+/*
+ * Same with the number of bf16 addends that stand between the contractions chosen by the caller: 0 as stated
+ * above, 2 for two at every size, so that a token's rows are as exact in any batch as alone (the second
+ * product then takes twice its operations).  Its workspace size comes from
+ * more_expert_ffn_workspace_size_ex with the same addends.
+ */
+more_status more_expert_ffn_ex(const uint16_t* x, const uint16_t* W1t, const uint16_t* W2t, int64_t T,
+                               int32_t h, int32_t s, int32_t M, int32_t k, int32_t addends,
+                               const int32_t* idx, const int32_t* offsets, const int32_t* sorted,
+                               const float* gate, uint16_t* y, void* workspace, size_t workspace_bytes,
+                               void* stream);
+more_status more_expert_ffn_workspace_size_ex(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k,
+                                              int32_t addends, size_t* bytes);
 
 /* The form in which more_expert_ffn (backward == 0) or its backward pass runs this shape (written to *plan,
  * host): for tests of every form and for a caller who wants to know how the hidden units are rounded. */
@@ -364,7 +380,7 @@ typedef struct more_expert_plan {
     int32_t dw1_span;  /* (backward, else 0) columns of h that a workgroup takes of dW1t ...         */
     int32_t dw2_span;  /* ... and rows of h of dW2t                                                  */
 } more_expert_plan;
-more_status more_expert_ffn_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k,
+more_status more_expert_ffn_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, int32_t addends,
                                  int32_t backward, more_expert_plan* plan);
 
 /*
@@ -379,9 +395,9 @@ more_status more_expert_ffn_plan(int64_t T, int32_t h, int32_t s, int32_t M, int
  *   workspace / workspace_bytes   at least more_expert_ffn_backward_workspace_size() bytes, 256-byte
  *                              aligned (NULL allowed when T == 0)
  * Limits as for more_expert_ffn.  Numerics: bf16 operands with fp32 accumulation; the gradients of the
- * pre-activations and gate A are rounded to bf16 once (to a sum of two bf16 where T k s <= 2^15), the entries' shares of dx are added in fp32,
- * dgate comes from unrounded fp32 values.  Nothing is added atomically: a call gives the same bits on
- * every run.
+ * pre-activations and gate A are rounded to bf16 once, or to a sum of two bf16 where T k s <= 2^15 (at every size
+ * with addends == 2, below); the entries' shares of dx are added in fp32, dgate comes from unrounded fp32
+ * values.  Nothing is added atomically: a call gives the same bits on every run.
  */
 more_status more_expert_ffn_backward(const uint16_t* x, const uint16_t* W1t, const uint16_t* W2t,
                                      int64_t T, int32_t h, int32_t s, int32_t M, int32_t k,
@@ -391,6 +407,16 @@ more_status more_expert_ffn_backward(const uint16_t* x, const uint16_t* W1t, con
                                      size_t workspace_bytes, void* stream);
 more_status more_expert_ffn_backward_workspace_size(int64_t T, int32_t h, int32_t s, int32_t M,
                                                     int32_t k, size_t* bytes);
+/* Same with the number of addends as in more_expert_ffn_ex (2: dx and both weight gradients take twice
+ * their operations). */
+more_status more_expert_ffn_backward_ex(const uint16_t* x, const uint16_t* W1t, const uint16_t* W2t,
+                                        int64_t T, int32_t h, int32_t s, int32_t M, int32_t k,
+                                        int32_t addends, const int32_t* idx, const int32_t* offsets,
+                                        const int32_t* sorted, const float* gate, const uint16_t* du,
+                                        uint16_t* dx, uint16_t* dW1t, uint16_t* dW2t, float* dgate,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+more_status more_expert_ffn_backward_workspace_size_ex(int64_t T, int32_t h, int32_t s, int32_t M,
+                                                       int32_t k, int32_t addends, size_t* bytes);
 
 /*
  * The end of a block and the norm before the next one, in one pass:

@@ -61,10 +61,17 @@ SIGNATURES = {
     "more_expert_ffn": (_I32, [_P, _P, _P, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _P, _P,
                                _SZ, _P]),
     "more_expert_ffn_workspace_size": (_I32, [_I64, _I32, _I32, _I32, _I32, _PSZ]),
-    "more_expert_ffn_plan": (_I32, [_I64, _I32, _I32, _I32, _I32, _I32, ctypes.POINTER(ExpertPlan)]),
+    "more_expert_ffn_ex": (_I32, [_P, _P, _P, _I64, _I32, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _P,
+                                  _P, _SZ, _P]),
+    "more_expert_ffn_workspace_size_ex": (_I32, [_I64, _I32, _I32, _I32, _I32, _I32, _PSZ]),
+    "more_expert_ffn_plan": (_I32, [_I64, _I32, _I32, _I32, _I32, _I32, _I32,
+                                    ctypes.POINTER(ExpertPlan)]),
     "more_expert_ffn_backward": (_I32, [_P, _P, _P, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _P,
                                         _P, _P, _P, _P, _P, _P, _SZ, _P]),
     "more_expert_ffn_backward_workspace_size": (_I32, [_I64, _I32, _I32, _I32, _I32, _PSZ]),
+    "more_expert_ffn_backward_ex": (_I32, [_P, _P, _P, _I64, _I32, _I32, _I32, _I32, _I32, _P, _P, _P,
+                                           _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "more_expert_ffn_backward_workspace_size_ex": (_I32, [_I64, _I32, _I32, _I32, _I32, _I32, _PSZ]),
     "more_block_norm": (_I32, [_P, _I32, _P, _I64, _I32, _I32, _P, _P, _P, _F32, _F32, _I32, _P,
                                _P, _P, _P]),
     "more_block_norm_backward": (_I32, [_P, _P, _I32, _P, _P, _P, _I64, _I32, _P, _P, _P, _F32,

@@ -34,10 +34,15 @@ struct FfnPlan {
     int32_t span;     // columns of y (backward: of the shares of dx) that a workgroup takes
     int32_t da0_span; // (backward, tiles of 256 rows) columns of dA0 that a workgroup takes
     // The hidden units (and, backward, the gradients of the pre-activations) go from kernel to kernel in bf16,
-    // the matrix cores' operand type.  A rounding error of each then sits in all its products, as large as the
-    // results' own rounding (together 1.41 of it) on average over many; where few are rounded (n s <= 2^15;
-    // below it the factor scatters by 2% and more, at 512 values by 10%) and the products are small, they are
-    // carried as a sum of two bf16 (planes = 2), [planes][n][s] and [planes][n][2s].
+    // the matrix cores' operand type: one rounding each (planes = 1), which sits in all its products and makes the
+    // results' error 1.41 times that of their own rounding, on average over many; or a sum of two bf16
+    // (planes = 2; [planes][n][s] and [planes][n][2s]), which leaves the results' own rounding alone and doubles
+    // the operations of the products that read them.  Two where the caller asks for them, in the kernels without
+    // tiles, and for n s <= 2^15, where the errors of few roundings do not average out (at 512 values the factor
+    // scatters by 10%) and two cost a few us.  us, one : two, forward and backward: 600 experts of h = 2048, s = 64
+    // with one row 58 : 68 and 205 : 232; a dense block of h = 4096, s = 128, 300 rows 41 : 43 and 110 : 119; and
+    // far above, 4096 experts of h = 512, s = 64 with 32 rows 226 : 248 and 660 : 784; 32 experts of h = 2048,
+    // s = 1024 with 1024 rows 473 : 594 and 1435 : 2498 (on tiles of 128 rows).
     int32_t planes;
     int64_t tiles;    // bound on the number of tiles
     int32_t sums;     // workgroups that count tiles ahead of the list (0: none)
@@ -48,8 +53,9 @@ struct FfnPlan {
     size_t workspace_bytes;
 };
 
-void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p);
-void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p);
+// addends: 2 for two planes at every size, 0 for the rule beside FfnPlan::planes
+void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, int32_t addends, FfnPlan* p);
+void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, int32_t addends, FfnPlan* p);
 hipError_t ffn_launch(const FfnPlan& p, FfnArgs a, uint16_t* y, void* workspace, hipStream_t stream);
 hipError_t ffn_backward_launch(const FfnPlan& p, FfnArgs a, void* workspace, hipStream_t stream);
 

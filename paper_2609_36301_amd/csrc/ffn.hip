@@ -535,7 +535,7 @@ static bool few_split(const FfnPlan& p, int32_t h, int32_t s, int32_t M) {
     return 4 * few_starts(p, M) * ((h + kFewWaves * kFewCols - 1) / (kFewWaves * kFewCols)) <= s;
 }
 
-void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {
+void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, int32_t addends, FfnPlan* p) {
     ffn_tiles_plan(T * k, M, tile_rows(T * k, h, s, M), p);
     p->few = few(*p, h, s, M);
     if (p->few) {
@@ -545,7 +545,7 @@ void ffn_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPla
         p->span = ffn_span(s, p->bm == 256 ? DownShape<256, 2>::kCols : DownShape<128, 2>::kCols, p->tiles, h);
         p->stages = p->bm >= 128 ? 2 : p->bm == 64 ? 3 : p->tiles * ((h + p->span - 1) / p->span) >= 2048 ? 2 : 3;
     }
-    p->planes = p->few || p->n * s <= kFfnTwoPlanes ? 2 : 1;
+    p->planes = addends == 2 || p->few || p->n * s <= kFfnTwoPlanes ? 2 : 1;
     p->off_hidden = p->workspace_bytes;
     p->workspace_bytes += align256((size_t)p->n * s * 2 * p->planes);
 }

@@ -742,9 +742,9 @@ void dw_plan(int64_t n, int32_t h, int32_t s, int32_t M, FfnPlan* p) {
 // Rows of a tile, as in the forward pass (over the same 196 shapes 0.6% off the best on geometric mean, at
 // most 18%; us for 64 : 128 : 256 rows, 32 experts of h = 2048, s = 1024, 96 rows 359 : 299 : 326, 384 rows 778 :
 // 712 : 607; 4096 experts of h = 512, s = 64, 32 rows 622 : 662 : 1051).
-int32_t backward_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
+int32_t backward_rows(int64_t n, int32_t h, int32_t s, int32_t M, int32_t planes) {
     if (n / std::max<int64_t>(1, std::min<int64_t>(n, M)) < 24) return 32;
-    const int32_t most = n * s <= kFfnTwoPlanes ? 128 : 256;  // (the kernels of 256 rows write one plane)
+    const int32_t most = planes == 2 ? 128 : 256;  // (the kernels of 256 rows write one plane)
     int32_t best = 64;
     int64_t least = INT64_MAX;
     const int64_t hsteps = (h + kFfnBK - 1) / kFfnBK, ssteps = (2 * s + kFfnBK - 1) / kFfnBK;
@@ -770,9 +770,10 @@ int32_t backward_rows(int64_t n, int32_t h, int32_t s, int32_t M) {
 
 }  // namespace
 
-void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, FfnPlan* p) {
-    ffn_tiles_plan(T * k, M, backward_rows(T * k, h, s, M), p);
-    p->planes = p->n * s <= kFfnTwoPlanes ? 2 : 1;
+void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, int32_t addends, FfnPlan* p) {
+    const int32_t planes = addends == 2 || T * k * s <= kFfnTwoPlanes ? 2 : 1;
+    ffn_tiles_plan(T * k, M, backward_rows(T * k, h, s, M, planes), p);
+    p->planes = planes;
     dw_plan(p->n, h, s, M, p);
     const int32_t cols = p->bm == 256 ? RowsShape<256>::kCols : RowsShape<128>::kCols;
     p->span = ffn_span(2 * s, cols, p->tiles, h);

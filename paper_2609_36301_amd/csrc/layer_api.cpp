@@ -21,8 +21,8 @@ bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p
 
 more_status from_hip(hipError_t e) { return e == hipSuccess ? MORE_OK : MORE_ERR_HIP; }
 
-more_status check_ffn(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k) {
-    if (T < 0 || h <= 0 || s <= 0 || M <= 0 || k < 1) return MORE_ERR_INVALID_ARG;
+more_status check_ffn(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, int32_t addends) {
+    if (T < 0 || h <= 0 || s <= 0 || M <= 0 || k < 1 || (addends != 0 && addends != 2)) return MORE_ERR_INVALID_ARG;
     if (h % 16 != 0 || s % 8 != 0 || h > kMaxWidth || s > kMaxWidth || k > MORE_K_MAX || M >= kMaxM ||
         T > kMaxFfnEntries || T * (int64_t)k > kMaxFfnEntries)
         return MORE_ERR_UNSUPPORTED;
@@ -60,43 +60,56 @@ more::FfnArgs ffn_args(const uint16_t* x, const uint16_t* W1t, const uint16_t* W
 
 extern "C" {
 
-more_status more_expert_ffn_workspace_size(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, size_t* bytes) {
+more_status more_expert_ffn_workspace_size_ex(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, int32_t addends,
+                                              size_t* bytes) {
     if (!bytes) return MORE_ERR_INVALID_ARG;
-    more_status st = check_ffn(T, h, s, M, k);
+    more_status st = check_ffn(T, h, s, M, k, addends);
     if (st != MORE_OK) return st;
     more::FfnPlan p;
-    more::ffn_make_plan(T, h, s, M, k, &p);
+    more::ffn_make_plan(T, h, s, M, k, addends, &p);
     *bytes = T == 0 ? 0 : p.workspace_bytes;
     return MORE_OK;
+}
+
+more_status more_expert_ffn_workspace_size(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, size_t* bytes) {
+    return more_expert_ffn_workspace_size_ex(T, h, s, M, k, 0, bytes);
+}
+
+more_status more_expert_ffn_ex(const uint16_t* x, const uint16_t* W1t, const uint16_t* W2t, int64_t T, int32_t h,
+                               int32_t s, int32_t M, int32_t k, int32_t addends, const int32_t* idx,
+                               const int32_t* offsets, const int32_t* sorted, const float* gate, uint16_t* y,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+    if (!W1t || !W2t || !offsets || (T != 0 && (!x || !idx || !sorted || !y))) return MORE_ERR_INVALID_ARG;
+    if (!aligned(x, 16) || !aligned(W1t, 16) || !aligned(W2t, 16) || !aligned(y, 16) || !aligned(idx, 4) ||
+        !aligned(offsets, 4) || !aligned(sorted, 4) || !aligned(gate, 4) || !aligned(workspace, 256))
+        return MORE_ERR_INVALID_ARG;
+    more_status st = check_ffn(T, h, s, M, k, addends);
+    if (st != MORE_OK) return st;
+    if (T == 0) return MORE_OK;
+    more::FfnPlan p;
+    more::ffn_make_plan(T, h, s, M, k, addends, &p);
+    if (!workspace || workspace_bytes < p.workspace_bytes) return MORE_ERR_WORKSPACE;
+    return from_hip(more::ffn_launch(p, ffn_args(x, W1t, W2t, T, h, s, M, k, idx, offsets, sorted, gate), y, workspace,
+                                     static_cast<hipStream_t>(stream)));
 }
 
 more_status more_expert_ffn(const uint16_t* x, const uint16_t* W1t, const uint16_t* W2t, int64_t T, int32_t h,
                             int32_t s, int32_t M, int32_t k, const int32_t* idx, const int32_t* offsets,
                             const int32_t* sorted, const float* gate, uint16_t* y, void* workspace,
                             size_t workspace_bytes, void* stream) {
-    if (!W1t || !W2t || !offsets || (T != 0 && (!x || !idx || !sorted || !y))) return MORE_ERR_INVALID_ARG;
-    if (!aligned(x, 16) || !aligned(W1t, 16) || !aligned(W2t, 16) || !aligned(y, 16) || !aligned(idx, 4) ||
-        !aligned(offsets, 4) || !aligned(sorted, 4) || !aligned(gate, 4) || !aligned(workspace, 256))
-        return MORE_ERR_INVALID_ARG;
-    more_status st = check_ffn(T, h, s, M, k);
-    if (st != MORE_OK) return st;
-    if (T == 0) return MORE_OK;
-    more::FfnPlan p;
-    more::ffn_make_plan(T, h, s, M, k, &p);
-    if (!workspace || workspace_bytes < p.workspace_bytes) return MORE_ERR_WORKSPACE;
-    return from_hip(more::ffn_launch(p, ffn_args(x, W1t, W2t, T, h, s, M, k, idx, offsets, sorted, gate), y, workspace,
-                                     static_cast<hipStream_t>(stream)));
+    return more_expert_ffn_ex(x, W1t, W2t, T, h, s, M, k, 0, idx, offsets, sorted, gate, y, workspace, workspace_bytes,
+                              stream);
 }
 
-more_status more_expert_ffn_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, int32_t backward,
-                                 more_expert_plan* plan) {
+more_status more_expert_ffn_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k, int32_t addends,
+                                 int32_t backward, more_expert_plan* plan) {
     if (!plan) return MORE_ERR_INVALID_ARG;
-    more_status st = check_ffn(T, h, s, M, k);
+    more_status st = check_ffn(T, h, s, M, k, addends);
     if (st != MORE_OK) return st;
     more::FfnPlan p;
     *plan = {};
     if (backward) {
-        more::ffn_backward_make_plan(T, h, s, M, k, &p);
+        more::ffn_backward_make_plan(T, h, s, M, k, addends, &p);
         plan->tile_rows = p.bm;
         plan->stages = 2;
         plan->dw_tile = p.dw_tile;
@@ -104,7 +117,7 @@ more_status more_expert_ffn_plan(int64_t T, int32_t h, int32_t s, int32_t M, int
         plan->dw1_span = p.dw1_span;
         plan->dw2_span = p.dw2_span;
     } else {
-        more::ffn_make_plan(T, h, s, M, k, &p);
+        more::ffn_make_plan(T, h, s, M, k, addends, &p);
         plan->tile_rows = p.few ? 0 : p.bm;
         plan->stages = p.stages;
     }
@@ -113,22 +126,27 @@ more_status more_expert_ffn_plan(int64_t T, int32_t h, int32_t s, int32_t M, int
     return MORE_OK;
 }
 
-more_status more_expert_ffn_backward_workspace_size(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k,
-                                                    size_t* bytes) {
+more_status more_expert_ffn_backward_workspace_size_ex(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k,
+                                                       int32_t addends, size_t* bytes) {
     if (!bytes) return MORE_ERR_INVALID_ARG;
-    more_status st = check_ffn(T, h, s, M, k);
+    more_status st = check_ffn(T, h, s, M, k, addends);
     if (st != MORE_OK) return st;
     more::FfnPlan p;
-    more::ffn_backward_make_plan(T, h, s, M, k, &p);
+    more::ffn_backward_make_plan(T, h, s, M, k, addends, &p);
     *bytes = T == 0 ? 0 : p.workspace_bytes;
     return MORE_OK;
 }
 
-more_status more_expert_ffn_backward(const uint16_t* x, const uint16_t* W1t, const uint16_t* W2t, int64_t T, int32_t h,
-                                     int32_t s, int32_t M, int32_t k, const int32_t* idx, const int32_t* offsets,
-                                     const int32_t* sorted, const float* gate, const uint16_t* du, uint16_t* dx,
-                                     uint16_t* dW1t, uint16_t* dW2t, float* dgate, void* workspace,
-                                     size_t workspace_bytes, void* stream) {
+more_status more_expert_ffn_backward_workspace_size(int64_t T, int32_t h, int32_t s, int32_t M, int32_t k,
+                                                    size_t* bytes) {
+    return more_expert_ffn_backward_workspace_size_ex(T, h, s, M, k, 0, bytes);
+}
+
+more_status more_expert_ffn_backward_ex(const uint16_t* x, const uint16_t* W1t, const uint16_t* W2t, int64_t T,
+                                        int32_t h, int32_t s, int32_t M, int32_t k, int32_t addends, const int32_t* idx,
+                                        const int32_t* offsets, const int32_t* sorted, const float* gate,
+                                        const uint16_t* du, uint16_t* dx, uint16_t* dW1t, uint16_t* dW2t, float* dgate,
+                                        void* workspace, size_t workspace_bytes, void* stream) {
     if (!W1t || !W2t || !offsets || !dW1t || !dW2t || (T != 0 && (!x || !idx || !sorted || !du || !dx)) ||
         (dgate && !gate))
         return MORE_ERR_INVALID_ARG;
@@ -136,10 +154,10 @@ more_status more_expert_ffn_backward(const uint16_t* x, const uint16_t* W1t, con
         !aligned(dW1t, 16) || !aligned(dW2t, 16) || !aligned(idx, 4) || !aligned(offsets, 4) || !aligned(sorted, 4) ||
         !aligned(gate, 4) || !aligned(dgate, 4) || !aligned(workspace, 256))
         return MORE_ERR_INVALID_ARG;
-    more_status st = check_ffn(T, h, s, M, k);
+    more_status st = check_ffn(T, h, s, M, k, addends);
     if (st != MORE_OK) return st;
     more::FfnPlan p;
-    more::ffn_backward_make_plan(T, h, s, M, k, &p);
+    more::ffn_backward_make_plan(T, h, s, M, k, addends, &p);
     if (T != 0 && (!workspace || workspace_bytes < p.workspace_bytes)) return MORE_ERR_WORKSPACE;
     more::FfnArgs a = ffn_args(x, W1t, W2t, T, h, s, M, k, idx, offsets, sorted, gate);
     a.du = du;
@@ -148,6 +166,15 @@ more_status more_expert_ffn_backward(const uint16_t* x, const uint16_t* W1t, con
     a.dW2t = dW2t;
     a.dgate = dgate;
     return from_hip(more::ffn_backward_launch(p, a, workspace, static_cast<hipStream_t>(stream)));
+}
+
+more_status more_expert_ffn_backward(const uint16_t* x, const uint16_t* W1t, const uint16_t* W2t, int64_t T, int32_t h,
+                                     int32_t s, int32_t M, int32_t k, const int32_t* idx, const int32_t* offsets,
+                                     const int32_t* sorted, const float* gate, const uint16_t* du, uint16_t* dx,
+                                     uint16_t* dW1t, uint16_t* dW2t, float* dgate, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+    return more_expert_ffn_backward_ex(x, W1t, W2t, T, h, s, M, k, 0, idx, offsets, sorted, gate, du, dx, dW1t, dW2t,
+                                       dgate, workspace, workspace_bytes, stream);
 }
 
 more_status more_block_norm(const void* r, int32_t resid_bits, const uint16_t* y, int64_t T, int32_t h, int32_t k,

@@ -84,18 +84,20 @@ def _workspace(nbytes: int, device) -> torch.Tensor:
 
 
 # ---------------------------------------------------------------------------------- experts
-def expert_ffn_workspace_size(T: int, h: int, s: int, M: int, k: int) -> int:
-    return _size("more_expert_ffn_workspace_size", T, h, s, M, k)
+# addends (of every call on the experts): 0 rounds the hidden units between the two products to one bf16 where there
+# are many and to a sum of two where there are few; 2 takes two at every size (more_expert_ffn_ex).
+def expert_ffn_workspace_size(T: int, h: int, s: int, M: int, k: int, addends: int = 0) -> int:
+    return _size("more_expert_ffn_workspace_size_ex", T, h, s, M, k, addends)
 
 
-def expert_ffn_backward_workspace_size(T: int, h: int, s: int, M: int, k: int) -> int:
-    return _size("more_expert_ffn_backward_workspace_size", T, h, s, M, k)
+def expert_ffn_backward_workspace_size(T: int, h: int, s: int, M: int, k: int, addends: int = 0) -> int:
+    return _size("more_expert_ffn_backward_workspace_size_ex", T, h, s, M, k, addends)
 
 
-def expert_ffn_plan(T: int, h: int, s: int, M: int, k: int, backward: bool = False) -> dict[str, int]:
+def expert_ffn_plan(T: int, h: int, s: int, M: int, k: int, backward: bool = False, addends: int = 0) -> dict[str, int]:
     """The form in which expert_ffn (or its backward pass) runs this shape: the fields of more_expert_plan."""
     plan = _lib.ExpertPlan()
-    _lib.check(_lib.load().more_expert_ffn_plan(T, h, s, M, k, int(backward), ctypes.byref(plan)),
+    _lib.check(_lib.load().more_expert_ffn_plan(T, h, s, M, k, addends, int(backward), ctypes.byref(plan)),
                "more_expert_ffn_plan")
     return {name: getattr(plan, name) for name, _ in plan._fields_}
 
@@ -125,27 +127,28 @@ def _ffn_shape(x, W1t, W2t, idx):
 class ExpertFFN:
     """Pre-allocated output and workspace for repeated expert_ffn calls with one shape."""
 
-    def __init__(self, T: int, h: int, s: int, M: int, k: int, *, device=None):
-        self.shape, self.spec = (T, h, s, M, k), _ffn_spec(T, h, s, M, k)
+    def __init__(self, T: int, h: int, s: int, M: int, k: int, *, addends: int = 0, device=None):
+        self.shape, self.spec, self.addends = (T, h, s, M, k), _ffn_spec(T, h, s, M, k), addends
         self.device = _device(device)
-        self.workspace_bytes = expert_ffn_workspace_size(T, h, s, M, k)
+        self.workspace_bytes = expert_ffn_workspace_size(*self.shape, addends)
         self.workspace = _workspace(self.workspace_bytes, self.device)
         self.y = torch.empty((T * k, h), dtype=torch.bfloat16, device=self.device)
 
     def __call__(self, x, W1t, W2t, idx, offsets, sorted, gate=None) -> torch.Tensor:
         _check_ffn(self.spec, self.device, x, W1t, W2t, idx, offsets, sorted, gate)
-        _call("more_expert_ffn", self.device, _ptr(x), _ptr(W1t), _ptr(W2t), *self.shape, _ptr(idx),
-              _ptr(offsets), _ptr(sorted), _ptr(gate), _ptr(self.y), _ptr(self.workspace),
+        _call("more_expert_ffn_ex", self.device, _ptr(x), _ptr(W1t), _ptr(W2t), *self.shape, self.addends,
+              _ptr(idx), _ptr(offsets), _ptr(sorted), _ptr(gate), _ptr(self.y), _ptr(self.workspace),
               self.workspace_bytes)
         return self.y
 
 
-def expert_ffn(x, W1t, W2t, idx, offsets, sorted, gate=None) -> torch.Tensor:
+def expert_ffn(x, W1t, W2t, idx, offsets, sorted, gate=None, *, addends: int = 0) -> torch.Tensor:
     """y [T k][h] bf16: row t k + j is gate[t][j] times the gated feed-forward block of expert
     idx[t][j] applied to x[t]; zero rows for ids outside [0, M).  offsets and sorted are
-    dispatch_sort(idx, M)'s (more_expert_ffn)."""
+    dispatch_sort(idx, M)'s.  addends = 2 carries the hidden units as two bf16 addends at every size
+    (more_expert_ffn_ex)."""
     shape = _ffn_shape(x, W1t, W2t, idx)
-    return ExpertFFN(*shape, device=x.device)(x, W1t, W2t, idx, offsets, sorted, gate)
+    return ExpertFFN(*shape, addends=addends, device=x.device)(x, W1t, W2t, idx, offsets, sorted, gate)
 
 
 @dataclasses.dataclass
@@ -160,10 +163,10 @@ class ExpertGradients:
 class ExpertFFNBackward:
     """Pre-allocated gradients and workspace for repeated expert_ffn_backward calls with one shape."""
 
-    def __init__(self, T: int, h: int, s: int, M: int, k: int, *, device=None):
-        self.shape, self.spec = (T, h, s, M, k), _ffn_spec(T, h, s, M, k)
+    def __init__(self, T: int, h: int, s: int, M: int, k: int, *, addends: int = 0, device=None):
+        self.shape, self.spec, self.addends = (T, h, s, M, k), _ffn_spec(T, h, s, M, k), addends
         self.device = dev = _device(device)
-        self.workspace_bytes = expert_ffn_backward_workspace_size(T, h, s, M, k)
+        self.workspace_bytes = expert_ffn_backward_workspace_size(*self.shape, addends)
         self.workspace = _workspace(self.workspace_bytes, dev)
         bf16 = torch.bfloat16
         self.dx = torch.empty((T, h), dtype=bf16, device=dev)
@@ -174,17 +177,17 @@ class ExpertFFNBackward:
     def __call__(self, x, W1t, W2t, idx, offsets, sorted, gate, du) -> ExpertGradients:
         _check_ffn(self.spec, self.device, x, W1t, W2t, idx, offsets, sorted, gate, du)
         dgate = None if gate is None else self.dgate
-        _call("more_expert_ffn_backward", self.device, _ptr(x), _ptr(W1t), _ptr(W2t), *self.shape,
-              _ptr(idx), _ptr(offsets), _ptr(sorted), _ptr(gate), _ptr(du), _ptr(self.dx),
+        _call("more_expert_ffn_backward_ex", self.device, _ptr(x), _ptr(W1t), _ptr(W2t), *self.shape,
+              self.addends, _ptr(idx), _ptr(offsets), _ptr(sorted), _ptr(gate), _ptr(du), _ptr(self.dx),
               _ptr(self.dW1t), _ptr(self.dW2t), _ptr(dgate), _ptr(self.workspace), self.workspace_bytes)
         return ExpertGradients(self.dx, self.dW1t, self.dW2t, dgate)
 
 
-def expert_ffn_backward(x, W1t, W2t, idx, offsets, sorted, gate, du) -> ExpertGradients:
+def expert_ffn_backward(x, W1t, W2t, idx, offsets, sorted, gate, du, *, addends: int = 0) -> ExpertGradients:
     """Gradients of expert_ffn given du [T][h] bf16, the gradient with respect to the sum of a token's
-    k rows of y (more_expert_ffn_backward); gate may be None (then dgate is None)."""
+    k rows of y; gate may be None (then dgate is None); addends as in expert_ffn (more_expert_ffn_backward_ex)."""
     shape = _ffn_shape(x, W1t, W2t, idx)
-    return ExpertFFNBackward(*shape, device=x.device)(x, W1t, W2t, idx, offsets, sorted, gate, du)
+    return ExpertFFNBackward(*shape, addends=addends, device=x.device)(x, W1t, W2t, idx, offsets, sorted, gate, du)
 
 
 # ---------------------------------------------------------------------------------- norms

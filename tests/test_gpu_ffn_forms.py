@@ -87,5 +87,5 @@ def test_plan_refuses():
     for args, status in (((64, 64, 16, 8, 2), _lib.OK), ((0, 64, 16, 8, 2), _lib.OK), ((-1, 64, 16, 8, 2), _lib.ERR_INVALID_ARG),
                          ((64, 72, 16, 8, 2), _lib.ERR_UNSUPPORTED), ((64, 64, 16, 8, 33), _lib.ERR_UNSUPPORTED)):
         for backward in (0, 1):
-            assert lib.more_expert_ffn_plan(*args, backward, ctypes.byref(plan)) == status
-    assert lib.more_expert_ffn_plan(64, 64, 16, 8, 2, 0, None) == _lib.ERR_INVALID_ARG
+            assert lib.more_expert_ffn_plan(*args, 0, backward, ctypes.byref(plan)) == status
+    assert lib.more_expert_ffn_plan(64, 64, 16, 8, 2, 0, 0, None) == _lib.ERR_INVALID_ARG
