@@ -62,7 +62,8 @@ hipError_t ffn_backward_launch(const FfnPlan& p, FfnArgs a, void* workspace, hip
 // Columns that a workgroup takes, in steps of `step`, of a product whose contraction is `len` long: a
 // single step where the contraction alone fills the pipeline (eight stages), or where the groups of rows are
 // too few to fill the chip four times over with more; else up to 512.  us, forward and backward, single step :
-// up to 512: 4096 experts of h = 512, s = 64, 32 rows 256 + 680 : 215 + 621; 128 experts of h = 2048, s = 320,
+// up to 512 (experts chosen evenly, as for all rules here; with popularities that fall off as in a trained router
+// the first shape takes 226 + 660): 4096 experts of h = 512, s = 64, 32 rows 256 + 680 : 215 + 621; 128 experts of h = 2048, s = 320,
 // 256 rows 276 + 886 : 264 + 844; 200 experts of h = 528, s = 72, 9 rows 24 + 61 : 26 + 74.
 inline int32_t ffn_span(int32_t len, int32_t step, int64_t groups, int32_t cols) {
     return len > 512 || groups * ((cols + 511) / 512) < 1024 ? step : 512;

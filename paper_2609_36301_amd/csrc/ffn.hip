@@ -454,7 +454,7 @@ unsigned few_grid(int64_t items) { return (unsigned)std::min<int64_t>(items, 1 <
 // again; us, 32 : 64 rows, 4096 experts of h = 512, s = 64 with 12 rows 164 : 185, with 24 185 : 205, with 32
 // 222 : 215; 64 experts of h = 1024, s = 256 with 24 rows 32 : 27), else what costs least by ffn_cost.  Large
 // tiles need less from the caches, small ones fill the chip: us for 64 : 128 : 256 rows,
-//   32 experts of h = 2048, s = 1024, 48 rows 99 : 107 : 120, 384 rows 288 : 244 : 196, 1024 rows - : 528 : 453
+//   32 experts of h = 2048, s = 1024, 48 rows 99 : 107 : 120, 384 rows 295 : 242 : 189, 1024 rows - : 535 : 473
 //   64 experts of h = 1024, s = 512, 192 rows 81 : 73 : 66, 256 rows 101 : 92 : 109 (the 256-row tiles take one and
 //   a half rounds), 1024 rows - : 310 : 276
 //   a dense block of h = 2048, s = 1024, 1024 rows 36 : 47 : 82, 4096 rows 78 : 65 : 87, 8192 rows 148 : 124 : 98

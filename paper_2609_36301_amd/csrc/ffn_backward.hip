@@ -18,8 +18,8 @@
 //                 zeros
 // Every sum runs in a fixed order: nothing is added atomically, and a call gives the same bits on every
 // run.  Numerics: bf16 operands with fp32 accumulation; [dG dU] and gate A are rounded to bf16 once (the
-// matrix cores' operand type), or to two bf16 addends where few values are (FfnPlan::planes), the entries' shares of dx stay in fp32 until they are summed, dgate comes
-// from unrounded fp32 values.
+// matrix cores' operand type), or to two bf16 addends (FfnPlan::planes), the entries' shares of dx stay in fp32
+// until they are summed, dgate comes from unrounded fp32 values.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -719,12 +719,14 @@ void dw_launch(const FfnPlan& p, const FfnArgs& a, char* ws, hipStream_t stream)
 }
 
 // Tile size of the weight gradients, by the same cost as the rows' tiles (call in us, 256 : 128, 32 experts of
-// h = 2048, s = 1024 with 1024 rows 1599 : 1803, a dense block of 16384 rows 1037 : 728, whose 96 large tiles leave
+// h = 2048, s = 1024 with 1024 rows 1402 : 1658, a dense block of 16384 rows 854 : 697, whose 96 large tiles leave
 // most CUs idle), and the runs into which an expert's entries are cut: as many as bring the tiles to 512, of
-// four stages at least, and at most 32 (runs : us of the call, a dense block of h = 512, s = 128, 16384 rows 1 : 341,
-// 8 : 95, 32 : 75, 64 : 88; 1024 rows 1 : 48, 4 : 39, 16 : 42; four experts of h = 2016, s = 8, 12000 rows 1 : 477,
-// 2 : 373, 4 : 322, 16 : 338; two of h = 1024, s = 512, 4096 rows 1 : 188, 2 : 166, 8 : 188; and where there are
-// 512 tiles and more, h = 2048, s = 1024, 16384 rows 1 : 728, 2 : 761).
+// four stages at least, and at most 32 (runs : us of the call, a dense block of h = 512, s = 128, 16384 rows 1 : 343,
+// 8 : 97, 32 : 76, 64 : 85; 1024 rows 1 : 49, 4 : 41, 16 : 43; four experts of h = 2016, s = 8, 12000 rows 1 : 509,
+// 2 : 407, 4 : 383, 16 : 400; two of h = 1024, s = 512, 4096 rows 1 : 191, 2 : 162, 8 : 186; and where there are
+// 512 tiles and more, h = 2048, s = 1024, 16384 rows 1 : 697, 2 : 715).  The means of all experts decide: an expert
+// that far more tokens select than others belongs to few workgroups (4096 experts of h = 512, s = 64, 16384
+// tokens, k = 8: 622 us with experts chosen evenly, 1699 where every token selects one of them).
 void dw_plan(int64_t n, int32_t h, int32_t s, int32_t M, FfnPlan* p) {
     const int64_t steps = std::max<int64_t>(1, n / M / kFfnBK);
     auto tiles = [&](int32_t a, int32_t b) { return (int64_t)((a + b - 1) / b); };
@@ -740,8 +742,8 @@ void dw_plan(int64_t n, int32_t h, int32_t s, int32_t M, FfnPlan* p) {
 }
 
 // Rows of a tile, as in the forward pass (over the same 196 shapes 0.6% off the best on geometric mean, at
-// most 18%; us for 64 : 128 : 256 rows, 32 experts of h = 2048, s = 1024, 96 rows 359 : 299 : 326, 384 rows 778 :
-// 712 : 607; 4096 experts of h = 512, s = 64, 32 rows 622 : 662 : 1051).
+// most 18%; us for 64 : 128 : 256 rows, 32 experts of h = 2048, s = 1024, 96 rows 357 : 294 : 338, 384 rows 775 :
+// 719 : 594; 4096 experts of h = 512, s = 64, 32 rows 622 : 663 : 1030).
 int32_t backward_rows(int64_t n, int32_t h, int32_t s, int32_t M, int32_t planes) {
     if (n / std::max<int64_t>(1, std::min<int64_t>(n, M)) < 24) return 32;
     const int32_t most = planes == 2 ? 128 : 256;  // (the kernels of 256 rows write one plane)
@@ -814,7 +816,7 @@ hipError_t ffn_backward_launch(const FfnPlan& p, FfnArgs a, void* workspace, hip
             reinterpret_cast<const float*>(ws + p.off_dgp), dgate_parts(p, a.s), a.sorted, a.dgate);
     }
     // Nontemporal stores keep what the next kernels read in the caches (h = 512, s = 64, 4096 experts of 32
-    // rows: 623 us for the call against 651; s = 72, 1024 experts of 16 rows: 180 with dW1t alone against 209).
+    // rows, experts chosen evenly: 623 us for the call against 651; s = 72, 1024 experts of 16 rows: 180 with dW1t alone against 209).
     // Not for dW2t where a row takes several tiles of 64 columns that split a line (s = 72: 188 with both).
     if (p.dw_tile == 256)
         dw_launch<256, 256, 256, 8, false, true>(p, a, ws, stream);

@@ -1,8 +1,8 @@
 // The experts' up kernel, shared by the forward and the backward pass (ffn.hip, ffn_backward.hip).
 //
 // What bounds it, and what it takes: with few rows per expert the weights' way from memory (4096 experts
-// of h = 512, s = 64 with 32 rows each: 118 us, 4.8 TB/s; 1800 experts of h = 4096 with one row: 280 us,
-// 6.8 TB/s); with many rows the stages of the matrix product (32 experts of h = 2048, s = 1024 with 1024 rows: 317
+// of h = 512, s = 64 with one row each: 79 us, 6.8 TB/s; with 32 rows 118 us, 4.8 TB/s of weights or 5.8 with the
+// gathered token rows; 1800 experts of h = 4096 with one row: 280 us, 6.8 TB/s); with many rows the stages of the matrix product (32 experts of h = 2048, s = 1024 with 1024 rows: 317
 // us, 867 TFLOP/s, backward 358 us): 1.14 us for 256 rows and 2 x 128 units with everything in LDS, 1.5 to 1.7 with
 // the loads, and by the card's power with both.  Hence tiles as large as the rows allow, and no tile larger
 // (256 x 256 of rows and hidden units would need 256 accumulators a lane for the two projections).
@@ -21,7 +21,7 @@ struct UpShape {
     static constexpr int kWaves = BM == 256 ? 8 : 4;
     static constexpr int kThreads = 64 * kWaves;
     // an expert has one tile, mostly, so its weights are read once (nontemporal: 1800 experts of h = 4096,
-    // s = 64 with one row 447 us for both kernels against 498)
+    // s = 64 with one row 465 us for both kernels against 520)
     static constexpr bool kOnce = BM == 32;
     static constexpr int kWavesS = BM >= 64 ? 2 : 4;      // waves along the hidden units
     static constexpr int kUnits = BM == 256 ? 128 : 64;

@@ -6,6 +6,8 @@
 // the gradients and a write; in place a factor of one writes nothing.  538 MB of gradients: 138 us for the
 // squares (3.9 TB/s) and 270 us for the scaling (4.0 TB/s; with an ordinary second read and ordinary stores,
 // and uneven shares, the call took 466 us); 1.6 MB: 4.4 and 5.4 us, each a launch and the latency of its reads.
+// Many tensors are bound by the launches, two for every kClipBatch: 1000 of 4096 elements 197 us, 10000 2.4 ms; every
+// scaling workgroup adds the partials of all batches, which shows from there on (30000 tensors 8.8 ms).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -14,6 +14,9 @@ on the tensors' device, and passes raw device pointers and that device's current
 libmore.so.  The classes hold outputs and workspace for repeated calls with one shape: a call only
 launches, can be captured in a HIP graph, and overwrites the outputs of the call before; calls of one
 object must be ordered on one stream.
+
+As the router's, these calls record nothing for torch's autograd, whatever requires_grad says: the
+*_backward functions are the gradients, for a program to call or to wrap in a torch.autograd.Function.
 """
 from __future__ import annotations
 

@@ -9,7 +9,7 @@ from test_gpu_ffn import check
 
 pytestmark = pytest.mark.gpu
 
-# every row layout (one wave or four, one to four chunks per lane) with full and ragged widths
+# every row layout (one, four or eight waves, one or two chunks per lane) with full and ragged widths
 WIDTHS = [16, 512, 528, 1024, 1040, 2048, 2064, 4096, 4112, 8192]
 
 

@@ -47,6 +47,7 @@ def check(name, got, want, bound, tag):
         tag, name, worst, got[worst], want[worst], bound[worst])
 
 
+# (Names of cases are of the rules that they were written for; test_gpu_ffn_forms.py states what its shapes take.)
 CASES = {
     "one_token": dict(T=1, h=512, s=64, M=64, k=8),
     "one_value": dict(T=1, h=16, s=8, M=1, k=1),
@@ -125,7 +126,7 @@ def test_backward(name):
         check(field, out.float().cpu().numpy(), v, b, name)
 
 
-# T k s <= 2^15, with and without tiles, on every tile size that such calls take
+# T k s <= 2^15 (forward without tiles, but for long_row_of_y; test_gpu_ffn_forms.py has them on tiles)
 FEW_VALUES = {name: CASES[name] for name in (
     "one_token", "one_value", "three_tokens", "token_of_wide_experts", "few_rows", "few_rows_dense", "all_experts",
     "more_slots_than_experts", "dense", "all_dropped", "long_rows", "long_rows_on_tiles", "repeated_ids", "hot_expert",
