@@ -345,7 +345,8 @@ more_status more_route_lowrank_noalloc(const uint16_t* x, const uint16_t* R1t, c
  * contractions A is rounded to bf16 once (the matrix cores' operand type; with y's own rounding an error of
  * 1.41 times the latter, on average), or to a sum of two bf16 (y's own rounding alone) where T k s <= 2^15 and
  * in the kernels without tiles, where it costs little; more_expert_ffn_plan tells which for a shape, and
- * more_expert_ffn_ex takes two addends at every size.  The sums run in a fixed order.
+ * more_expert_ffn_ex takes two addends at every size.  An A past bf16's largest value becomes an infinity
+ * either way.  The sums run in a fixed order.
  */
 more_status more_expert_ffn(const uint16_t* x, const uint16_t* W1t, const uint16_t* W2t, int64_t T,
                             int32_t h, int32_t s, int32_t M, int32_t k, const int32_t* idx,
