@@ -19,7 +19,10 @@
  * (more_dispatch_sort); and the layer around the router: the experts' gated feed-forward block with
  * its backward pass (more_expert_ffn, more_expert_ffn_backward), the norms after and before a block
  * fused with its gate and residual scale (more_block_norm, more_block_norm_backward) and the clipping
- * of all gradients by their common norm (more_grad_clip).
+ * of all gradients by their common norm (more_grad_clip); the experts' linear maps by themselves, in bf16
+ * with their backward pass (more_expert_linear, more_expert_linear_backward) and in 8-bit integers
+ * (more_quantize_rows, more_expert_linear_q8); and distillation from a teacher's top logits
+ * (more_distill, more_distill_backward).
  *
  * Conventions shared by every call
  * --------------------------------
@@ -487,6 +490,136 @@ more_status more_grad_clip(const void* const* in, void* const* out, const int64_
                            const int32_t* bits, int32_t n, float max_norm, float eps, float* norm,
                            void* workspace, size_t workspace_bytes, void* stream);
 more_status more_grad_clip_workspace_size(const int64_t* numel, int32_t n, size_t* bytes);
+
+/*
+ * A linear map per expert, applied to the entries of a selection (the efficiency appendix's expert linear
+ * (N, h) -> (N k, 2s) by itself, for experts of another form than more_expert_ffn's).  For every entry
+ * p = t k + j with expert e = idx[t][j]:
+ *   y_p = x_t W_e^T
+ * A map that follows takes the entries' rows as its tokens: T k rows, k = 1, idx as [T k][1], and the same
+ * offsets and sorted.  One dense map is M = 1, k = 1, idx = 0.
+ *   x        bf16 [T][K]
+ *   Wt       bf16 [M][N][K]    per expert W_e, one row per output column
+ *   idx, offsets, sorted       as in more_expert_ffn; entries with an id outside [0, M) are dropped: their y
+ *                              rows are zero
+ *   y        [T k][N] out      bf16 (y_bits == 16) or fp32 (y_bits == 32)
+ *   workspace / workspace_bytes   at least more_expert_linear_workspace_size() bytes (it may be 0), 256-byte
+ *                              aligned
+ * Limits: K and N positive multiples of 8, K <= 65536, N <= MORE_LINEAR_N_MAX; 1 <= k <= MORE_K_MAX;
+ * T k <= 2^31 - 2^16, M < 2^30.  T == 0 writes nothing.  offsets and sorted that are not those of idx give
+ * undefined values in y (no access outside the buffers).
+ * Numerics: fp32 accumulation of exact bf16 products in a fixed order, rounded once to y's type.
+ */
+#define MORE_LINEAR_N_MAX (1 << 20)
+more_status more_expert_linear(const uint16_t* x, const uint16_t* Wt, int64_t T, int32_t K, int32_t N,
+                               int32_t M, int32_t k, const int32_t* idx, const int32_t* offsets,
+                               const int32_t* sorted, void* y, int32_t y_bits, void* workspace,
+                               size_t workspace_bytes, void* stream);
+more_status more_expert_linear_workspace_size(int64_t T, int32_t K, int32_t N, int32_t M, int32_t k,
+                                              size_t* bytes);
+
+/*
+ * Backward pass of more_expert_linear:
+ *   dx_t = sum_j dy_p W_e        dW_e = sum over the entries p of e of dy_p^T x_t
+ *   x .. sorted  as in more_expert_linear
+ *   dy       bf16 [T k][N]     rows of dropped entries are not read
+ *   dx       bf16 [T][K] out   or NULL
+ *   dWt      bf16 [M][N][K] out, or NULL; zero for experts without entries (all zero when T == 0)
+ *                              (not both NULL)
+ *   workspace / workspace_bytes   at least more_expert_linear_backward_workspace_size() bytes, 256-byte
+ *                              aligned
+ * Limits as for more_expert_linear.  Numerics: fp32 accumulation of exact bf16 products, each result rounded
+ * once.  Nothing is added atomically: a call gives the same bits on every run.
+ */
+more_status more_expert_linear_backward(const uint16_t* x, const uint16_t* Wt, int64_t T, int32_t K,
+                                        int32_t N, int32_t M, int32_t k, const int32_t* idx,
+                                        const int32_t* offsets, const int32_t* sorted, const uint16_t* dy,
+                                        uint16_t* dx, uint16_t* dWt, void* workspace,
+                                        size_t workspace_bytes, void* stream);
+more_status more_expert_linear_backward_workspace_size(int64_t T, int32_t K, int32_t N, int32_t M, int32_t k,
+                                                       size_t* bytes);
+
+/*
+ * Rows in 8-bit integers with a scale each.  With a_t the largest magnitude of row t:
+ *   inv = 127 / a_t and scale_t = a_t / 127, each rounded to fp32;  q_ti = x_ti inv, rounded once to the nearest
+ *   integer (ties to even), so that x_ti is about q_ti scale_t
+ *   x        bf16 [T][width];  gated != 0: [T][2 width], a row is [g u] and stands for silu(g) u in fp32 (the
+ *                              activation between the two maps of a gated block)
+ *   q        int8 [T][width] out
+ *   scale    fp32 [T] out
+ * For tokens (a scale per row of x) and for weights (Wt as [M N][K]: a scale per output channel).  Rows whose
+ * a_t is below 2^-100 get zeros and scale 0; rows with an infinity or a NaN get zeros and scale NaN.
+ * Limits: width a positive multiple of 16 up to 65536, T <= 2^31 - 1.  No workspace.
+ */
+more_status more_quantize_rows(const uint16_t* x, int64_t T, int32_t width, int32_t gated, int8_t* q,
+                               float* scale, void* stream);
+
+/*
+ * more_expert_linear in 8-bit integers:
+ *   y_p = gate_p q_scale[t] w_scale[e][c] sum_i q[t][i] Wq[e][c][i]
+ *   q        int8 [T][K], q_scale fp32 [T]          of more_quantize_rows
+ *   Wq       int8 [M][N][K], w_scale fp32 [M][N]
+ *   gate     fp32 [T][k]       or NULL (all ones); gates of dropped entries are not read
+ *   idx, offsets, sorted, y, y_bits, workspace      as in more_expert_linear
+ * Limits as for more_expert_linear, K a multiple of 16.  Numerics: the integer sums are exact; they are
+ * converted to fp32, multiplied by the three factors in fp32, and rounded once to y's type.
+ */
+more_status more_expert_linear_q8(const int8_t* q, const float* q_scale, const int8_t* Wq,
+                                  const float* w_scale, int64_t T, int32_t K, int32_t N, int32_t M, int32_t k,
+                                  const int32_t* idx, const int32_t* offsets, const int32_t* sorted,
+                                  const float* gate, void* y, int32_t y_bits, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+more_status more_expert_linear_q8_workspace_size(int64_t T, int32_t K, int32_t N, int32_t M, int32_t k,
+                                                 size_t* bytes);
+
+/* The form in which a linear map runs a shape (written to *plan, host): kind 0 more_expert_linear, 1 its
+ * backward pass, 2 more_expert_linear_q8.  For tests of every form. */
+typedef struct more_linear_plan {
+    int32_t tile_rows; /* rows of a tile: 32, 64, 128 or 256; 0: the kernel without tiles               */
+    int32_t cols;      /* columns of a step (kind 1: of dx); without tiles: of a workgroup              */
+    int32_t span;      /* columns that a workgroup takes                                                */
+    int32_t stages;    /* of the LDS ring (0 without tiles)                                             */
+    int32_t dw_rows;   /* (kind 1, else 0) rows ...                                                     */
+    int32_t dw_cols;   /* ... and columns of a tile of dWt                                              */
+    int32_t dw_runs;   /* (kind 1, else 0) runs of an expert's entries that are summed apart            */
+    int32_t dw_span;   /* (kind 1, else 0) columns (dw_cols > 64) or rows of dWt that a workgroup takes */
+} more_linear_plan;
+more_status more_expert_linear_plan(int64_t T, int32_t K, int32_t N, int32_t M, int32_t k, int32_t kind,
+                                    more_linear_plan* plan);
+
+/*
+ * Distillation from a teacher's top logits, row by row: z a student's logits over V classes (the experts, a
+ * vocabulary), (id_j, v_j), j < k, the teacher's largest logits (idx and topval of more_route_fullrank), tau the
+ * temperature:
+ *   Q = softmax(v / tau) over the row's valid entries      P = softmax(z / tau) over all V
+ *   loss = tau^2 sum_j Q_j (ln Q_j - ln P_{id_j})          dz_e = weight tau (P_e - sum_{j: id_j = e} Q_j)
+ * An entry is valid where id_j lies in [0, V) and v_j is not -infinity; an id may occur more than once.  A row
+ * without valid entries has loss 0 and a zero gradient.
+ *   logits        [T] rows of V values, row t at logits + t ld: fp32 (bits == 32) or bf16 (bits == 16)
+ *   teacher_idx   int32 [T][k], teacher_val fp32 [T][k]
+ *   weight        fp32 [T], or NULL (all ones): the gradient of what is minimised with respect to each loss
+ *   loss          fp32 [T] out, or NULL
+ *   m, Z          fp32 [T] out, each or NULL: m_t = max_e z_e and Z_t = sum_e exp((z_e - m_t) / tau), which the
+ *                 backward pass takes
+ *   dlogits       [T] rows of V values of the logits' type, ld_dlogits apart, out, or NULL: the weighted
+ *                 gradient at once.  May be logits itself (with ld_dlogits == ld).  What lies between the rows
+ *                 is left as it was.
+ * Limits: 1 <= V <= 2^30, 1 <= k <= MORE_TEACHER_K_MAX, V <= ld, ld_dlogits <= 2^40, T <= 2^31 - 1, tau positive
+ * and finite.  Elements must be aligned to their size (rows that begin at a multiple of 16 bytes in both tensors
+ * are faster).  No workspace.
+ * Numerics: fp32; sums in a fixed order; the gradient is rounded once.  -infinity among the logits is a class of
+ * probability 0 (a row of nothing else has the loss NaN, as has one with a NaN or +infinity).
+ */
+#define MORE_TEACHER_K_MAX 1024
+more_status more_distill(const void* logits, int32_t bits, int64_t T, int32_t V, int64_t ld,
+                         const int32_t* teacher_idx, const float* teacher_val, int32_t k, float tau,
+                         const float* weight, float* loss, float* m, float* Z, void* dlogits,
+                         int64_t ld_dlogits, void* stream);
+/* The gradient alone, given m and Z of the forward pass of the same logits, and dloss fp32 [T] (weight above). */
+more_status more_distill_backward(const void* logits, int32_t bits, int64_t T, int32_t V, int64_t ld,
+                                  const float* m, const float* Z, const int32_t* teacher_idx,
+                                  const float* teacher_val, int32_t k, float tau, const float* dloss,
+                                  void* dlogits, int64_t ld_dlogits, void* stream);
 
 /* Static, never NULL. */
 const char* more_status_string(more_status s);

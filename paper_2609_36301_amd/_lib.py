@@ -16,6 +16,8 @@ LOWRANK_K_MAX = 32
 LOWRANK_TRAIN_K_MAX = 16
 ROUTE_WIDE = 4
 NORM_H_MAX = 8192
+LINEAR_N_MAX = 1 << 20
+TEACHER_K_MAX = 1024
 NOALLOC_SCRATCH_BYTES = 256 << 20
 
 # (name, restype, argtypes) for every symbol declared in include/more.h
@@ -29,6 +31,12 @@ class ExpertPlan(ctypes.Structure):
     """more_expert_plan."""
     _fields_ = [(name, ctypes.c_int32) for name in ("tile_rows", "addends", "span", "stages", "dw_tile", "dw_runs",
                                                     "dw1_span", "dw2_span")]
+
+
+class LinearPlan(ctypes.Structure):
+    """more_linear_plan."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("tile_rows", "cols", "span", "stages", "dw_rows", "dw_cols",
+                                                    "dw_runs", "dw_span")]
 
 
 SIGNATURES = {
@@ -79,6 +87,19 @@ SIGNATURES = {
     "more_block_norm_backward_workspace_size": (_I32, [_I64, _I32, _PSZ]),
     "more_grad_clip": (_I32, [_P, _P, _P, _P, _I32, _F32, _F32, _P, _P, _SZ, _P]),
     "more_grad_clip_workspace_size": (_I32, [_P, _I32, _PSZ]),
+    "more_expert_linear": (_I32, [_P, _P, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _I32, _P, _SZ, _P]),
+    "more_expert_linear_workspace_size": (_I32, [_I64, _I32, _I32, _I32, _I32, _PSZ]),
+    "more_expert_linear_backward": (_I32, [_P, _P, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _P, _P,
+                                           _P, _SZ, _P]),
+    "more_expert_linear_backward_workspace_size": (_I32, [_I64, _I32, _I32, _I32, _I32, _PSZ]),
+    "more_quantize_rows": (_I32, [_P, _I64, _I32, _I32, _P, _P, _P]),
+    "more_expert_linear_q8": (_I32, [_P, _P, _P, _P, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _P, _I32,
+                                     _P, _SZ, _P]),
+    "more_expert_linear_q8_workspace_size": (_I32, [_I64, _I32, _I32, _I32, _I32, _PSZ]),
+    "more_expert_linear_plan": (_I32, [_I64, _I32, _I32, _I32, _I32, _I32, ctypes.POINTER(LinearPlan)]),
+    "more_distill": (_I32, [_P, _I32, _I64, _I32, _I64, _P, _P, _I32, _F32, _P, _P, _P, _P, _P, _I64, _P]),
+    "more_distill_backward": (_I32, [_P, _I32, _I64, _I32, _I64, _P, _P, _P, _P, _I32, _F32, _P, _P, _I64,
+                                     _P]),
     "more_status_string": (ctypes.c_char_p, [_I32]),
     "more_version": (ctypes.c_char_p, []),
 }

@@ -59,6 +59,12 @@ void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t 
 hipError_t ffn_launch(const FfnPlan& p, FfnArgs a, uint16_t* y, void* workspace, hipStream_t stream);
 hipError_t ffn_backward_launch(const FfnPlan& p, FfnArgs a, void* workspace, hipStream_t stream);
 
+// out[t] = the sum of a token's k rows of `rows` (fp32 [T k][h]) in order, without those of dropped entries.
+hipError_t ffn_entry_sum_launch(const float* rows, const int32_t* idx, int32_t T, int32_t h, int32_t M, int32_t k,
+                                uint16_t* out, hipStream_t stream);
+// out[i] = the sum of `count` addends parts[q size + i] in order (size a multiple of 8).
+hipError_t ffn_parts_sum_launch(const float* parts, int32_t count, int64_t size, uint16_t* out, hipStream_t stream);
+
 // Columns that a workgroup takes, in steps of `step`, of a product whose contraction is `len` long: a
 // single step where the contraction alone fills the pipeline (eight stages), or where the groups of rows are
 // too few to fill the chip four times over with more; else up to 512.  us, forward and backward, single step :

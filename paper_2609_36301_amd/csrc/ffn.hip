@@ -264,41 +264,8 @@ __global__ __launch_bounds__(down_threads(BM), 2) void ffn_down_kernel(FfnArgs a
 // takes that and the next 15 entries, the others end at once.  One token, 8 experts of h = 2048, s = 64: 7.5 us
 // up and 4.1 us down, most of it the three dependent reads (sorted, idx, weights) and the launch.
 constexpr int kFewWaves = 8;
-constexpr int kFewRows = 16;
 constexpr int kFewUnits = 16;    // hidden units of an up workgroup
 constexpr int kFewCols = 32;     // columns of y per wave of a down workgroup
-
-// What the wave's lanes know of the sixteen sorted entries from i on: lane l has entry i + l % 16.
-struct FewRows {
-    uint32_t p;      // the lane's entry (t k + j)
-    int32_t expert;  // of entry i; -1: dropped
-    int32_t rows;    // of that expert (1 for a dropped entry); 0: entry i is not the first of its sixteen
-};
-// Two dependent reads (sorted, idx) for an expert that starts at i; offsets is read only where the entry
-// before i is of the same expert.
-__device__ __forceinline__ FewRows few_rows(const FfnArgs& a, int32_t n, int32_t i) {
-    const int32_t at = i + (ffn_lane() & 15);
-    FewRows f;
-    f.p = (uint32_t)a.sorted[min(at, n - 1)];
-    const uint32_t before = (uint32_t)a.sorted[max(i - 1, 0)];
-    const int32_t e = f.p < (uint32_t)n ? a.idx[f.p] : -1;
-    const int32_t eb = before < (uint32_t)n ? a.idx[before] : -1;
-    f.expert = __builtin_amdgcn_readfirstlane(e);
-    const uint32_t same = (uint32_t)__ballot(e == f.expert && at < n) & 0xFFFFu;
-    f.rows = __builtin_ctz(~same);
-    if ((uint32_t)f.expert >= (uint32_t)a.M) {
-        f.expert = -1;
-        f.rows = 1;
-    } else if (i > 0 && eb == f.expert && (i - a.offsets[f.expert]) % kFewRows != 0) {
-        f.rows = 0;
-    }
-    return f;
-}
-
-// 16 bytes at p, or zeros
-__device__ __forceinline__ bf16x8 few_load(const uint16_t* p, bool in) {
-    return load_bf16x8(in ? p : ffn_zeros);
-}
 
 // Waves take pieces of 64 contraction values in turn and their sums are added in wave order.  (These kernels
 // always carry A as two planes.)
@@ -310,7 +277,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void ffn_few_up_kernel(FfnArgs a, u
     const int wave = ffn_wave(), lane = ffn_lane();
     for (int64_t item = blockIdx.x; item < (int64_t)n * groups; item += gridDim.x) {
         const int32_t i = (int32_t)(item / groups), s0 = (int32_t)(item % groups) * kFewUnits;
-        const FewRows f = few_rows(a, n, i);
+        const FewRows f = few_rows(a.sorted, a.idx, a.offsets, a.M, n, i);
         const int32_t e = f.expert, rows = f.rows;
         if (rows == 0 || e < 0) continue;
         const int32_t at = 8 * (lane >> 4);
@@ -378,7 +345,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void ffn_few_down_kernel(FfnArgs a,
         const int32_t i = (int32_t)(item / spans);
         const int32_t c0 = (int32_t)(item % spans) * kSpan + (SPLIT ? 0 : wave * kFewCols);
         if (c0 >= h) continue;  // (SPLIT: never)
-        const FewRows f = few_rows(a, n, i);
+        const FewRows f = few_rows(a.sorted, a.idx, a.offsets, a.M, n, i);
         const int32_t e = f.expert, rows = f.rows;
         if (rows == 0) continue;
         const uint32_t p = f.p;

@@ -440,6 +440,41 @@ struct FfnGroups {
 
 __device__ __forceinline__ f32x4 zero_f32x4() { return f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
 
+constexpr int kFewRows = 16;  // entries that the kernels without tiles take at a time
+
+// What the wave's lanes know of the sixteen sorted entries from i on: lane l has entry i + l % 16.
+struct FewRows {
+    uint32_t p;      // the lane's entry (t k + j)
+    int32_t expert;  // of entry i; -1: dropped
+    int32_t rows;    // of that expert (1 for a dropped entry); 0: entry i is not the first of its sixteen
+};
+// Two dependent reads (sorted, idx) for an expert that starts at i; offsets is read only where the entry
+// before i is of the same expert.
+__device__ __forceinline__ FewRows few_rows(const int32_t* __restrict__ sorted, const int32_t* __restrict__ idx,
+                                            const int32_t* __restrict__ offsets, int32_t M, int32_t n, int32_t i) {
+    const int32_t at = i + (ffn_lane() & 15);
+    FewRows f;
+    f.p = (uint32_t)sorted[min(at, n - 1)];
+    const uint32_t before = (uint32_t)sorted[max(i - 1, 0)];
+    const int32_t e = f.p < (uint32_t)n ? idx[f.p] : -1;
+    const int32_t eb = before < (uint32_t)n ? idx[before] : -1;
+    f.expert = __builtin_amdgcn_readfirstlane(e);
+    const uint32_t same = (uint32_t)__ballot(e == f.expert && at < n) & 0xFFFFu;
+    f.rows = __builtin_ctz(~same);
+    if ((uint32_t)f.expert >= (uint32_t)M) {
+        f.expert = -1;
+        f.rows = 1;
+    } else if (i > 0 && eb == f.expert && (i - offsets[f.expert]) % kFewRows != 0) {
+        f.rows = 0;
+    }
+    return f;
+}
+
+// 16 bytes at p, or zeros
+__device__ __forceinline__ bf16x8 few_load(const uint16_t* p, bool in) {
+    return load_bf16x8(in ? p : ffn_zeros);
+}
+
 // 1 / (1 + e^-v): v_exp_f32 and v_rcp_f32 (1 ulp each); e^-v = inf gives 0.
 __device__ __forceinline__ float ffn_sigmoid(float v) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * v));

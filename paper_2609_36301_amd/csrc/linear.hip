@@ -1,0 +1,382 @@
+// The experts' linear maps for gfx950: for every entry p = t k + j of a selection with expert e = idx[t][j],
+//   y_p = x_t W_e^T      [N]
+// in bf16, or in int8 with a scale per row of x and per row of W:
+//   y_p = gate_p xs_t ws_e[c] (sum_i q_t[i] Wq_e[c][i])
+// The entries are taken in the order of Sort + Count and cut into tiles of rows of one expert (ffn_tiles);
+// linear_kernel multiplies a tile, linear_few_kernel does without tiles where there are few entries.  y goes to the
+// entry's row, so nothing is scattered afterwards; dropped entries get rows of zeros.
+// Numerics: bf16, exact products and fp32 sums; int8, exact 32-bit integer sums (at most 2^16 values of at most 2^14),
+// then three fp32 factors.  One rounding to y's type.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "ffn_device.h"
+#include "linear.h"
+
+namespace more {
+
+// The two types share everything but the matrix instruction: a 16-byte fragment holds eight bf16 or sixteen
+// int8 values of a row, and both operands take the same ones.
+template <bool I8>
+struct LinearType {
+    using Acc = f32x4;
+    static __device__ __forceinline__ Acc zero() { return zero_f32x4(); }
+    static __device__ __forceinline__ Acc multiply(bf16x8 a, bf16x8 b, Acc c) { return mfma_16x16x32(a, b, c); }
+};
+template <>
+struct LinearType<true> {
+    using Acc = i32x4;
+    static __device__ __forceinline__ Acc zero() { return i32x4{0, 0, 0, 0}; }
+    static __device__ __forceinline__ Acc multiply(bf16x8 a, bf16x8 b, Acc c) {
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+    }
+};
+
+// The factor of entry p's row, and four columns of an accumulator as they are stored.
+template <bool I8>
+__device__ __forceinline__ float linear_row_scale(const LinearArgs& a, uint32_t p, int32_t n) {
+    if constexpr (!I8) return 1.0f;
+    if (p >= (uint32_t)n) return 0.0f;
+    const float s = a.x_scale[p / (uint32_t)a.k];
+    return a.gate ? s * a.gate[p] : s;
+}
+template <bool I8>
+__device__ __forceinline__ void linear_store(const LinearArgs& a, typename LinearType<I8>::Acc acc, float row_scale,
+                                             const float* w_scale, uint32_t p, int32_t c) {
+    f32x4 v;
+    if constexpr (I8) {
+        const f32x4 ws = *reinterpret_cast<const f32x4*>(w_scale + c);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = (float)acc[q] * ws[q] * row_scale;
+    } else {
+        v = acc;
+    }
+    const int64_t at = (int64_t)p * a.N + c;
+    if (a.wide)
+        *reinterpret_cast<f32x4*>(static_cast<float*>(a.y) + at) = v;
+    else
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + at) = pack_bf16x4(v[0], v[1], v[2], v[3]);
+}
+// Zeros to columns c .. c + 7 of entry p's row.
+__device__ __forceinline__ void linear_zero(const LinearArgs& a, uint32_t p, int32_t c) {
+    const int64_t at = (int64_t)p * a.N + c;
+    const u32x4 z = {0u, 0u, 0u, 0u};
+    if (a.wide) {
+        u32x4* y = reinterpret_cast<u32x4*>(static_cast<float*>(a.y) + at);
+        y[0] = z;
+        y[1] = z;
+    } else {
+        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.y) + at) = z;
+    }
+}
+
+// ------------------------------------------------------------------------------ tiles
+// A workgroup computes a tile's rows of y, `span` columns in steps of COLS: the rows of W are the M side, the
+// entries' rows of x the N side.  The pipeline runs over (column step, contraction step) pairs, so that a
+// short contraction does not drain it.
+template <int BM, int COLS, int STAGES>
+struct LinearShape {
+    static constexpr int kWaves = BM == 256 ? 8 : 4;
+    static constexpr int kThreads = 64 * kWaves;
+    static constexpr bool kOnce = BM == 32;  // an expert has one tile, mostly: nontemporal weights
+    static constexpr int kWavesM = BM >= 64 ? 2 : 4;
+    static constexpr int kM = COLS / kWavesM / 16;
+    static constexpr int kN = BM / (kWaves / kWavesM) / 16;
+    static constexpr int kRowsAt = COLS * 128;
+    static constexpr int kStageBytes = kRowsAt + BM * 128;
+    static constexpr int kLoads = (COLS + BM) / kWaves / 8;
+};
+
+constexpr int linear_threads(int bm) { return bm == 256 ? 512 : 256; }
+template <bool I8, int BM, int COLS, int STAGES>
+__global__ __launch_bounds__(linear_threads(BM), 2) void linear_kernel(LinearArgs a, const void* __restrict__ list,
+                                                                    int32_t span) {
+    using S = LinearShape<BM, COLS, STAGES>;
+    using Type = LinearType<I8>;
+    static_assert(S::kThreads == linear_threads(BM), "");
+    __shared__ __attribute__((aligned(1024))) char smem_raw[STAGES * S::kStageBytes];
+    LdsChar* smem = (LdsChar*)smem_raw;
+    const FfnTile* tiles = ffn_tile_list(list);
+    const int32_t len = a.len, N = a.N;
+    const int32_t n = a.T * a.k;
+    const int32_t spans = (N + span - 1) / span;
+    const int wave = ffn_wave(), lane = ffn_lane();
+    const int wm = wave % S::kWavesM, wn = wave / S::kWavesM;
+    const int64_t total = (int64_t)*static_cast<const int32_t*>(list) * spans;
+    ffn_for_each(total, [&](int64_t item) {
+        const FfnTile tile = tiles[item / spans];
+        const int32_t c0 = (int32_t)(item % spans) * span, c1 = min(N, c0 + span);
+        if (tile.expert < 0) {  // dropped entries: zero rows
+            const int32_t pieces = (c1 - c0) / 8;
+            for (int32_t i = threadIdx.x; i < tile.rows * pieces; i += S::kThreads) {
+                const uint32_t p = a.sorted[tile.row0 + i / pieces];
+                if (p < (uint32_t)n) linear_zero(a, p, c0 + 8 * (i % pieces));
+            }
+            return;
+        }
+        const uint16_t* W = a.W + (int64_t)tile.expert * N * len;
+        const float* w_scale = I8 ? a.w_scale + (int64_t)tile.expert * N : nullptr;
+        RowTileLoader<COLS, S::kWaves, S::kOnce> weights;
+        RowTileLoader<BM, S::kWaves> rows;
+        rows.init([&](int i) {
+            const uint32_t p = a.sorted[tile.row0 + min(i, tile.rows - 1)];
+            return a.x + (int64_t)(p < (uint32_t)n ? p / (uint32_t)a.k : 0) * len;
+        });
+        uint32_t place[S::kN];
+        float row_scale[S::kN];
+#pragma unroll
+        for (int j = 0; j < S::kN; ++j) {
+            const int32_t row = 16 * (wn * S::kN + j) + (lane & 15);
+            place[j] = row < tile.rows ? (uint32_t)a.sorted[tile.row0 + row] : 0xFFFFFFFFu;
+            row_scale[j] = linear_row_scale<I8>(a, place[j], n);
+        }
+        typename Type::Acc acc[S::kM][S::kN];
+#pragma unroll
+        for (int i = 0; i < S::kM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::kN; ++j) acc[i][j] = Type::zero();
+        const int32_t ksteps = (len + kFfnBK - 1) / kFfnBK;
+        const int32_t csteps = (c1 - c0 + COLS - 1) / COLS;
+        // (column step, contraction step) of the next load and of the next product
+        int32_t lc = c0, lk = 0, cc = c0, ck = 0;
+        using G = FfnGroups<S::kM, S::kM == 8 ? 4 : 2>;
+        using M = FfnFragments<G::kSize>;
+        using F = FfnFragments<S::kN>;
+        ffn_pipeline<STAGES, S::kLoads, G::kGroups, BM == 256, M, F>(
+            ksteps * csteps, 16 * wn * S::kN < tile.rows,
+            [&](int, int slot) {
+                if (lk == 0) weights.init([&](int i) { return W + (int64_t)min(lc + i, N - 1) * len; });
+                weights.load(smem + slot * S::kStageBytes, lk * kFfnBK, len);
+            },
+            [&](int, int slot) {
+                rows.load(smem + slot * S::kStageBytes + S::kRowsAt, lk * kFfnBK, len);
+                if (++lk == ksteps) {
+                    lk = 0;
+                    lc += COLS;
+                }
+            },
+            ffn_work(
+                [&](int slot, int kk, int group, M& m) {
+#pragma unroll
+                    for (int i = 0; i < G::kSize; ++i)
+                        if (G::tile(group, i) < S::kM)
+                            m.v[i] = row_fragment(smem + slot * S::kStageBytes, 16 * (wm * S::kM + G::tile(group, i)), kk);
+                },
+                [&](int slot, int kk, F& f) {
+#pragma unroll
+                    for (int j = 0; j < S::kN; ++j)
+                        f.v[j] = row_fragment(smem + slot * S::kStageBytes + S::kRowsAt, 16 * (wn * S::kN + j), kk);
+                },
+                [&](int group, const M& m, const F& f) {
+#pragma unroll
+                    for (int i = 0; i < G::kSize; ++i)
+                        if (G::tile(group, i) < S::kM)
+#pragma unroll
+                            for (int j = 0; j < S::kN; ++j) {
+                                auto& c = acc[G::tile(group, i)][j];
+                                c = Type::multiply(m.v[i], f.v[j], c);
+                            }
+                },
+                [&] {
+                    if (++ck < ksteps) return;
+#pragma unroll
+                    for (int j = 0; j < S::kN; ++j) {
+#pragma unroll
+                        for (int i = 0; i < S::kM; ++i) {
+                            const int32_t c = cc + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
+                            if (place[j] < (uint32_t)n && c < c1)
+                                linear_store<I8>(a, acc[i][j], row_scale[j], w_scale, place[j], c);
+                            acc[i][j] = Type::zero();
+                        }
+                    }
+                    ck = 0;
+                    cc += COLS;
+                }));
+    });
+}
+
+// ------------------------------------------------------------------------------ few entries
+// Where there are few entries, the weights' way from memory is all that counts: they go straight into the
+// registers of the matrix instruction (16 weight rows against 16 entries), with no LDS, no tile list and no
+// barrier on the way.  Workgroups are laid over the sorted entries; the one whose entry is the first, 17th, ...
+// of its expert takes that and the next 15 entries, the others end at once.
+// SPLIT: the waves share 16 columns, take pieces of 64 words of the contraction in turn, and their sums are
+// added in wave order; else each wave has 32 columns of its own.
+constexpr int kFewWaves = 8;
+template <bool SPLIT>
+constexpr int few_span() {
+    return SPLIT ? 16 : 32 * kFewWaves;
+}
+
+template <bool I8, bool SPLIT>
+__global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a) {
+    using Type = LinearType<I8>;
+    using Acc = typename Type::Acc;
+    constexpr int kR = SPLIT ? 1 : 2;      // groups of 16 columns per wave
+    constexpr int kAhead = SPLIT ? 4 : 2;  // pieces of 64 words in flight per wave
+    constexpr int kStep = SPLIT ? 64 * kFewWaves : 64;
+    constexpr int kSpan = few_span<SPLIT>();
+    __shared__ Acc part[SPLIT ? kFewWaves : 1][64];
+    const int32_t len = a.len, N = a.N, n = a.T * a.k;
+    const int32_t spans = (N + kSpan - 1) / kSpan;
+    const int wave = ffn_wave(), lane = ffn_lane();
+    for (int64_t item = blockIdx.x; item < (int64_t)n * spans; item += gridDim.x) {
+        const int32_t i = (int32_t)(item / spans);
+        const int32_t c0 = (int32_t)(item % spans) * kSpan + (SPLIT ? 0 : 32 * wave);
+        if (c0 >= N) continue;  // (SPLIT: never)
+        const FewRows f = few_rows(a.sorted, a.idx, a.offsets, a.M, n, i);
+        if (f.rows == 0) continue;
+        const bool mine = (lane & 15) < f.rows && f.p < (uint32_t)n;
+        if (f.expert < 0) {  // a dropped entry
+            const int32_t c = c0 + 8 * (lane >> 4);
+            if (mine && (!SPLIT || (wave == 0 && lane < 32)) && c < N) linear_zero(a, f.p, c);
+            continue;
+        }
+        const int32_t at = 8 * (lane >> 4);
+        const uint16_t* w[kR];
+#pragma unroll
+        for (int r = 0; r < kR; ++r)
+            w[r] = a.W + ((int64_t)f.expert * N + min(c0 + 16 * r + (lane & 15), N - 1)) * len + at;
+        // (the columns of lanes past the rows are not stored)
+        const uint16_t* x = a.x + (int64_t)(f.p < (uint32_t)n ? f.p / (uint32_t)a.k : 0) * len + at;
+        Acc acc[kR];
+#pragma unroll
+        for (int r = 0; r < kR; ++r) acc[r] = Type::zero();
+        for (int32_t k0 = SPLIT ? 64 * wave : 0; k0 < len; k0 += kStep * kAhead) {
+            bf16x8 fw[kR][kAhead][2], fx[kAhead][2];
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int32_t k = k0 + kStep * q + 32 * c;
+                    const bool in = k + at < len;
+                    fx[q][c] = few_load(x + k, in);
+#pragma unroll
+                    for (int r = 0; r < kR; ++r) fw[r][q][c] = few_load(w[r] + k, in);
+                }
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int r = 0; r < kR; ++r) acc[r] = Type::multiply(fw[r][q][c], fx[q][c], acc[r]);
+        }
+        if constexpr (SPLIT) {
+            __syncthreads();  // the item before has been read
+            part[wave][lane] = acc[0];
+            __syncthreads();
+            if (wave > 0) continue;
+#pragma unroll
+            for (int v = 1; v < kFewWaves; ++v) acc[0] += part[v][lane];
+        }
+        if (!mine) continue;
+        const float row_scale = linear_row_scale<I8>(a, f.p, n);
+        const float* w_scale = I8 ? a.w_scale + (int64_t)f.expert * N : nullptr;
+#pragma unroll
+        for (int r = 0; r < kR; ++r) {
+            const int32_t c = c0 + 16 * r + 4 * (lane >> 4);
+            if (c < N) linear_store<I8>(a, acc[r], row_scale, w_scale, f.p, c);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------ host
+namespace {
+
+constexpr int64_t kMaxBlocks = 1 << 19;
+unsigned grid_of(int64_t items) { return (unsigned)(std::min<int64_t>((items + 7) / 8, kMaxBlocks / 8) * 8); }
+unsigned few_grid(int64_t items) { return (unsigned)std::min<int64_t>(items, 1 << 22); }
+
+template <bool I8, int BM, int COLS, int STAGES>
+void tiled(const LinearPlan& p, const LinearArgs& a, const char* ws, hipStream_t stream) {
+    linear_kernel<I8, BM, COLS, STAGES>
+        <<<grid_of(p.tiles.tiles * ((a.N + p.span - 1) / p.span)), linear_threads(BM), 0, stream>>>(
+            a, ws + p.tiles.off_tiles, p.span);
+}
+
+template <bool I8>
+void forward(const LinearPlan& p, const LinearArgs& a, const char* ws, hipStream_t stream) {
+    if (p.few) {
+        const unsigned blocks = few_grid(p.tiles.n * ((a.N + p.span - 1) / p.span));
+        if (p.split)
+            linear_few_kernel<I8, true><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
+        else
+            linear_few_kernel<I8, false><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
+        return;
+    }
+    switch (p.tiles.bm) {
+        case 256: return tiled<I8, 256, 256, 2>(p, a, ws, stream);
+        case 128: return p.cols == 64 ? tiled<I8, 128, 64, 2>(p, a, ws, stream) : tiled<I8, 128, 128, 2>(p, a, ws, stream);
+        case 64: return p.cols == 64 ? tiled<I8, 64, 64, 3>(p, a, ws, stream) : tiled<I8, 64, 128, 3>(p, a, ws, stream);
+        default:
+            if (p.cols == 64) return tiled<I8, 32, 64, 3>(p, a, ws, stream);
+            return p.stages == 2 ? tiled<I8, 32, 128, 2>(p, a, ws, stream) : tiled<I8, 32, 128, 3>(p, a, ws, stream);
+    }
+}
+
+}  // namespace
+
+int32_t linear_tile_rows(int64_t n, int32_t M, int32_t cols, int32_t cols_of, int64_t steps) {
+    if (n / std::max<int64_t>(1, std::min<int64_t>(n, M)) < 24) return 32;
+    int32_t best = 64;
+    int64_t least = INT64_MAX;
+    for (int32_t bm = 64; bm <= 256; bm *= 2) {
+        const int64_t tiles2 = ffn_expected_tiles2(n, M, bm);
+        const int32_t step = bm == 256 ? 256 : cols_of;
+        const int64_t cost = ffn_cost(tiles2 * ((cols + step - 1) / step) / 2, steps, bm);
+        if (cost < least) {
+            least = cost;
+            best = bm;
+        }
+    }
+    return best;
+}
+
+// Upper bound on the workgroups along the entries that have work in the kernel without tiles.
+static int64_t few_starts(int64_t n, int32_t M) { return std::min<int64_t>(n, std::min<int64_t>(n, M) + n / kFewRows); }
+
+void linear_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, bool q8, LinearPlan* p) {
+    (void)q8;
+    const int64_t n = T * k;
+    *p = LinearPlan{};
+    p->cols = N <= 64 ? 64 : 128;
+    const int32_t bm = linear_tile_rows(n, M, N, p->cols, (len + kFfnBK - 1) / kFfnBK);
+    ffn_tiles_plan(n, M, bm, &p->tiles);
+    // The kernel without tiles saves a launch and the latency of the stages, while the weights that it reads (once
+    // for every 16 entries) are few bytes and few workgroups end at once.
+    p->few = few_starts(n, M) * 2 * N * len <= ((int64_t)8 << 20) + (int64_t)40960 * 2 * len &&
+             n * ((N + few_span<false>() - 1) / few_span<false>()) <= 4096;
+    if (p->few) {
+        p->split = len > 64;
+        p->span = p->split ? few_span<true>() : few_span<false>();
+        return;
+    }
+    if (bm == 256) p->cols = 256;
+    p->span = ffn_span(len, p->cols, p->tiles.tiles, N);
+    p->stages = bm >= 128 ? 2 : bm == 64 || p->cols == 64 ? 3 : p->tiles.tiles * ((N + p->span - 1) / p->span) >= 2048 ? 2 : 3;
+    p->workspace_bytes = p->tiles.workspace_bytes;
+}
+
+hipError_t linear_tiles_launch(const LinearPlan& p, const LinearArgs& a, void* workspace, hipStream_t stream) {
+    FfnArgs f = {};
+    f.offsets = a.offsets;
+    f.M = a.M;
+    return ffn_tiles_launch(p.tiles, f, workspace, stream);
+}
+
+hipError_t linear_launch(const LinearPlan& p, const LinearArgs& a, void* workspace, hipStream_t stream) {
+    if (!p.few) {
+        const hipError_t e = linear_tiles_launch(p, a, workspace, stream);
+        if (e != hipSuccess) return e;
+    }
+    const char* ws = static_cast<const char*>(workspace);
+    if (a.q8)
+        forward<true>(p, a, ws, stream);
+    else
+        forward<false>(p, a, ws, stream);
+    return hipGetLastError();
+}
+
+}  // namespace more

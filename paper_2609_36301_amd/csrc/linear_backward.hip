@@ -1,0 +1,463 @@
+// Backward pass of the experts' linear maps (linear.hip) for gfx950: for every entry p = t k + j of expert
+// e = idx[t][j],
+//   dx_t = sum_j dy_p W_e       dW_e = sum_{p of e} dy_p^T x_t
+//
+// Kernels of one call (entries in the order of Sort + Count, cut into tiles of one expert; either gradient may be
+// left out):
+//   ffn_tiles         lists the tiles
+//   linear_dx         dy_p W_e of one tile: with one entry per token dx itself (bf16), else the entries' shares
+//                     (fp32, entry order), which ffn_entry_sum adds in the entries' order
+//   linear_dw         dW: contractions over the rows of an expert; an expert without rows gets zeros.  Long
+//                     rows of few experts are cut into runs whose fp32 sums ffn_parts_sum adds
+// Every sum runs in a fixed order: nothing is added atomically, and a call gives the same bits on every run.
+// Numerics: exact products of bf16 and fp32 sums, one rounding to bf16.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "ffn_device.h"
+#include "linear.h"
+
+namespace more {
+
+// ------------------------------------------------------------------------------ dx
+// The weights lie with the contraction axis (N) slowest: they are a column tile (M side), the entries' rows of dy
+// a row tile (N side).  A workgroup computes `span` columns in steps of COLS; the pipeline runs over (column
+// step, contraction step) pairs.
+constexpr int dx_threads(int bm) { return bm == 256 ? 512 : 256; }
+template <int BM, int COLS>
+struct DxShape {
+    static constexpr int kThreads = dx_threads(BM);
+    static constexpr int kWaves = kThreads / 64;
+    static constexpr int kWavesM = BM >= 64 ? 2 : 4;
+    static constexpr int kM = COLS / kWavesM / 16;
+    static constexpr int kN = BM / (kWaves / kWavesM) / 16;
+    static constexpr int kRowsAt = COLS * 128;
+    static constexpr int kStageBytes = kRowsAt + BM * 128;
+};
+
+// DIRECT: one entry per token, `out` is dx (bf16); else the shares (fp32).
+template <int BM, int COLS, bool DIRECT>
+__global__ __launch_bounds__(dx_threads(BM), 2) void linear_dx_kernel(LinearArgs a, const void* __restrict__ list,
+                                                                  int32_t span, void* __restrict__ out) {
+    using S = DxShape<BM, COLS>;
+    __shared__ __attribute__((aligned(1024))) char smem_raw[2 * S::kStageBytes];
+    LdsChar* smem = (LdsChar*)smem_raw;
+    const FfnTile* tiles = ffn_tile_list(list);
+    const int32_t n = a.T * a.k, len = a.N, cols = a.len;
+    const int32_t spans = (cols + span - 1) / span;
+    const int wave = ffn_wave(), lane = ffn_lane();
+    const int wm = wave % S::kWavesM, wn = wave / S::kWavesM;
+    const int64_t total = (int64_t)*static_cast<const int32_t*>(list) * spans;
+    ffn_for_each(total, [&](int64_t item) {
+        const FfnTile tile = tiles[item / spans];
+        const int32_t c0 = (int32_t)(item % spans) * span, c1 = min(cols, c0 + span);
+        if (tile.expert < 0) {  // dropped entries: zero rows of dx; the sum leaves their shares out
+            if constexpr (DIRECT) {
+                const int32_t pieces = (c1 - c0) / 8;
+                for (int32_t i = threadIdx.x; i < tile.rows * pieces; i += S::kThreads) {
+                    const uint32_t p = a.sorted[tile.row0 + i / pieces];
+                    if (p < (uint32_t)n)
+                        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + (int64_t)p * cols + c0 + 8 * (i % pieces)) =
+                            u32x4{0u, 0u, 0u, 0u};
+                }
+            }
+            return;
+        }
+        const uint16_t* We = a.W + (int64_t)tile.expert * len * cols;
+        RowTileLoader<BM, S::kWaves> rows;
+        rows.init([&](int i) {
+            const uint32_t p = a.sorted[tile.row0 + min(i, tile.rows - 1)];
+            return a.dy + (int64_t)(p < (uint32_t)n ? p : 0) * len;
+        });
+        ColTileLoader<COLS, S::kWaves> weights;
+        weights.init();
+        uint32_t place[S::kN];
+#pragma unroll
+        for (int j = 0; j < S::kN; ++j) {
+            const int32_t row = 16 * (wn * S::kN + j) + (lane & 15);
+            place[j] = row < tile.rows ? (uint32_t)a.sorted[tile.row0 + row] : 0xFFFFFFFFu;
+        }
+        f32x4 acc[S::kM][S::kN];
+#pragma unroll
+        for (int i = 0; i < S::kM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::kN; ++j) acc[i][j] = zero_f32x4();
+        const int32_t ksteps = (len + kFfnBK - 1) / kFfnBK;
+        const int32_t csteps = (c1 - c0 + COLS - 1) / COLS;
+        // (column step, contraction step) of the next load and of the next product
+        int32_t lc = c0, lk = 0, cc = c0, ck = 0;
+        using G = FfnGroups<S::kM, S::kM == 8 ? 4 : 2>;
+        using M = FfnFragments<G::kSize>;
+        using F = FfnFragments<S::kN>;
+        auto weight_row = [&](int i) -> const uint16_t* {
+            const int kappa = lk * kFfnBK + weights.row(i);
+            return kappa < len ? We + (int64_t)kappa * cols + lc : nullptr;
+        };
+        auto advance = [&] {
+            if (++lk < ksteps) return;
+            lk = 0;
+            lc += COLS;
+        };
+        auto read_n = [&](int slot, int kk, F& f) {
+#pragma unroll
+            for (int j = 0; j < S::kN; ++j)
+                f.v[j] = row_fragment(smem + slot * S::kStageBytes + S::kRowsAt, 16 * (wn * S::kN + j), kk);
+        };
+        auto multiply = [&](int group, const M& m, const F& f) {
+#pragma unroll
+            for (int i = 0; i < G::kSize; ++i)
+                if (G::tile(group, i) < S::kM)
+#pragma unroll
+                    for (int j = 0; j < S::kN; ++j) {
+                        f32x4& c = acc[G::tile(group, i)][j];
+                        c = mfma_16x16x32(m.v[i], f.v[j], c);
+                    }
+        };
+        auto done = [&] {
+            if (++ck < ksteps) return;
+#pragma unroll
+            for (int j = 0; j < S::kN; ++j) {
+#pragma unroll
+                for (int i = 0; i < S::kM; ++i) {
+                    const int32_t c = cc + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
+                    const f32x4 v = acc[i][j];
+                    if (place[j] < (uint32_t)n && c < c1) {
+                        const int64_t at = (int64_t)place[j] * cols + c;
+                        if constexpr (DIRECT)
+                            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = pack_bf16x4(v[0], v[1], v[2], v[3]);
+                        else
+                            *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = v;
+                    }
+                    acc[i][j] = zero_f32x4();
+                }
+            }
+            ck = 0;
+            cc += COLS;
+        };
+        if constexpr (BM == 256) {
+            constexpr int kLoads = weights.kLoads + rows.kLoads;
+            ffn_pipeline<2, kLoads, G::kGroups, true, M, F>(
+                ksteps * csteps, 16 * wn * S::kN < tile.rows,
+                [&](int, int slot) { weights.load(smem + slot * S::kStageBytes, cols - lc, weight_row); },
+                [&](int, int slot) {
+                    rows.load(smem + slot * S::kStageBytes + S::kRowsAt, lk * kFfnBK, len);
+                    advance();
+                },
+                ffn_work(
+                    [&](int slot, int kk, int group, M& m) {
+                        col_fragments2(smem + slot * S::kStageBytes, 16 * (wm * S::kM + G::tile(group, 0)), kk, m.v[0],
+                                       m.v[1]);
+                    },
+                    read_n, multiply, done));
+        } else {
+            using Stage = StagePair<decltype(weights), decltype(rows)>;
+            ffn_pipeline_staged<Stage, G::kGroups, M, F>(
+                ksteps * csteps, 16 * wn * S::kN < tile.rows,
+                [&](int, Stage& st) {
+                    weights.fetch(st.a, cols - lc, weight_row);
+                    rows.fetch(st.b, lk * kFfnBK, len);
+                    advance();
+                },
+                [&](int slot, const Stage& st) {
+                    weights.put(smem + slot * S::kStageBytes, st.a);
+                    rows.put(smem + slot * S::kStageBytes + S::kRowsAt, st.b);
+                },
+                ffn_work(
+                    [&](int slot, int kk, int group, M& m) {
+#pragma unroll
+                        for (int i = 0; i < G::kSize; ++i)
+                            if (G::tile(group, i) < S::kM)
+                                m.v[i] = col_fragment(smem + slot * S::kStageBytes,
+                                                      16 * (wm * S::kM + G::tile(group, i)), kk);
+                    },
+                    read_n, multiply, done));
+        }
+    });
+}
+
+// ------------------------------------------------------------------------------ dW
+// dW_e [N][K] = sum over the entries p of e of dy_p^T x_t: both operands are column tiles (the contraction runs over
+// rows), dy the N side and x the M side, and both are gathered.  A workgroup computes tiles of RT rows (of N) and CT
+// columns (of K) one after the other over `span` of one side (BY_COLS: of K), and the pipeline runs over (tile, 64
+// entries) pairs, so that the few rows of a small expert do not drain it.
+// PARTS: the entries of an expert are cut into `runs` runs and a workgroup takes one tile and one run; the fp32
+// results of run i go to parts + i M N K.
+struct LinearDw {
+    int32_t span, runs, once;  // once: nontemporal stores (whole lines)
+    float* parts;
+};
+
+template <int CT, int RT, int WAVES, bool BY_COLS, bool PARTS>
+__global__ __launch_bounds__(64 * WAVES, 2) void linear_dw_kernel(LinearArgs a, LinearDw d) {
+    constexpr int kStageBytes = (CT + RT) * 128;
+    __shared__ __attribute__((aligned(1024))) char smem_raw[2 * kStageBytes];
+    __shared__ __attribute__((aligned(16))) char scratch_raw[WAVES * kFfnScratch];
+    LdsChar* smem = (LdsChar*)smem_raw;
+    LdsChar* scratch = (LdsChar*)scratch_raw + ffn_wave() * kFfnScratch;
+    constexpr int kWavesM = CT >= 128 ? 2 : 1, kWavesN = WAVES / kWavesM;
+    constexpr int kM = CT / kWavesM / 16, kN = RT / kWavesN / 16;  // 16 x 16 tiles per wave
+    static_assert(kM % 4 == 0, "whole lines of dW: 64 columns");
+    using XLoader = ColTileLoader<CT, WAVES>;
+    using YLoader = ColTileLoader<RT, WAVES>;
+    constexpr int kGroups = XLoader::kGroups;  // entries per lane (the same ones of both operands)
+    const int wm = ffn_wave() % kWavesM, wn = ffn_wave() / kWavesM;
+    constexpr int kStep = BY_COLS ? CT : RT;
+    const int32_t n = a.T * a.k, K = a.len, N = a.N;
+    const int32_t side = BY_COLS ? K : N;
+    const int32_t spans = (side + d.span - 1) / d.span;
+    const int32_t others = BY_COLS ? (N + RT - 1) / RT : (K + CT - 1) / CT;
+    const int32_t runs = PARTS ? d.runs : 1;
+    for (int64_t work = blockIdx.x; work < (int64_t)a.M * spans * others * runs; work += gridDim.x) {
+        const int32_t run = PARTS ? (int32_t)(work % runs) : 0;
+        const int64_t item = PARTS ? work / runs : work;
+        const int64_t per = (int64_t)spans * others;
+        const int32_t e = (int32_t)(item / per), q = (int32_t)(item % per);
+        const int32_t s0 = (q % spans) * d.span, s1 = min(side, s0 + d.span);
+        const int32_t other = (q / spans) * (BY_COLS ? RT : CT);  // first row (column) of the other side
+        int32_t begin = min(max(a.offsets[e], 0), n), end = min(max(a.offsets[e + 1], begin), n);
+        if constexpr (PARTS) {  // whole stages
+            const int32_t len = ((end - begin + runs - 1) / runs + kFfnBK - 1) / kFfnBK * kFfnBK;
+            begin = (int32_t)min((int64_t)begin + (int64_t)run * len, (int64_t)end);
+            end = (int32_t)min((int64_t)begin + len, (int64_t)end);
+        }
+        XLoader xl;
+        YLoader yl;
+        xl.init();
+        yl.init();
+        const int32_t ksteps = (end - begin + kFfnBK - 1) / kFfnBK;
+        const int32_t ssteps = (s1 - s0 + kStep - 1) / kStep;
+        uint32_t entry[kGroups];  // of the next load (read one load ahead)
+        auto fetch = [&](int32_t step) {
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+                const int32_t at = begin + step * kFfnBK + xl.row(i);
+                entry[i] = at < end ? (uint32_t)a.sorted[at] : 0xFFFFFFFFu;
+            }
+        };
+        f32x4 acc[kM][kN];
+#pragma unroll
+        for (int i = 0; i < kM; ++i)
+#pragma unroll
+            for (int j = 0; j < kN; ++j) acc[i][j] = zero_f32x4();
+        int32_t ls = s0, lk = 0, cs = s0, ck = 0;
+        auto store = [&] {
+            if constexpr (PARTS) {
+                float* o = d.parts + ((int64_t)run * a.M + e) * N * K;
+#pragma unroll
+                for (int j = 0; j < kN; ++j)
+#pragma unroll
+                    for (int i = 0; i < kM; ++i) {
+                        const int32_t c = (BY_COLS ? cs : other) + 16 * (wm * kM + i) + 4 * (ffn_lane() >> 4);
+                        const int32_t r = (BY_COLS ? other : cs) + 16 * (wn * kN + j) + (ffn_lane() & 15);
+                        if (c < (BY_COLS ? s1 : K) && r < (BY_COLS ? N : s1))
+                            *reinterpret_cast<f32x4*>(o + (int64_t)r * K + c) = acc[i][j];
+                        acc[i][j] = zero_f32x4();
+                    }
+                cs += kStep;
+                return;
+            }
+            uint16_t* o = a.dW + (int64_t)e * N * K;
+#pragma unroll
+            for (int j = 0; j < kN; ++j)
+#pragma unroll
+                for (int i0 = 0; i0 < kM; i0 += 4) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        place_bf16(scratch, i, acc[i0 + i][j]);
+                        acc[i0 + i][j] = zero_f32x4();
+                    }
+                    const int32_t c = (BY_COLS ? cs : other) + 16 * (wm * kM + i0);
+                    const int32_t r = (BY_COLS ? other : cs) + 16 * (wn * kN + j);
+                    const int32_t left = ((BY_COLS ? s1 : K) - c) * 2;
+                    auto row_of = [&](int row) {
+                        return r + row < (BY_COLS ? N : s1) ? o + (int64_t)(r + row) * K + c : nullptr;
+                    };
+                    if (d.once)
+                        flush_rows<true>(scratch, left, row_of);
+                    else
+                        flush_rows<false>(scratch, left, row_of);
+                }
+            cs += kStep;
+        };
+        if (ksteps == 0) {  // no entries: zeros
+            if constexpr (PARTS) {
+                for (int32_t step = 0; step < ssteps; ++step) store();
+            } else {  // the expert's items share its matrix in runs of whole lines
+                const int64_t pieces = (int64_t)N * K / 8;
+                const int64_t share = (pieces / per + 8) / 8 * 8;
+                u32x4* o = reinterpret_cast<u32x4*>(a.dW + (int64_t)e * N * K);
+                const int64_t last = min(pieces, (q + 1) * share);
+                for (int64_t i = q * share + threadIdx.x; i < last; i += 64 * WAVES)
+                    __builtin_nontemporal_store(u32x4{0u, 0u, 0u, 0u}, o + i);
+            }
+            continue;
+        }
+        using G = FfnGroups<kM, kM == 8 ? 4 : 2>;
+        using MF = FfnFragments<G::kSize>;
+        using NF = FfnFragments<kN>;
+        using Stage = StagePair<XLoader, YLoader>;
+        fetch(0);
+        ffn_pipeline_staged<Stage, G::kGroups, MF, NF>(
+            ksteps * ssteps, true,
+            [&](int, Stage& st) {
+                const int32_t c = BY_COLS ? ls : other, r = BY_COLS ? other : ls;
+                xl.fetch(st.a, K - c, [&](int i) -> const uint16_t* {
+                    return entry[i] < (uint32_t)n ? a.x + (int64_t)(entry[i] / (uint32_t)a.k) * K + c : nullptr;
+                });
+                yl.fetch(st.b, N - r, [&](int i) -> const uint16_t* {
+                    return entry[i] < (uint32_t)n ? a.dy + (int64_t)entry[i] * N + r : nullptr;
+                });
+                if (++lk == ksteps) {
+                    lk = 0;
+                    ls += kStep;
+                }
+                if (ksteps > 1) fetch(lk);
+            },
+            [&](int slot, const Stage& st) {
+                xl.put(smem + slot * kStageBytes, st.a);
+                yl.put(smem + slot * kStageBytes + CT * 128, st.b);
+            },
+            ffn_work(
+                [&](int slot, int kk, int group, MF& m) {
+#pragma unroll
+                    for (int i = 0; i < G::kSize; ++i)
+                        if (G::tile(group, i) < kM)
+                            m.v[i] = col_fragment(smem + slot * kStageBytes, 16 * (wm * kM + G::tile(group, i)), kk);
+                },
+                [&](int slot, int kk, NF& f) {
+#pragma unroll
+                    for (int j = 0; j < kN; ++j)
+                        f.v[j] = col_fragment(smem + slot * kStageBytes + CT * 128, 16 * (wn * kN + j), kk);
+                },
+                [&](int group, const MF& m, const NF& f) {
+#pragma unroll
+                    for (int i = 0; i < G::kSize; ++i)
+                        if (G::tile(group, i) < kM)
+#pragma unroll
+                            for (int j = 0; j < kN; ++j) {
+                                f32x4& c = acc[G::tile(group, i)][j];
+                                c = mfma_16x16x32(m.v[i], f.v[j], c);
+                            }
+                },
+                [&] {
+                    if (++ck < ksteps) return;
+                    ck = 0;
+                    store();
+                }));
+    }
+}
+
+// ------------------------------------------------------------------------------ host
+namespace {
+
+size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
+constexpr int64_t kMaxBlocks = 1 << 19;
+unsigned grid_of(int64_t items) { return (unsigned)(std::min<int64_t>((items + 7) / 8, kMaxBlocks / 8) * 8); }
+
+template <int BM, int COLS>
+void dx_launch(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t stream) {
+    const unsigned blocks = grid_of(p.tiles.tiles * ((a.len + p.span - 1) / p.span));
+    const void* list = ws + p.tiles.off_tiles;
+    if (a.k == 1)
+        linear_dx_kernel<BM, COLS, true><<<blocks, dx_threads(BM), 0, stream>>>(a, list, p.span, a.dx);
+    else
+        linear_dx_kernel<BM, COLS, false><<<blocks, dx_threads(BM), 0, stream>>>(a, list, p.span, ws + p.off_shares);
+}
+
+int64_t dw_items(const LinearPlan& p, int32_t K, int32_t N, int32_t M, bool by_cols) {
+    const int32_t side = by_cols ? K : N, other = by_cols ? N : K, step = by_cols ? p.dw_rows : p.dw_cols;
+    return (int64_t)M * ((side + p.dw_span - 1) / p.dw_span) * ((other + step - 1) / step);
+}
+
+template <int CT, int RT, int WAVES, bool BY_COLS>
+void dw_launch(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t stream) {
+    LinearDw d;
+    d.span = p.dw_span;
+    d.runs = p.dw_parts;
+    d.once = a.len % 64 == 0;
+    d.parts = reinterpret_cast<float*>(ws + p.off_parts);
+    const unsigned blocks = grid_of(dw_items(p, a.len, a.N, a.M, BY_COLS) * d.runs);
+    if (p.dw_parts > 1) {
+        if constexpr (CT < 256) linear_dw_kernel<CT, RT, WAVES, BY_COLS, true><<<blocks, 64 * WAVES, 0, stream>>>(a, d);
+    } else {
+        linear_dw_kernel<CT, RT, WAVES, BY_COLS, false><<<blocks, 64 * WAVES, 0, stream>>>(a, d);
+    }
+}
+
+// Tile of dW, by the same cost as the rows' tiles, and the runs into which an expert's entries are cut: as many
+// as bring the tiles to 512, of four stages at least, and at most 32.
+void dw_plan(int64_t n, int32_t K, int32_t N, int32_t M, LinearPlan* p) {
+    const int64_t steps = std::max<int64_t>(1, n / M / kFfnBK);
+    auto tiles = [&](int32_t a, int32_t b) { return (int64_t)((a + b - 1) / b); };
+    p->dw_cols = K <= 64 ? 64 : 128;
+    p->dw_rows = K > 64 && N <= 64 ? 64 : 128;
+    const int64_t large = M * tiles(K, 256) * tiles(N, 256), small = M * tiles(K, p->dw_cols) * tiles(N, p->dw_rows);
+    p->dw_parts = 1;
+    if (ffn_cost(large, steps, 256) < ffn_cost(small, steps, 128))
+        p->dw_rows = p->dw_cols = 256;
+    else
+        p->dw_parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({512 / small, steps / 4, 32}));
+    const bool by_cols = p->dw_cols > 64;
+    const int32_t step = by_cols ? p->dw_cols : p->dw_rows, side = by_cols ? K : N;
+    const int64_t groups = M * (by_cols ? tiles(N, p->dw_rows) : tiles(K, p->dw_cols));
+    p->dw_span = p->dw_parts > 1 ? step : ffn_span((int32_t)std::min<int64_t>(n / M, 1 << 20), step, groups, side);
+}
+
+}  // namespace
+
+void linear_backward_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, LinearPlan* p) {
+    const int64_t n = T * k;
+    *p = LinearPlan{};
+    p->cols = len <= 64 ? 64 : 128;
+    const int32_t bm = linear_tile_rows(n, M, len, p->cols, (N + kFfnBK - 1) / kFfnBK);
+    ffn_tiles_plan(n, M, bm, &p->tiles);
+    if (bm == 256) p->cols = 256;
+    p->span = ffn_span(N, p->cols, p->tiles.tiles, len);
+    dw_plan(n, len, N, M, p);
+    size_t at = p->tiles.workspace_bytes;
+    p->off_shares = at;
+    at += k > 1 ? align256((size_t)n * len * 4) : 0;
+    p->off_parts = at;
+    at += p->dw_parts > 1 ? align256((size_t)p->dw_parts * M * N * len * 4) : 0;
+    p->workspace_bytes = at;
+}
+
+hipError_t linear_backward_launch(const LinearPlan& p, const LinearArgs& a, void* workspace, hipStream_t stream) {
+    char* ws = static_cast<char*>(workspace);
+    hipError_t e = hipSuccess;
+    if (p.tiles.n > 0 && a.dx) {
+        e = linear_tiles_launch(p, a, ws, stream);
+        if (e != hipSuccess) return e;
+        switch (p.tiles.bm) {
+            case 256: dx_launch<256, 256>(p, a, ws, stream); break;
+            case 128: p.cols == 64 ? dx_launch<128, 64>(p, a, ws, stream) : dx_launch<128, 128>(p, a, ws, stream); break;
+            case 64: p.cols == 64 ? dx_launch<64, 64>(p, a, ws, stream) : dx_launch<64, 128>(p, a, ws, stream); break;
+            default: p.cols == 64 ? dx_launch<32, 64>(p, a, ws, stream) : dx_launch<32, 128>(p, a, ws, stream);
+        }
+        if (a.k > 1) {
+            e = ffn_entry_sum_launch(reinterpret_cast<const float*>(ws + p.off_shares), a.idx, a.T, a.len, a.M, a.k, a.dx,
+                                     stream);
+            if (e != hipSuccess) return e;
+        }
+    }
+    if (!a.dW) return hipGetLastError();
+    if (p.dw_cols == 256)
+        dw_launch<256, 256, 8, true>(p, a, ws, stream);
+    else if (p.dw_cols == 64)
+        dw_launch<64, 128, 4, false>(p, a, ws, stream);
+    else if (p.dw_rows == 64)
+        dw_launch<128, 64, 4, true>(p, a, ws, stream);
+    else
+        dw_launch<128, 128, 4, true>(p, a, ws, stream);
+    if (p.dw_parts > 1) {
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        return ffn_parts_sum_launch(reinterpret_cast<const float*>(ws + p.off_parts), p.dw_parts,
+                                    (int64_t)a.M * a.N * a.len, a.dW, stream);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace more
