@@ -9,14 +9,15 @@
 //
 // Memory-bound: a row's logits are read once and stay in registers between maximum, sum and gradient, so that the loss
 // with its gradient is one read and one write.  A group of threads takes a row, R pieces of 16 bytes to a thread; rows
-// that do not fit are read again instead.  Rows start at any element: pieces are aligned in memory, the first and the
-// last piece of a row are taken by elements, so nothing outside the row is touched.
-// The teacher's entries lie in LDS; after its stores a thread goes through them and stores the gradients of those
-// in its own pieces over the first ones (same lane, same address: in order).
+// that do not fit are read again instead.  Rows start at any element: the pieces are those that lie at multiples of 16
+// bytes, and each of the few elements before and behind them is some thread's own, so nothing outside the row is touched.
+// The teacher's entries lie in LDS; after its stores a wave goes through those in its own pieces, and the lane that
+// holds it stores the entry's gradient over the first one (same lane, same address: in order).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "distill.h"
 #include "device_common.h"
@@ -56,28 +57,16 @@ struct Piece {
         }
         return v;
     }
-    // piece u of a row that begins `off` elements into piece 0
-    static __device__ __forceinline__ u32x4 load(const Element* row, int32_t off, int32_t V, int32_t u) {
-        const int32_t e0 = u * kCount - off;
-        if (e0 >= 0 && e0 + kCount <= V) return *reinterpret_cast<const u32x4*>(row + e0);
-        u32x4 v = {kNone, kNone, kNone, kNone};
-#pragma unroll
-        for (int i = 0; i < kCount; ++i) {
-            if (e0 + i < 0 || e0 + i >= V) continue;
-            if constexpr (WIDE) {
-                v[i] = __builtin_bit_cast(uint32_t, row[e0 + i]);
-            } else {
-                const uint32_t b = row[e0 + i];
-                v[i / 2] = i % 2 ? (v[i / 2] & 0xFFFFu) | b << 16 : (v[i / 2] & 0xFFFF0000u) | b;
-            }
-        }
-        return v;
-    }
 };
 
-struct Stats {
-    float m, s;  // the maximum, and the sum of exp2((z - m) c)
-};
+// What keeps a row of bf16 in as many registers as it has bytes: its pieces are unpacked again where they are used next,
+// and one after the other (unpacked all at once, 8192 rows of 32001 take 812 us).
+__device__ __forceinline__ void one_by_one() { __builtin_amdgcn_sched_barrier(0); }
+template <int R>
+__device__ __forceinline__ void keep_packed(u32x4 (&v)[R]) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) asm volatile("" : "+v"(v[r]));
+}
 
 template <int THREADS>
 __device__ __forceinline__ void group_sync() {
@@ -88,15 +77,24 @@ __device__ __forceinline__ void group_sync() {
     }
 }
 
+// Over the wave's lanes, by moves that stay in the vector unit.
+template <typename F>
+__device__ __forceinline__ float wave_reduce(float v, F f) {
+    v = f(v, lane_xor<1>(v));
+    v = f(v, lane_xor<2>(v));
+    v = f(v, lane_xor<4>(v));
+    v = f(v, lane_xor<8>(v));
+    float a, b;
+    lane_pair16(v, a, b);
+    v = f(a, b);
+    lane_pair32(v, a, b);
+    return f(a, b);
+}
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
-    return v;
+    return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
-    return v;
+    return wave_reduce(v, [](float a, float b) { return a + b; });
 }
 
 // The value of every thread's v over a row's group (waves in order).
@@ -112,99 +110,147 @@ __device__ __forceinline__ float group_reduce(float v, float* part) {
     return v;
 }
 
-// RESIDENT: the row's pieces (R per thread) stay in registers; else they are read again (R at a time).
-template <bool WIDE, int THREADS, int R, bool RESIDENT>
+// RESIDENT: the row's pieces (R per thread) stay in registers; else they are read again (R at a time).  ONCE: nontemporal
+// loads and stores.
+template <bool WIDE, int THREADS, int R, bool RESIDENT, bool ONCE>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void distill_kernel(DistillArgs a) {
     using P = Piece<WIDE>;
     using Element = typename P::Element;
+    using Bits = typename std::conditional<WIDE, uint32_t, uint16_t>::type;
     constexpr int kRows = THREADS < 256 ? 256 / THREADS : 1;  // rows of a workgroup
     constexpr int kCount = P::kCount;
-    extern __shared__ float dynamic[];  // per row: q (or 0), z and id of the teacher's entries
+    extern __shared__ __attribute__((aligned(16))) float dynamic[];
     __shared__ float part_max[16], part_sum[16], total[kRows];
-    const int group = threadIdx.x / THREADS, tid = threadIdx.x % THREADS;
-    float* q_of = dynamic + (int64_t)group * 3 * a.k;
-    float* z_of = q_of + a.k;
-    int32_t* id_of = reinterpret_cast<int32_t*>(z_of + a.k);
+    const int group = kRows == 1 ? 0 : threadIdx.x / THREADS;
+    // the teacher's entries: q (first v), id, z, and the sum of q over the entries of their class
+    const int32_t k4 = (a.k + 3) & ~3;
+    float* q_of = dynamic + (int64_t)group * 4 * k4;
+    int32_t* id_of = reinterpret_cast<int32_t*>(q_of + k4);
+    float* z_of = q_of + 2 * k4;
+    float* sum_of = q_of + 3 * k4;
     const float c = kLog2e / a.tau;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + group; row < a.T; row += (int64_t)gridDim.x * kRows) {
-        const Element* z = static_cast<const Element*>(a.logits) + row * a.ld;
-        const int32_t off = (int32_t)((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(Element));
-        const int32_t pieces = (int32_t)(((int64_t)off + a.V + kCount - 1) / kCount);
+
+    // What a thread has of a row: pieces, an element before or behind them, one of the first 64 teacher's entries.
+    struct Mine {
         u32x4 v[R];
-        if constexpr (RESIDENT) {
+        float own, value;
+        int32_t id;
+    };
+    struct Place {
+        const Element* z;
+        int32_t head, pieces, edge;  // elements before the pieces; the thread's own element (V or more: none)
+    };
+    auto place = [&](int64_t row, int tid) {
+        Place at;
+        at.z = static_cast<const Element*>(a.logits) + row * a.ld;
+        const int32_t off = (int32_t)((reinterpret_cast<uintptr_t>(at.z) & 15) / sizeof(Element));
+        at.head = off ? min(kCount - off, a.V) : 0;
+        at.pieces = (a.V - at.head) / kCount;
+        at.edge = tid < at.head ? tid : tid < 2 * kCount ? tid + at.pieces * kCount : a.V;
+        return at;
+    };
+    auto load = [&](Mine& x, const Place& at, int32_t u0) {
+        const u32x4* p = reinterpret_cast<const u32x4*>(at.z + at.head);
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const int32_t u = tid + r * THREADS;
-                v[r] = u32x4{P::kNone, P::kNone, P::kNone, P::kNone};
-                if (u < pieces) v[r] = P::load(z, off, a.V, u);
-            }
+        for (int r = 0; r < R; ++r) {
+            const int32_t u = u0 + r * THREADS;
+            x.v[r] = u32x4{P::kNone, P::kNone, P::kNone, P::kNone};
+            if (u >= at.pieces) continue;
+            if constexpr (ONCE) x.v[r] = __builtin_nontemporal_load(p + (uint32_t)u);
+            else x.v[r] = p[(uint32_t)u];
         }
+    };
+    auto fetch = [&](Mine& x, const Place& at, int64_t row, int tid) {
+        x.id = -1;
+        x.value = x.own = minus_inf();
+        if (tid < 64 && tid < a.k) {
+            x.id = a.ids[row * a.k + tid];
+            x.value = a.values[row * a.k + tid];
+        }
+        if (at.edge < a.V) x.own = P::value(at.z[at.edge]);
+        if constexpr (RESIDENT) load(x, at, tid);
+    };
+
+    for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.T; first += (int64_t)gridDim.x * kRows) {
+        const int64_t row = first + group;
+        if (kRows > 1 && row >= a.T) break;
+        int tid = kRows == 1 ? threadIdx.x : threadIdx.x % THREADS;
+        asm volatile("" : "+v"(tid));  // (places are computed again for each row, not kept in registers)
+        const Place at = place(row, tid);
+        Mine x;
+        fetch(x, at, row, tid);
         // the teacher, by the group's first wave
-        float top = minus_inf(), sum_q = 0.0f;
+        float top = minus_inf();
         if (tid < 64) {
-            for (int32_t j = tid; j < a.k; j += 64) {
-                const int32_t id = a.ids[row * a.k + j];
-                const float t = a.values[row * a.k + j];
-                const bool valid = (uint32_t)id < (uint32_t)a.V && t != minus_inf();
+            float z0 = 0.0f;
+            const bool valid0 = (uint32_t)x.id < (uint32_t)a.V && x.value != minus_inf();
+            if (valid0) z0 = P::value(at.z[x.id]);
+            for (int32_t j = tid; j < k4; j += 64) {
+                const bool first64 = j < 64;
+                const int32_t id = first64 ? x.id : j < a.k ? a.ids[row * a.k + j] : -1;
+                const float t = first64 ? x.value : j < a.k ? a.values[row * a.k + j] : minus_inf();
+                const bool valid = first64 ? valid0 : (uint32_t)id < (uint32_t)a.V && t != minus_inf();
                 id_of[j] = valid ? id : -1;
                 q_of[j] = t;
-                z_of[j] = valid ? P::value(z[id]) : 0.0f;
+                z_of[j] = first64 ? z0 : valid ? P::value(at.z[id]) : 0.0f;
                 if (valid) top = fmaxf(top, t);
             }
             top = wave_max(top);
+            float sum = 0.0f;
             bool any = false;
             for (int32_t j = tid; j < a.k; j += 64) {
                 const bool valid = id_of[j] >= 0;
-                const float e = valid ? __builtin_amdgcn_exp2f((q_of[j] - top) * c) : 0.0f;
-                sum_q += e;
+                sum += valid ? __builtin_amdgcn_exp2f((q_of[j] - top) * c) : 0.0f;
                 any |= valid;
             }
-            sum_q = wave_sum(sum_q);
-            if (__ballot(any) == 0) sum_q = 0.0f;
-            if (tid == 0) total[group] = __ballot(any) == 0 ? 0.0f : sum_q;
+            sum = wave_sum(sum);
+            const bool none = __ballot(any) == 0;
+            if (tid == 0) total[group] = none ? 0.0f : sum;
         }
-        // maximum and sum of the row
-        Stats st;
+        // maximum m and sum Z of the row
+        float m = x.own, Z;
         if (a.m_in) {
-            st = Stats{a.m_in[row], a.Z_in[row]};
+            m = a.m_in[row];
+            Z = a.Z_in[row];
         } else if constexpr (RESIDENT) {
-            float m = minus_inf();
 #pragma unroll
-            for (int r = 0; r < R; ++r)
+            for (int r = 0; r < R; ++r) {
 #pragma unroll
-                for (int i = 0; i < kCount; ++i) m = fmaxf(m, P::value(v[r], i));
-            st.m = group_reduce<THREADS, true>(m, part_max);
-            float s = 0.0f;
+                for (int i = 0; i < kCount; ++i) m = fmaxf(m, P::value(x.v[r], i));
+                one_by_one();
+            }
+            m = group_reduce<THREADS, true>(m, part_max);
+            keep_packed(x.v);
+            Z = __builtin_amdgcn_exp2f((x.own - m) * c);
 #pragma unroll
-            for (int r = 0; r < R; ++r)
+            for (int r = 0; r < R; ++r) {
 #pragma unroll
-                for (int i = 0; i < kCount; ++i) s += __builtin_amdgcn_exp2f((P::value(v[r], i) - st.m) * c);
-            st.s = group_reduce<THREADS, false>(s, part_sum);
+                for (int i = 0; i < kCount; ++i) Z += __builtin_amdgcn_exp2f((P::value(x.v[r], i) - m) * c);
+                one_by_one();
+            }
+            Z = group_reduce<THREADS, false>(Z, part_sum);
+            keep_packed(x.v);
         } else {
             // a running maximum and sum per thread
-            float m = minus_inf(), s = 0.0f;
-            for (int32_t u0 = tid; u0 < pieces; u0 += R * THREADS) {
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const int32_t u = u0 + r * THREADS;
-                    v[r] = u32x4{P::kNone, P::kNone, P::kNone, P::kNone};
-                    if (u < pieces) v[r] = P::load(z, off, a.V, u);
-                }
+            Z = m == minus_inf() ? 0.0f : m == m ? 1.0f : m;
+            for (int32_t u0 = tid; u0 < at.pieces; u0 += R * THREADS) {
+                load(x, at, u0);
                 float to = m;
 #pragma unroll
                 for (int r = 0; r < R; ++r)
 #pragma unroll
-                    for (int i = 0; i < kCount; ++i) to = fmaxf(to, P::value(v[r], i));
+                    for (int i = 0; i < kCount; ++i) to = fmaxf(to, P::value(x.v[r], i));
                 const float base = to == minus_inf() ? 0.0f : to;  // (nothing but -infinity so far)
-                s *= __builtin_amdgcn_exp2f((m - base) * c);
+                Z *= __builtin_amdgcn_exp2f((m - base) * c);
 #pragma unroll
                 for (int r = 0; r < R; ++r)
 #pragma unroll
-                    for (int i = 0; i < kCount; ++i) s += __builtin_amdgcn_exp2f((P::value(v[r], i) - base) * c);
+                    for (int i = 0; i < kCount; ++i) Z += __builtin_amdgcn_exp2f((P::value(x.v[r], i) - base) * c);
                 m = to;
             }
-            st.m = group_reduce<THREADS, true>(m, part_max);
-            st.s = group_reduce<THREADS, false>(m == st.m ? s : s * __builtin_amdgcn_exp2f((m - st.m) * c), part_sum);
+            const float mine = m;
+            m = group_reduce<THREADS, true>(m, part_max);
+            Z = group_reduce<THREADS, false>(mine == m ? Z : Z * __builtin_amdgcn_exp2f((mine - m) * c), part_sum);
         }
         group_sync<THREADS>();  // the teacher's entries and their sum are there
         const float U = total[group];
@@ -212,70 +258,93 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void distill_kernel(
         if (tid < 64) {
             float dot = 0.0f;
             for (int32_t j = tid; j < a.k; j += 64) {
-                const bool valid = id_of[j] >= 0;
                 const float d = q_of[j] - top;
-                const float q = valid ? __builtin_amdgcn_exp2f(d * c) / U : 0.0f;
+                const float q = id_of[j] >= 0 ? __builtin_amdgcn_exp2f(d * c) / U : 0.0f;
                 // (an entry whose q is zero has no share, whatever the student says)
-                if (q != 0.0f) dot += q * (d - (z_of[j] - st.m));
+                if (q != 0.0f) dot += q * (d - (z_of[j] - m));
                 q_of[j] = q;
             }
             dot = wave_sum(dot);
             if (tid == 0) {
                 if (a.loss)
                     a.loss[row] = some ? a.tau * a.tau *
-                                             ((__builtin_amdgcn_logf(st.s) - __builtin_amdgcn_logf(U)) * kLn2 + dot / a.tau)
+                                             ((__builtin_amdgcn_logf(Z) - __builtin_amdgcn_logf(U)) * kLn2 + dot / a.tau)
                                        : 0.0f;
-                if (a.m) a.m[row] = st.m;
-                if (a.Z) a.Z[row] = st.s;
+                if (a.m) a.m[row] = m;
+                if (a.Z) a.Z[row] = Z;
             }
         }
         if (a.dlogits) {
-            Element* dz = static_cast<Element*>(a.dlogits) + row * a.ldd;
-            const float g = a.tau * (a.weight ? a.weight[row] : 1.0f), gp = g / st.s;
-            // the stores' pieces are the loads' (they need not be aligned in dlogits)
-            const bool vector = ((reinterpret_cast<uintptr_t>(dz) & 15) / sizeof(Element)) == (uintptr_t)off;
-            auto store = [&](int32_t u, const u32x4& w) {
-                const int32_t e0 = u * kCount - off;
-                float f[kCount];
+            // an id may occur more than once: its entries' q together (by all waves where there are many; those of the
+            // first 64 by the wave that made them)
+            if (a.k > 64) group_sync<THREADS>();
+            else wave_lds_sync();
+            for (int32_t j = tid; j < a.k; j += THREADS) {
+                const int32_t id = id_of[j];
+                float q = 0.0f;
+                for (int32_t i = 0; i < k4; i += 4) {
+                    const i32x4 ids = *reinterpret_cast<const i32x4*>(id_of + i);
+                    const f32x4 qs = *reinterpret_cast<const f32x4*>(q_of + i);
 #pragma unroll
-                for (int i = 0; i < kCount; ++i)
-                    f[i] = some ? gp * __builtin_amdgcn_exp2f((P::value(w, i) - st.m) * c) : 0.0f;
-                if (vector && e0 >= 0 && e0 + kCount <= a.V) {
-                    *reinterpret_cast<u32x4*>(dz + e0) = P::pack(f);
+                    for (int e = 0; e < 4; ++e) q += ids[e] == id ? qs[e] : 0.0f;
+                }
+                sum_of[j] = q;
+            }
+            Element* dz = static_cast<Element*>(a.dlogits) + row * a.ldd;
+            const float g = a.tau * (a.weight ? a.weight[row] : 1.0f), gp = g / Z;
+            // (the pieces of z need not lie at multiples of 16 bytes of dlogits)
+            u32x4* to = reinterpret_cast<u32x4*>(dz + at.head);
+            const bool vector = (reinterpret_cast<uintptr_t>(to) & 15) == 0;
+            auto put = [&](int32_t u, const u32x4& w) {
+                if (vector) {
+                    if constexpr (ONCE) __builtin_nontemporal_store(w, to + (uint32_t)u);
+                    else to[(uint32_t)u] = w;
                 } else {
 #pragma unroll
-                    for (int i = 0; i < kCount; ++i)
-                        if (e0 + i >= 0 && e0 + i < a.V) dz[e0 + i] = P::element(f[i]);
+                    for (int i = 0; i < kCount; ++i) {
+                        const uint32_t b = w[WIDE ? i : i / 2];
+                        dz[at.head + u * kCount + i] = __builtin_bit_cast(Element, (Bits)(WIDE || i % 2 == 0 ? b : b >> 16));
+                    }
                 }
             };
-            if constexpr (RESIDENT) {
+            auto gradient = [&](const u32x4& w) {
+                float f[kCount];
+#pragma unroll
+                for (int i = 0; i < kCount; ++i) f[i] = gp * __builtin_amdgcn_exp2f((P::value(w, i) - m) * c);
+                return P::pack(f);
+            };
+            if (!some) {  // no teacher: zeros
+                for (int32_t u = tid; u < at.pieces; u += THREADS) put(u, u32x4{0u, 0u, 0u, 0u});
+            } else if constexpr (RESIDENT) {
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     const int32_t u = tid + r * THREADS;
-                    if (u < pieces) store(u, v[r]);
+                    if (u < at.pieces) put(u, gradient(x.v[r]));
+                    one_by_one();
                 }
             } else {
-                for (int32_t u0 = tid; u0 < pieces; u0 += R * THREADS) {
+                for (int32_t u0 = tid; u0 < at.pieces; u0 += R * THREADS) {
+                    load(x, at, u0);
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
                         const int32_t u = u0 + r * THREADS;
-                        if (u < pieces) v[r] = P::load(z, off, a.V, u);
-                    }
-#pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        const int32_t u = u0 + r * THREADS;
-                        if (u < pieces) store(u, v[r]);
+                        if (u < at.pieces) put(u, gradient(x.v[r]));
                     }
                 }
             }
-            group_sync<THREADS>();  // q is there
-            if (some) {
-                for (int32_t j = 0; j < a.k; ++j) {
-                    const int32_t id = id_of[j];
-                    if (id < 0 || (id + off) / kCount % THREADS != tid) continue;
-                    float q = 0.0f;  // (an id may occur more than once)
-                    for (int32_t i = 0; i < a.k; ++i) q += id_of[i] == id ? q_of[i] : 0.0f;
-                    dz[id] = P::element(gp * __builtin_amdgcn_exp2f((z_of[j] - st.m) * c) - g * q);
+            if (at.edge < a.V) dz[at.edge] = P::element(some ? gp * __builtin_amdgcn_exp2f((x.own - m) * c) : 0.0f);
+            group_sync<THREADS>();  // the sums are there
+            for (int32_t j0 = 0; some && j0 < a.k; j0 += 64) {
+                const int lane = tid & 63;
+                const int32_t id = j0 + lane < a.k ? id_of[j0 + lane] : -1;
+                const int32_t in = id - at.head, end = at.pieces * kCount;
+                // the thread whose piece or own element it is
+                const int32_t owner = in < 0 ? id : in < end ? (int32_t)((uint32_t)in / kCount % THREADS) : id - end;
+                for (uint64_t mine = __ballot(id >= 0 && owner >> 6 == tid >> 6); mine; mine &= mine - 1) {
+                    const int l = __builtin_ctzll(mine);
+                    const int32_t the_id = __builtin_amdgcn_readlane(id, l);
+                    if (lane == (__builtin_amdgcn_readlane(owner, l) & 63))
+                        dz[the_id] = P::element(gp * __builtin_amdgcn_exp2f((z_of[j0 + l] - m) * c) - g * sum_of[j0 + l]);
                 }
             }
         }
@@ -283,31 +352,47 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void distill_kernel(
     }
 }
 
-template <bool WIDE, int THREADS, int R, bool RESIDENT = true>
+template <bool WIDE, int THREADS, int R, bool RESIDENT = true, bool LONG = true>
 void launch(const DistillArgs& a, hipStream_t stream) {
     const int rows = THREADS < 256 ? 256 / THREADS : 1, threads = THREADS < 256 ? 256 : THREADS;
     const unsigned blocks = (unsigned)std::min<int64_t>(((int64_t)a.T + rows - 1) / rows, 1 << 20);
-    distill_kernel<WIDE, THREADS, R, RESIDENT><<<blocks, threads, (size_t)rows * 3 * a.k * sizeof(float), stream>>>(a);
+    const size_t lds = (size_t)rows * 4 * ((a.k + 3) & ~3) * sizeof(float);
+    // Long rows of logits beyond the last-level cache's 256 MB pass by it (us, plain : nontemporal, 8192 rows of 32001
+    // bf16 203 : 191, of 16384 fp32 213 : 199; short rows are slower by it, 32768 of 512 fp32 36 : 43).
+    const bool once = LONG && (int64_t)a.T * a.V * (WIDE ? 4 : 2) > (int64_t)256 << 20;
+    if (once)
+        distill_kernel<WIDE, THREADS, R, RESIDENT, LONG><<<blocks, threads, lds, stream>>>(a);
+    else
+        distill_kernel<WIDE, THREADS, R, RESIDENT, false><<<blocks, threads, lds, stream>>>(a);
 }
 
+// Threads and pieces by the row's length: as few threads as leave a thread up to 8 pieces (more workgroups to a CU, that
+// compute while others wait), then up to 16 (us, 8192 rows of 32001 bf16, 512 threads : 1024 191 : 300; 4096 of 65536
+// 221 : 241; 16384 of 4096, 64 threads : 256 54 : 67).  A call that reads its rows once, for the loss alone or with known
+// statistics, need not keep them (us, kept : not, 4096 rows of 65536 bf16, loss 91 : 81, gradient 195 : 186; 2048 of
+// 131072, loss 122 : 91; with both 219 : 274).
 template <bool WIDE>
 void launch(const DistillArgs& a, hipStream_t stream) {
-    const int32_t count = Piece<WIDE>::kCount;
-    const int64_t pieces = ((int64_t)a.V + 2 * count - 2) / count;  // of a row that begins at the worst place
-    if (pieces <= 64)
-        launch<WIDE, 64, 1>(a, stream);
-    else if (pieces <= 128)
-        launch<WIDE, 64, 2>(a, stream);
-    else if (pieces <= 256)
-        launch<WIDE, 64, 4>(a, stream);
+    const int32_t pieces = a.V / Piece<WIDE>::kCount;
+    const bool few = a.k <= 256;  // (four rows' entries in LDS)
+    if (few && pieces <= 64)
+        launch<WIDE, 64, 1, true, false>(a, stream);
+    else if (few && pieces <= 128)
+        launch<WIDE, 64, 2, true, false>(a, stream);
+    else if (few && pieces <= 256)
+        launch<WIDE, 64, 4, true, false>(a, stream);
+    else if (few && pieces <= 512)
+        launch<WIDE, 64, 8, true, false>(a, stream);
     else if (pieces <= 1024)
         launch<WIDE, 256, 4>(a, stream);
     else if (pieces <= 2048)
         launch<WIDE, 256, 8>(a, stream);
     else if (pieces <= 4096)
         launch<WIDE, 512, 8>(a, stream);
+    else if (!a.dlogits || a.m_in)
+        launch<WIDE, 512, 8, false>(a, stream);
     else if (pieces <= 8192)
-        launch<WIDE, 1024, 8>(a, stream);
+        launch<WIDE, 512, 16>(a, stream);
     else if (pieces <= 16384)
         launch<WIDE, 1024, 16>(a, stream);
     else

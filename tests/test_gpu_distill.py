@@ -68,7 +68,10 @@ def test_distill(V, bits):
         two = distill_backward(logits, d.m, d.Z, to_dev(ids), to_dev(values), to_dev(w), temperature=tau)
         assert torch.equal(two, d.dlogits)
         alone = distill_loss(logits, to_dev(ids), to_dev(values), temperature=tau)
-        assert torch.equal(alone.loss, d.loss) and torch.equal(alone.Z, d.Z) and alone.dlogits is None
+        # (long rows are summed in another order without the gradient)
+        close(alone.loss, loss, bl, "loss")
+        close(alone.Z, Z, bZ, "Z")
+        assert torch.equal(alone.m, d.m) and alone.dlogits is None
 
 
 @pytest.mark.parametrize("bits", [16, 32])
