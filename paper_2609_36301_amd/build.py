@@ -21,7 +21,8 @@ LIB = os.path.join(PKG, "libmore.so")
 SOURCES = ["lowrank.hip", "bucket.hip", "fullrank.hip", "histogram.hip", "dispatch.hip", "stats.hip", "fullrank_fused.hip",
            "backward.hip", "wide.hip",
            "noalloc.hip", "more_api.cpp", "ffn.hip", "ffn_backward.hip", "block_norm.hip",
-           "grad_clip.hip", "layer_api.cpp", "linear.hip", "linear_backward.hip", "quantize.hip", "distill.hip",
+           "grad_clip.hip", "layer_api.cpp", "linear.hip", "linear_stream.hip",
+           "linear_backward.hip", "quantize.hip", "distill.hip",
            "linear_api.cpp"]
 ARCH = "gfx950"
 

@@ -117,7 +117,10 @@ __global__ __launch_bounds__(kTileThreads) void ffn_tiles_kernel(const int32_t* 
                 const int32_t row = valid + (r << log_bm);
                 tiles[total + r] = FfnTile{-1, row, min(n - row, bm1 + 1), 0};
             }
-        if (tid == 0) *list = (int32_t)std::min<int64_t>(total + extra, bound);
+        // the count, the count without the dropped entries' tiles, and counters that a reader of the list may use
+        if (tid == 0) list[0] = (int32_t)std::min<int64_t>(total + extra, bound);
+        if (tid == 1) list[1] = (int32_t)std::min<int64_t>(total, bound);
+        if (tid >= 8 && tid < 16) list[tid] = 0;
     }
 }
 

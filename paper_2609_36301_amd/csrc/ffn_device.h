@@ -23,7 +23,8 @@ constexpr int kFfnBK = 64;  // contraction values per stage
 struct FfnTile {
     int32_t expert, row0, rows, pad;
 };
-// The tile list: a count, then (256 bytes on) the tiles.
+// The tile list: the count (also without the dropped entries' tiles, which come last), eight zeros at 8 .. 15, and
+// (256 bytes on) the tiles.
 constexpr size_t kFfnTileHeader = 256;
 __device__ __forceinline__ const FfnTile* ffn_tile_list(const void* tiles) {
     return reinterpret_cast<const FfnTile*>(static_cast<const char*>(tiles) + kFfnTileHeader);

@@ -36,6 +36,7 @@ struct LinearPlan {
     int32_t cols;     // columns of a step
     int32_t stages;   // (forward, tiles) of the LDS ring
     int32_t span;     // columns that a workgroup takes
+    int32_t stream;   // (q8, tiles of 256 rows) the pipeline runs on from tile to tile
     int32_t dw_rows, dw_cols;  // rows and columns of a tile of dW
     int32_t dw_parts;          // runs of an expert's entries that are summed apart
     int32_t dw_span;           // of dW's longer side that a workgroup takes
@@ -47,6 +48,11 @@ void linear_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, b
 void linear_backward_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, LinearPlan* p);
 hipError_t linear_launch(const LinearPlan& p, const LinearArgs& a, void* workspace, hipStream_t stream);
 hipError_t linear_backward_launch(const LinearPlan& p, const LinearArgs& a, void* workspace, hipStream_t stream);
+
+// The product in 8-bit integers on tiles of 256 rows and 256 columns whose contraction has at least kStreamSteps
+// stages (linear_stream.hip), after the tile list.
+constexpr int32_t kStreamSteps = 5;
+hipError_t linear_stream_launch(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t stream);
 
 // Lists the tiles of a plan.
 hipError_t linear_tiles_launch(const LinearPlan& p, const LinearArgs& a, void* workspace, hipStream_t stream);

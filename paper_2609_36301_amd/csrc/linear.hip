@@ -14,63 +14,9 @@
 
 #include "ffn_device.h"
 #include "linear.h"
+#include "linear_device.h"
 
 namespace more {
-
-// The two types share everything but the matrix instruction: a 16-byte fragment holds eight bf16 or sixteen
-// int8 values of a row, and both operands take the same ones.
-template <bool I8>
-struct LinearType {
-    using Acc = f32x4;
-    static __device__ __forceinline__ Acc zero() { return zero_f32x4(); }
-    static __device__ __forceinline__ Acc multiply(bf16x8 a, bf16x8 b, Acc c) { return mfma_16x16x32(a, b, c); }
-};
-template <>
-struct LinearType<true> {
-    using Acc = i32x4;
-    static __device__ __forceinline__ Acc zero() { return i32x4{0, 0, 0, 0}; }
-    static __device__ __forceinline__ Acc multiply(bf16x8 a, bf16x8 b, Acc c) {
-        return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
-    }
-};
-
-// The factor of entry p's row, and four columns of an accumulator as they are stored.
-template <bool I8>
-__device__ __forceinline__ float linear_row_scale(const LinearArgs& a, uint32_t p, int32_t n) {
-    if constexpr (!I8) return 1.0f;
-    if (p >= (uint32_t)n) return 0.0f;
-    const float s = a.x_scale[p / (uint32_t)a.k];
-    return a.gate ? s * a.gate[p] : s;
-}
-template <bool I8>
-__device__ __forceinline__ void linear_store(const LinearArgs& a, typename LinearType<I8>::Acc acc, float row_scale,
-                                             const float* w_scale, uint32_t p, int32_t c) {
-    f32x4 v;
-    if constexpr (I8) {
-        const f32x4 ws = *reinterpret_cast<const f32x4*>(w_scale + c);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = (float)acc[q] * ws[q] * row_scale;
-    } else {
-        v = acc;
-    }
-    const int64_t at = (int64_t)p * a.N + c;
-    if (a.wide)
-        *reinterpret_cast<f32x4*>(static_cast<float*>(a.y) + at) = v;
-    else
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + at) = pack_bf16x4(v[0], v[1], v[2], v[3]);
-}
-// Zeros to columns c .. c + 7 of entry p's row.
-__device__ __forceinline__ void linear_zero(const LinearArgs& a, uint32_t p, int32_t c) {
-    const int64_t at = (int64_t)p * a.N + c;
-    const u32x4 z = {0u, 0u, 0u, 0u};
-    if (a.wide) {
-        u32x4* y = reinterpret_cast<u32x4*>(static_cast<float*>(a.y) + at);
-        y[0] = z;
-        y[1] = z;
-    } else {
-        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.y) + at) = z;
-    }
-}
 
 // ------------------------------------------------------------------------------ tiles
 // A workgroup computes a tile's rows of y, `span` columns in steps of COLS: the rows of W are the M side, the
@@ -181,12 +127,29 @@ __global__ __launch_bounds__(linear_threads(BM), 2) void linear_kernel(LinearArg
                 },
                 [&] {
                     if (++ck < ksteps) return;
+                    if (S::kM % 2 == 0 && !a.wide) {
+#pragma unroll
+                        for (int j = 0; j < S::kN; ++j)
+#pragma unroll
+                            for (int i = 0; i < S::kM; i += 2) {
+                                const int32_t c = cc + 16 * (wm * S::kM + i);
+                                const u32x4 v = linear_pair(linear_value<I8>(a, acc[i][j], row_scale[j], w_scale, c),
+                                                            linear_value<I8>(a, acc[i + 1][j], row_scale[j], w_scale, c + 16));
+                                const int32_t mine = c + 8 * (lane >> 4);
+                                if (place[j] < (uint32_t)n && mine < c1)
+                                    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.y) + (int64_t)place[j] * N + mine) = v;
+                                acc[i][j] = acc[i + 1][j] = Type::zero();
+                            }
+                        ck = 0;
+                        cc += COLS;
+                        return;
+                    }
 #pragma unroll
                     for (int j = 0; j < S::kN; ++j) {
 #pragma unroll
                         for (int i = 0; i < S::kM; ++i) {
-                            const int32_t c = cc + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
-                            if (place[j] < (uint32_t)n && c < c1)
+                            const int32_t c = cc + 16 * (wm * S::kM + i);
+                            if (place[j] < (uint32_t)n && c + 4 * (lane >> 4) < c1)
                                 linear_store<I8>(a, acc[i][j], row_scale[j], w_scale, place[j], c);
                             acc[i][j] = Type::zero();
                         }
@@ -276,8 +239,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a
         const float* w_scale = I8 ? a.w_scale + (int64_t)f.expert * N : nullptr;
 #pragma unroll
         for (int r = 0; r < kR; ++r) {
-            const int32_t c = c0 + 16 * r + 4 * (lane >> 4);
-            if (c < N) linear_store<I8>(a, acc[r], row_scale, w_scale, f.p, c);
+            const int32_t c = c0 + 16 * r;
+            if (c + 4 * (lane >> 4) < N) linear_store<I8>(a, acc[r], row_scale, w_scale, f.p, c);
         }
     }
 }
@@ -297,7 +260,7 @@ void tiled(const LinearPlan& p, const LinearArgs& a, const char* ws, hipStream_t
 }
 
 template <bool I8>
-void forward(const LinearPlan& p, const LinearArgs& a, const char* ws, hipStream_t stream) {
+void forward(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t stream) {
     if (p.few) {
         const unsigned blocks = few_grid(p.tiles.n * ((a.N + p.span - 1) / p.span));
         if (p.split)
@@ -338,7 +301,6 @@ int32_t linear_tile_rows(int64_t n, int32_t M, int32_t cols, int32_t cols_of, in
 static int64_t few_starts(int64_t n, int32_t M) { return std::min<int64_t>(n, std::min<int64_t>(n, M) + n / kFewRows); }
 
 void linear_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, bool q8, LinearPlan* p) {
-    (void)q8;
     const int64_t n = T * k;
     *p = LinearPlan{};
     p->cols = N <= 64 ? 64 : 128;
@@ -354,7 +316,8 @@ void linear_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, b
         return;
     }
     if (bm == 256) p->cols = 256;
-    p->span = ffn_span(len, p->cols, p->tiles.tiles, N);
+    p->stream = q8 && bm == 256 && (len + kFfnBK - 1) / kFfnBK >= kStreamSteps;
+    p->span = p->stream ? p->cols : ffn_span(len, p->cols, p->tiles.tiles, N);
     p->stages = bm >= 128 ? 2 : bm == 64 || p->cols == 64 ? 3 : p->tiles.tiles * ((N + p->span - 1) / p->span) >= 2048 ? 2 : 3;
     p->workspace_bytes = p->tiles.workspace_bytes;
 }
@@ -371,7 +334,8 @@ hipError_t linear_launch(const LinearPlan& p, const LinearArgs& a, void* workspa
         const hipError_t e = linear_tiles_launch(p, a, workspace, stream);
         if (e != hipSuccess) return e;
     }
-    const char* ws = static_cast<const char*>(workspace);
+    char* ws = static_cast<char*>(workspace);
+    if (p.stream) return linear_stream_launch(p, a, ws, stream);
     if (a.q8)
         forward<true>(p, a, ws, stream);
     else

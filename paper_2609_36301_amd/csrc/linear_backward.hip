@@ -18,6 +18,7 @@
 
 #include "ffn_device.h"
 #include "linear.h"
+#include "linear_device.h"
 
 namespace more {
 
@@ -117,6 +118,21 @@ __global__ __launch_bounds__(dx_threads(BM), 2) void linear_dx_kernel(LinearArgs
         };
         auto done = [&] {
             if (++ck < ksteps) return;
+            if constexpr (DIRECT && S::kM % 2 == 0) {
+#pragma unroll
+                for (int j = 0; j < S::kN; ++j)
+#pragma unroll
+                    for (int i = 0; i < S::kM; i += 2) {
+                        const int32_t c = cc + 16 * (wm * S::kM + i) + 8 * (lane >> 4);
+                        const u32x4 v = linear_pair(acc[i][j], acc[i + 1][j]);
+                        if (place[j] < (uint32_t)n && c < c1)
+                            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + (int64_t)place[j] * cols + c) = v;
+                        acc[i][j] = acc[i + 1][j] = zero_f32x4();
+                    }
+                ck = 0;
+                cc += COLS;
+                return;
+            }
 #pragma unroll
             for (int j = 0; j < S::kN; ++j) {
 #pragma unroll

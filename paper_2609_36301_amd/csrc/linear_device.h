@@ -1,0 +1,82 @@
+// Device helpers of the experts' linear maps (gfx950): the two operand types, and how results are stored.
+#pragma once
+
+#include "ffn_device.h"
+#include "linear.h"
+
+namespace more {
+
+// The two types share everything but the matrix instruction: a 16-byte fragment holds eight bf16 or sixteen
+// int8 values of a row, and both operands take the same ones.
+template <bool I8>
+struct LinearType {
+    using Acc = f32x4;
+    static __device__ __forceinline__ Acc zero() { return zero_f32x4(); }
+    static __device__ __forceinline__ Acc multiply(bf16x8 a, bf16x8 b, Acc c) { return mfma_16x16x32(a, b, c); }
+};
+template <>
+struct LinearType<true> {
+    using Acc = i32x4;
+    static __device__ __forceinline__ Acc zero() { return i32x4{0, 0, 0, 0}; }
+    static __device__ __forceinline__ Acc multiply(bf16x8 a, bf16x8 b, Acc c) {
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+    }
+};
+
+// The factor of entry p's row, and four columns of an accumulator as they are stored.
+template <bool I8>
+__device__ __forceinline__ float linear_row_scale(const LinearArgs& a, uint32_t p, int32_t n) {
+    if constexpr (!I8) return 1.0f;
+    if (p >= (uint32_t)n) return 0.0f;
+    const float s = a.x_scale[p / (uint32_t)a.k];
+    return a.gate ? s * a.gate[p] : s;
+}
+__device__ __forceinline__ void linear_put(void* out, bool wide, int64_t at, f32x4 v) {
+    if (wide)
+        *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = v;
+    else
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = pack_bf16x4(v[0], v[1], v[2], v[3]);
+}
+// c: the first of the accumulator's 16 columns.
+template <bool I8>
+__device__ __forceinline__ f32x4 linear_value(const LinearArgs& a, typename LinearType<I8>::Acc acc, float row_scale,
+                                              const float* w_scale, int32_t c) {
+    if constexpr (!I8) return acc;
+    // (columns past the last are not stored)
+    const f32x4 ws = *reinterpret_cast<const f32x4*>(w_scale + min(c + 4 * (ffn_lane() >> 4), a.N - 4));
+    f32x4 v;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = (float)acc[q] * ws[q] * row_scale;
+    return v;
+}
+template <bool I8>
+__device__ __forceinline__ void linear_store(const LinearArgs& a, typename LinearType<I8>::Acc acc, float row_scale,
+                                             const float* w_scale, uint32_t p, int32_t c) {
+    linear_put(a.y, a.wide, (int64_t)p * a.N + c + 4 * (ffn_lane() >> 4),
+               linear_value<I8>(a, acc, row_scale, w_scale, c));
+}
+// Two neighbouring accumulators in bf16, exchanged among the lanes of a row so that a lane holds eight of its 32 columns,
+// the ones from 8 (l / 16) on: stored 16 bytes a lane, a row's 64 bytes are whole (8 bytes a lane, as the
+// accumulators lie, they are written in two halves, twice as many requests to L2).
+__device__ __forceinline__ u32x4 linear_pair(f32x4 a, f32x4 b) {
+    const uint2 x = pack_bf16x4(a[0], a[1], a[2], a[3]), y = pack_bf16x4(b[0], b[1], b[2], b[3]);
+    auto r = __builtin_amdgcn_permlane32_swap(x.x, y.x, false, false);
+    r = __builtin_amdgcn_permlane16_swap(r[0], r[1], false, false);
+    auto s = __builtin_amdgcn_permlane32_swap(x.y, y.y, false, false);
+    s = __builtin_amdgcn_permlane16_swap(s[0], s[1], false, false);
+    return u32x4{(uint32_t)r[0], (uint32_t)s[0], (uint32_t)r[1], (uint32_t)s[1]};
+}
+// Zeros to columns c .. c + 7 of entry p's row.
+__device__ __forceinline__ void linear_zero(const LinearArgs& a, uint32_t p, int32_t c) {
+    const int64_t at = (int64_t)p * a.N + c;
+    const u32x4 z = {0u, 0u, 0u, 0u};
+    if (a.wide) {
+        u32x4* y = reinterpret_cast<u32x4*>(static_cast<float*>(a.y) + at);
+        y[0] = z;
+        y[1] = z;
+    } else {
+        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.y) + at) = z;
+    }
+}
+
+}  // namespace more
