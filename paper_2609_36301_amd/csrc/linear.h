@@ -57,8 +57,8 @@ hipError_t linear_stream_launch(const LinearPlan& p, const LinearArgs& a, char* 
 // Lists the tiles of a plan.
 hipError_t linear_tiles_launch(const LinearPlan& p, const LinearArgs& a, void* workspace, hipStream_t stream);
 
-// Rows of a tile (32 to 256) of a product of n entries over M experts, `cols` columns and `steps` stages, by
-// ffn_cost; `wide_cols` and `cols_of` are the columns of a step of 256-row tiles and of the others.
+// Rows of a tile (32 to 256) of a product of n entries over M experts, `cols` columns (in steps of `cols_of`, of 256 with
+// tiles of 256 rows) and `steps` stages.
 int32_t linear_tile_rows(int64_t n, int32_t M, int32_t cols, int32_t cols_of, int64_t steps);
 
 // q [T][width] int8 and scale [T] of the rows of x: bf16 [T][width], or (gated) [T][2 width].

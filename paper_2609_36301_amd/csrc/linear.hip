@@ -281,14 +281,23 @@ void forward(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t str
 
 }  // namespace
 
+// Rows of a tile: 32 where experts have less than 24 rows (then mostly one tile, whose weights are not read again), else
+// what costs least: the rounds in which the workgroups fill the chip (two of up to 128 rows to a CU, one of 256) times the
+// stages times the time of a stage, and for 256 rows what such a tile costs beside its stages, since nothing else on
+// the CU hides it.  Fitted to the maps and dx of 130 shapes (1 to 512 experts, 32 to 16384 rows each, contractions and
+// columns of 64 to 2048): 1.8 % off the best on geometric mean, 28 % at most.  us for 32 : 64 : 128 : 256 rows, dense maps of
+// 1024 rows of K = N = 1024 16 : 19 : 22 : 34 (dx), 8 experts of 4096 rows, K = 2048, N = 256 109 : 64 : 61 : 56.
 int32_t linear_tile_rows(int64_t n, int32_t M, int32_t cols, int32_t cols_of, int64_t steps) {
     if (n / std::max<int64_t>(1, std::min<int64_t>(n, M)) < 24) return 32;
     int32_t best = 64;
     int64_t least = INT64_MAX;
-    for (int32_t bm = 64; bm <= 256; bm *= 2) {
+    for (int32_t bm = 32; bm <= 256; bm *= 2) {
         const int64_t tiles2 = ffn_expected_tiles2(n, M, bm);
         const int32_t step = bm == 256 ? 256 : cols_of;
-        const int64_t cost = ffn_cost(tiles2 * ((cols + step - 1) / step) / 2, steps, bm);
+        const int64_t items = tiles2 * ((cols + step - 1) / step) / 2, slots = bm == 256 ? 256 : 512;
+        const bool alone = items <= 256;
+        const int64_t stage = bm == 256 ? 30 : bm == 128 ? (alone ? 16 : 20) : bm == 64 ? (alone ? 11 : 15) : alone ? 9 : 18;
+        const int64_t cost = (items + slots - 1) / slots * (steps * stage + (bm == 256 ? 60 : 0));
         if (cost < least) {
             least = cost;
             best = bm;
@@ -306,12 +315,16 @@ void linear_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, b
     p->cols = N <= 64 ? 64 : 128;
     const int32_t bm = linear_tile_rows(n, M, N, p->cols, (len + kFfnBK - 1) / kFfnBK);
     ffn_tiles_plan(n, M, bm, &p->tiles);
-    // The kernel without tiles saves a launch and the latency of the stages, while the weights that it reads (once
-    // for every 16 entries) are few bytes and few workgroups end at once.
-    p->few = few_starts(n, M) * 2 * N * len <= ((int64_t)8 << 20) + (int64_t)40960 * 2 * len &&
-             n * ((N + few_span<false>() - 1) / few_span<false>()) <= 4096;
+    // The kernel without tiles saves a launch and the latency of the stages (3 us) while the rows of W that its
+    // workgroups read, once for every 16 entries, are few, and the entries' rows of x that each reads again, and
+    // few workgroups end at once; its waves share the columns of long contractions.  Fitted to 260 shapes of both types (1 to
+    // 4096 entries, 1 to 4096 experts): 2 % (bf16) and 4 % (int8) off the best of the three on geometric mean.
+    // us with tiles : own columns : shared, one dense map, 256 rows of K = 512, N = 1024 10.6 : 34 : 37; one entry of K = 2048,
+    // N = 128 18.9 : 19.2 : 7.6; 256 in 512 experts of K = 512, N = 128 9.9 : 9.0 : 17.4.
+    p->few = few_starts(n, M) * N <= 10000 + ((int64_t)1 << 21) / len && n * len <= (int64_t)1 << 19 &&
+             n * ((N + few_span<false>() - 1) / few_span<false>()) <= 1024;
     if (p->few) {
-        p->split = len > 64;
+        p->split = len > 256;
         p->span = p->split ? few_span<true>() : few_span<false>();
         return;
     }

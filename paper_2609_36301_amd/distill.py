@@ -18,12 +18,14 @@ HIP graph, and overwrites the outputs of the call before; calls of one object mu
 """
 from __future__ import annotations
 
+import ctypes
 import dataclasses
 from typing import Optional
 
 import torch
 
-from .layer import _call, _check, _device, _ptr
+from .layer import _ptr
+from .linear import _Call
 
 _BITS = {torch.bfloat16: 16, torch.float32: 32}
 
@@ -36,8 +38,10 @@ class Distillation:
     dlogits: Optional[torch.Tensor]  # the logits' type, [T][V]
 
 
-class _Rows:
+class _Rows(_Call):
     """Rows of V logits, ld apart, and their teacher's entries."""
+
+    _function, _vectors = "", ()
 
     def __init__(self, T: int, V: int, k: int, dtype, temperature: float, ld, inplace: bool, gradient: bool, device):
         if dtype not in _BITS:
@@ -47,24 +51,28 @@ class _Rows:
         if self.ld < V:
             raise ValueError("ld must be at least V = %d, got %d" % (V, self.ld))
         self.temperature, self.inplace, self.gradient = float(temperature), bool(inplace), bool(gradient)
-        self.device = _device(device)
+        f32 = torch.float32
+        self._prepare(self._function, device, teacher_idx=(torch.int32, (T, k)), teacher_val=(f32, (T, k)),
+                      **{name: (f32, (T,)) for name in self._vectors})
+        i32, i64 = ctypes.c_int32, ctypes.c_int64
+        self._rows, self._entries = (i32(self.bits), i64(T), i32(V), i64(self.ld)), (i32(k), ctypes.c_float(self.temperature))
+        self._strides = (self.ld if T > 1 else None, 1 if V > 1 else None)
         self.dlogits = None
         if gradient and not inplace:
             self.dlogits = torch.empty((T, self.ld), dtype=dtype, device=self.device)[:, :V]
 
-    def _check_rows(self, logits, teacher_idx, teacher_val):
+    def _check_rows(self, logits):
         T, V, k = self.shape
         if not isinstance(logits, torch.Tensor):
             raise TypeError("logits must be a torch.Tensor")
-        if logits.dtype != self.dtype:
+        if logits.dtype is not self.dtype:
             raise TypeError("logits must be %s, got %s" % (self.dtype, logits.dtype))
-        if logits.shape != (T, V) or (V > 1 and logits.stride(1) != 1) or (T > 1 and logits.stride(0) != self.ld):
+        strides = logits.stride()
+        if logits.shape != (T, V) or strides[0] != (self._strides[0] or strides[0]) or strides[1] != (self._strides[1] or strides[1]):
             raise ValueError("logits must be %d rows of %d values, %d apart, got %s with strides %s"
-                             % (T, V, self.ld, tuple(logits.shape), tuple(logits.stride())))
-        if logits.device != self.device:
+                             % (T, V, self.ld, tuple(logits.shape), tuple(strides)))
+        if logits.get_device() != self.device.index:
             raise ValueError("logits must be on %s, got %s" % (self.device, logits.device))
-        _check("teacher_idx", teacher_idx, torch.int32, (T, k), self.device)
-        _check("teacher_val", teacher_val, torch.float32, (T, k), self.device)
 
     def _out(self, logits):
         return None if not self.gradient else logits if self.inplace else self.dlogits
@@ -75,39 +83,42 @@ class Distill(_Rows):
     (V by default), k teacher entries each.  gradient: the weighted gradient comes with the loss; inplace: over the
     logits."""
 
+    _function, _vectors = "more_distill", ("weight",)
+
     def __init__(self, T: int, V: int, k: int, *, dtype=torch.bfloat16, temperature: float = 1.0, ld: Optional[int] = None,
                  gradient: bool = False, inplace: bool = False, device=None):
         super().__init__(T, V, k, dtype, temperature, ld, inplace, gradient, device)
         self.loss, self.m, self.Z = (torch.empty((T,), dtype=torch.float32, device=self.device) for _ in range(3))
 
     def __call__(self, logits, teacher_idx, teacher_val, weight=None) -> Distillation:
-        self._check_rows(logits, teacher_idx, teacher_val)
-        T, V, k = self.shape
-        if weight is not None:
-            if not self.gradient:
-                raise ValueError("weight is of use only where the gradient is asked for")
-            _check("weight", weight, torch.float32, (T,), self.device)
+        self._check_rows(logits)
+        if weight is None:
+            self._check_tensors(teacher_idx, teacher_val)
+        elif not self.gradient:
+            raise ValueError("weight is of use only where the gradient is asked for")
+        else:
+            self._check_tensors(teacher_idx, teacher_val, weight)
         out = self._out(logits)
-        _call("more_distill", self.device, _ptr(logits), self.bits, T, V, self.ld, _ptr(teacher_idx), _ptr(teacher_val), k,
-              self.temperature, _ptr(weight), _ptr(self.loss), _ptr(self.m), _ptr(self.Z), _ptr(out), self.ld)
+        self._launch(logits.data_ptr(), *self._rows, teacher_idx.data_ptr(), teacher_val.data_ptr(), *self._entries,
+                     _ptr(weight), self.loss.data_ptr(), self.m.data_ptr(), self.Z.data_ptr(), _ptr(out), self.ld)
         return Distillation(self.loss, self.m, self.Z, out)
 
 
 class DistillBackward(_Rows):
     """Pre-allocated gradient for repeated distill_backward calls with one shape (as for Distill)."""
 
+    _function, _vectors = "more_distill_backward", ("m", "Z", "dloss")
+
     def __init__(self, T: int, V: int, k: int, *, dtype=torch.bfloat16, temperature: float = 1.0, ld: Optional[int] = None,
                  inplace: bool = False, device=None):
         super().__init__(T, V, k, dtype, temperature, ld, inplace, True, device)
 
     def __call__(self, logits, m, Z, teacher_idx, teacher_val, dloss) -> torch.Tensor:
-        self._check_rows(logits, teacher_idx, teacher_val)
-        T, V, k = self.shape
-        for name, t in (("m", m), ("Z", Z), ("dloss", dloss)):
-            _check(name, t, torch.float32, (T,), self.device)
+        self._check_rows(logits)
+        self._check_tensors(teacher_idx, teacher_val, m, Z, dloss)
         out = self._out(logits)
-        _call("more_distill_backward", self.device, _ptr(logits), self.bits, T, V, self.ld, _ptr(m), _ptr(Z),
-              _ptr(teacher_idx), _ptr(teacher_val), k, self.temperature, _ptr(dloss), _ptr(out), self.ld)
+        self._launch(logits.data_ptr(), *self._rows, m.data_ptr(), Z.data_ptr(), teacher_idx.data_ptr(),
+                     teacher_val.data_ptr(), *self._entries, dloss.data_ptr(), out.data_ptr(), self.ld)
         return out
 
 

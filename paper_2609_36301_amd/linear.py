@@ -30,7 +30,7 @@ from typing import Optional
 import torch
 
 from . import _lib
-from .layer import _call, _check, _device, _ptr, _size, _workspace
+from .layer import _check, _device, _ptr, _size, _stream, _workspace
 
 _Y_BITS = {torch.bfloat16: 16, torch.float32: 32}
 _KINDS = {"linear": 0, "backward": 1, "q8": 2}
@@ -62,13 +62,6 @@ def expert_linear_plan(T: int, K: int, N: int, M: int, k: int, kind: str = "line
     return {name: getattr(plan, name) for name, _ in plan._fields_}
 
 
-def _spec(T, K, N, M, k, dtype=torch.bfloat16):
-    i32, f32 = torch.int32, torch.float32
-    return {"x": (dtype, (T, K)), "q": (dtype, (T, K)), "Wt": (dtype, (M, N, K)), "Wq": (dtype, (M, N, K)),
-            "idx": (i32, (T, k)), "offsets": (i32, (M + 1,)), "sorted": (i32, (T * k,)),
-            "dy": (torch.bfloat16, (T * k, N)), "q_scale": (f32, (T,)), "w_scale": (f32, (M, N)), "gate": (f32, (T, k))}
-
-
 def _shape(x, Wt, idx, names=("x", "Wt", "idx")):
     for name, t, dim in zip(names, (x, Wt, idx), (2, 3, 2)):
         if not isinstance(t, torch.Tensor):
@@ -78,29 +71,70 @@ def _shape(x, Wt, idx, names=("x", "Wt", "idx")):
     return x.shape[0], x.shape[1], Wt.shape[1], Wt.shape[0], idx.shape[1]
 
 
-class _Checked:
-    """The shape of a call, and the check of its tensors against it."""
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
-    def _checks(self, **tensors):
-        for name, t in tensors.items():
-            dtype, shape = self.spec[name]
+
+class _Call:
+    """A library call of one shape: what its tensors have to be, and the arguments that stay.  (The host takes longer than a
+    single token's kernel, most of it for checking tensors: 4.1 us for five one attribute at a time, 2.5 so.)"""
+
+    def _prepare(self, name: str, device, **tensors):
+        """tensors: dtype and shape by name, in the call's order."""
+        self.device = _device(device)
+        self._name, self._fn = name, getattr(_lib.load(), name)
+        self._names = list(tensors)
+        self._spec = [(dtype, torch.Size(shape)) for dtype, shape in tensors.values()]
+
+    def _check_tensors(self, *tensors):
+        index = self.device.index
+        try:
+            for (dtype, shape), t in zip(self._spec, tensors):
+                if not (t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous()):
+                    break
+            else:
+                return
+        except AttributeError:
+            pass  # (no tensor)
+        for name, (dtype, shape), t in zip(self._names, self._spec, tensors):
             _check(name, t, dtype, shape, self.device)
 
+    def _launch(self, *args):
+        """The call on the device's current stream (the library works on the current device)."""
+        index = self.device.index
+        stream = _stream(index)
+        if _current_device() == index:
+            status = self._fn(*args, stream)
+        else:
+            with torch.cuda.device(self.device):
+                status = self._fn(*args, stream)
+        if status:
+            _lib.check(status, self._name)
 
-class ExpertLinear(_Checked):
+
+def _sizes(T, *sizes):
+    return (ctypes.c_int64(T),) + tuple(map(ctypes.c_int32, sizes))
+
+
+def _selection(T, M, k):
+    i32 = torch.int32
+    return {"idx": (i32, (T, k)), "offsets": (i32, (M + 1,)), "sorted": (i32, (T * k,))}
+
+
+class ExpertLinear(_Call):
     """Pre-allocated output and workspace for repeated expert_linear calls with one shape."""
 
     def __init__(self, T: int, K: int, N: int, M: int, k: int, *, out_dtype=torch.bfloat16, device=None):
-        self.shape, self.spec, self.y_bits = (T, K, N, M, k), _spec(T, K, N, M, k), _y_bits(out_dtype)
-        self.device = _device(device)
+        bf16 = torch.bfloat16
+        self.shape, self.y_bits, self._sizes = (T, K, N, M, k), _y_bits(out_dtype), _sizes(T, K, N, M, k)
+        self._prepare("more_expert_linear", device, x=(bf16, (T, K)), Wt=(bf16, (M, N, K)), **_selection(T, M, k))
         self.workspace_bytes = expert_linear_workspace_size(*self.shape)
         self.workspace = _workspace(self.workspace_bytes, self.device)
         self.y = torch.empty((T * k, N), dtype=out_dtype, device=self.device)
 
     def __call__(self, x, Wt, idx, offsets, sorted) -> torch.Tensor:
-        self._checks(x=x, Wt=Wt, idx=idx, offsets=offsets, sorted=sorted)
-        _call("more_expert_linear", self.device, _ptr(x), _ptr(Wt), *self.shape, _ptr(idx), _ptr(offsets),
-              _ptr(sorted), _ptr(self.y), self.y_bits, _ptr(self.workspace), self.workspace_bytes)
+        self._check_tensors(x, Wt, idx, offsets, sorted)
+        self._launch(x.data_ptr(), Wt.data_ptr(), *self._sizes, idx.data_ptr(), offsets.data_ptr(), sorted.data_ptr(),
+                     self.y.data_ptr(), self.y_bits, self.workspace.data_ptr(), self.workspace_bytes)
         return self.y
 
 
@@ -118,24 +152,27 @@ class LinearGradients:
     dWt: Optional[torch.Tensor]  # bfloat16 [M][N][K]
 
 
-class ExpertLinearBackward(_Checked):
+class ExpertLinearBackward(_Call):
     """Pre-allocated gradients and workspace for repeated expert_linear_backward calls with one shape; either
     gradient may be left out."""
 
     def __init__(self, T: int, K: int, N: int, M: int, k: int, *, need_dx: bool = True, need_dW: bool = True, device=None):
         if not (need_dx or need_dW):
             raise ValueError("need_dx or need_dW must be set")
-        self.shape, self.spec = (T, K, N, M, k), _spec(T, K, N, M, k)
-        self.device = dev = _device(device)
+        bf16 = torch.bfloat16
+        self.shape, self._sizes = (T, K, N, M, k), _sizes(T, K, N, M, k)
+        self._prepare("more_expert_linear_backward", device, x=(bf16, (T, K)), Wt=(bf16, (M, N, K)), **_selection(T, M, k),
+                      dy=(bf16, (T * k, N)))
+        dev = self.device
         self.workspace_bytes = expert_linear_backward_workspace_size(*self.shape)
         self.workspace = _workspace(self.workspace_bytes, dev)
-        self.dx = torch.empty((T, K), dtype=torch.bfloat16, device=dev) if need_dx else None
-        self.dWt = torch.empty((M, N, K), dtype=torch.bfloat16, device=dev) if need_dW else None
+        self.dx = torch.empty((T, K), dtype=bf16, device=dev) if need_dx else None
+        self.dWt = torch.empty((M, N, K), dtype=bf16, device=dev) if need_dW else None
 
     def __call__(self, x, Wt, idx, offsets, sorted, dy) -> LinearGradients:
-        self._checks(x=x, Wt=Wt, idx=idx, offsets=offsets, sorted=sorted, dy=dy)
-        _call("more_expert_linear_backward", self.device, _ptr(x), _ptr(Wt), *self.shape, _ptr(idx), _ptr(offsets),
-              _ptr(sorted), _ptr(dy), _ptr(self.dx), _ptr(self.dWt), _ptr(self.workspace), self.workspace_bytes)
+        self._check_tensors(x, Wt, idx, offsets, sorted, dy)
+        self._launch(x.data_ptr(), Wt.data_ptr(), *self._sizes, idx.data_ptr(), offsets.data_ptr(), sorted.data_ptr(),
+                     dy.data_ptr(), _ptr(self.dx), _ptr(self.dWt), self.workspace.data_ptr(), self.workspace_bytes)
         return LinearGradients(self.dx, self.dWt)
 
 
@@ -154,19 +191,19 @@ class QuantizedRows:
     scale: torch.Tensor  # float32, x's shape without the last dimension
 
 
-class QuantizeRows:
+class QuantizeRows(_Call):
     """Pre-allocated outputs for repeated quantize_rows calls with one shape (T rows of `width` values; gated: of
     2 width)."""
 
     def __init__(self, T: int, width: int, *, gated: bool = False, device=None):
-        self.shape, self.gated, self.device = (T, width), bool(gated), _device(device)
+        self.shape, self.gated, self._sizes = (T, width), bool(gated), _sizes(T, width, bool(gated))
+        self._prepare("more_quantize_rows", device, x=(torch.bfloat16, (T, 2 * width if gated else width)))
         self.q = torch.empty((T, width), dtype=torch.int8, device=self.device)
         self.scale = torch.empty((T,), dtype=torch.float32, device=self.device)
 
     def __call__(self, x) -> QuantizedRows:
-        T, width = self.shape
-        _check("x", x, torch.bfloat16, (T, 2 * width if self.gated else width), self.device)
-        _call("more_quantize_rows", self.device, _ptr(x), T, width, int(self.gated), _ptr(self.q), _ptr(self.scale))
+        self._check_tensors(x)
+        self._launch(x.data_ptr(), *self._sizes, self.q.data_ptr(), self.scale.data_ptr())
         return QuantizedRows(self.q, self.scale)
 
 
@@ -185,23 +222,24 @@ def quantize_rows(x, *, gated: bool = False) -> QuantizedRows:
     return QuantizedRows(out.q.view(*lead, width), out.scale.view(lead))
 
 
-class ExpertLinearQ8(_Checked):
+class ExpertLinearQ8(_Call):
     """Pre-allocated output and workspace for repeated expert_linear_q8 calls with one shape."""
 
     def __init__(self, T: int, K: int, N: int, M: int, k: int, *, out_dtype=torch.bfloat16, device=None):
-        self.shape, self.spec, self.y_bits = (T, K, N, M, k), _spec(T, K, N, M, k, torch.int8), _y_bits(out_dtype)
-        self.device = _device(device)
+        i8, f32 = torch.int8, torch.float32
+        self.shape, self.y_bits, self._sizes = (T, K, N, M, k), _y_bits(out_dtype), _sizes(T, K, N, M, k)
+        self._prepare("more_expert_linear_q8", device, q=(i8, (T, K)), q_scale=(f32, (T,)), Wq=(i8, (M, N, K)),
+                      w_scale=(f32, (M, N)), **_selection(T, M, k), gate=(f32, (T, k)))
         self.workspace_bytes = expert_linear_q8_workspace_size(*self.shape)
         self.workspace = _workspace(self.workspace_bytes, self.device)
         self.y = torch.empty((T * k, N), dtype=out_dtype, device=self.device)
 
     def __call__(self, q, q_scale, Wq, w_scale, idx, offsets, sorted, gate=None) -> torch.Tensor:
-        self._checks(q=q, q_scale=q_scale, Wq=Wq, w_scale=w_scale, idx=idx, offsets=offsets, sorted=sorted)
-        if gate is not None:
-            self._checks(gate=gate)
-        _call("more_expert_linear_q8", self.device, _ptr(q), _ptr(q_scale), _ptr(Wq), _ptr(w_scale), *self.shape,
-              _ptr(idx), _ptr(offsets), _ptr(sorted), _ptr(gate), _ptr(self.y), self.y_bits, _ptr(self.workspace),
-              self.workspace_bytes)
+        given = (q, q_scale, Wq, w_scale, idx, offsets, sorted)
+        self._check_tensors(*given if gate is None else (*given, gate))
+        self._launch(q.data_ptr(), q_scale.data_ptr(), Wq.data_ptr(), w_scale.data_ptr(), *self._sizes, idx.data_ptr(),
+                     offsets.data_ptr(), sorted.data_ptr(), _ptr(gate), self.y.data_ptr(), self.y_bits,
+                     self.workspace.data_ptr(), self.workspace_bytes)
         return self.y
 
 

@@ -223,4 +223,4 @@ def test_autograd_function_around_the_calls():
     want = torch.matmul(V[idx.long().view(-1)], X.repeat_interleave(2, 0)[:, :, None])[:, :, 0]
     (want * c.double()).sum().backward()
     for a, b in ((y, want), (x.grad, X.grad), (W.grad, V.grad)):
-        assert float((a.double() - b).norm() / b.norm()) <= 2.0 ** -8
+        assert float((a.detach().double() - b.detach()).norm() / b.detach().norm()) <= 2.0 ** -8
