@@ -11,6 +11,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "ffn_device.h"
 #include "linear.h"
@@ -22,6 +23,8 @@ namespace more {
 // A workgroup computes a tile's rows of y, `span` columns in steps of COLS: the rows of W are the M side, the
 // entries' rows of x the N side.  The pipeline runs over (column step, contraction step) pairs, so that a
 // short contraction does not drain it.
+// LINES: y is stored in whole lines by way of LDS, where a wave has whole lines of a row (us, in halves of lines : whole,
+// 65536 rows, N = 2048, 16 experts, bf16 K = 128 115 : 78, K = 512 194 : 173; 32 experts of 2048 x 2048, 32768 entries 290 : 280).
 template <int BM, int COLS, int STAGES>
 struct LinearShape {
     static constexpr int kWaves = BM == 256 ? 8 : 4;
@@ -36,14 +39,16 @@ struct LinearShape {
 };
 
 constexpr int linear_threads(int bm) { return bm == 256 ? 512 : 256; }
-template <bool I8, int BM, int COLS, int STAGES>
+template <bool I8, int BM, int COLS, int STAGES, bool LINES>
 __global__ __launch_bounds__(linear_threads(BM), 2) void linear_kernel(LinearArgs a, const void* __restrict__ list,
                                                                     int32_t span) {
     using S = LinearShape<BM, COLS, STAGES>;
     using Type = LinearType<I8>;
-    static_assert(S::kThreads == linear_threads(BM), "");
-    __shared__ __attribute__((aligned(1024))) char smem_raw[STAGES * S::kStageBytes];
+    static_assert(S::kThreads == linear_threads(BM) && (!LINES || S::kM % 4 == 0), "");
+    constexpr int kRing = STAGES * S::kStageBytes;
+    __shared__ __attribute__((aligned(1024))) char smem_raw[kRing + (LINES ? S::kWaves * kLinesScratch : 0)];
     LdsChar* smem = (LdsChar*)smem_raw;
+    LdsChar* lines = smem + (LINES ? kRing + ffn_wave() * kLinesScratch : 0);
     const FfnTile* tiles = ffn_tile_list(list);
     const int32_t len = a.len, N = a.N;
     const int32_t n = a.T * a.k;
@@ -127,33 +132,59 @@ __global__ __launch_bounds__(linear_threads(BM), 2) void linear_kernel(LinearArg
                 },
                 [&] {
                     if (++ck < ksteps) return;
-                    if (S::kM % 2 == 0 && !a.wide) {
+                    auto store_lines = [&](auto wide) {
+                        using L = Lines<decltype(wide)::value>;
+                        using Out = typename L::Element;
 #pragma unroll
-                        for (int j = 0; j < S::kN; ++j)
+                        for (int i0 = 0; i0 < S::kM; i0 += L::kTiles) {
+                            const int32_t c = cc + 16 * (wm * S::kM + i0);
+                            f32x4 ws[L::kTiles];
 #pragma unroll
-                            for (int i = 0; i < S::kM; i += 2) {
-                                const int32_t c = cc + 16 * (wm * S::kM + i);
-                                const u32x4 v = linear_pair(linear_value<I8>(a, acc[i][j], row_scale[j], w_scale, c),
-                                                            linear_value<I8>(a, acc[i + 1][j], row_scale[j], w_scale, c + 16));
-                                const int32_t mine = c + 8 * (lane >> 4);
+                            for (int i = 0; i < L::kTiles; ++i) ws[i] = linear_w_scale<I8>(w_scale, c + 16 * i, N);
+#pragma unroll
+                            for (int j = 0; j < S::kN; ++j) {
+#pragma unroll
+                                for (int i = 0; i < L::kTiles; ++i)
+                                    L::place(lines, i, linear_value<I8>(acc[i0 + i][j], row_scale[j], ws[i]));
+                                L::store(lines, c1 - c, [&](int r) -> Out* {
+                                    const uint32_t p = (uint32_t)__shfl((int)place[j], r, 64);
+                                    return p < (uint32_t)n ? static_cast<Out*>(a.y) + (int64_t)p * N + c : nullptr;
+                                });
+                            }
+                        }
+                    };
+                    if constexpr (LINES) {
+                        if (a.wide) store_lines(std::true_type{});
+                        else store_lines(std::false_type{});
+                    } else if (S::kM % 2 == 0 && !a.wide) {
+#pragma unroll
+                        for (int i = 0; i + 1 < S::kM; i += 2) {
+                            const int32_t c = cc + 16 * (wm * S::kM + i), mine = c + 8 * (lane >> 4);
+                            const f32x4 ws0 = linear_w_scale<I8>(w_scale, c, N), ws1 = linear_w_scale<I8>(w_scale, c + 16, N);
+#pragma unroll
+                            for (int j = 0; j < S::kN; ++j) {
+                                const u32x4 v = linear_pair(linear_value<I8>(acc[i][j], row_scale[j], ws0),
+                                                            linear_value<I8>(acc[i + 1][j], row_scale[j], ws1));
                                 if (place[j] < (uint32_t)n && mine < c1)
                                     *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.y) + (int64_t)place[j] * N + mine) = v;
-                                acc[i][j] = acc[i + 1][j] = Type::zero();
                             }
-                        ck = 0;
-                        cc += COLS;
-                        return;
-                    }
-#pragma unroll
-                    for (int j = 0; j < S::kN; ++j) {
+                        }
+                    } else {
 #pragma unroll
                         for (int i = 0; i < S::kM; ++i) {
-                            const int32_t c = cc + 16 * (wm * S::kM + i);
-                            if (place[j] < (uint32_t)n && c + 4 * (lane >> 4) < c1)
-                                linear_store<I8>(a, acc[i][j], row_scale[j], w_scale, place[j], c);
-                            acc[i][j] = Type::zero();
+                            const int32_t c = cc + 16 * (wm * S::kM + i), mine = c + 4 * (lane >> 4);
+                            const f32x4 ws = linear_w_scale<I8>(w_scale, c, N);
+#pragma unroll
+                            for (int j = 0; j < S::kN; ++j)
+                                if (place[j] < (uint32_t)n && mine < c1)
+                                    linear_put(a.y, a.wide, (int64_t)place[j] * N + mine,
+                                               linear_value<I8>(acc[i][j], row_scale[j], ws));
                         }
                     }
+#pragma unroll
+                    for (int i = 0; i < S::kM; ++i)
+#pragma unroll
+                        for (int j = 0; j < S::kN; ++j) acc[i][j] = Type::zero();
                     ck = 0;
                     cc += COLS;
                 }));
@@ -239,8 +270,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a
         const float* w_scale = I8 ? a.w_scale + (int64_t)f.expert * N : nullptr;
 #pragma unroll
         for (int r = 0; r < kR; ++r) {
-            const int32_t c = c0 + 16 * r;
-            if (c + 4 * (lane >> 4) < N) linear_store<I8>(a, acc[r], row_scale, w_scale, f.p, c);
+            const int32_t c = c0 + 16 * r, at_c = c + 4 * (lane >> 4);
+            const f32x4 v = linear_value<I8>(acc[r], row_scale, linear_w_scale<I8>(w_scale, c, N));
+            if (at_c < N) linear_put(a.y, a.wide, (int64_t)f.p * N + at_c, v);
         }
     }
 }
@@ -252,9 +284,9 @@ constexpr int64_t kMaxBlocks = 1 << 19;
 unsigned grid_of(int64_t items) { return (unsigned)(std::min<int64_t>((items + 7) / 8, kMaxBlocks / 8) * 8); }
 unsigned few_grid(int64_t items) { return (unsigned)std::min<int64_t>(items, 1 << 22); }
 
-template <bool I8, int BM, int COLS, int STAGES>
+template <bool I8, int BM, int COLS, int STAGES, bool LINES = (BM >= 64 && COLS >= 128)>
 void tiled(const LinearPlan& p, const LinearArgs& a, const char* ws, hipStream_t stream) {
-    linear_kernel<I8, BM, COLS, STAGES>
+    linear_kernel<I8, BM, COLS, STAGES, LINES>
         <<<grid_of(p.tiles.tiles * ((a.N + p.span - 1) / p.span)), linear_threads(BM), 0, stream>>>(
             a, ws + p.tiles.off_tiles, p.span);
 }
@@ -287,7 +319,7 @@ void forward(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t str
 // the CU hides it.  Fitted to the maps and dx of 130 shapes (1 to 512 experts, 32 to 16384 rows each, contractions and
 // columns of 64 to 2048): 1.8 % off the best on geometric mean, 28 % at most.  us for 32 : 64 : 128 : 256 rows, dense maps of
 // 1024 rows of K = N = 1024 16 : 19 : 22 : 34 (dx), 8 experts of 4096 rows, K = 2048, N = 256 109 : 64 : 61 : 56.
-int32_t linear_tile_rows(int64_t n, int32_t M, int32_t cols, int32_t cols_of, int64_t steps) {
+int32_t linear_tile_rows(int64_t n, int32_t M, int32_t cols, int32_t cols_of, int64_t steps, bool q8) {
     if (n / std::max<int64_t>(1, std::min<int64_t>(n, M)) < 24) return 32;
     int32_t best = 64;
     int64_t least = INT64_MAX;
@@ -296,7 +328,7 @@ int32_t linear_tile_rows(int64_t n, int32_t M, int32_t cols, int32_t cols_of, in
         const int32_t step = bm == 256 ? 256 : cols_of;
         const int64_t items = tiles2 * ((cols + step - 1) / step) / 2, slots = bm == 256 ? 256 : 512;
         const bool alone = items <= 256;
-        const int64_t stage = bm == 256 ? 30 : bm == 128 ? (alone ? 16 : 20) : bm == 64 ? (alone ? 11 : 15) : alone ? 9 : 18;
+        const int64_t stage = bm == 256 ? (q8 ? 20 : 28) : bm == 128 ? (alone ? 16 : 20) : bm == 64 ? (alone ? 11 : 15) : alone ? 9 : 18;
         const int64_t cost = (items + slots - 1) / slots * (steps * stage + (bm == 256 ? 60 : 0));
         if (cost < least) {
             least = cost;
@@ -313,7 +345,7 @@ void linear_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, b
     const int64_t n = T * k;
     *p = LinearPlan{};
     p->cols = N <= 64 ? 64 : 128;
-    const int32_t bm = linear_tile_rows(n, M, N, p->cols, (len + kFfnBK - 1) / kFfnBK);
+    const int32_t bm = linear_tile_rows(n, M, N, p->cols, (len + kFfnBK - 1) / kFfnBK, q8);
     ffn_tiles_plan(n, M, bm, &p->tiles);
     // The kernel without tiles saves a launch and the latency of the stages (3 us) while the rows of W that its
     // workgroups read, once for every 16 entries, are few, and the entries' rows of x that each reads again, and

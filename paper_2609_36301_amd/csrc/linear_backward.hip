@@ -36,6 +36,7 @@ struct DxShape {
     static constexpr int kN = BM / (kWaves / kWavesM) / 16;
     static constexpr int kRowsAt = COLS * 128;
     static constexpr int kStageBytes = kRowsAt + BM * 128;
+    static constexpr bool kLines = kM % 4 == 0;  // a wave's columns are whole lines of dx
 };
 
 // DIRECT: one entry per token, `out` is dx (bf16); else the shares (fp32).
@@ -43,8 +44,10 @@ template <int BM, int COLS, bool DIRECT>
 __global__ __launch_bounds__(dx_threads(BM), 2) void linear_dx_kernel(LinearArgs a, const void* __restrict__ list,
                                                                   int32_t span, void* __restrict__ out) {
     using S = DxShape<BM, COLS>;
-    __shared__ __attribute__((aligned(1024))) char smem_raw[2 * S::kStageBytes];
+    constexpr int kRing = 2 * S::kStageBytes;
+    __shared__ __attribute__((aligned(1024))) char smem_raw[kRing + (S::kLines ? S::kWaves * kLinesScratch : 0)];
     LdsChar* smem = (LdsChar*)smem_raw;
+    LdsChar* lines = smem + (S::kLines ? kRing + ffn_wave() * kLinesScratch : 0);
     const FfnTile* tiles = ffn_tile_list(list);
     const int32_t n = a.T * a.k, len = a.N, cols = a.len;
     const int32_t spans = (cols + span - 1) / span;
@@ -118,7 +121,22 @@ __global__ __launch_bounds__(dx_threads(BM), 2) void linear_dx_kernel(LinearArgs
         };
         auto done = [&] {
             if (++ck < ksteps) return;
-            if constexpr (DIRECT && S::kM % 2 == 0) {
+            if constexpr (S::kLines) {
+                using L = Lines<!DIRECT>;
+                using Out = typename L::Element;
+#pragma unroll
+                for (int j = 0; j < S::kN; ++j)
+#pragma unroll
+                    for (int i0 = 0; i0 < S::kM; i0 += L::kTiles) {
+#pragma unroll
+                        for (int i = 0; i < L::kTiles; ++i) L::place(lines, i, acc[i0 + i][j]);
+                        const int32_t c = cc + 16 * (wm * S::kM + i0);
+                        L::store(lines, c1 - c, [&](int r) -> Out* {
+                            const uint32_t p = (uint32_t)__shfl((int)place[j], r, 64);
+                            return p < (uint32_t)n ? static_cast<Out*>(out) + (int64_t)p * cols + c : nullptr;
+                        });
+                    }
+            } else if constexpr (DIRECT && S::kM % 2 == 0) {
 #pragma unroll
                 for (int j = 0; j < S::kN; ++j)
 #pragma unroll
@@ -127,28 +145,20 @@ __global__ __launch_bounds__(dx_threads(BM), 2) void linear_dx_kernel(LinearArgs
                         const u32x4 v = linear_pair(acc[i][j], acc[i + 1][j]);
                         if (place[j] < (uint32_t)n && c < c1)
                             *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + (int64_t)place[j] * cols + c) = v;
-                        acc[i][j] = acc[i + 1][j] = zero_f32x4();
                     }
-                ck = 0;
-                cc += COLS;
-                return;
+            } else {
+#pragma unroll
+                for (int j = 0; j < S::kN; ++j)
+#pragma unroll
+                    for (int i = 0; i < S::kM; ++i) {
+                        const int32_t c = cc + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
+                        if (place[j] < (uint32_t)n && c < c1) linear_put(out, !DIRECT, (int64_t)place[j] * cols + c, acc[i][j]);
+                    }
             }
 #pragma unroll
-            for (int j = 0; j < S::kN; ++j) {
+            for (int i = 0; i < S::kM; ++i)
 #pragma unroll
-                for (int i = 0; i < S::kM; ++i) {
-                    const int32_t c = cc + 16 * (wm * S::kM + i) + 4 * (lane >> 4);
-                    const f32x4 v = acc[i][j];
-                    if (place[j] < (uint32_t)n && c < c1) {
-                        const int64_t at = (int64_t)place[j] * cols + c;
-                        if constexpr (DIRECT)
-                            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = pack_bf16x4(v[0], v[1], v[2], v[3]);
-                        else
-                            *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = v;
-                    }
-                    acc[i][j] = zero_f32x4();
-                }
-            }
+                for (int j = 0; j < S::kN; ++j) acc[i][j] = zero_f32x4();
             ck = 0;
             cc += COLS;
         };
@@ -201,17 +211,17 @@ __global__ __launch_bounds__(dx_threads(BM), 2) void linear_dx_kernel(LinearArgs
 // PARTS: the entries of an expert are cut into `runs` runs and a workgroup takes one tile and one run; the fp32
 // results of run i go to parts + i M N K.
 struct LinearDw {
-    int32_t span, runs, once;  // once: nontemporal stores (whole lines)
+    int32_t span, runs;
     float* parts;
 };
 
 template <int CT, int RT, int WAVES, bool BY_COLS, bool PARTS>
 __global__ __launch_bounds__(64 * WAVES, 2) void linear_dw_kernel(LinearArgs a, LinearDw d) {
     constexpr int kStageBytes = (CT + RT) * 128;
-    __shared__ __attribute__((aligned(1024))) char smem_raw[2 * kStageBytes];
-    __shared__ __attribute__((aligned(16))) char scratch_raw[WAVES * kFfnScratch];
+    constexpr int kRing = 2 * kStageBytes;
+    __shared__ __attribute__((aligned(1024))) char smem_raw[kRing + (PARTS ? 0 : WAVES * kLinesScratch)];
     LdsChar* smem = (LdsChar*)smem_raw;
-    LdsChar* scratch = (LdsChar*)scratch_raw + ffn_wave() * kFfnScratch;
+    LdsChar* lines = smem + (PARTS ? 0 : kRing + ffn_wave() * kLinesScratch);
     constexpr int kWavesM = CT >= 128 ? 2 : 1, kWavesN = WAVES / kWavesM;
     constexpr int kM = CT / kWavesM / 16, kN = RT / kWavesN / 16;  // 16 x 16 tiles per wave
     static_assert(kM % 4 == 0, "whole lines of dW: 64 columns");
@@ -281,19 +291,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void linear_dw_kernel(LinearArgs a, 
                 for (int i0 = 0; i0 < kM; i0 += 4) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        place_bf16(scratch, i, acc[i0 + i][j]);
+                        Lines<false>::place(lines, i, acc[i0 + i][j]);
                         acc[i0 + i][j] = zero_f32x4();
                     }
                     const int32_t c = (BY_COLS ? cs : other) + 16 * (wm * kM + i0);
                     const int32_t r = (BY_COLS ? other : cs) + 16 * (wn * kN + j);
-                    const int32_t left = ((BY_COLS ? s1 : K) - c) * 2;
-                    auto row_of = [&](int row) {
+                    Lines<false>::store(lines, (BY_COLS ? s1 : K) - c, [&](int row) {
                         return r + row < (BY_COLS ? N : s1) ? o + (int64_t)(r + row) * K + c : nullptr;
-                    };
-                    if (d.once)
-                        flush_rows<true>(scratch, left, row_of);
-                    else
-                        flush_rows<false>(scratch, left, row_of);
+                    });
                 }
             cs += kStep;
         };
@@ -392,7 +397,6 @@ void dw_launch(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t s
     LinearDw d;
     d.span = p.dw_span;
     d.runs = p.dw_parts;
-    d.once = a.len % 64 == 0;
     d.parts = reinterpret_cast<float*>(ws + p.off_parts);
     const unsigned blocks = grid_of(dw_items(p, a.len, a.N, a.M, BY_COLS) * d.runs);
     if (p.dw_parts > 1) {
@@ -427,7 +431,7 @@ void linear_backward_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int
     const int64_t n = T * k;
     *p = LinearPlan{};
     p->cols = len <= 64 ? 64 : 128;
-    const int32_t bm = linear_tile_rows(n, M, len, p->cols, (N + kFfnBK - 1) / kFfnBK);
+    const int32_t bm = linear_tile_rows(n, M, len, p->cols, (N + kFfnBK - 1) / kFfnBK, false);
     ffn_tiles_plan(n, M, bm, &p->tiles);
     if (bm == 256) p->cols = 256;
     p->span = ffn_span(N, p->cols, p->tiles.tiles, len);

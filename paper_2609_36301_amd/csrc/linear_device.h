@@ -1,6 +1,8 @@
 // Device helpers of the experts' linear maps (gfx950): the two operand types, and how results are stored.
 #pragma once
 
+#include <type_traits>
+
 #include "ffn_device.h"
 #include "linear.h"
 
@@ -37,23 +39,19 @@ __device__ __forceinline__ void linear_put(void* out, bool wide, int64_t at, f32
     else
         *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = pack_bf16x4(v[0], v[1], v[2], v[3]);
 }
-// c: the first of the accumulator's 16 columns.
+// The factors of the lane's four of 16 columns from c on (columns past the last are not stored).
 template <bool I8>
-__device__ __forceinline__ f32x4 linear_value(const LinearArgs& a, typename LinearType<I8>::Acc acc, float row_scale,
-                                              const float* w_scale, int32_t c) {
-    if constexpr (!I8) return acc;
-    // (columns past the last are not stored)
-    const f32x4 ws = *reinterpret_cast<const f32x4*>(w_scale + min(c + 4 * (ffn_lane() >> 4), a.N - 4));
-    f32x4 v;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = (float)acc[q] * ws[q] * row_scale;
-    return v;
+__device__ __forceinline__ f32x4 linear_w_scale(const float* w_scale, int32_t c, int32_t N) {
+    if constexpr (!I8) return zero_f32x4();
+    return *reinterpret_cast<const f32x4*>(w_scale + min(c + 4 * (ffn_lane() >> 4), N - 4));
 }
 template <bool I8>
-__device__ __forceinline__ void linear_store(const LinearArgs& a, typename LinearType<I8>::Acc acc, float row_scale,
-                                             const float* w_scale, uint32_t p, int32_t c) {
-    linear_put(a.y, a.wide, (int64_t)p * a.N + c + 4 * (ffn_lane() >> 4),
-               linear_value<I8>(a, acc, row_scale, w_scale, c));
+__device__ __forceinline__ f32x4 linear_value(typename LinearType<I8>::Acc acc, float row_scale, f32x4 w_scale) {
+    if constexpr (!I8) return acc;
+    f32x4 v;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = (float)acc[q] * w_scale[q] * row_scale;
+    return v;
 }
 // Two neighbouring accumulators in bf16, exchanged among the lanes of a row so that a lane holds eight of its 32 columns,
 // the ones from 8 (l / 16) on: stored 16 bytes a lane, a row's 64 bytes are whole (8 bytes a lane, as the
@@ -66,6 +64,44 @@ __device__ __forceinline__ u32x4 linear_pair(f32x4 a, f32x4 b) {
     s = __builtin_amdgcn_permlane16_swap(s[0], s[1], false, false);
     return u32x4{(uint32_t)r[0], (uint32_t)s[0], (uint32_t)r[1], (uint32_t)s[1]};
 }
+// Whole lines: 16 rows of 128 bytes (64 columns of bf16, 32 of fp32) by way of a wave's own 2 KiB of LDS, from where a
+// store takes eight rows.  The 16-byte pieces of a row are XORed with the row's number, which spreads them over the banks.
+// A wave's LDS accesses are in order, so there is no barrier.  Nontemporal whole lines reach memory without being read
+// first: the gradients of 4096 experts, N = 512, K = 64, 32 rows 65 us, plain lines 98, nontemporal halves of lines 84; also
+// where K splits the lines (K = 72 122 : 164).
+constexpr int kLinesScratch = 16 * 128;
+template <bool WIDE>
+struct Lines {
+    static constexpr int kTiles = WIDE ? 2 : 4;  // accumulators of 16 columns to a line
+    using Element = typename std::conditional<WIDE, float, uint16_t>::type;
+    // accumulator i of the line
+    static __device__ __forceinline__ void place(LdsChar* scratch, int i, f32x4 v) {
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        const int l = ffn_lane(), row = l & 15, g = l >> 4;
+        if constexpr (WIDE) {
+            *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(scratch + row * 128 + (((4 * i + g) ^ (row & 7)) << 4)) = v;
+        } else {
+            const uint2 b = pack_bf16x4(v[0], v[1], v[2], v[3]);
+            *reinterpret_cast<__attribute__((address_space(3))) u32x2*>(
+                scratch + row * 128 + (((2 * i + (g >> 1)) ^ (row & 7)) << 4) + ((g & 1) << 3)) = u32x2{b.x, b.y};
+        }
+    }
+    // row_of(r): where row r goes (NULL: nowhere); `left` elements of it at most (whole pieces)
+    template <typename F>
+    static __device__ __forceinline__ void store(LdsChar* scratch, int left, F row_of) {
+        const int l = ffn_lane(), piece = l & 7;
+#pragma unroll
+        for (int r = 0; r < 16; r += 8) {
+            const int row = r + (l >> 3);
+            char* p = reinterpret_cast<char*>(row_of(row));
+            const u32x4 v =
+                *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(scratch + row * 128 + ((piece ^ (row & 7)) << 4));
+            if (p && piece * (16 / (int)sizeof(Element)) < left)
+                __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p + 16 * piece));
+        }
+    }
+};
+
 // Zeros to columns c .. c + 7 of entry p's row.
 __device__ __forceinline__ void linear_zero(const LinearArgs& a, uint32_t p, int32_t c) {
     const int64_t at = (int64_t)p * a.N + c;

@@ -38,6 +38,7 @@ struct StreamTile {
 struct StreamLds {
     char stage[2][kStageBytes];
     StreamTile ahead[3];
+    char lines[kStreamWaves][kLinesScratch];
 };
 typedef __attribute__((address_space(3))) StreamLds LdsStream;
 typedef __attribute__((address_space(3))) StreamTile LdsTile;
@@ -91,6 +92,7 @@ __global__ __launch_bounds__(kStreamThreads, 2) void linear_stream_kernel(Linear
     const int32_t spans = (cols + kTile - 1) / kTile, ksteps = (len + kFfnBK - 1) / kFfnBK;
     const int wave = ffn_wave(), lane = ffn_lane();
     const int wm = wave % kWavesM, wn = wave / kWavesM;
+    LdsChar* lines = (LdsChar*)lds->lines[wave];
     const FfnTile* tiles = ffn_tile_list(list);
     // this XCD's share of the work: items [base, base + count)
     const int64_t total = (int64_t)list[1] * spans, share = (total + 7) / 8;
@@ -227,7 +229,6 @@ __global__ __launch_bounds__(kStreamThreads, 2) void linear_stream_kernel(Linear
 #pragma unroll
                     for (int j = 0; j < kN; ++j) {
                         const int32_t row0 = 16 * (wn * kN + j), row = row0 + (lane & 15);
-                        const uint32_t p = t->entry[row];
                         const float factor = a.gate ? t->x_scale[row] * t->gate[row] : t->x_scale[row];
                         auto value = [&](int i) {
                             const f32x4 ws = *reinterpret_cast<LdsF32x4*>(t->w_scale + in_tile + 16 * i);
@@ -236,22 +237,23 @@ __global__ __launch_bounds__(kStreamThreads, 2) void linear_stream_kernel(Linear
                             for (int q = 0; q < 4; ++q) v[q] = (float)acc[i][j][q] * ws[q] * factor;
                             return v;
                         };
-                        if (a.wide) {
-                            float* y = static_cast<float*>(a.y) + (int64_t)p * cols + c0;
+                        auto store = [&](auto wide) {
+                            using L = Lines<decltype(wide)::value>;
+                            using Out = typename L::Element;
 #pragma unroll
-                            for (int i = 0; i < kM; ++i)
-                                if (row < t->tile.rows && p < (uint32_t)n && c0 + 16 * i < cols)
-                                    *reinterpret_cast<f32x4*>(y + 16 * i) = value(i);
-                        } else {
-                            const int32_t mine = c0 + 4 * (lane >> 4);
-                            uint16_t* y = static_cast<uint16_t*>(a.y) + (int64_t)p * cols + mine;
+                            for (int i0 = 0; i0 < kM; i0 += L::kTiles) {
 #pragma unroll
-                            for (int i = 0; i < kM; i += 2) {
-                                const u32x4 v = linear_pair(value(i), value(i + 1));
-                                if (row < t->tile.rows && p < (uint32_t)n && mine + 16 * i < cols)
-                                    *reinterpret_cast<u32x4*>(y + 16 * i) = v;
+                                for (int i = 0; i < L::kTiles; ++i) L::place(lines, i, value(i0 + i));
+                                const int32_t c = c0 - 4 * (lane >> 4) + 16 * i0;
+                                L::store(lines, cols - c, [&](int r) -> Out* {
+                                    const uint32_t e = t->entry[row0 + r];
+                                    return row0 + r < t->tile.rows && e < (uint32_t)n
+                                               ? static_cast<Out*>(a.y) + (int64_t)e * cols + c : nullptr;
+                                });
                             }
-                        }
+                        };
+                        if (a.wide) store(std::true_type{});
+                        else store(std::false_type{});
 #pragma unroll
                         for (int i = 0; i < kM; ++i) acc[i][j] = Type::zero();
                     }
