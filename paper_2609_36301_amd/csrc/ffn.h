@@ -59,9 +59,6 @@ void ffn_backward_make_plan(int64_t T, int32_t h, int32_t s, int32_t M, int32_t 
 hipError_t ffn_launch(const FfnPlan& p, FfnArgs a, uint16_t* y, void* workspace, hipStream_t stream);
 hipError_t ffn_backward_launch(const FfnPlan& p, FfnArgs a, void* workspace, hipStream_t stream);
 
-// out[t] = the sum of a token's k rows of `rows` (fp32 [T k][h]) in order, without those of dropped entries.
-hipError_t ffn_entry_sum_launch(const float* rows, const int32_t* idx, int32_t T, int32_t h, int32_t M, int32_t k,
-                                uint16_t* out, hipStream_t stream);
 // out[i] = the sum of `count` addends parts[q size + i] in order (size a multiple of 8).
 hipError_t ffn_parts_sum_launch(const float* parts, int32_t count, int64_t size, uint16_t* out, hipStream_t stream);
 

@@ -829,14 +829,6 @@ hipError_t ffn_backward_launch(const FfnPlan& p, FfnArgs a, void* workspace, hip
     return hipGetLastError();
 }
 
-hipError_t ffn_entry_sum_launch(const float* rows, const int32_t* idx, int32_t T, int32_t h, int32_t M, int32_t k,
-                                uint16_t* out, hipStream_t stream) {
-    const int64_t blocks = std::min<int64_t>(((int64_t)T * (h / 8) + 255) / 256, 1 << 16);
-    ffn_bwd_sum_kernel<<<(unsigned)blocks, 256, 0, stream>>>(rows, idx, T, h, M, k, out, blocks, nullptr, 0, nullptr,
-                                                             nullptr);
-    return hipGetLastError();
-}
-
 hipError_t ffn_parts_sum_launch(const float* parts, int32_t count, int64_t size, uint16_t* out, hipStream_t stream) {
     ffn_bwd_dw_sum_kernel<<<(unsigned)std::min<int64_t>((size / 8 + 255) / 256, 1 << 14), 256, 0, stream>>>(
         parts, count, size, size, out, nullptr);

@@ -153,7 +153,8 @@ struct ColTileLoader {
     // row_of(i): the address of column 0 of the lane's row in group i, or NULL (zeros); columns from
     // `cols` on (a multiple of 8) are zeros
     using Stage = Staged<kLoads>;
-    template <typename F>
+    // ONCE marks data that no other workgroup wants (nontemporal)
+    template <bool ONCE = false, typename F>
     __device__ __forceinline__ void fetch(Stage& s, int cols, F row_of) const {
 #pragma unroll
         for (int i = 0; i < kGroups; ++i) {
@@ -161,7 +162,11 @@ struct ColTileLoader {
 #pragma unroll
             for (int q = 0; q < kPanels; ++q) {
                 const int c = 64 * q + col[i];
-                s.v[i * kPanels + q] = *reinterpret_cast<const u32x4*>(r && c < cols ? r + c : ffn_zeros);
+                const u32x4* g = reinterpret_cast<const u32x4*>(r && c < cols ? r + c : ffn_zeros);
+                if constexpr (ONCE)
+                    s.v[i * kPanels + q] = __builtin_nontemporal_load(g);
+                else
+                    s.v[i * kPanels + q] = *g;
             }
         }
     }

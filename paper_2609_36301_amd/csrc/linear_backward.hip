@@ -6,7 +6,7 @@
 // left out):
 //   ffn_tiles         lists the tiles
 //   linear_dx         dy_p W_e of one tile: with one entry per token dx itself (bf16), else the entries' shares
-//                     (fp32, entry order), which ffn_entry_sum adds in the entries' order
+//                     (fp32, entry order), which linear_sum adds in the entries' order
 //   linear_dw         dW: contractions over the rows of an expert; an expert without rows gets zeros.  Long
 //                     rows of few experts are cut into runs whose fp32 sums ffn_parts_sum adds
 // Every sum runs in a fixed order: nothing is added atomically, and a call gives the same bits on every run.
@@ -37,6 +37,9 @@ struct DxShape {
     static constexpr int kRowsAt = COLS * 128;
     static constexpr int kStageBytes = kRowsAt + BM * 128;
     static constexpr bool kLines = kM % 4 == 0;  // a wave's columns are whole lines of dx
+    // An expert has one tile, mostly, and its weights lie one line after the other: nontemporal (4096 experts, K = 64,
+    // N = 512, 32 rows 68 us, without 88; of wider weights, taken 128 columns at a time, 262 : 227).
+    static constexpr bool kOnce = BM <= 64 && COLS == 64;
 };
 
 // DIRECT: one entry per token, `out` is dx (bf16); else the shares (fp32).
@@ -182,7 +185,7 @@ __global__ __launch_bounds__(dx_threads(BM), 2) void linear_dx_kernel(LinearArgs
             ffn_pipeline_staged<Stage, G::kGroups, M, F>(
                 ksteps * csteps, 16 * wn * S::kN < tile.rows,
                 [&](int, Stage& st) {
-                    weights.fetch(st.a, cols - lc, weight_row);
+                    weights.template fetch<S::kOnce>(st.a, cols - lc, weight_row);
                     rows.fetch(st.b, lk * kFfnBK, len);
                     advance();
                 },
@@ -201,6 +204,39 @@ __global__ __launch_bounds__(dx_threads(BM), 2) void linear_dx_kernel(LinearArgs
                     read_n, multiply, done));
         }
     });
+}
+
+// A thread adds eight columns of a token's k shares in order; dropped entries are left out.  The shares and ids of four
+// entries are read at a time, whether wanted or not: one after the other their reads would wait for the ids.
+__global__ __launch_bounds__(256) void linear_sum_kernel(LinearArgs a, const float* __restrict__ shares) {
+    constexpr int kAhead = 4;
+    const int32_t pieces = a.len / 8, k = a.k;
+    const int64_t total = (int64_t)a.T * pieces;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t t = i / pieces;
+        const int32_t c = (int32_t)(i - t * pieces) * 8;
+        f32x4 lo = zero_f32x4(), hi = zero_f32x4();
+        for (int32_t j0 = 0; j0 < k; j0 += kAhead) {
+            uint32_t id[kAhead];
+            f32x4 v[kAhead][2];
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) {
+                const int64_t p = t * k + min(j0 + q, k - 1);
+                id[q] = j0 + q < k ? (uint32_t)a.idx[p] : 0xFFFFFFFFu;
+                const f32x4* s = reinterpret_cast<const f32x4*>(shares + p * a.len + c);
+                v[q][0] = s[0];
+                v[q][1] = s[1];
+            }
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) {
+                if (id[q] >= (uint32_t)a.M) continue;
+                lo += v[q][0];
+                hi += v[q][1];
+            }
+        }
+        const uint2 x = pack_bf16x4(lo[0], lo[1], lo[2], lo[3]), y = pack_bf16x4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<u32x4*>(a.dx + t * a.len + c) = u32x4{x.x, x.y, y.x, y.y};
+    }
 }
 
 // ------------------------------------------------------------------------------ dW
@@ -457,8 +493,9 @@ hipError_t linear_backward_launch(const LinearPlan& p, const LinearArgs& a, void
             default: p.cols == 64 ? dx_launch<32, 64>(p, a, ws, stream) : dx_launch<32, 128>(p, a, ws, stream);
         }
         if (a.k > 1) {
-            e = ffn_entry_sum_launch(reinterpret_cast<const float*>(ws + p.off_shares), a.idx, a.T, a.len, a.M, a.k, a.dx,
-                                     stream);
+            const int64_t blocks = std::min<int64_t>(((int64_t)a.T * (a.len / 8) + 255) / 256, 1 << 16);
+            linear_sum_kernel<<<(unsigned)blocks, 256, 0, stream>>>(a, reinterpret_cast<const float*>(ws + p.off_shares));
+            e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
     }
