@@ -119,9 +119,10 @@ def test_linear_forms(form, deep):
     (T, K, N, M, k), plan = smallest(form, "linear", deep=deep and form != {"tile_rows": 0, "cols": 256})
     x, W, _, idx, offsets, srt = case(T, T, K, N, M, k, hot=True)
     announce("expert_linear T=%d K=%d N=%d M=%d k=%d %s" % (T, K, N, M, k, plan))
-    y = expert_linear(to_dev(x), to_dev(W), to_dev(idx), to_dev(offsets), to_dev(srt), out_dtype=torch.float32)
-    want, bound = ref.linear(from_bf16(x), from_bf16(W), idx, 32)
-    within(to_np(y), want, bound, "y")
+    for bits, dtype in ((16, torch.bfloat16), (32, torch.float32)):
+        y = expert_linear(to_dev(x), to_dev(W), to_dev(idx), to_dev(offsets), to_dev(srt), out_dtype=dtype)
+        want, bound = ref.linear(from_bf16(x), from_bf16(W), idx, bits)
+        within(to_np(y), want, bound, "y")
 
 
 @pytest.mark.parametrize("entries,deep", [(1, False), (2, False), (1, True)])
@@ -210,6 +211,54 @@ def test_guards_around_outputs():
             assert (big[:128] == 7).all() and (big[-128:] == 7).all()
 
 
+@pytest.mark.parametrize("M", [65537, 70000])
+def test_more_experts_than_one_list_counts(M):
+    """Beyond 2^16 experts their tiles are counted ahead of the list."""
+    require_gpu()
+    from paper_2609_36301_amd import expert_linear, expert_linear_backward, expert_linear_plan
+    T, K, N, k = 1500, 16, 16, 2
+    assert expert_linear_plan(T, K, N, M, k)["tile_rows"]
+    x, W, dy, idx, offsets, srt = case(M, T, K, N, M, k)
+    announce("expert_linear of %d experts" % M)
+    args = [to_dev(v) for v in (x, W, idx, offsets, srt)]
+    within(to_np(expert_linear(*args)), *ref.linear(from_bf16(x), from_bf16(W), idx), "y")
+    g = expert_linear_backward(*args, to_dev(dy))
+    (dx, dW), (bx, bW) = ref.linear_backward(from_bf16(x), from_bf16(W), idx, from_bf16(dy))
+    within(to_np(g.dx), dx, bx, "dx")
+    within(to_np(g.dWt), dW, bW, "dW")
+
+
+def test_offsets_and_sorted_of_another_selection():
+    """Values are undefined then; nothing outside the buffers is touched (the kernels' own checks), and every call ends."""
+    torch = require_gpu()
+    from paper_2609_36301_amd import linear
+    rng = np.random.default_rng(8)
+    for T, K, N, M, k in ((5, 32, 24, 4, 2), (300, 144, 136, 9, 3), (9000, 2064, 520, 3, 1)):
+        x, W, dy, idx, offsets, srt = case(T, T, K, N, M, k)
+        n = T * k
+        wild = rng.integers(-2 ** 31, 2 ** 31, M + 1).astype(np.int32)
+        near = rng.integers(-3, n + 4, M + 1).astype(np.int32)
+        for o, s in ((wild, srt), (near, srt), (np.zeros_like(offsets), srt), (np.full_like(offsets, n), srt),
+                     (offsets, rng.integers(-2 ** 31, 2 ** 31, n).astype(np.int32)), (offsets[::-1].copy(), np.zeros_like(srt))):
+            announce("other offsets and sorted T=%d K=%d N=%d M=%d k=%d" % (T, K, N, M, k))
+            f, b = linear.ExpertLinear(T, K, N, M, k), linear.ExpertLinearBackward(T, K, N, M, k)
+            q = linear.ExpertLinearQ8(T, K, N, M, k)
+            bufs = []
+            for obj, name in ((f, "y"), (q, "y"), (b, "dx"), (b, "dWt")):
+                size = getattr(obj, name).numel()
+                big = torch.full((size + 256,), 7.0, dtype=torch.bfloat16, device="cuda")
+                setattr(obj, name, big[128:128 + size].view(getattr(obj, name).shape))
+                bufs.append(big)
+            f(to_dev(x), to_dev(W), to_dev(idx), to_dev(o), to_dev(s))
+            b(to_dev(x), to_dev(W), to_dev(idx), to_dev(o), to_dev(s), to_dev(dy))
+            ones = lambda *shape: torch.ones(shape, device="cuda")  # noqa: E731
+            eights = lambda *shape: torch.ones(shape, device="cuda", dtype=torch.int8)  # noqa: E731
+            q(eights(T, K), ones(T), eights(M, N, K), ones(M, N), to_dev(idx), to_dev(o), to_dev(s), ones(T, k))
+            torch.cuda.synchronize()
+            for big in bufs:
+                assert (big[:128] == 7).all() and (big[-128:] == 7).all()
+
+
 def test_same_bits_every_run():
     require_gpu()
     from paper_2609_36301_amd import expert_linear, expert_linear_backward
@@ -263,6 +312,23 @@ def q8_case(T, K, N, M, k):
         want, bound = ref.linear_q8(q, qs.astype(np.float64), Wq, ws.astype(np.float64), idx,
                                     None if g is None else g.astype(np.float64), bits)
         within(to_np(y), want, bound, "y")
+
+
+def test_q8_largest_sums():
+    """65536 products of (-128)^2: 2^30, exact in the sum's 32 bits; tiles and the kernel without them."""
+    torch = require_gpu()
+    from paper_2609_36301_amd import expert_linear_q8
+    K, N, M = 65536, 264, 1
+    for T in (3, 700):
+        announce("expert_linear_q8 T=%d K=%d N=%d, largest sums" % (T, K, N))
+        q = torch.full((T, K), -128, dtype=torch.int8, device="cuda")
+        Wq = torch.full((M, N, K), -128, dtype=torch.int8, device="cuda")
+        q[T - 1, 5] = 127
+        idx = np.zeros((T, 1), np.int32)
+        offsets, srt = dispatch(idx, M)
+        y = expert_linear_q8(q, torch.ones(T, device="cuda"), Wq, torch.ones((M, N), device="cuda"), to_dev(idx), to_dev(offsets),
+                             to_dev(srt), out_dtype=torch.float32)
+        assert (y[:T - 1] == 2.0 ** 30).all() and (y[T - 1] == 2.0 ** 30 - 128 * 255).all()
 
 
 def test_q8_bad_rows_are_nan_and_alone():
