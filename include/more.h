@@ -583,6 +583,7 @@ typedef struct more_linear_plan {
     int32_t dw_cols;   /* ... and columns of a tile of dWt                                              */
     int32_t dw_runs;   /* (kind 1, else 0) runs of an expert's entries that are summed apart            */
     int32_t dw_span;   /* (kind 1, else 0) columns (dw_cols > 64) or rows of dWt that a workgroup takes */
+    int32_t listed;    /* the tiles are listed by a launch of their own; else workgroups find them       */
 } more_linear_plan;
 more_status more_expert_linear_plan(int64_t T, int32_t K, int32_t N, int32_t M, int32_t k, int32_t kind,
                                     more_linear_plan* plan);
@@ -604,8 +605,8 @@ more_status more_expert_linear_plan(int64_t T, int32_t K, int32_t N, int32_t M, 
  *   dlogits       [T] rows of V values of the logits' type, ld_dlogits apart, out, or NULL: the weighted
  *                 gradient at once.  May be logits itself (with ld_dlogits == ld).  What lies between the rows
  *                 is left as it was.
- * Limits: 1 <= V <= 2^30, 1 <= k <= MORE_TEACHER_K_MAX, V <= ld, ld_dlogits <= 2^40, T <= 2^31 - 1, tau positive
- * and finite.  Elements must be aligned to their size (rows that begin at a multiple of 16 bytes in both tensors
+ * Limits: 1 <= V <= 2^30, 1 <= k <= MORE_TEACHER_K_MAX, V <= ld, ld_dlogits <= 2^40, T <= 2^31 - 1, 2^-40 <=
+ * tau <= 2^40.  Elements must be aligned to their size (rows that begin at a multiple of 16 bytes in both tensors
  * are faster).  No workspace.
  * Numerics: fp32; sums in a fixed order; the gradient is rounded once.  -infinity among the logits is a class of
  * probability 0 (a row of nothing else has the loss NaN, as has one with a NaN or +infinity).

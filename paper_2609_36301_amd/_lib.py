@@ -36,7 +36,7 @@ class ExpertPlan(ctypes.Structure):
 class LinearPlan(ctypes.Structure):
     """more_linear_plan."""
     _fields_ = [(name, ctypes.c_int32) for name in ("tile_rows", "cols", "span", "stages", "dw_rows", "dw_cols",
-                                                    "dw_runs", "dw_span")]
+                                                    "dw_runs", "dw_span", "listed")]
 
 
 SIGNATURES = {

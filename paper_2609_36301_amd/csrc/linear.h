@@ -31,6 +31,7 @@ struct LinearArgs {
 
 struct LinearPlan {
     FfnPlan tiles;    // the tile list: n, bm, tiles, sums and their places
+    int32_t listed;   // the tiles are listed by a launch of their own
     int32_t few;      // (forward) the kernels without tiles
     int32_t split;    // (forward, without tiles) the waves of a workgroup share its columns
     int32_t cols;     // columns of a step
@@ -53,6 +54,11 @@ hipError_t linear_backward_launch(const LinearPlan& p, const LinearArgs& a, void
 // stages (linear_stream.hip), after the tile list.
 constexpr int32_t kStreamSteps = 5;
 hipError_t linear_stream_launch(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t stream);
+
+// Whether the tiles of a plan are listed by a launch of their own; else each workgroup finds its tile from the offsets, of
+// at most kLinearOwn experts.
+constexpr int32_t kLinearOwn = 1024;
+bool linear_listed(const FfnPlan& tiles, int32_t M, int64_t spans);
 
 // Lists the tiles of a plan.
 hipError_t linear_tiles_launch(const LinearPlan& p, const LinearArgs& a, void* workspace, hipStream_t stream);

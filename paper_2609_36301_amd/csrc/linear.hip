@@ -40,9 +40,9 @@ struct LinearShape {
 };
 
 constexpr int linear_threads(int bm) { return bm == 256 ? 512 : 256; }
-template <bool I8, int BM, int COLS, int STAGES, bool LINES>
+template <bool I8, int BM, int COLS, int STAGES, bool LINES, bool OWN>
 __global__ __launch_bounds__(linear_threads(BM), 2) void linear_kernel(LinearArgs a, const void* __restrict__ list,
-                                                                    int32_t span) {
+                                                                    int32_t bound, int32_t span) {
     using S = LinearShape<BM, COLS, STAGES>;
     using Type = LinearType<I8>;
     static_assert(S::kThreads == linear_threads(BM) && (!LINES || S::kM % 4 == 0), "");
@@ -50,16 +50,13 @@ __global__ __launch_bounds__(linear_threads(BM), 2) void linear_kernel(LinearArg
     __shared__ __attribute__((aligned(1024))) char smem_raw[kRing + (LINES ? S::kWaves * kLinesScratch : 0)];
     LdsChar* smem = (LdsChar*)smem_raw;
     LdsChar* lines = smem + (LINES ? kRing + ffn_wave() * kLinesScratch : 0);
-    const FfnTile* tiles = ffn_tile_list(list);
     const int32_t len = a.len, N = a.N;
     const int32_t n = a.T * a.k;
     const int32_t spans = (N + span - 1) / span;
     const int wave = ffn_wave(), lane = ffn_lane();
     const int wm = wave % S::kWavesM, wn = wave / S::kWavesM;
-    const int64_t total = (int64_t)*static_cast<const int32_t*>(list) * spans;
-    ffn_for_each(total, [&](int64_t item) {
-        const FfnTile tile = tiles[item / spans];
-        const int32_t c0 = (int32_t)(item % spans) * span, c1 = min(N, c0 + span);
+    linear_for_each<BM, S::kThreads, OWN>(a, list, bound, spans, smem, [&](const FfnTile& tile, int32_t turn) {
+        const int32_t c0 = turn * span, c1 = min(N, c0 + span);
         if (tile.expert < 0) {  // dropped entries: zero rows
             const int32_t pieces = (c1 - c0) / 8;
             for (int32_t i = threadIdx.x; i < tile.rows * pieces; i += S::kThreads) {
@@ -285,11 +282,17 @@ constexpr int64_t kMaxBlocks = 1 << 19;
 unsigned grid_of(int64_t items) { return (unsigned)(std::min<int64_t>((items + 7) / 8, kMaxBlocks / 8) * 8); }
 unsigned few_grid(int64_t items) { return (unsigned)std::min<int64_t>(items, 1 << 22); }
 
-template <bool I8, int BM, int COLS, int STAGES, bool LINES = (BM >= 64 && COLS >= 128)>
+template <bool I8, int BM, int COLS, int STAGES>
 void tiled(const LinearPlan& p, const LinearArgs& a, const char* ws, hipStream_t stream) {
-    linear_kernel<I8, BM, COLS, STAGES, LINES>
-        <<<grid_of(p.tiles.tiles * ((a.N + p.span - 1) / p.span)), linear_threads(BM), 0, stream>>>(
-            a, ws + p.tiles.off_tiles, p.span);
+    constexpr bool kLines = BM >= 64 && COLS >= 128;
+    constexpr bool kOwn = BM < 256 && !(BM == 32 && STAGES == 2);  // (else there is always a list)
+    const unsigned blocks = grid_of(p.tiles.tiles * ((a.N + p.span - 1) / p.span));
+    const void* list = ws + p.tiles.off_tiles;
+    const int32_t bound = (int32_t)p.tiles.tiles;
+    if (p.listed)
+        linear_kernel<I8, BM, COLS, STAGES, kLines, false><<<blocks, linear_threads(BM), 0, stream>>>(a, list, bound, p.span);
+    else if constexpr (kOwn)
+        linear_kernel<I8, BM, COLS, STAGES, kLines, true><<<blocks, linear_threads(BM), 0, stream>>>(a, nullptr, bound, p.span);
 }
 
 template <bool I8>
@@ -339,6 +342,14 @@ int32_t linear_tile_rows(int64_t n, int32_t M, int32_t cols, int32_t cols_of, in
     return best;
 }
 
+// A workgroup finds its tile itself while few of them do the same: up to kLinearOwn experts and three workgroups to a
+// place (two to a CU).  us, found : listed by a launch ahead, 240 shapes of up to 512 workgroups 2.9 less, of up to 1024 2.4,
+// to 2048 0.6, to 4096 -0.3 (T = 200, k = 4, 64 experts of 512 x 512 10.3 : 13.6; T = 16384, 256 experts 80.6 : 77.3).  With
+// 256 rows to a tile it would take registers that the products want.
+bool linear_listed(const FfnPlan& tiles, int32_t M, int64_t spans) {
+    return M > kLinearOwn || tiles.bm == 256 || tiles.tiles * spans > 1536;
+}
+
 // Upper bound on the workgroups along the entries that have work in the kernel without tiles.
 static int64_t few_starts(int64_t n, int32_t M) { return std::min<int64_t>(n, std::min<int64_t>(n, M) + n / kFewRows); }
 
@@ -348,16 +359,19 @@ void linear_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, b
     p->cols = N <= 64 ? 64 : 128;
     const int32_t bm = linear_tile_rows(n, M, N, p->cols, (len + kFfnBK - 1) / kFfnBK, q8);
     ffn_tiles_plan(n, M, bm, &p->tiles);
-    // The kernel without tiles saves a launch and the latency of the stages (3 us) while the rows of W that its
-    // workgroups read, once for every 16 entries, are few, and the entries' rows of x that each reads again, and
-    // few workgroups end at once; its waves share the columns of long contractions.  Fitted to 260 shapes of both types (1 to
-    // 4096 entries, 1 to 4096 experts): 2 % (bf16) and 4 % (int8) off the best of the three on geometric mean.
-    // us with tiles : own columns : shared, one dense map, 256 rows of K = 512, N = 1024 10.6 : 34 : 37; one entry of K = 2048,
-    // N = 128 18.9 : 19.2 : 7.6; 256 in 512 experts of K = 512, N = 128 9.9 : 9.0 : 17.4.
-    p->few = few_starts(n, M) * N <= 10000 + ((int64_t)1 << 21) / len && n * len <= (int64_t)1 << 19 &&
-             n * ((N + few_span<false>() - 1) / few_span<false>()) <= 1024;
+    // The kernel without tiles has a short way to its first operands, but reads the weights again for every 16 entries, the
+    // rows of x in every workgroup, and starts a workgroup for each entry, of which most end at once: it is taken
+    // while these are few, fewer where the other one does without a launch for its list.  Its waves share the columns of
+    // contractions beyond 256, up to 512 only while that leaves few workgroups.  Fitted to 500 shapes of both types (1 to 4096
+    // entries, 1 to 8192 experts): 2.4 % off the best of the three on geometric mean, 3.7 % beyond kLinearOwn experts.  us with
+    // tiles : own columns : shared, bf16, one dense map of K = 192, N = 480, 180 rows 6.3 : 11.4 : 12.9; 8-bit, one entry of
+    // K = 2048, N = 128 18.9 : 19.2 : 7.6; bf16, 93 entries in 3107 experts of K = 96, N = 432 9.3 : 6.0 : 10.6.
+    const int64_t starts = few_starts(n, M), spans = (N + few_span<false>() - 1) / few_span<false>();
+    const bool own = M <= kLinearOwn;
+    p->few = n * len <= (int64_t)1 << 20 && n * spans <= (own ? 256 : 2048) &&
+             starts * N <= 12000 + (own ? 0 : ((int64_t)1 << 24) / len);
     if (p->few) {
-        p->split = len > 256;
+        p->split = len > 512 || (len > 256 && starts * spans < 64);
         p->span = p->split ? few_span<true>() : few_span<false>();
         return;
     }
@@ -365,7 +379,8 @@ void linear_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, b
     p->stream = q8 && bm == 256 && (len + kFfnBK - 1) / kFfnBK >= kStreamSteps;
     p->span = p->stream ? p->cols : ffn_span(len, p->cols, p->tiles.tiles, N);
     p->stages = bm >= 128 ? 2 : bm == 64 || p->cols == 64 ? 3 : p->tiles.tiles * ((N + p->span - 1) / p->span) >= 2048 ? 2 : 3;
-    p->workspace_bytes = p->tiles.workspace_bytes;
+    p->listed = linear_listed(p->tiles, M, (N + p->span - 1) / p->span);
+    p->workspace_bytes = p->listed ? p->tiles.workspace_bytes : 0;
 }
 
 hipError_t linear_tiles_launch(const LinearPlan& p, const LinearArgs& a, void* workspace, hipStream_t stream) {
@@ -376,7 +391,7 @@ hipError_t linear_tiles_launch(const LinearPlan& p, const LinearArgs& a, void* w
 }
 
 hipError_t linear_launch(const LinearPlan& p, const LinearArgs& a, void* workspace, hipStream_t stream) {
-    if (!p.few) {
+    if (p.listed) {
         const hipError_t e = linear_tiles_launch(p, a, workspace, stream);
         if (e != hipSuccess) return e;
     }

@@ -85,6 +85,8 @@ more_status check_distill(const void* logits, int32_t bits, int64_t T, int32_t V
         (dlogits && dlogits == logits && ldd != ld))
         return MORE_ERR_INVALID_ARG;
     constexpr int64_t kMaxStride = (int64_t)1 << 40;
+    // (beyond these tau^2 and log2(e) / tau leave fp32)
+    if (tau < 0x1p-40f || tau > 0x1p40f) return MORE_ERR_UNSUPPORTED;
     if (V > 1 << 30 || k > MORE_TEACHER_K_MAX || T > kMaxRows || ld > kMaxStride || (dlogits && ldd > kMaxStride))
         return MORE_ERR_UNSUPPORTED;
     return MORE_OK;
@@ -198,6 +200,7 @@ more_status more_expert_linear_plan(int64_t T, int32_t K, int32_t N, int32_t M, 
     plan->tile_rows = p.few ? 0 : p.tiles.bm;
     plan->cols = p.few ? p.span : p.cols;
     plan->span = p.span;
+    plan->listed = p.listed;
     return MORE_OK;
 }
 

@@ -25,6 +25,81 @@ struct LinearType<true> {
     }
 };
 
+// Work items (tile, span) over the grid, for workgroups of THREADS threads: body(tile, span), a span by its number.  The tiles
+// come from the list (ffn_for_each), or (OWN, a workgroup for every item) each workgroup counts them up to its own, in the
+// list's order.  Offsets that Sort + Count cannot have written are cut as for the list: to [0, n], and there are `bound`
+// tiles at most (few, so that the counts of kLinearOwn experts fit 32 bits whatever the offsets are).  `lds` holds the
+// counts ahead of the body.
+template <int BM, int THREADS, bool OWN, typename F>
+__device__ __forceinline__ void linear_for_each(const LinearArgs& a, const void* __restrict__ list, int32_t bound,
+                                                int32_t spans, LdsChar* lds, F body) {
+    if constexpr (!OWN) {
+        ffn_for_each((int64_t)*static_cast<const int32_t*>(list) * spans, [&](int64_t item) {
+            const FfnTile tile = ffn_tile_list(list)[item / spans];
+            body(tile, (int32_t)(item % spans));
+        });
+    } else {
+        typedef __attribute__((address_space(3))) int32_t LdsInt;
+        constexpr int kEach = kLinearOwn / THREADS, kWaves = THREADS / 64;
+        const int lane = ffn_lane(), wave = ffn_wave();
+        LdsInt* part = (LdsInt*)lds;
+        LdsInt* found = part + kWaves;
+        // a thread's experts from e0 on: where they begin, their tiles; the tiles before them and of all experts
+        const int32_t n = a.T * a.k, e0 = (int32_t)threadIdx.x * kEach;
+        auto offset = [&](int32_t e) { return min(max(a.offsets[min(e, a.M)], 0), n); };
+        int32_t begin[kEach + 1];
+        const int32_t valid = offset(a.M);
+#pragma unroll
+        for (int i = 0; i <= kEach; ++i) begin[i] = offset(e0 + i);
+        auto count = [&](int i) { return (max(begin[i + 1] - begin[i], 0) + BM - 1) / BM; };
+        int32_t mine = 0, sum = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) mine += count(i);
+        int32_t first = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int32_t o = __shfl_up(first, d, 64);
+            first += lane >= d ? o : 0;
+        }
+        if (lane == 63) part[wave] = first;
+        first -= mine;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            first += w < wave ? part[w] : 0;
+            sum += part[w];
+        }
+        const int32_t tiles = __builtin_amdgcn_readfirstlane(min(sum + (n - valid + BM - 1) / BM, bound));
+        const int32_t total = tiles * spans, chunk = (total + 7) / 8;
+        const int32_t q = (int32_t)(blockIdx.x >> 3), item = (int32_t)(blockIdx.x & 7) * chunk + q;
+        if (q >= chunk || item >= total) return;
+        const int32_t at = item / spans;
+        if (at >= sum) {  // of the dropped entries
+            if (threadIdx.x == 0) {
+                const int32_t row = valid + (at - sum) * BM;
+                found[0] = -1, found[1] = row, found[2] = min(n - row, BM);
+            }
+        } else if (at >= first && at < first + mine) {
+            int32_t left = at - first;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                if (left >= 0 && left < count(i)) {
+                    const int32_t row = begin[i] + left * BM;
+                    found[0] = e0 + i, found[1] = row, found[2] = min(begin[i + 1] - row, BM);
+                }
+                left -= count(i);
+            }
+        }
+        __syncthreads();
+        FfnTile tile;
+        tile.expert = __builtin_amdgcn_readfirstlane(found[0]);
+        tile.row0 = __builtin_amdgcn_readfirstlane(found[1]);
+        tile.rows = __builtin_amdgcn_readfirstlane(found[2]);
+        __syncthreads();  // the body may write its LDS
+        body(tile, item % spans);
+    }
+}
+
 // The factor of entry p's row, and four columns of an accumulator as they are stored.
 template <bool I8>
 __device__ __forceinline__ float linear_row_scale(const LinearArgs& a, uint32_t p, int32_t n) {

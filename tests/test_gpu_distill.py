@@ -1,5 +1,7 @@
 """Distillation from a teacher's top logits against its 64-bit form: every row length, odd strides, rows without a teacher,
 masked logits."""
+import math
+
 import numpy as np
 import pytest
 
@@ -106,6 +108,61 @@ def test_in_place_and_nothing_beside_the_rows(V, ld, start, bits):
         beside = torch.ones_like(big, dtype=torch.bool)
         beside[start:start + T * ld].view(T, ld)[:, :V] = False
         assert (big[beside] == 7).all()
+
+
+@pytest.mark.parametrize("bits", [16, 32])
+@pytest.mark.parametrize("V,ld,start,ldd,start_d", [(13, 13, 0, 17, 1), (300, 304, 0, 301, 3), (3000, 3001, 5, 3008, 0), (9001, 9001, 3, 9008, 8),
+                                                    (33000, 33000, 0, 33003, 1), (300001, 300001, 1, 300002, 5)])
+def test_gradients_of_other_strides(V, ld, start, ldd, start_d, bits):
+    """The library's call with gradients that lie otherwise than the logits."""
+    torch = require_gpu()
+    from paper_2609_36301_amd import _lib, distill_loss
+    T, k, tau = 5, 3, 2.0
+    z, ids, values, w = case(V, T, V, k, bits)
+    announce("distill V=%d bits=%d gradients ldd=%d start=%d" % (V, bits, ldd, start_d))
+    _, logits = rows_on_device(z, bits, ld, start)
+    ids, values, w = to_dev(ids), to_dev(values), to_dev(w)
+    want = distill_loss(logits, ids, values, w, temperature=tau, gradient=True)
+    for given in (False, True):
+        buffer = torch.full((T * ldd + 32,), 5.0, dtype=logits.dtype, device="cuda")
+        rows = buffer[start_d:start_d + T * ldd].view(T, ldd)[:, :V]
+        head = (logits.data_ptr(), bits, T, V, ld)
+        entries = (ids.data_ptr(), values.data_ptr(), k, tau)
+        tail = (rows.data_ptr(), ldd, torch.cuda.current_stream().cuda_stream)
+        lib = _lib.load()
+        if given:
+            status = lib.more_distill_backward(*head, want.m.data_ptr(), want.Z.data_ptr(), *entries, w.data_ptr(), *tail)
+        else:
+            status = lib.more_distill(*head, *entries, w.data_ptr(), None, None, None, *tail)
+        assert status == _lib.OK and torch.equal(rows, want.dlogits)
+        beside = torch.ones_like(buffer, dtype=torch.bool)
+        beside[start_d:start_d + T * ldd].view(T, ldd)[:, :V] = False
+        assert (buffer[beside] == 5).all()
+
+
+@pytest.mark.parametrize("tau", [2.0 ** -40, 2.0 ** 40])
+def test_outermost_temperatures(tau):
+    """Finite results; at the lowest the largest logit has all the probability, at the highest all classes have the same."""
+    torch = require_gpu()
+    from paper_2609_36301_amd import distill_loss
+    T, V, k = 4, 700, 3
+    announce("distill tau=%g" % tau)
+    z = torch.zeros((T, V), device="cuda")
+    z[:, 9] = 1.0
+    ids = torch.tensor([[5, 9, 11]] * T, dtype=torch.int32, device="cuda")
+    values = torch.tensor([[1.0, 0.0, -1.0]] * T, device="cuda")
+    d = distill_loss(z, ids, values, temperature=tau, gradient=True)
+    want = torch.zeros((T, V), dtype=torch.float64)
+    if tau < 1:
+        want[:, 9], want[:, 5] = tau, -tau
+        loss = tau  # tau^2 (z_9 - z_5) / tau
+    else:
+        want[:] = tau / V
+        want[:, [5, 9, 11]] -= tau / 3
+        loss = tau * tau * math.log(V / 3)
+    # a quotient of two fp32 numbers and a product: four roundings and two function values of 2^-21 each
+    assert (d.dlogits.double().cpu() - want).abs().max() <= 2.0 ** -19 * tau
+    assert (d.loss.double() - loss).abs().max() <= 2.0 ** -18 * loss
 
 
 @pytest.mark.parametrize("k", [1, 63, 64, 65, 200, 1024])

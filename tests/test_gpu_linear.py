@@ -211,6 +211,32 @@ def test_guards_around_outputs():
             assert (big[:128] == 7).all() and (big[-128:] == 7).all()
 
 
+@pytest.mark.parametrize("M", [1, 2, 5, 255, 256, 257, 513, 1023, 1024, 1025])
+@pytest.mark.parametrize("hot", [False, True])
+def test_tiles_found_and_listed(M, hot):
+    """Workgroups find their tiles among up to 1024 experts, of which many are empty or one has most entries, and dropped ones."""
+    torch = require_gpu()
+    from paper_2609_36301_amd import expert_linear, expert_linear_backward, expert_linear_plan, expert_linear_q8
+    seen = set()
+    for T, K, N, k in ((1700, 64, 72, 2), (611, 48, 264, 3), (9000, 16, 136, 1), (20000, 80, 8, 1)):
+        plan = expert_linear_plan(T, K, N, M, k)
+        seen.add((plan["tile_rows"], plan["listed"]))
+        x, W, dy, idx, offsets, srt = case(M, T, K, N, M, k, hot=hot)
+        announce("expert_linear of %d experts T=%d K=%d N=%d k=%d hot=%s %s" % (M, T, K, N, k, hot, plan))
+        args = [to_dev(v) for v in (x, W, idx, offsets, srt)]
+        within(to_np(expert_linear(*args)), *ref.linear(from_bf16(x), from_bf16(W), idx), "y")
+        g = expert_linear_backward(*args, to_dev(dy))
+        (dx, dW), (bx, bW) = ref.linear_backward(from_bf16(x), from_bf16(W), idx, from_bf16(dy))
+        within(to_np(g.dx), dx, bx, "dx")
+        within(to_np(g.dWt), dW, bW, "dW")
+        q, Wq = (torch.from_numpy(np.random.default_rng(M).integers(-128, 128, s).astype(np.int8)) for s in ((T, K), (M, N, K)))
+        qs, ws = np.full(T, 0.5, np.float32), np.full((M, N), 0.25, np.float32)
+        y = expert_linear_q8(q.cuda(), to_dev(qs), Wq.cuda(), to_dev(ws), *args[2:])
+        want, bound = ref.linear_q8(q.numpy(), qs.astype(np.float64), Wq.numpy(), ws.astype(np.float64), idx)
+        within(to_np(y), want, bound, "y of 8 bits")
+    assert any(rows and not listed for rows, listed in seen) == (M <= 1024)
+
+
 @pytest.mark.parametrize("M", [65537, 70000])
 def test_more_experts_than_one_list_counts(M):
     """Beyond 2^16 experts their tiles are counted ahead of the list."""

@@ -22,7 +22,7 @@ def lib():
     return _lib.load()
 
 
-BIG = dict(T=4096, K=512, N=512, M=64, k=2)  # tiles: a workspace is needed
+BIG = dict(T=4096, K=512, N=512, M=4096, k=2)  # listed tiles: a workspace is needed
 
 
 def linear(lib, T=64, K=64, N=16, M=8, k=2, x=FAKE, W=FAKE, idx=FAKE, offsets=FAKE, srt=FAKE, y=FAKE, bits=16, ws=None, wsb=0):
@@ -97,6 +97,7 @@ BOTH = [(dict(T=-1), INVALID), (dict(V=0), INVALID), (dict(k=0), INVALID), (dict
         (dict(weight=ODD), INVALID), (dict(m=ODD), INVALID), (dict(Z=ODD), INVALID), (dict(d=ODD), INVALID),
         (dict(d=FAKE, ldd=64), INVALID),  # in place with another stride
         (dict(V=(1 << 30) + 1, ld=1 << 31, ldd=1 << 31), UNSUPPORTED), (dict(k=1025), UNSUPPORTED), (dict(T=1 << 31), UNSUPPORTED),
+        (dict(tau=2.0 ** -41), UNSUPPORTED), (dict(tau=1e-45), UNSUPPORTED), (dict(tau=2.0 ** 41), UNSUPPORTED),
         (dict(ld=(1 << 40) + 1), UNSUPPORTED), (dict(ldd=(1 << 40) + 1), UNSUPPORTED),
         (dict(T=0, z=None, ids=None, values=None), _lib.OK)]
 
