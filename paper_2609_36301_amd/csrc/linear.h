@@ -55,6 +55,10 @@ hipError_t linear_backward_launch(const LinearPlan& p, const LinearArgs& a, void
 constexpr int32_t kStreamSteps = 5;
 hipError_t linear_stream_launch(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t stream);
 
+// Columns (rows of dW) that a workgroup takes, in steps of `step`, of a product whose contraction is `len` long over `groups`
+// groups of rows.
+int32_t linear_span(int64_t len, int32_t step, int64_t groups, int32_t side);
+
 // Whether the tiles of a plan are listed by a launch of their own; else each workgroup finds its tile from the offsets, of
 // at most kLinearOwn experts.
 constexpr int32_t kLinearOwn = 1024;

@@ -342,6 +342,19 @@ int32_t linear_tile_rows(int64_t n, int32_t M, int32_t cols, int32_t cols_of, in
     return best;
 }
 
+// A single step where the contraction alone fills the pipeline (three stages), where the groups are too few to fill the chip
+// with more, or where the workgroups would be uneven; else 256, or 512 of very many groups.  Fitted to 200 shapes: the map 2.5 %,
+// in 8 bits 3.6 %, dx 2.4 % and dW 5.7 % off the best of the three on geometric mean (us, a step of 128 : 256 : 512, dx of
+// 5338 groups, K = 736, N = 48 73 : 56 : 65; dW of 64 experts of 1024 x 1024, 31 entries 34 : 29 : 37; of 4096, K = 64,
+// N = 512, 32 entries 99 : 79 : 66; of 32, 1024 x 520, 250 entries 31 : 33 : 59).
+int32_t linear_span(int64_t len, int32_t step, int64_t groups, int32_t side) {
+    if (len > 3 * kFfnBK) return step;
+    const int32_t steps = (side + step - 1) / step;
+    if ((steps % 4 == 0 || steps >= 18) && groups * ((side + 511) / 512) >= 2048) return std::max(step, 512);
+    if ((steps % 2 == 0 || steps >= 9) && groups * ((side + 255) / 256) >= 512) return std::max(step, 256);
+    return step;
+}
+
 // A workgroup finds its tile itself while few of them do the same: up to kLinearOwn experts and three workgroups to a
 // place (two to a CU).  us, found : listed by a launch ahead, 240 shapes of up to 512 workgroups 2.9 less, of up to 1024 2.4,
 // to 2048 0.6, to 4096 -0.3 (T = 200, k = 4, 64 experts of 512 x 512 10.3 : 13.6; T = 16384, 256 experts 80.6 : 77.3).  With
@@ -377,7 +390,7 @@ void linear_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, b
     }
     if (bm == 256) p->cols = 256;
     p->stream = q8 && bm == 256 && (len + kFfnBK - 1) / kFfnBK >= kStreamSteps;
-    p->span = p->stream ? p->cols : ffn_span(len, p->cols, p->tiles.tiles, N);
+    p->span = p->stream ? p->cols : linear_span(len, p->cols, p->tiles.tiles, N);
     p->stages = bm >= 128 ? 2 : bm == 64 || p->cols == 64 ? 3 : p->tiles.tiles * ((N + p->span - 1) / p->span) >= 2048 ? 2 : 3;
     p->listed = linear_listed(p->tiles, M, (N + p->span - 1) / p->span);
     p->workspace_bytes = p->listed ? p->tiles.workspace_bytes : 0;

@@ -466,7 +466,7 @@ void dw_plan(int64_t n, int32_t K, int32_t N, int32_t M, LinearPlan* p) {
     const bool by_cols = p->dw_cols > 64;
     const int32_t step = by_cols ? p->dw_cols : p->dw_rows, side = by_cols ? K : N;
     const int64_t groups = M * (by_cols ? tiles(N, p->dw_rows) : tiles(K, p->dw_cols));
-    p->dw_span = p->dw_parts > 1 ? step : ffn_span((int32_t)std::min<int64_t>(n / M, 1 << 20), step, groups, side);
+    p->dw_span = p->dw_parts > 1 ? step : linear_span(n / M, step, groups, side);
 }
 
 }  // namespace
@@ -478,7 +478,7 @@ void linear_backward_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int
     const int32_t bm = linear_tile_rows(n, M, len, p->cols, (N + kFfnBK - 1) / kFfnBK, false);
     ffn_tiles_plan(n, M, bm, &p->tiles);
     if (bm == 256) p->cols = 256;
-    p->span = ffn_span(N, p->cols, p->tiles.tiles, len);
+    p->span = linear_span(N, p->cols, p->tiles.tiles, len);
     dw_plan(n, len, N, M, p);
     p->listed = linear_listed(p->tiles, M, (len + p->span - 1) / p->span);
     size_t at = p->listed ? p->tiles.workspace_bytes : 0;
