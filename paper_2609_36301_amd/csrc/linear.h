@@ -38,6 +38,7 @@ struct LinearPlan {
     int32_t stages;   // (forward, tiles) of the LDS ring
     int32_t span;     // columns that a workgroup takes
     int32_t stream;   // (q8, tiles of 256 rows) the pipeline runs on from tile to tile
+    int32_t both;              // (backward) one launch makes both gradients
     int32_t dw_rows, dw_cols;  // rows and columns of a tile of dW
     int32_t dw_parts;          // runs of an expert's entries that are summed apart
     int32_t dw_span;           // of dW's longer side that a workgroup takes

@@ -36,7 +36,9 @@ struct DxShape {
     static constexpr int kN = BM / (kWaves / kWavesM) / 16;
     static constexpr int kRowsAt = COLS * 128;
     static constexpr int kStageBytes = kRowsAt + BM * 128;
+    static constexpr int kRing = 2 * kStageBytes;
     static constexpr bool kLines = kM % 4 == 0;  // a wave's columns are whole lines of dx
+    static constexpr int kLds = kRing + (kLines ? kWaves * kLinesScratch : 0);
     // An expert has one tile, mostly, and its weights lie one line after the other: nontemporal (4096 experts, K = 64,
     // N = 512, 32 rows 68 us, without 88; of wider weights, taken 128 columns at a time, 262 : 227).
     static constexpr bool kOnce = BM <= 64 && COLS == 64;
@@ -44,13 +46,10 @@ struct DxShape {
 
 // DIRECT: one entry per token, `out` is dx (bf16); else the shares (fp32).
 template <int BM, int COLS, bool DIRECT, bool OWN>
-__global__ __launch_bounds__(dx_threads(BM), 2) void linear_dx_kernel(LinearArgs a, const void* __restrict__ list,
-                                                                  int32_t bound, int32_t span, void* __restrict__ out) {
+__device__ __forceinline__ void linear_dx(const LinearArgs& a, const void* __restrict__ list, int32_t bound, int32_t span,
+                                          void* __restrict__ out, LdsChar* smem) {
     using S = DxShape<BM, COLS>;
-    constexpr int kRing = 2 * S::kStageBytes;
-    __shared__ __attribute__((aligned(1024))) char smem_raw[kRing + (S::kLines ? S::kWaves * kLinesScratch : 0)];
-    LdsChar* smem = (LdsChar*)smem_raw;
-    LdsChar* lines = smem + (S::kLines ? kRing + ffn_wave() * kLinesScratch : 0);
+    LdsChar* lines = smem + (S::kLines ? S::kRing + ffn_wave() * kLinesScratch : 0);
     const int32_t n = a.T * a.k, len = a.N, cols = a.len;
     const int32_t spans = (cols + span - 1) / span;
     const int wave = ffn_wave(), lane = ffn_lane();
@@ -203,6 +202,13 @@ __global__ __launch_bounds__(dx_threads(BM), 2) void linear_dx_kernel(LinearArgs
     });
 }
 
+template <int BM, int COLS, bool DIRECT, bool OWN>
+__global__ __launch_bounds__(dx_threads(BM), 2) void linear_dx_kernel(LinearArgs a, const void* __restrict__ list,
+                                                                  int32_t bound, int32_t span, void* __restrict__ out) {
+    __shared__ __attribute__((aligned(1024))) char smem[DxShape<BM, COLS>::kLds];
+    linear_dx<BM, COLS, DIRECT, OWN>(a, list, bound, span, out, (LdsChar*)smem);
+}
+
 // A thread adds eight columns of a token's k shares in order; dropped entries are left out.  The shares and ids of four
 // entries are read at a time, whether wanted or not: one after the other their reads would wait for the ids.
 __global__ __launch_bounds__(256) void linear_sum_kernel(LinearArgs a, const float* __restrict__ shares) {
@@ -248,13 +254,16 @@ struct LinearDw {
     float* parts;
 };
 
+template <int CT, int RT, int WAVES, bool PARTS>
+constexpr int dw_lds() {
+    return 2 * (CT + RT) * 128 + (PARTS ? 0 : WAVES * kLinesScratch);
+}
+
+// The work of workgroup `block` of `blocks`.
 template <int CT, int RT, int WAVES, bool BY_COLS, bool PARTS>
-__global__ __launch_bounds__(64 * WAVES, 2) void linear_dw_kernel(LinearArgs a, LinearDw d) {
+__device__ __forceinline__ void linear_dw(const LinearArgs& a, const LinearDw& d, uint32_t block, uint32_t blocks, LdsChar* smem) {
     constexpr int kStageBytes = (CT + RT) * 128;
-    constexpr int kRing = 2 * kStageBytes;
-    __shared__ __attribute__((aligned(1024))) char smem_raw[kRing + (PARTS ? 0 : WAVES * kLinesScratch)];
-    LdsChar* smem = (LdsChar*)smem_raw;
-    LdsChar* lines = smem + (PARTS ? 0 : kRing + ffn_wave() * kLinesScratch);
+    LdsChar* lines = smem + (PARTS ? 0 : 2 * kStageBytes + ffn_wave() * kLinesScratch);
     constexpr int kWavesM = CT >= 128 ? 2 : 1, kWavesN = WAVES / kWavesM;
     constexpr int kM = CT / kWavesM / 16, kN = RT / kWavesN / 16;  // 16 x 16 tiles per wave
     static_assert(kM % 4 == 0, "whole lines of dW: 64 columns");
@@ -268,7 +277,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void linear_dw_kernel(LinearArgs a, 
     const int32_t spans = (side + d.span - 1) / d.span;
     const int32_t others = BY_COLS ? (N + RT - 1) / RT : (K + CT - 1) / CT;
     const int32_t runs = PARTS ? d.runs : 1;
-    for (int64_t work = blockIdx.x; work < (int64_t)a.M * spans * others * runs; work += gridDim.x) {
+    for (int64_t work = block; work < (int64_t)a.M * spans * others * runs; work += blocks) {
         const int32_t run = PARTS ? (int32_t)(work % runs) : 0;
         const int64_t item = PARTS ? work / runs : work;
         const int64_t per = (int64_t)spans * others;
@@ -403,6 +412,24 @@ __global__ __launch_bounds__(64 * WAVES, 2) void linear_dw_kernel(LinearArgs a, 
     }
 }
 
+template <int CT, int RT, int WAVES, bool BY_COLS, bool PARTS>
+__global__ __launch_bounds__(64 * WAVES, 2) void linear_dw_kernel(LinearArgs a, LinearDw d) {
+    __shared__ __attribute__((aligned(1024))) char smem[dw_lds<CT, RT, WAVES, PARTS>()];
+    linear_dw<CT, RT, WAVES, BY_COLS, PARTS>(a, d, blockIdx.x, gridDim.x, (LdsChar*)smem);
+}
+
+// Both gradients of a small call at once: the first `dx_blocks` workgroups take dx, the others dW.
+template <int BM, int COLS, bool DIRECT, int CT, int RT, bool BY_COLS, bool PARTS>
+__global__ __launch_bounds__(256, 2) void linear_both_kernel(LinearArgs a, int32_t bound, int32_t span, void* __restrict__ out,
+                                                             uint32_t dx_blocks, LinearDw d) {
+    constexpr int kDx = DxShape<BM, COLS>::kLds, kDw = dw_lds<CT, RT, 4, PARTS>();
+    __shared__ __attribute__((aligned(1024))) char smem[kDx > kDw ? kDx : kDw];
+    if (blockIdx.x < dx_blocks)
+        linear_dx<BM, COLS, DIRECT, true>(a, nullptr, bound, span, out, (LdsChar*)smem);
+    else
+        linear_dw<CT, RT, 4, BY_COLS, PARTS>(a, d, blockIdx.x - dx_blocks, gridDim.x - dx_blocks, (LdsChar*)smem);
+}
+
 // ------------------------------------------------------------------------------ host
 namespace {
 
@@ -410,9 +437,13 @@ size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 constexpr int64_t kMaxBlocks = 1 << 19;
 unsigned grid_of(int64_t items) { return (unsigned)(std::min<int64_t>((items + 7) / 8, kMaxBlocks / 8) * 8); }
 
+unsigned dx_blocks(const LinearPlan& p, const LinearArgs& a) {
+    return grid_of(p.tiles.tiles * ((a.len + p.span - 1) / p.span));
+}
+
 template <int BM, int COLS, bool OWN>
 void dx_launch(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t stream) {
-    const unsigned blocks = grid_of(p.tiles.tiles * ((a.len + p.span - 1) / p.span));
+    const unsigned blocks = dx_blocks(p, a);
     const void* list = OWN ? nullptr : ws + p.tiles.off_tiles;
     const int32_t bound = (int32_t)p.tiles.tiles;
     if (a.k == 1)
@@ -433,18 +464,46 @@ int64_t dw_items(const LinearPlan& p, int32_t K, int32_t N, int32_t M, bool by_c
     return (int64_t)M * ((side + p.dw_span - 1) / p.dw_span) * ((other + step - 1) / step);
 }
 
+LinearDw dw_args(const LinearPlan& p, char* ws) {
+    return LinearDw{p.dw_span, p.dw_parts, reinterpret_cast<float*>(ws + p.off_parts)};
+}
+
 template <int CT, int RT, int WAVES, bool BY_COLS>
 void dw_launch(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t stream) {
-    LinearDw d;
-    d.span = p.dw_span;
-    d.runs = p.dw_parts;
-    d.parts = reinterpret_cast<float*>(ws + p.off_parts);
+    const LinearDw d = dw_args(p, ws);
     const unsigned blocks = grid_of(dw_items(p, a.len, a.N, a.M, BY_COLS) * d.runs);
     if (p.dw_parts > 1) {
         if constexpr (CT < 256) linear_dw_kernel<CT, RT, WAVES, BY_COLS, true><<<blocks, 64 * WAVES, 0, stream>>>(a, d);
     } else {
         linear_dw_kernel<CT, RT, WAVES, BY_COLS, false><<<blocks, 64 * WAVES, 0, stream>>>(a, d);
     }
+}
+
+template <int BM, int COLS, bool DIRECT, int CT, int RT, bool BY_COLS>
+void both_launch(const LinearPlan& p, const LinearArgs& a, char* ws, void* out, hipStream_t stream) {
+    const LinearDw d = dw_args(p, ws);
+    const unsigned dx = dx_blocks(p, a), dw = grid_of(dw_items(p, a.len, a.N, a.M, BY_COLS) * d.runs);
+    const int32_t bound = (int32_t)p.tiles.tiles;
+    if (p.dw_parts > 1)
+        linear_both_kernel<BM, COLS, DIRECT, CT, RT, BY_COLS, true><<<dx + dw, 256, 0, stream>>>(a, bound, p.span, out, dx, d);
+    else
+        linear_both_kernel<BM, COLS, DIRECT, CT, RT, BY_COLS, false><<<dx + dw, 256, 0, stream>>>(a, bound, p.span, out, dx, d);
+}
+template <int BM, int COLS, int CT, int RT, bool BY_COLS>
+void both_launch(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t stream) {
+    if (a.k == 1)
+        both_launch<BM, COLS, true, CT, RT, BY_COLS>(p, a, ws, a.dx, stream);
+    else
+        both_launch<BM, COLS, false, CT, RT, BY_COLS>(p, a, ws, ws + p.off_shares, stream);
+}
+template <int BM>
+void both_launch(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t stream) {
+    if (p.dw_cols == 64)
+        both_launch<BM, 64, 64, 128, false>(p, a, ws, stream);
+    else if (p.dw_rows == 64)
+        both_launch<BM, 128, 128, 64, true>(p, a, ws, stream);
+    else
+        both_launch<BM, 128, 128, 128, true>(p, a, ws, stream);
 }
 
 // Tile of dW, by the rounds in which its workgroups fill the chip (two of 128 x 128 to a CU, one of 256 x 256) times the
@@ -481,6 +540,7 @@ void linear_backward_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int
     p->span = linear_span(N, p->cols, p->tiles.tiles, len);
     dw_plan(n, len, N, M, p);
     p->listed = linear_listed(p->tiles, M, (len + p->span - 1) / p->span);
+    p->both = !p->listed && p->dw_cols < 256;
     size_t at = p->listed ? p->tiles.workspace_bytes : 0;
     p->off_shares = at;
     at += k > 1 ? align256((size_t)n * len * 4) : 0;
@@ -491,8 +551,15 @@ void linear_backward_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int
 
 hipError_t linear_backward_launch(const LinearPlan& p, const LinearArgs& a, void* workspace, hipStream_t stream) {
     char* ws = static_cast<char*>(workspace);
+    const bool dx = p.tiles.n > 0 && a.dx, both = p.both && dx && a.dW;
     hipError_t e = hipSuccess;
-    if (p.tiles.n > 0 && a.dx) {
+    if (both) {
+        switch (p.tiles.bm) {
+            case 128: both_launch<128>(p, a, ws, stream); break;
+            case 64: both_launch<64>(p, a, ws, stream); break;
+            default: both_launch<32>(p, a, ws, stream);
+        }
+    } else if (dx) {
         if (p.listed) e = linear_tiles_launch(p, a, ws, stream);
         if (e != hipSuccess) return e;
         switch (p.tiles.bm) {
@@ -501,29 +568,29 @@ hipError_t linear_backward_launch(const LinearPlan& p, const LinearArgs& a, void
             case 64: p.cols == 64 ? dx_launch<64, 64>(p, a, ws, stream) : dx_launch<64, 128>(p, a, ws, stream); break;
             default: p.cols == 64 ? dx_launch<32, 64>(p, a, ws, stream) : dx_launch<32, 128>(p, a, ws, stream);
         }
-        if (a.k > 1) {
-            const int64_t blocks = std::min<int64_t>(((int64_t)a.T * (a.len / 8) + 255) / 256, 1 << 16);
-            linear_sum_kernel<<<(unsigned)blocks, 256, 0, stream>>>(a, reinterpret_cast<const float*>(ws + p.off_shares));
-            e = hipGetLastError();
-            if (e != hipSuccess) return e;
-        }
     }
-    if (!a.dW) return hipGetLastError();
-    if (p.dw_cols == 256)
-        dw_launch<256, 256, 8, true>(p, a, ws, stream);
-    else if (p.dw_cols == 64)
-        dw_launch<64, 128, 4, false>(p, a, ws, stream);
-    else if (p.dw_rows == 64)
-        dw_launch<128, 64, 4, true>(p, a, ws, stream);
-    else
-        dw_launch<128, 128, 4, true>(p, a, ws, stream);
-    if (p.dw_parts > 1) {
+    if (dx && a.k > 1) {
         e = hipGetLastError();
         if (e != hipSuccess) return e;
-        return ffn_parts_sum_launch(reinterpret_cast<const float*>(ws + p.off_parts), p.dw_parts,
-                                    (int64_t)a.M * a.N * a.len, a.dW, stream);
+        const int64_t blocks = std::min<int64_t>(((int64_t)a.T * (a.len / 8) + 255) / 256, 1 << 16);
+        linear_sum_kernel<<<(unsigned)blocks, 256, 0, stream>>>(a, reinterpret_cast<const float*>(ws + p.off_shares));
     }
-    return hipGetLastError();
+    if (a.dW && !both) {
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (p.dw_cols == 256)
+            dw_launch<256, 256, 8, true>(p, a, ws, stream);
+        else if (p.dw_cols == 64)
+            dw_launch<64, 128, 4, false>(p, a, ws, stream);
+        else if (p.dw_rows == 64)
+            dw_launch<128, 64, 4, true>(p, a, ws, stream);
+        else
+            dw_launch<128, 128, 4, true>(p, a, ws, stream);
+    }
+    e = hipGetLastError();
+    if (e != hipSuccess || !a.dW || p.dw_parts == 1) return e;
+    return ffn_parts_sum_launch(reinterpret_cast<const float*>(ws + p.off_parts), p.dw_parts, (int64_t)a.M * a.N * a.len, a.dW,
+                                stream);
 }
 
 }  // namespace more
