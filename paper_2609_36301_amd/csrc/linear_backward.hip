@@ -254,16 +254,49 @@ struct LinearDw {
     float* parts;
 };
 
+// Narrow tiles (64 rows or columns) do with one stage in LDS, so that four workgroups fit on a CU instead of two (us, two
+// stages : one, 4096 experts of K = 64, N = 512, 32 entries 99 : 84; 2000 of K = 40, N = 520, 30 entries 62 : 38; wide tiles,
+// whose registers leave room for three, 4096 of K = 512, N = 128 109 : 115).
+template <int CT, int RT>
+constexpr int dw_slots() {
+    return CT + RT <= 192 ? 1 : 2;
+}
 template <int CT, int RT, int WAVES, bool PARTS>
 constexpr int dw_lds() {
-    return 2 * (CT + RT) * 128 + (PARTS ? 0 : WAVES * kLinesScratch);
+    return dw_slots<CT, RT>() * (CT + RT) * 128 + (PARTS ? 0 : WAVES * kLinesScratch);
+}
+
+// The pipeline by way of registers with one stage in LDS (the arguments are ffn_pipeline_staged's): the next stage is read
+// into registers while the present one is multiplied.
+template <typename S, int GROUPS, typename M, typename N, typename F, typename P, typename W>
+__device__ __forceinline__ void pipeline_single(int steps, F fetch, P put, W w) {
+    S s;
+    M m;
+    N n;
+    fetch(0, s);
+    for (int step = 0; step < steps; ++step) {
+        ffn_barrier<63>();  // the stage before has been read
+        put(0, s);
+        if (step + 1 < steps) fetch(step + 1, s);
+        ffn_barrier<63>();
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            w.read_n(0, kk, n);
+#pragma unroll
+            for (int group = 0; group < GROUPS; ++group) {
+                w.read_m(0, kk, group, m);
+                w.multiply(group, m, n);
+            }
+        }
+        w.done();
+    }
 }
 
 // The work of workgroup `block` of `blocks`.
 template <int CT, int RT, int WAVES, bool BY_COLS, bool PARTS>
 __device__ __forceinline__ void linear_dw(const LinearArgs& a, const LinearDw& d, uint32_t block, uint32_t blocks, LdsChar* smem) {
     constexpr int kStageBytes = (CT + RT) * 128;
-    LdsChar* lines = smem + (PARTS ? 0 : 2 * kStageBytes + ffn_wave() * kLinesScratch);
+    LdsChar* lines = smem + (PARTS ? 0 : dw_slots<CT, RT>() * kStageBytes + ffn_wave() * kLinesScratch);
     constexpr int kWavesM = CT >= 128 ? 2 : 1, kWavesN = WAVES / kWavesM;
     constexpr int kM = CT / kWavesM / 16, kN = RT / kWavesN / 16;  // 16 x 16 tiles per wave
     static_assert(kM % 4 == 0, "whole lines of dW: 64 columns");
@@ -362,53 +395,55 @@ __device__ __forceinline__ void linear_dw(const LinearArgs& a, const LinearDw& d
         using NF = FfnFragments<kN>;
         using Stage = StagePair<XLoader, YLoader>;
         fetch(0);
-        ffn_pipeline_staged<Stage, G::kGroups, MF, NF>(
-            ksteps * ssteps, true,
-            [&](int, Stage& st) {
-                const int32_t c = BY_COLS ? ls : other, r = BY_COLS ? other : ls;
-                xl.fetch(st.a, K - c, [&](int i) -> const uint16_t* {
-                    return entry[i] < (uint32_t)n ? a.x + (int64_t)(entry[i] / (uint32_t)a.k) * K + c : nullptr;
-                });
-                yl.fetch(st.b, N - r, [&](int i) -> const uint16_t* {
-                    return entry[i] < (uint32_t)n ? a.dy + (int64_t)entry[i] * N + r : nullptr;
-                });
-                if (++lk == ksteps) {
-                    lk = 0;
-                    ls += kStep;
-                }
-                if (ksteps > 1) fetch(lk);
+        auto load = [&](int, Stage& st) {
+            const int32_t c = BY_COLS ? ls : other, r = BY_COLS ? other : ls;
+            xl.fetch(st.a, K - c, [&](int i) -> const uint16_t* {
+                return entry[i] < (uint32_t)n ? a.x + (int64_t)(entry[i] / (uint32_t)a.k) * K + c : nullptr;
+            });
+            yl.fetch(st.b, N - r, [&](int i) -> const uint16_t* {
+                return entry[i] < (uint32_t)n ? a.dy + (int64_t)entry[i] * N + r : nullptr;
+            });
+            if (++lk == ksteps) {
+                lk = 0;
+                ls += kStep;
+            }
+            if (ksteps > 1) fetch(lk);
+        };
+        auto put = [&](int slot, const Stage& st) {
+            xl.put(smem + slot * kStageBytes, st.a);
+            yl.put(smem + slot * kStageBytes + CT * 128, st.b);
+        };
+        auto products = ffn_work(
+            [&](int slot, int kk, int group, MF& m) {
+#pragma unroll
+                for (int i = 0; i < G::kSize; ++i)
+                    if (G::tile(group, i) < kM)
+                        m.v[i] = col_fragment(smem + slot * kStageBytes, 16 * (wm * kM + G::tile(group, i)), kk);
             },
-            [&](int slot, const Stage& st) {
-                xl.put(smem + slot * kStageBytes, st.a);
-                yl.put(smem + slot * kStageBytes + CT * 128, st.b);
+            [&](int slot, int kk, NF& f) {
+#pragma unroll
+                for (int j = 0; j < kN; ++j)
+                    f.v[j] = col_fragment(smem + slot * kStageBytes + CT * 128, 16 * (wn * kN + j), kk);
             },
-            ffn_work(
-                [&](int slot, int kk, int group, MF& m) {
+            [&](int group, const MF& m, const NF& f) {
 #pragma unroll
-                    for (int i = 0; i < G::kSize; ++i)
-                        if (G::tile(group, i) < kM)
-                            m.v[i] = col_fragment(smem + slot * kStageBytes, 16 * (wm * kM + G::tile(group, i)), kk);
-                },
-                [&](int slot, int kk, NF& f) {
+                for (int i = 0; i < G::kSize; ++i)
+                    if (G::tile(group, i) < kM)
 #pragma unroll
-                    for (int j = 0; j < kN; ++j)
-                        f.v[j] = col_fragment(smem + slot * kStageBytes + CT * 128, 16 * (wn * kN + j), kk);
-                },
-                [&](int group, const MF& m, const NF& f) {
-#pragma unroll
-                    for (int i = 0; i < G::kSize; ++i)
-                        if (G::tile(group, i) < kM)
-#pragma unroll
-                            for (int j = 0; j < kN; ++j) {
-                                f32x4& c = acc[G::tile(group, i)][j];
-                                c = mfma_16x16x32(m.v[i], f.v[j], c);
-                            }
-                },
-                [&] {
-                    if (++ck < ksteps) return;
-                    ck = 0;
-                    store();
-                }));
+                        for (int j = 0; j < kN; ++j) {
+                            f32x4& c = acc[G::tile(group, i)][j];
+                            c = mfma_16x16x32(m.v[i], f.v[j], c);
+                        }
+            },
+            [&] {
+                if (++ck < ksteps) return;
+                ck = 0;
+                store();
+            });
+        if constexpr (dw_slots<CT, RT>() == 1)
+            pipeline_single<Stage, G::kGroups, MF, NF>(ksteps * ssteps, load, put, products);
+        else
+            ffn_pipeline_staged<Stage, G::kGroups, MF, NF>(ksteps * ssteps, true, load, put, products);
     }
 }
 
@@ -526,6 +561,7 @@ void dw_plan(int64_t n, int32_t K, int32_t N, int32_t M, LinearPlan* p) {
     const int32_t step = by_cols ? p->dw_cols : p->dw_rows, side = by_cols ? K : N;
     const int64_t groups = M * (by_cols ? tiles(N, p->dw_rows) : tiles(K, p->dw_cols));
     p->dw_span = p->dw_parts > 1 ? step : linear_span(n / M, step, groups, side);
+    if (p->dw_rows != p->dw_cols) p->dw_span = std::min(p->dw_span, 256);  // (512 89 us of the 84 above)
 }
 
 }  // namespace
