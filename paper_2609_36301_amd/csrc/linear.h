@@ -40,8 +40,9 @@ struct LinearPlan {
     int32_t stream;   // (q8, tiles of 256 rows) the pipeline runs on from tile to tile
     int32_t both;              // (backward) one launch makes both gradients
     int32_t dw_rows, dw_cols;  // rows and columns of a tile of dW
+    int32_t dw_by_rows;        // a workgroup's tiles lie along N, not K
     int32_t dw_parts;          // runs of an expert's entries that are summed apart
-    int32_t dw_span;           // of dW's longer side that a workgroup takes
+    int32_t dw_span;           // of that side that a workgroup takes
     size_t off_shares, off_parts;
     size_t workspace_bytes;
 };

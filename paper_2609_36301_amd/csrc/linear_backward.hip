@@ -557,7 +557,10 @@ void dw_plan(int64_t n, int32_t K, int32_t N, int32_t M, LinearPlan* p) {
         p->dw_rows = p->dw_cols = 256;
     else
         p->dw_parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({512 / small, steps / 4, 32}));
-    const bool by_cols = p->dw_cols > 64;
+    // along the longer side, where the launch is dW's alone (us, 4096 experts of K = 128, N = 512, 32 entries, along K : N
+    // 185 : 154; 1024 of K = 128, N = 1024, 128 entries 139 : 144)
+    p->dw_by_rows = p->dw_cols == 64 || (p->dw_cols == 128 && p->dw_rows == 128 && p->listed && K <= 128 && N > 128);
+    const bool by_cols = !p->dw_by_rows;
     const int32_t step = by_cols ? p->dw_cols : p->dw_rows, side = by_cols ? K : N;
     const int64_t groups = M * (by_cols ? tiles(N, p->dw_rows) : tiles(K, p->dw_cols));
     p->dw_span = p->dw_parts > 1 ? step : linear_span(n / M, step, groups, side);
@@ -574,8 +577,8 @@ void linear_backward_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int
     ffn_tiles_plan(n, M, bm, &p->tiles);
     if (bm == 256) p->cols = 256;
     p->span = linear_span(N, p->cols, p->tiles.tiles, len);
-    dw_plan(n, len, N, M, p);
     p->listed = linear_listed(p->tiles, M, (len + p->span - 1) / p->span);
+    dw_plan(n, len, N, M, p);
     p->both = !p->listed && p->dw_cols < 256;
     size_t at = p->listed ? p->tiles.workspace_bytes : 0;
     p->off_shares = at;
@@ -620,6 +623,8 @@ hipError_t linear_backward_launch(const LinearPlan& p, const LinearArgs& a, void
             dw_launch<64, 128, 4, false>(p, a, ws, stream);
         else if (p.dw_rows == 64)
             dw_launch<128, 64, 4, true>(p, a, ws, stream);
+        else if (p.dw_by_rows)
+            dw_launch<128, 128, 4, false>(p, a, ws, stream);
         else
             dw_launch<128, 128, 4, true>(p, a, ws, stream);
     }

@@ -237,6 +237,22 @@ def test_tiles_found_and_listed(M, hot):
     assert any(rows and not listed for rows, listed in seen) == (M <= 1024)
 
 
+@pytest.mark.parametrize("T,K,N,M,k", [(9000, 72, 264, 1500, 1), (5000, 128, 520, 1100, 2), (40000, 40, 520, 1200, 1), (30000, 528, 56, 1200, 1),
+                                       (20000, 128, 136, 1300, 3)])
+def test_gradients_of_many_small_experts(T, K, N, M, k):
+    """Narrow tiles of dW with one stage, tiles along N, several tiles to a workgroup, experts of none to several stages."""
+    require_gpu()
+    from paper_2609_36301_amd import expert_linear_backward, expert_linear_plan
+    for hot in (False, True):
+        x, W, dy, idx, offsets, srt = case(K + N, T, K, N, M, k, hot=hot)
+        announce("expert_linear_backward T=%d K=%d N=%d M=%d k=%d hot=%s %s"
+                 % (T, K, N, M, k, hot, expert_linear_plan(T, K, N, M, k, "backward")))
+        g = expert_linear_backward(*[to_dev(v) for v in (x, W, idx, offsets, srt, dy)])
+        (dx, dW), (bx, bW) = ref.linear_backward(from_bf16(x), from_bf16(W), idx, from_bf16(dy))
+        within(to_np(g.dx), dx, bx, "dx")
+        within(to_np(g.dWt), dW, bW, "dW")
+
+
 @pytest.mark.parametrize("M", [65537, 70000])
 def test_more_experts_than_one_list_counts(M):
     """Beyond 2^16 experts their tiles are counted ahead of the list."""
