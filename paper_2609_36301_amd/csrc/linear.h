@@ -19,6 +19,7 @@ struct LinearArgs {
     const int32_t* offsets;  // [M + 1]
     const int32_t* sorted;   // [T k]
     int32_t q8, wide;        // int8 operands; y in fp32
+    int32_t whole;           // rows of the result (y; dx or its shares) are whole lines of 128 bytes
     const float* x_scale;    // (q8) [T]
     const float* w_scale;    // (q8) [M][N]
     const float* gate;       // (q8) [T][k] or NULL
@@ -47,10 +48,15 @@ struct LinearPlan {
     size_t workspace_bytes;
 };
 
+// Whether rows of `bytes` bytes from p on are whole lines.
+inline int32_t linear_whole(const void* p, int64_t bytes) {
+    return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)bytes) & 127) == 0;
+}
+
 void linear_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, bool q8, LinearPlan* p);
 void linear_backward_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, LinearPlan* p);
 hipError_t linear_launch(const LinearPlan& p, const LinearArgs& a, void* workspace, hipStream_t stream);
-hipError_t linear_backward_launch(const LinearPlan& p, const LinearArgs& a, void* workspace, hipStream_t stream);
+hipError_t linear_backward_launch(const LinearPlan& p, LinearArgs a, void* workspace, hipStream_t stream);
 
 // The product in 8-bit integers on tiles of 256 rows and 256 columns whose contraction has at least kStreamSteps
 // stages (linear_stream.hip), after the tile list.

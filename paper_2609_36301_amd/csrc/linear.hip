@@ -147,7 +147,7 @@ __global__ __launch_bounds__(linear_threads(BM), 2) void linear_kernel(LinearArg
 #pragma unroll
                                 for (int i = 0; i < L::kTiles; ++i)
                                     L::place(lines, i, linear_value<I8>(acc[i0 + i][j], row_scale[j], ws[i]));
-                                L::store(lines, c1 - c, [&](int r) -> Out* {
+                                L::store(lines, c1 - c, a.whole, [&](int r) -> Out* {
                                     const uint32_t p = (uint32_t)__shfl((int)place[j], r, 64);
                                     return p < (uint32_t)n ? static_cast<Out*>(a.y) + (int64_t)p * N + c : nullptr;
                                 });

@@ -47,6 +47,7 @@ more_status forward(more::LinearArgs a, int64_t T, int32_t y_bits, void* workspa
     if (p.workspace_bytes != 0 && (!workspace || workspace_bytes < p.workspace_bytes)) return MORE_ERR_WORKSPACE;
     a.T = (int32_t)T;
     a.wide = y_bits == 32;
+    a.whole = more::linear_whole(a.y, a.N * (int64_t)(y_bits / 8));
     return from_hip(more::linear_launch(p, a, workspace, static_cast<hipStream_t>(stream)));
 }
 

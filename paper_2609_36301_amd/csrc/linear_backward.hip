@@ -132,7 +132,7 @@ __device__ __forceinline__ void linear_dx(const LinearArgs& a, const void* __res
 #pragma unroll
                         for (int i = 0; i < L::kTiles; ++i) L::place(lines, i, acc[i0 + i][j]);
                         const int32_t c = cc + 16 * (wm * S::kM + i0);
-                        L::store(lines, c1 - c, [&](int r) -> Out* {
+                        L::store(lines, c1 - c, a.whole, [&](int r) -> Out* {
                             const uint32_t p = (uint32_t)__shfl((int)place[j], r, 64);
                             return p < (uint32_t)n ? static_cast<Out*>(out) + (int64_t)p * cols + c : nullptr;
                         });
@@ -376,7 +376,7 @@ __device__ __forceinline__ void linear_dw(const LinearArgs& a, const LinearDw& d
                     }
                     const int32_t c = (BY_COLS ? cs : other) + 16 * (wm * kM + i0);
                     const int32_t r = (BY_COLS ? other : cs) + 16 * (wn * kN + j);
-                    Lines<false>::store(lines, (BY_COLS ? s1 : K) - c, [&](int row) {
+                    Lines<false>::store(lines, (BY_COLS ? s1 : K) - c, true, [&](int row) {
                         return r + row < (BY_COLS ? N : s1) ? o + (int64_t)(r + row) * K + c : nullptr;
                     });
                 }
@@ -595,8 +595,9 @@ void linear_backward_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int
     p->workspace_bytes = at;
 }
 
-hipError_t linear_backward_launch(const LinearPlan& p, const LinearArgs& a, void* workspace, hipStream_t stream) {
+hipError_t linear_backward_launch(const LinearPlan& p, LinearArgs a, void* workspace, hipStream_t stream) {
     char* ws = static_cast<char*>(workspace);
+    a.whole = a.k == 1 ? linear_whole(a.dx, a.len * (int64_t)2) : linear_whole(nullptr, a.len * (int64_t)4);
     const bool dx = p.tiles.n > 0 && a.dx, both = p.both && dx && a.dW;
     hipError_t e = hipSuccess;
     if (both) {

@@ -142,8 +142,10 @@ __device__ __forceinline__ u32x4 linear_pair(f32x4 a, f32x4 b) {
 // Whole lines: 16 rows of 128 bytes (64 columns of bf16, 32 of fp32) by way of a wave's own 2 KiB of LDS, from where a
 // store takes eight rows.  The 16-byte pieces of a row are XORed with the row's number, which spreads them over the banks.
 // A wave's LDS accesses are in order, so there is no barrier.  Nontemporal whole lines reach memory without being read
-// first: the gradients of 4096 experts, N = 512, K = 64, 32 rows 65 us, plain lines 98, nontemporal halves of lines 84; also
-// where K splits the lines (K = 72 122 : 164).
+// first: the gradients of 4096 experts, N = 512, K = 64, 32 rows 65 us, plain lines 98, nontemporal halves of lines 84.  Rows
+// that split lines are stored plainly, so that L2 joins the parts of different workgroups (us, nontemporal : plain,
+// 65536 rows, K = 128, N = 2040 182 : 122, but N = 2048 78 : 119; dx of K = 1808, N = 24, 34656 rows 67 : 38), but for dW,
+// whose rows lie one after the other and make lines together (K = 528, N = 128, 4096 experts 175 : 266).
 constexpr int kLinesScratch = 16 * 128;
 template <bool WIDE>
 struct Lines {
@@ -161,9 +163,9 @@ struct Lines {
                 scratch + row * 128 + (((2 * i + (g >> 1)) ^ (row & 7)) << 4) + ((g & 1) << 3)) = u32x2{b.x, b.y};
         }
     }
-    // row_of(r): where row r goes (NULL: nowhere); `left` elements of it at most (whole pieces)
+    // row_of(r): where row r goes (NULL: nowhere); `left` elements of it at most (whole pieces); `whole` as in LinearArgs
     template <typename F>
-    static __device__ __forceinline__ void store(LdsChar* scratch, int left, F row_of) {
+    static __device__ __forceinline__ void store(LdsChar* scratch, int left, bool whole, F row_of) {
         const int l = ffn_lane(), piece = l & 7;
 #pragma unroll
         for (int r = 0; r < 16; r += 8) {
@@ -171,8 +173,14 @@ struct Lines {
             char* p = reinterpret_cast<char*>(row_of(row));
             const u32x4 v =
                 *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(scratch + row * 128 + ((piece ^ (row & 7)) << 4));
-            if (p && piece * (16 / (int)sizeof(Element)) < left)
-                __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p + 16 * piece));
+            u32x4* to = reinterpret_cast<u32x4*>(p + 16 * piece);
+            const bool in = p && piece * (16 / (int)sizeof(Element)) < left;
+            if (whole) {
+                if (in) __builtin_nontemporal_store(v, to);
+                asm volatile("; whole lines");  // (else the compiler makes one plain store of both)
+            } else {
+                if (in) *to = v;
+            }
         }
     }
 };

@@ -247,7 +247,7 @@ __global__ __launch_bounds__(kStreamThreads, 2) void linear_stream_kernel(Linear
 #pragma unroll
                                 for (int i = 0; i < L::kTiles; ++i) L::place(lines, i, value(i0 + i));
                                 const int32_t c = c0 - 4 * (lane >> 4) + 16 * i0;
-                                L::store(lines, cols - c, [&](int r) -> Out* {
+                                L::store(lines, cols - c, a.whole, [&](int r) -> Out* {
                                     const uint32_t e = t->entry[row0 + r];
                                     return row0 + r < t->tile.rows && e < (uint32_t)n
                                                ? static_cast<Out*>(a.y) + (int64_t)e * cols + c : nullptr;
