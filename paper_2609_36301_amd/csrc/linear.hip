@@ -322,23 +322,36 @@ void forward(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t str
 
 }  // namespace
 
-// Rows of a tile: 32 where experts have less than 24 rows (then mostly one tile, whose weights are not read again), else
-// what costs least: the rounds in which the workgroups fill the chip (two of up to 128 rows to a CU, one of 256) times the
-// stages times the time of a stage, and for 256 rows what such a tile costs beside its stages, since nothing else on
-// the CU hides it.  Fitted to the maps and dx of 130 shapes (1 to 512 experts, 32 to 16384 rows each, contractions and
-// columns of 64 to 2048): 1.8 % off the best on geometric mean, 28 % at most.  us for 32 : 64 : 128 : 256 rows, dense maps of
-// 1024 rows of K = N = 1024 16 : 19 : 22 : 34 (dx), 8 experts of 4096 rows, K = 2048, N = 256 109 : 64 : 61 : 56.
-int32_t linear_tile_rows(int64_t n, int32_t M, int32_t cols, int32_t cols_of, int64_t steps, bool q8) {
-    if (n / std::max<int64_t>(1, std::min<int64_t>(n, M)) < 24) return 32;
+// Rows of a tile: 32 where experts have less than 8 rows (then mostly one tile, whose weights are not read again), else
+// what costs least: the rounds in which the workgroups fill the chip (two of up to 128 rows to a CU, one of 256), beyond three
+// with half a round of rest, times the stages times the time of a stage and what a tile costs beside its stages.
+// Fitted to 800 shapes (1 to 8192 experts, 4 to 16384 rows each, contractions and columns of 16 to 4096, of which half are not
+// multiples of 64): 2.1 % off the best on geometric mean, five in a hundred more than 15 %.  us for
+// 32 : 64 : 128 : 256 rows, one expert of K = 2912, N = 1160 with 1976 rows 83 : 65 : 34 : 76; 8 bits, 15 of K = 3200, N = 3008
+// with 225 rows 174 : 105 : 55 : 89; dx, 11 of K = 3648, N = 576 with 2523 rows 287 : 234 : 174 : 148.
+namespace {
+struct TileCost {
+    int32_t alone, two;  // time of a stage, one workgroup and two to a CU
+    int32_t fixed;       // of a tile beside its stages
+    int32_t narrow;      // sixteenths of a stage's time where a step has 64 columns
+};
+constexpr TileCost kTileCost[3][4] = {{{7, 18, 18, 13}, {14, 17, 30, 14}, {14, 17, 46, 13}, {25, 25, 119, 16}},
+                                      {{7, 10, 8, 14}, {9, 12, 26, 10}, {16, 16, 27, 10}, {21, 21, 87, 16}},
+                                      {{14, 21, 31, 17}, {8, 18, 43, 16}, {12, 16, 61, 8}, {14, 14, 163, 16}}};
+}  // namespace
+int32_t linear_tile_rows(int64_t n, int32_t M, int32_t cols, int32_t cols_of, int64_t steps, LinearProduct product) {
+    if (n / std::max<int64_t>(1, std::min<int64_t>(n, M)) < 8) return 32;
     int32_t best = 64;
     int64_t least = INT64_MAX;
-    for (int32_t bm = 32; bm <= 256; bm *= 2) {
-        const int64_t tiles2 = ffn_expected_tiles2(n, M, bm);
+    for (int32_t i = 0, bm = 32; bm <= 256; bm *= 2, ++i) {
+        if (bm == 256 && product == kProductQ8 && steps < kStreamSteps) break;  // (too slow without linear_stream_kernel)
+        const TileCost c = kTileCost[product][i];
         const int32_t step = bm == 256 ? 256 : cols_of;
-        const int64_t items = tiles2 * ((cols + step - 1) / step) / 2, slots = bm == 256 ? 256 : 512;
-        const bool alone = items <= 256;
-        const int64_t stage = bm == 256 ? (q8 ? 20 : 28) : bm == 128 ? (alone ? 16 : 20) : bm == 64 ? (alone ? 11 : 15) : alone ? 9 : 18;
-        const int64_t cost = (items + slots - 1) / slots * (steps * stage + (bm == 256 ? 60 : 0));
+        const int64_t slots = bm == 256 ? 256 : 512;
+        const int64_t items = ffn_expected_tiles2(n, M, bm) * ((cols + step - 1) / step) / 2;
+        const int64_t stage = (items <= 256 ? c.alone : c.two) * (step == 64 ? c.narrow : 16);
+        const int64_t item = steps * stage + 16 * c.fixed;
+        const int64_t cost = items <= 3 * slots ? (items + slots - 1) / slots * 2 * item : items * 2 * item / slots + item;
         if (cost < least) {
             least = cost;
             best = bm;
@@ -375,7 +388,7 @@ void linear_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, b
     const int64_t n = T * k;
     *p = LinearPlan{};
     p->cols = N <= 64 ? 64 : 128;
-    const int32_t bm = linear_tile_rows(n, M, N, p->cols, (len + kFfnBK - 1) / kFfnBK, q8);
+    const int32_t bm = linear_tile_rows(n, M, N, p->cols, (len + kFfnBK - 1) / kFfnBK, q8 ? kProductQ8 : kProductMap);
     ffn_tiles_plan(n, M, bm, &p->tiles);
     // The kernel without tiles has a short way to its first operands, but reads the weights again for every 16 entries, the
     // rows of x in every workgroup, and starts a workgroup for each entry, of which most end at once: it is taken

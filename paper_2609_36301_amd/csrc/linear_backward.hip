@@ -580,7 +580,7 @@ void linear_backward_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int
     const int64_t n = T * k;
     *p = LinearPlan{};
     p->cols = len <= 64 ? 64 : 128;
-    const int32_t bm = linear_tile_rows(n, M, len, p->cols, (N + kFfnBK - 1) / kFfnBK, false);
+    const int32_t bm = linear_tile_rows(n, M, len, p->cols, (N + kFfnBK - 1) / kFfnBK, kProductDx);
     ffn_tiles_plan(n, M, bm, &p->tiles);
     if (bm == 256) p->cols = 256;
     p->span = linear_span(N, p->cols, p->tiles.tiles, len);
