@@ -12,8 +12,9 @@
 // calls, 5.2 TB/s; 37 of 1001 5.3 us in a graph.  A group of threads takes a row, R pieces of 16 bytes to a thread; rows
 // that do not fit are read again instead.  Rows start at any element: the pieces are those that lie at multiples of 16
 // bytes, and each of the few elements before and behind them is some thread's own, so nothing outside the row is touched.
-// The teacher's entries lie in LDS; after its stores a wave goes through those in its own pieces, and the lane that
-// holds it stores the entry's gradient over the first one (same lane, same address: in order).
+// The teacher's entries lie in LDS; a wave waits for its stores, then its lanes store the gradients of those entries that
+// lie in its own pieces over the first ones (us, one entry after the other by the lane that holds it, without a wait : so,
+// 13370 rows of 194 fp32, k = 28 22.8 : 13.4; 16384 of 4096, k = 64 120 : 103, k = 8 93.9 : 95.6).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -335,17 +336,14 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void distill_kernel(
             }
             if (at.edge < a.V) dz[at.edge] = P::element(some ? gp * __builtin_amdgcn_exp2f((x.own - m) * c) : 0.0f);
             group_sync<THREADS>();  // the sums are there
-            for (int32_t j0 = 0; some && j0 < a.k; j0 += 64) {
-                const int lane = tid & 63;
-                const int32_t id = j0 + lane < a.k ? id_of[j0 + lane] : -1;
-                const int32_t in = id - at.head, end = at.pieces * kCount;
-                // the thread whose piece or own element it is
-                const int32_t owner = in < 0 ? id : in < end ? (int32_t)((uint32_t)in / kCount % THREADS) : id - end;
-                for (uint64_t mine = __ballot(id >= 0 && owner >> 6 == tid >> 6); mine; mine &= mine - 1) {
-                    const int l = __builtin_ctzll(mine);
-                    const int32_t the_id = __builtin_amdgcn_readlane(id, l);
-                    if (lane == (__builtin_amdgcn_readlane(owner, l) & 63))
-                        dz[the_id] = P::element(gp * __builtin_amdgcn_exp2f((z_of[j0 + l] - m) * c) - g * sum_of[j0 + l]);
+            if (some) {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the wave's pieces have been written
+                for (int32_t j = tid & 63; j < a.k; j += 64) {
+                    const int32_t id = id_of[j], in = id - at.head, end = at.pieces * kCount;
+                    // the thread whose piece or own element it is
+                    const int32_t owner = in < 0 ? id : in < end ? (int32_t)((uint32_t)in / kCount % THREADS) : id - end;
+                    if (id >= 0 && owner >> 6 == tid >> 6)
+                        dz[id] = P::element(gp * __builtin_amdgcn_exp2f((z_of[j] - m) * c) - g * sum_of[j]);
                 }
             }
         }

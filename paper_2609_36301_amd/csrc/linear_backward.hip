@@ -550,7 +550,9 @@ void both_launch(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t
 
 // Tile of dW, by the rounds in which its workgroups fill the chip (two of 128 x 128 to a CU, one of 256 x 256) times the
 // stages times the time of a stage, and for 256 what such a tile costs beside its stages; and the runs into which an expert's
-// entries are cut: as many as bring the tiles to 512, of four stages at least, and at most 32.  0.9 % off the better tile on
+// entries are cut: as many as bring the tiles to 512, of four stages at least, at most 32, or 128 of 14 stages (us, 32 : 128
+// runs of 115849 rows, K = 144, N = 8 54 : 29, 131072 of K = 256, N = 128 82 : 42; 32 : 39 of 10000, 3 experts, K = 200,
+// N = 136 21 : 23).  0.9 % off the better tile on
 // geometric mean over 240 shapes (us, 128 : 256, 94 experts of 192 x 304, 30249 entries 26 : 34; 31 of 960 x 2048, 12500
 // 210 : 148).
 void dw_plan(int64_t n, int32_t K, int32_t N, int32_t M, LinearPlan* p) {
@@ -563,7 +565,8 @@ void dw_plan(int64_t n, int32_t K, int32_t N, int32_t M, LinearPlan* p) {
     if (std::max<int64_t>(256, large) * 2 * (32 * steps + 10) < std::max<int64_t>(512, small) * (small <= 256 ? 16 : 20) * steps)
         p->dw_rows = p->dw_cols = 256;
     else
-        p->dw_parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({512 / small, steps / 4, 32}));
+        p->dw_parts = (int32_t)std::max<int64_t>(
+            1, std::min({512 / small, steps / 4, std::max<int64_t>(32, std::min<int64_t>(steps / 14, 128))}));
     // along the longer side, where the launch is dW's alone (us, 4096 experts of K = 128, N = 512, 32 entries, along K : N
     // 185 : 154; 1024 of K = 128, N = 1024, 128 entries 139 : 144)
     p->dw_by_rows = p->dw_cols == 64 || (p->dw_cols == 128 && p->dw_rows == 128 && p->listed && K <= 128 && N > 128);
