@@ -8,8 +8,8 @@
 // and gradient 0.
 //
 // Memory-bound: a row's logits are read once and stay in registers between maximum, sum and gradient, so that the loss
-// with its gradient is one read and one write: 8192 rows of 32001 bf16 189 us, 5.5 TB/s; 16384 of 4096 fp32 156 us in two
-// calls, 5.2 TB/s; 37 of 1001 5.3 us in a graph.  A group of threads takes a row, R pieces of 16 bytes to a thread; rows
+// with its gradient is one read and one write: 8192 rows of 32001 bf16 187 us, 5.6 TB/s; 16384 of 4096 fp32 154 us in two
+// calls, 5.2 TB/s; 37 of 1001 4.9 us in a graph.  A group of threads takes a row, R pieces of 16 bytes to a thread; rows
 // that do not fit are read again instead.  Rows start at any element: the pieces are those that lie at multiples of 16
 // bytes, and each of the few elements before and behind them is some thread's own, so nothing outside the row is touched.
 // The teacher's entries lie in LDS; a wave waits for its stores, then its lanes store the gradients of those entries that

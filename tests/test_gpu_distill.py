@@ -266,3 +266,27 @@ def test_no_rows():
     e = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device="cuda")  # noqa: E731
     d = distill_loss(e(0, 50), e(0, 3, dtype=torch.int32), e(0, 3), gradient=True)
     assert d.loss.shape == (0,) and d.dlogits.shape == (0, 50)
+
+
+@pytest.mark.parametrize("V", [64, 900, 5000, 20000, 70000, 140000])
+@pytest.mark.parametrize("k", [32, 64, 200])
+def test_entries_that_meet(V, k):
+    """Entries next to one another, at a row's ends and more than once: each class has one gradient, of all its entries."""
+    torch = require_gpu()
+    from paper_2609_36301_amd import distill_loss
+    T, tau = 9, 2.0
+    for bits in (16, 32):
+        z, ids, values, w = case(V + k, T, V, k, bits)
+        rng = np.random.default_rng(V)
+        near = np.r_[np.arange(20), np.arange(V - 20, V)]
+        ids[:] = rng.choice(near, (T, k))
+        ids[3] = V // 2
+        ids[4, ::2] = -1
+        announce("distill V=%d k=%d bits=%d, entries that meet" % (V, k, bits))
+        (loss, _, _, grad), (bl, _, bg) = ref.distill(z, ids, values.astype(np.float64), tau, w.astype(np.float64), bits)
+        logits = rows_on_device(z, bits, V + 1, 1)[1]
+        d = distill_loss(logits, to_dev(ids), to_dev(values), to_dev(w), temperature=tau, gradient=True)
+        close(d.loss, loss, bl, "loss")
+        close(d.dlogits, grad, bg, "dlogits")
+        again = distill_loss(logits, to_dev(ids), to_dev(values), to_dev(w), temperature=tau, gradient=True)
+        assert torch.equal(again.dlogits, d.dlogits)

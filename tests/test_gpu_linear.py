@@ -238,9 +238,10 @@ def test_tiles_found_and_listed(M, hot):
 
 
 @pytest.mark.parametrize("T,K,N,M,k", [(9000, 72, 264, 1500, 1), (5000, 128, 520, 1100, 2), (40000, 40, 520, 1200, 1), (30000, 528, 56, 1200, 1),
-                                       (20000, 128, 136, 1300, 3)])
+                                       (20000, 128, 136, 1300, 3), (260000, 72, 136, 2, 1), (130000, 72, 136, 2, 2)])
 def test_gradients_of_many_small_experts(T, K, N, M, k):
-    """Narrow tiles of dW with one stage, tiles along N, several tiles to a workgroup, experts of none to several stages."""
+    """Narrow tiles of dW with one stage, tiles along N (in runs, too), several tiles to a workgroup, experts of none to several
+    stages."""
     require_gpu()
     from paper_2609_36301_amd import expert_linear_backward, expert_linear_plan
     for hot in (False, True):
