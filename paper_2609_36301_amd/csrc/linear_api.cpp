@@ -171,7 +171,8 @@ more_status more_expert_linear_backward(const uint16_t* x, const uint16_t* Wt, i
     if (st != MORE_OK) return st;
     more::LinearPlan p;
     more::linear_backward_make_plan(T, K, N, M, k, &p);
-    if (T != 0 && (!workspace || workspace_bytes < p.workspace_bytes)) return MORE_ERR_WORKSPACE;
+    if (T != 0 && p.workspace_bytes != 0 && (!workspace || workspace_bytes < p.workspace_bytes))
+        return MORE_ERR_WORKSPACE;
     more::LinearArgs a = linear_args(x, Wt, K, N, M, k, idx, offsets, sorted, false);
     a.T = (int32_t)T;
     a.dy = dy;

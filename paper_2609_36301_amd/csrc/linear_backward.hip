@@ -266,9 +266,9 @@ template <int CT, int RT>
 constexpr int dw_slots() {
     return CT + RT <= 192 ? 1 : 2;
 }
-template <int CT, int RT, int WAVES, bool PARTS>
+template <int CT, int RT, int WAVES>
 constexpr int dw_lds() {
-    return dw_slots<CT, RT>() * (CT + RT) * 128 + (PARTS ? 0 : WAVES * kLinesScratch);
+    return dw_slots<CT, RT>() * (CT + RT) * 128 + WAVES * kLinesScratch;
 }
 
 // The pipeline by way of registers with one stage in LDS (the arguments are ffn_pipeline_staged's): the next stage is read
@@ -301,7 +301,7 @@ __device__ __forceinline__ void pipeline_single(int steps, F fetch, P put, W w) 
 template <int CT, int RT, int WAVES, bool BY_COLS, bool PARTS>
 __device__ __forceinline__ void linear_dw(const LinearArgs& a, const LinearDw& d, uint32_t block, uint32_t blocks, LdsChar* smem) {
     constexpr int kStageBytes = (CT + RT) * 128;
-    LdsChar* lines = smem + (PARTS ? 0 : dw_slots<CT, RT>() * kStageBytes + ffn_wave() * kLinesScratch);
+    LdsChar* lines = smem + dw_slots<CT, RT>() * kStageBytes + ffn_wave() * kLinesScratch;
     constexpr int kWavesM = CT >= 128 ? 2 : 1, kWavesN = WAVES / kWavesM;
     constexpr int kM = CT / kWavesM / 16, kN = RT / kWavesN / 16;  // 16 x 16 tiles per wave
     static_assert(kM % 4 == 0, "whole lines of dW: 64 columns");
@@ -354,12 +354,17 @@ __device__ __forceinline__ void linear_dw(const LinearArgs& a, const LinearDw& d
 #pragma unroll
                 for (int j = 0; j < kN; ++j)
 #pragma unroll
-                    for (int i = 0; i < kM; ++i) {
-                        const int32_t c = (BY_COLS ? cs : other) + 16 * (wm * kM + i) + 4 * (ffn_lane() >> 4);
-                        const int32_t r = (BY_COLS ? other : cs) + 16 * (wn * kN + j) + (ffn_lane() & 15);
-                        if (c < (BY_COLS ? s1 : K) && r < (BY_COLS ? N : s1))
-                            *reinterpret_cast<f32x4*>(o + (int64_t)r * K + c) = acc[i][j];
-                        acc[i][j] = zero_f32x4();
+                    for (int i0 = 0; i0 < kM; i0 += 2) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            Lines<true>::place(lines, i, acc[i0 + i][j]);
+                            acc[i0 + i][j] = zero_f32x4();
+                        }
+                        const int32_t c = (BY_COLS ? cs : other) + 16 * (wm * kM + i0);
+                        const int32_t r = (BY_COLS ? other : cs) + 16 * (wn * kN + j);
+                        Lines<true>::store(lines, (BY_COLS ? s1 : K) - c, false, [&](int row) {
+                            return r + row < (BY_COLS ? N : s1) ? o + (int64_t)(r + row) * K + c : nullptr;
+                        });
                     }
                 cs += kStep;
                 return;
@@ -454,7 +459,7 @@ __device__ __forceinline__ void linear_dw(const LinearArgs& a, const LinearDw& d
 
 template <int CT, int RT, int WAVES, bool BY_COLS, bool PARTS>
 __global__ __launch_bounds__(64 * WAVES, 2) void linear_dw_kernel(LinearArgs a, LinearDw d) {
-    __shared__ __attribute__((aligned(1024))) char smem[dw_lds<CT, RT, WAVES, PARTS>()];
+    __shared__ __attribute__((aligned(1024))) char smem[dw_lds<CT, RT, WAVES>()];
     linear_dw<CT, RT, WAVES, BY_COLS, PARTS>(a, d, blockIdx.x, gridDim.x, (LdsChar*)smem);
 }
 
@@ -464,7 +469,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void linear_dw_kernel(LinearArgs a, 
 template <int BM, int COLS, bool DIRECT, int CT, int RT, bool BY_COLS, bool PARTS>
 __global__ __launch_bounds__(256, 2) void linear_both_kernel(LinearArgs a, int32_t bound, int32_t span, void* __restrict__ out,
                                                              uint32_t dx_blocks, LinearDw d) {
-    constexpr int kDx = DxShape<BM, COLS>::kLds, kDw = dw_lds<CT, RT, 4, PARTS>();
+    constexpr int kDx = DxShape<BM, COLS>::kLds, kDw = dw_lds<CT, RT, 4>();
     __shared__ __attribute__((aligned(1024))) char smem[kDx > kDw ? kDx : kDw];
     if (blockIdx.x < dx_blocks)
         linear_dx<BM, COLS, DIRECT, true>(a, nullptr, bound, span, out, (LdsChar*)smem);

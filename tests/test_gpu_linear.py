@@ -302,6 +302,24 @@ def test_offsets_and_sorted_of_another_selection():
                 assert (big[:128] == 7).all() and (big[-128:] == 7).all()
 
 
+def test_calls_without_a_workspace():
+    """Where none is needed it may be NULL."""
+    torch = require_gpu()
+    from paper_2609_36301_amd import _lib, expert_linear, expert_linear_backward, linear
+    T, K, N, M, k = 400, 72, 40, 20, 1
+    assert linear.expert_linear_workspace_size(T, K, N, M, k) == linear.expert_linear_backward_workspace_size(T, K, N, M, k) == 0
+    announce("expert_linear and its backward pass without a workspace")
+    args = [to_dev(v) for v in case(4, T, K, N, M, k)]
+    x, W, dy, idx, offsets, srt = args
+    y, dx, dW = (torch.full(s, 7.0, dtype=torch.bfloat16, device="cuda") for s in ((T, N), (T, K), (M, N, K)))
+    lib, stream = _lib.load(), torch.cuda.current_stream().cuda_stream
+    head = [x.data_ptr(), W.data_ptr(), T, K, N, M, k, idx.data_ptr(), offsets.data_ptr(), srt.data_ptr()]
+    assert lib.more_expert_linear(*head, y.data_ptr(), 16, None, 0, stream) == _lib.OK
+    assert lib.more_expert_linear_backward(*head, dy.data_ptr(), dx.data_ptr(), dW.data_ptr(), None, 0, stream) == _lib.OK
+    g = expert_linear_backward(x, W, idx, offsets, srt, dy)
+    assert torch.equal(y, expert_linear(x, W, idx, offsets, srt)) and torch.equal(dx, g.dx) and torch.equal(dW, g.dWt)
+
+
 def test_same_bits_every_run():
     require_gpu()
     from paper_2609_36301_amd import expert_linear, expert_linear_backward
