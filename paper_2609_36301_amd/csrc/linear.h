@@ -77,7 +77,8 @@ hipError_t linear_tiles_launch(const LinearPlan& p, const LinearArgs& a, void* w
 
 // Rows of a tile (32 to 256) of a product of n entries over M experts, `cols` columns (in steps of `cols_of`, of 256 with
 // tiles of 256 rows) and `steps` stages.
-enum LinearProduct { kProductMap, kProductDx, kProductQ8 };
+// (kProductSplit: a map whose stages of a row touch two lines)
+enum LinearProduct { kProductMap, kProductSplit, kProductDx, kProductQ8 };
 int32_t linear_tile_rows(int64_t n, int32_t M, int32_t cols, int32_t cols_of, int64_t steps, LinearProduct product);
 
 // q [T][width] int8 and scale [T] of the rows of x: bf16 [T][width], or (gated) [T][2 width].

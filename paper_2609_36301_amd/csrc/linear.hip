@@ -326,7 +326,8 @@ void forward(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t str
 // what costs least: the rounds in which the workgroups fill the chip (two of up to 128 rows to a CU, one of 256), beyond three
 // with half a round of rest, times the stages times the time of a stage and what a tile costs beside its stages.
 // Fitted to 800 shapes (1 to 8192 experts, 4 to 16384 rows each, contractions and columns of 16 to 4096, of which half are not
-// multiples of 64): 2.1 % off the best on geometric mean, five in a hundred more than 15 %.  us for
+// multiples of 64): 2.0 % off the best on geometric mean, five in a hundred more than 14 %.  Bf16 rows that split lines have costs of their
+// own: small tiles touch more lines for a product (27 experts of K = 2952, N = 152 with 552 rows, 64 : 128 rows 73 : 40).  us for
 // 32 : 64 : 128 : 256 rows, one expert of K = 2912, N = 1160 with 1976 rows 83 : 65 : 34 : 76; 8 bits, 15 of K = 3200, N = 3008
 // with 225 rows 174 : 105 : 55 : 89; dx, 11 of K = 3648, N = 576 with 2523 rows 287 : 234 : 174 : 148.
 namespace {
@@ -335,7 +336,8 @@ struct TileCost {
     int32_t fixed;       // of a tile beside its stages
     int32_t narrow;      // sixteenths of a stage's time where a step has 64 columns
 };
-constexpr TileCost kTileCost[3][4] = {{{7, 18, 18, 13}, {14, 17, 30, 14}, {14, 17, 46, 13}, {25, 25, 119, 16}},
+constexpr TileCost kTileCost[4][4] = {{{7, 18, 18, 13}, {14, 17, 30, 14}, {14, 17, 46, 13}, {25, 25, 119, 16}},
+                                      {{7, 25, 18, 13}, {14, 20, 30, 14}, {17, 17, 46, 13}, {25, 25, 119, 16}},
                                       {{7, 10, 8, 14}, {9, 12, 26, 10}, {16, 16, 27, 10}, {21, 21, 87, 16}},
                                       {{14, 21, 31, 17}, {8, 18, 43, 16}, {12, 16, 61, 8}, {14, 14, 163, 16}}};
 }  // namespace
@@ -388,7 +390,8 @@ void linear_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, b
     const int64_t n = T * k;
     *p = LinearPlan{};
     p->cols = N <= 64 ? 64 : 128;
-    const int32_t bm = linear_tile_rows(n, M, N, p->cols, (len + kFfnBK - 1) / kFfnBK, q8 ? kProductQ8 : kProductMap);
+    const int32_t bm = linear_tile_rows(n, M, N, p->cols, (len + kFfnBK - 1) / kFfnBK,
+                                        q8 ? kProductQ8 : len % kFfnBK ? kProductSplit : kProductMap);
     ffn_tiles_plan(n, M, bm, &p->tiles);
     // The kernel without tiles has a short way to its first operands, but reads the weights again for every 16 entries, the
     // rows of x in every workgroup, and starts a workgroup for each entry, of which most end at once: it is taken
