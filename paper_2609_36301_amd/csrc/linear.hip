@@ -311,7 +311,9 @@ void forward(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t str
         return;
     }
     switch (p.tiles.bm) {
-        case 256: return tiled<I8, 256, 256, 2>(p, a, ws, stream);
+        case 256:  // (8 bits: linear_stream_launch)
+            if constexpr (!I8) tiled<I8, 256, 256, 2>(p, a, ws, stream);
+            return;
         case 128: return p.cols == 64 ? tiled<I8, 128, 64, 2>(p, a, ws, stream) : tiled<I8, 128, 128, 2>(p, a, ws, stream);
         case 64: return p.cols == 64 ? tiled<I8, 64, 64, 3>(p, a, ws, stream) : tiled<I8, 64, 128, 3>(p, a, ws, stream);
         default:
@@ -326,10 +328,10 @@ void forward(const LinearPlan& p, const LinearArgs& a, char* ws, hipStream_t str
 // what costs least: the rounds in which the workgroups fill the chip (two of up to 128 rows to a CU, one of 256), beyond three
 // with half a round of rest, times the stages times the time of a stage and what a tile costs beside its stages.
 // Fitted to 800 shapes (1 to 8192 experts, 4 to 16384 rows each, contractions and columns of 16 to 4096, of which half are not
-// multiples of 64): 2.0 % off the best on geometric mean, five in a hundred more than 14 %.  Bf16 rows that split lines have costs of their
-// own: small tiles touch more lines for a product (27 experts of K = 2952, N = 152 with 552 rows, 64 : 128 rows 73 : 40).  us for
-// 32 : 64 : 128 : 256 rows, one expert of K = 2912, N = 1160 with 1976 rows 83 : 65 : 34 : 76; 8 bits, 15 of K = 3200, N = 3008
-// with 225 rows 174 : 105 : 55 : 89; dx, 11 of K = 3648, N = 576 with 2523 rows 287 : 234 : 174 : 148.
+// multiples of 64): 2.0 % off the best on geometric mean, five in a hundred more than 14 %.  Bf16 rows that split lines have
+// costs of their own: small tiles touch more lines for a product (27 experts of K = 2952, N = 152 with 552 rows, 64 : 128 rows
+// 73 : 40).  us for 32 : 64 : 128 : 256 rows, one expert of K = 2912, N = 1160 with 1976 rows 83 : 65 : 34 : 76; 8 bits,
+// 15 of K = 3200, N = 3008 with 225 rows 174 : 105 : 55 : 89; dx, 11 of K = 3648, N = 576 with 2523 rows 287 : 234 : 174 : 148.
 namespace {
 struct TileCost {
     int32_t alone, two;  // time of a stage, one workgroup and two to a CU
@@ -346,7 +348,7 @@ int32_t linear_tile_rows(int64_t n, int32_t M, int32_t cols, int32_t cols_of, in
     int32_t best = 64;
     int64_t least = INT64_MAX;
     for (int32_t i = 0, bm = 32; bm <= 256; bm *= 2, ++i) {
-        if (bm == 256 && product == kProductQ8 && steps < kStreamSteps) break;  // (too slow without linear_stream_kernel)
+        if (bm == 256 && product == kProductQ8 && steps < kStreamSteps) break;  // (linear_stream_kernel needs them)
         const TileCost c = kTileCost[product][i];
         const int32_t step = bm == 256 ? 256 : cols_of;
         const int64_t slots = bm == 256 ? 256 : 512;
@@ -410,7 +412,7 @@ void linear_make_plan(int64_t T, int32_t len, int32_t N, int32_t M, int32_t k, b
         return;
     }
     if (bm == 256) p->cols = 256;
-    p->stream = q8 && bm == 256 && (len + kFfnBK - 1) / kFfnBK >= kStreamSteps;
+    p->stream = q8 && bm == 256;
     p->span = p->stream ? p->cols : linear_span(len, p->cols, p->tiles.tiles, N);
     p->stages = bm >= 128 ? 2 : bm == 64 || p->cols == 64 ? 3 : p->tiles.tiles * ((N + p->span - 1) / p->span) >= 2048 ? 2 : 3;
     p->listed = linear_listed(p->tiles, M, (N + p->span - 1) / p->span);
