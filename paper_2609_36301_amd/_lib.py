@@ -137,3 +137,18 @@ def status_string(status: int) -> str:
 def check(status: int, where: str):
     if status != OK:
         raise MoreError(status, where)
+
+
+def integer(value: int, where: str, kind=_I32):
+    """value as the library takes it.  (ctypes cuts a number to the type's bits without a word, and the library's limits
+    would then be checked on what is left of it.)"""
+    most = 1 << (8 * ctypes.sizeof(kind) - 1)
+    if not -most <= value < most:
+        raise MoreError(ERR_UNSUPPORTED, where)
+    return kind(value)
+
+
+def query(name: str, *args):
+    """The host query `name` of sizes; args: its own, in order."""
+    fn = getattr(load(), name)
+    check(fn(*[integer(v, name, t) if t in (_I32, _I64) and isinstance(v, int) else v for t, v in zip(fn.argtypes, args)]), name)

@@ -24,6 +24,7 @@ from typing import Optional
 
 import torch
 
+from . import _lib
 from .layer import _ptr
 from .linear import _Call
 
@@ -51,11 +52,12 @@ class _Rows(_Call):
         if self.ld < V:
             raise ValueError("ld must be at least V = %d, got %d" % (V, self.ld))
         self.temperature, self.inplace, self.gradient = float(temperature), bool(inplace), bool(gradient)
-        f32 = torch.float32
+        f32, i64 = torch.float32, ctypes.c_int64
+        self._rows = (ctypes.c_int32(self.bits), _lib.integer(T, self._function, i64), _lib.integer(V, self._function),
+                      _lib.integer(self.ld, self._function, i64))
+        self._entries = (_lib.integer(k, self._function), ctypes.c_float(self.temperature))
         self._prepare(self._function, device, teacher_idx=(torch.int32, (T, k)), teacher_val=(f32, (T, k)),
                       **{name: (f32, (T,)) for name in self._vectors})
-        i32, i64 = ctypes.c_int32, ctypes.c_int64
-        self._rows, self._entries = (i32(self.bits), i64(T), i32(V), i64(self.ld)), (i32(k), ctypes.c_float(self.temperature))
         self._strides = (self.ld if T > 1 else None, 1 if V > 1 else None)
         self.dlogits = None
         if gradient and not inplace:

@@ -78,7 +78,7 @@ def _call(name: str, device: torch.device, *args):
 
 def _size(name: str, *args) -> int:
     n = ctypes.c_size_t(0)
-    _lib.check(getattr(_lib.load(), name)(*args, ctypes.byref(n)), name)
+    _lib.query(name, *args, ctypes.byref(n))
     return n.value
 
 
@@ -100,8 +100,7 @@ def expert_ffn_backward_workspace_size(T: int, h: int, s: int, M: int, k: int, a
 def expert_ffn_plan(T: int, h: int, s: int, M: int, k: int, backward: bool = False, addends: int = 0) -> dict[str, int]:
     """The form in which expert_ffn (or its backward pass) runs this shape: the fields of more_expert_plan."""
     plan = _lib.ExpertPlan()
-    _lib.check(_lib.load().more_expert_ffn_plan(T, h, s, M, k, addends, int(backward), ctypes.byref(plan)),
-               "more_expert_ffn_plan")
+    _lib.query("more_expert_ffn_plan", T, h, s, M, k, addends, int(backward), ctypes.byref(plan))
     return {name: getattr(plan, name) for name, _ in plan._fields_}
 
 
@@ -218,6 +217,8 @@ class BlockNorm:
     def __init__(self, T: int, h: int, k: int = 1, *, resid_dtype=torch.bfloat16, norm_after: bool = True,
                  alpha: float = 1.0, eps: float = 1e-6, save_u: bool = False, inplace: bool = False, device=None):
         self.shape = (T, h, k)
+        for size in (h, k):
+            _lib.integer(size, "more_block_norm")
         self.resid_dtype, self.resid_bits = resid_dtype, _resid_bits(resid_dtype)
         self.norm_after, self.alpha, self.eps = bool(norm_after), float(alpha), float(eps)
         self.inplace = inplace

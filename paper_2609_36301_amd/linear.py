@@ -57,8 +57,7 @@ def expert_linear_q8_workspace_size(T: int, K: int, N: int, M: int, k: int) -> i
 def expert_linear_plan(T: int, K: int, N: int, M: int, k: int, kind: str = "linear") -> dict[str, int]:
     """The form in which a map ("linear", "backward" or "q8") runs this shape: the fields of more_linear_plan."""
     plan = _lib.LinearPlan()
-    _lib.check(_lib.load().more_expert_linear_plan(T, K, N, M, k, _KINDS[kind], ctypes.byref(plan)),
-               "more_expert_linear_plan")
+    _lib.query("more_expert_linear_plan", T, K, N, M, k, _KINDS[kind], ctypes.byref(plan))
     return {name: getattr(plan, name) for name, _ in plan._fields_}
 
 
@@ -111,8 +110,8 @@ class _Call:
             _lib.check(status, self._name)
 
 
-def _sizes(T, *sizes):
-    return (ctypes.c_int64(T),) + tuple(map(ctypes.c_int32, sizes))
+def _sizes(name, T, *sizes):
+    return (_lib.integer(T, name, ctypes.c_int64),) + tuple(_lib.integer(size, name) for size in sizes)
 
 
 def _selection(T, M, k):
@@ -125,7 +124,8 @@ class ExpertLinear(_Call):
 
     def __init__(self, T: int, K: int, N: int, M: int, k: int, *, out_dtype=torch.bfloat16, device=None):
         bf16 = torch.bfloat16
-        self.shape, self.y_bits, self._sizes = (T, K, N, M, k), _y_bits(out_dtype), _sizes(T, K, N, M, k)
+        self.shape, self.y_bits = (T, K, N, M, k), _y_bits(out_dtype)
+        self._sizes = _sizes("more_expert_linear", T, K, N, M, k)
         self._prepare("more_expert_linear", device, x=(bf16, (T, K)), Wt=(bf16, (M, N, K)), **_selection(T, M, k))
         self.workspace_bytes = expert_linear_workspace_size(*self.shape)
         self.workspace = _workspace(self.workspace_bytes, self.device)
@@ -160,7 +160,7 @@ class ExpertLinearBackward(_Call):
         if not (need_dx or need_dW):
             raise ValueError("need_dx or need_dW must be set")
         bf16 = torch.bfloat16
-        self.shape, self._sizes = (T, K, N, M, k), _sizes(T, K, N, M, k)
+        self.shape, self._sizes = (T, K, N, M, k), _sizes("more_expert_linear_backward", T, K, N, M, k)
         self._prepare("more_expert_linear_backward", device, x=(bf16, (T, K)), Wt=(bf16, (M, N, K)), **_selection(T, M, k),
                       dy=(bf16, (T * k, N)))
         dev = self.device
@@ -196,7 +196,8 @@ class QuantizeRows(_Call):
     2 width)."""
 
     def __init__(self, T: int, width: int, *, gated: bool = False, device=None):
-        self.shape, self.gated, self._sizes = (T, width), bool(gated), _sizes(T, width, bool(gated))
+        self.shape, self.gated = (T, width), bool(gated)
+        self._sizes = _sizes("more_quantize_rows", T, width, self.gated)
         self._prepare("more_quantize_rows", device, x=(torch.bfloat16, (T, 2 * width if gated else width)))
         self.q = torch.empty((T, width), dtype=torch.int8, device=self.device)
         self.scale = torch.empty((T,), dtype=torch.float32, device=self.device)
@@ -227,7 +228,8 @@ class ExpertLinearQ8(_Call):
 
     def __init__(self, T: int, K: int, N: int, M: int, k: int, *, out_dtype=torch.bfloat16, device=None):
         i8, f32 = torch.int8, torch.float32
-        self.shape, self.y_bits, self._sizes = (T, K, N, M, k), _y_bits(out_dtype), _sizes(T, K, N, M, k)
+        self.shape, self.y_bits = (T, K, N, M, k), _y_bits(out_dtype)
+        self._sizes = _sizes("more_expert_linear_q8", T, K, N, M, k)
         self._prepare("more_expert_linear_q8", device, q=(i8, (T, K)), q_scale=(f32, (T,)), Wq=(i8, (M, N, K)),
                       w_scale=(f32, (M, N)), **_selection(T, M, k), gate=(f32, (T, k)))
         self.workspace_bytes = expert_linear_q8_workspace_size(*self.shape)

@@ -48,9 +48,7 @@ def _check_bf16(name: str, t: torch.Tensor, ndim: int):
 
 def lowrank_workspace_size(T: int, h: int, r: int, M: int, k: int, m_chunks: int = 0) -> int:
     n = ctypes.c_size_t(0)
-    _lib.check(_lib.load().more_route_lowrank_workspace_size_ex(T, h, r, M, k, m_chunks,
-                                                                ctypes.byref(n)),
-               "more_route_lowrank_workspace_size_ex")
+    _lib.query("more_route_lowrank_workspace_size_ex", T, h, r, M, k, m_chunks, ctypes.byref(n))
     return n.value
 
 
@@ -58,8 +56,7 @@ def lowrank_plan(T: int, h: int, r: int, M: int, k: int) -> int:
     """Number of expert-axis chunks the library picks for this shape (0: the fused or the
     single-pass route, which no m_chunks >= 1 selects)."""
     c = ctypes.c_int32(0)
-    _lib.check(_lib.load().more_route_lowrank_plan(T, h, r, M, k, ctypes.byref(c)),
-               "more_route_lowrank_plan")
+    _lib.query("more_route_lowrank_plan", T, h, r, M, k, ctypes.byref(c))
     return c.value
 
 
@@ -69,16 +66,13 @@ ROUTE_NAMES = {0: "expert-resident", 1: "fused", 2: "fused-local", 3: "single-pa
 def lowrank_route(T: int, h: int, r: int, M: int, k: int) -> str:
     """Name of the route more_route_lowrank takes for this shape."""
     c = ctypes.c_int32(0)
-    _lib.check(_lib.load().more_route_lowrank_route(T, h, r, M, k, ctypes.byref(c)),
-               "more_route_lowrank_route")
+    _lib.query("more_route_lowrank_route", T, h, r, M, k, ctypes.byref(c))
     return ROUTE_NAMES[c.value]
 
 
 def fullrank_workspace_size(T: int, h: int, M: int, k: int, logit_bits: int = 32) -> int:
     n = ctypes.c_size_t(0)
-    _lib.check(_lib.load().more_route_fullrank_workspace_size(T, h, M, k, logit_bits,
-                                                              ctypes.byref(n)),
-               "more_route_fullrank_workspace_size")
+    _lib.query("more_route_fullrank_workspace_size", T, h, M, k, logit_bits, ctypes.byref(n))
     return n.value
 
 
@@ -157,9 +151,7 @@ class TrainRouting(Routing):
 
 def lowrank_train_workspace_size(T: int, h: int, r: int, M: int, k: int) -> int:
     n = ctypes.c_size_t(0)
-    _lib.check(_lib.load().more_route_lowrank_train_workspace_size(T, h, r, M, k,
-                                                                   ctypes.byref(n)),
-               "more_route_lowrank_train_workspace_size")
+    _lib.query("more_route_lowrank_train_workspace_size", T, h, r, M, k, ctypes.byref(n))
     return n.value
 
 
@@ -233,9 +225,7 @@ class Gradients:
 def lowrank_backward_workspace_size(T: int, h: int, r: int, M: int, k: int,
                                     balance: bool = True) -> int:
     n = ctypes.c_size_t(0)
-    _lib.check(_lib.load().more_route_lowrank_backward_workspace_size(T, h, r, M, k, int(balance),
-                                                                      ctypes.byref(n)),
-               "more_route_lowrank_backward_workspace_size")
+    _lib.query("more_route_lowrank_backward_workspace_size", T, h, r, M, k, int(balance), ctypes.byref(n))
     return n.value
 
 
@@ -356,8 +346,7 @@ def route_fullrank(x: torch.Tensor, Wt: torch.Tensor, k: int, *, topval: bool = 
 
 def fullrank_fused_workspace_size(T: int, h: int, M: int, k: int) -> int:
     n = ctypes.c_size_t(0)
-    _lib.check(_lib.load().more_route_fullrank_fused_workspace_size(T, h, M, k, ctypes.byref(n)),
-               "more_route_fullrank_fused_workspace_size")
+    _lib.query("more_route_fullrank_fused_workspace_size", T, h, M, k, ctypes.byref(n))
     return n.value
 
 
@@ -410,6 +399,7 @@ def expert_histogram(idx: torch.Tensor, M: int) -> torch.Tensor:
     if idx.device.type != "cuda":
         raise ValueError("idx must be on a GPU device")
     T, k = idx.shape
+    _lib.integer(M, "more_expert_histogram")
     counts = torch.empty((M,), dtype=torch.int32, device=idx.device)
     st = _lib.load().more_expert_histogram(_ptr(idx), T, k, M, _ptr(counts), _stream(idx.device))
     _lib.check(st, "more_expert_histogram")
@@ -427,8 +417,7 @@ def dispatch_sort(idx: torch.Tensor, M: int) -> tuple[torch.Tensor, torch.Tensor
     T, k = idx.shape
     lib = _lib.load()
     n = ctypes.c_size_t(0)
-    _lib.check(lib.more_dispatch_sort_workspace_size(T, k, M, ctypes.byref(n)),
-               "more_dispatch_sort_workspace_size")
+    _lib.query("more_dispatch_sort_workspace_size", T, k, M, ctypes.byref(n))
     ws = torch.empty((max(n.value, 1),), dtype=torch.uint8, device=idx.device)
     offsets = torch.empty((M + 1,), dtype=torch.int32, device=idx.device)
     srt = torch.empty((T * k,), dtype=torch.int32, device=idx.device)
@@ -446,8 +435,7 @@ class DispatchSorter:
         self.T, self.k, self.M = T, k, M
         dev = torch.device(device)
         n = ctypes.c_size_t(0)
-        _lib.check(_lib.load().more_dispatch_sort_workspace_size(T, k, M, ctypes.byref(n)),
-                   "more_dispatch_sort_workspace_size")
+        _lib.query("more_dispatch_sort_workspace_size", T, k, M, ctypes.byref(n))
         self.workspace_bytes = n.value
         self.workspace = torch.empty((max(n.value, 1),), dtype=torch.uint8, device=dev)
         self.offsets = torch.empty((M + 1,), dtype=torch.int32, device=dev)
