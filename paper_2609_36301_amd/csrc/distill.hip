@@ -112,6 +112,14 @@ __device__ __forceinline__ float group_reduce(float v, float* part) {
     return v;
 }
 
+// hi + low += v, of which only the lower part is rounded.
+__device__ __forceinline__ void join(float& hi, float& low, float v) {
+#pragma clang fp contract(off)
+    const float sum = hi + v, of_v = sum - hi;
+    low += (hi - (sum - of_v)) + (v - of_v);
+    hi = sum;
+}
+
 // RESIDENT: the row's pieces (R per thread) stay in registers; else they are read again (R at a time).  ONCE: nontemporal
 // loads and stores.
 template <bool WIDE, int THREADS, int R, bool RESIDENT, bool ONCE>
@@ -233,26 +241,32 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void distill_kernel(
             Z = group_reduce<THREADS, false>(Z, part_sum);
             keep_packed(x.v);
         } else {
-            // a running maximum and sum per thread
+            // A running maximum and sum per thread: R pieces are summed apart and then join a sum of two floats (one after
+            // the other, the roundings of V / THREADS terms add up: 2^26 equal ones 1.7e-3 off).  Its exponents count from
+            // `base`, which follows the maximum in steps of 2^8: a step rounds the sum, so that there are few.
+            float base = m, low = 0.0f;
             Z = m == minus_inf() ? 0.0f : m == m ? 1.0f : m;
             for (int32_t u0 = tid; u0 < at.pieces; u0 += R * THREADS) {
                 load(x, at, u0);
-                float to = m;
 #pragma unroll
                 for (int r = 0; r < R; ++r)
 #pragma unroll
-                    for (int i = 0; i < kCount; ++i) to = fmaxf(to, P::value(x.v[r], i));
-                const float base = to == minus_inf() ? 0.0f : to;  // (nothing but -infinity so far)
-                Z *= __builtin_amdgcn_exp2f((m - base) * c);
+                    for (int i = 0; i < kCount; ++i) m = fmaxf(m, P::value(x.v[r], i));
+                const bool move = (m - base) * c > 8.0f;  // (infinite where there was nothing but -infinity)
+                const float f = move ? __builtin_amdgcn_exp2f((base - m) * c) : 1.0f;
+                Z *= f;
+                low *= f;
+                base = move ? m : base;
+                const float from = base == minus_inf() ? 0.0f : base;
+                float part = 0.0f;
 #pragma unroll
                 for (int r = 0; r < R; ++r)
 #pragma unroll
-                    for (int i = 0; i < kCount; ++i) Z += __builtin_amdgcn_exp2f((P::value(x.v[r], i) - base) * c);
-                m = to;
+                    for (int i = 0; i < kCount; ++i) part += __builtin_amdgcn_exp2f((P::value(x.v[r], i) - from) * c);
+                join(Z, low, part);
             }
-            const float mine = m;
             m = group_reduce<THREADS, true>(m, part_max);
-            Z = group_reduce<THREADS, false>(mine == m ? Z : Z * __builtin_amdgcn_exp2f((mine - m) * c), part_sum);
+            Z = group_reduce<THREADS, false>((Z + low) * __builtin_amdgcn_exp2f((base - m) * c), part_sum);
         }
         group_sync<THREADS>();  // the teacher's entries and their sum are there
         const float U = total[group];
