@@ -608,7 +608,11 @@ more_status more_expert_linear_plan(int64_t T, int32_t K, int32_t N, int32_t M, 
  * Limits: 1 <= V <= 2^30, 1 <= k <= MORE_TEACHER_K_MAX, V <= ld, ld_dlogits <= 2^40, T <= 2^31 - 1, 2^-40 <=
  * tau <= 2^40.  Elements must be aligned to their size (rows that begin at a multiple of 16 bytes in both tensors
  * are faster).  No workspace.
- * Numerics: fp32; sums in a fixed order; the gradient is rounded once.  -infinity among the logits is a class of
+ * Numerics: fp32; sums in a fixed order; the gradient is rounded once.  With V <= 2 k, where the entries may cover all
+ * classes and P and Q come close as tau grows, both results are made of differences: at every tau they are off by
+ * a thousandth at worst where P and Q differ by as much as either varies.  With V > 2 k the loss is tau^2 times a
+ * difference of logarithms, off by about tau^2 2^-13 at worst (logits within 100 tau of the largest), which is not
+ * small beside a loss where the entries hold nearly all of P.  -infinity among the logits is a class of
  * probability 0 (a row of nothing else has the loss NaN, as has one with a NaN or +infinity).
  */
 #define MORE_TEACHER_K_MAX 1024

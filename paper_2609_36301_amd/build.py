@@ -22,7 +22,7 @@ SOURCES = ["lowrank.hip", "bucket.hip", "fullrank.hip", "histogram.hip", "dispat
            "backward.hip", "wide.hip",
            "noalloc.hip", "more_api.cpp", "ffn.hip", "ffn_backward.hip", "block_norm.hip",
            "grad_clip.hip", "layer_api.cpp", "linear.hip", "linear_stream.hip",
-           "linear_backward.hip", "quantize.hip", "distill.hip",
+           "linear_backward.hip", "quantize.hip", "distill.hip", "distill_cover.hip",
            "linear_api.cpp"]
 ARCH = "gfx950"
 

@@ -1,4 +1,4 @@
-// Launch entry point of the distillation loss (distill.hip).
+// Launch entry points of the distillation loss (distill.hip, distill_cover.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -23,5 +23,8 @@ struct DistillArgs {
 };
 
 hipError_t distill_launch(const DistillArgs& a, hipStream_t stream);
+
+// The same for V <= 2 k (distill_cover.hip).
+hipError_t distill_cover_launch(const DistillArgs& a, hipStream_t stream);
 
 }  // namespace more

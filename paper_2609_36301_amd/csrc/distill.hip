@@ -5,7 +5,7 @@
 //        = tau^2 (ln Z - ln sum e + sum_j q_j ((v_j - max v) - (z_(id_j) - m)) / tau)
 //   d loss / dz_e = tau (P_e - sum_(j: id_j = e) q_j)
 // An entry is valid if its id lies in [0, V) and its value is not -infinity; a row without valid entries has loss 0
-// and gradient 0.
+// and gradient 0.  (V > 2 k: with more entries P and Q may nearly cancel, see distill_cover.hip.)
 //
 // Memory-bound: a row's logits are read once and stay in registers between maximum, sum and gradient, so that the loss
 // with its gradient is one read and one write: 8192 rows of 32001 bf16 187 us, 5.6 TB/s; 16384 of 4096 fp32 154 us in two
@@ -22,44 +22,11 @@
 #include <type_traits>
 
 #include "distill.h"
-#include "device_common.h"
+#include "distill_device.h"
 
 namespace more {
 
 namespace {
-
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLn2 = 0.69314718055994530942f;
-__device__ __forceinline__ float minus_inf() { return -__builtin_huge_valf(); }
-
-// A 16-byte piece of a row: eight bf16 or four fp32 values.
-template <bool WIDE>
-struct Piece {
-    static constexpr int kCount = WIDE ? 4 : 8;
-    static constexpr uint32_t kNone = WIDE ? 0xFF800000u : 0xFF80FF80u;  // -infinity
-    using Element = typename std::conditional<WIDE, float, uint16_t>::type;
-    static __device__ __forceinline__ float value(const u32x4& v, int i) {
-        const uint32_t w = v[WIDE ? i : i / 2];  // (a copy: the bit cast of a vector's element took element 0)
-        return __builtin_bit_cast(float, WIDE ? w : i % 2 ? w & 0xFFFF0000u : w << 16);
-    }
-    static __device__ __forceinline__ float value(Element e) {
-        if constexpr (WIDE) return e;
-        else return bf16_bits_to_f32(e);
-    }
-    static __device__ __forceinline__ Element element(float f) {
-        if constexpr (WIDE) return f;
-        else return __builtin_bit_cast(uint16_t, (__bf16)f);
-    }
-    static __device__ __forceinline__ u32x4 pack(const float (&f)[kCount]) {
-        u32x4 v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (WIDE) v[i] = __builtin_bit_cast(uint32_t, f[i]);
-            else v[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)f[2 * i], (__bf16)f[2 * i + 1]});
-        }
-        return v;
-    }
-};
 
 // What keeps a row of bf16 in as many registers as it has bytes: its pieces are unpacked again where they are used next,
 // and one after the other (unpacked all at once, 8192 rows of 32001 take 812 us).
@@ -68,35 +35,6 @@ template <int R>
 __device__ __forceinline__ void keep_packed(u32x4 (&v)[R]) {
 #pragma unroll
     for (int r = 0; r < R; ++r) asm volatile("" : "+v"(v[r]));
-}
-
-template <int THREADS>
-__device__ __forceinline__ void group_sync() {
-    if constexpr (THREADS == 64) {
-        wave_lds_sync();
-    } else {
-        __syncthreads();
-    }
-}
-
-// Over the wave's lanes, by moves that stay in the vector unit.
-template <typename F>
-__device__ __forceinline__ float wave_reduce(float v, F f) {
-    v = f(v, lane_xor<1>(v));
-    v = f(v, lane_xor<2>(v));
-    v = f(v, lane_xor<4>(v));
-    v = f(v, lane_xor<8>(v));
-    float a, b;
-    lane_pair16(v, a, b);
-    v = f(a, b);
-    lane_pair32(v, a, b);
-    return f(a, b);
-}
-__device__ __forceinline__ float wave_max(float v) {
-    return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });
-}
-__device__ __forceinline__ float wave_sum(float v) {
-    return wave_reduce(v, [](float a, float b) { return a + b; });
 }
 
 // The value of every thread's v over a row's group (waves in order).
@@ -242,7 +180,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void distill_kernel(
             keep_packed(x.v);
         } else {
             // A running maximum and sum per thread: R pieces are summed apart and then join a sum of two floats (one after
-            // the other, the roundings of V / THREADS terms add up: 2^26 equal ones 1.7e-3 off).  Its exponents count from
+            // the other, the roundings of V / THREADS terms add up: 1.9e-4 of Z on 2^26 ascending fp32 logits).  Its exponents count from
             // `base`, which follows the maximum in steps of 2^8: a step rounds the sum, so that there are few.
             float base = m, low = 0.0f;
             Z = m == minus_inf() ? 0.0f : m == m ? 1.0f : m;
@@ -415,6 +353,7 @@ void launch(const DistillArgs& a, hipStream_t stream) {
 }  // namespace
 
 hipError_t distill_launch(const DistillArgs& a, hipStream_t stream) {
+    if (a.V <= 2 * a.k) return distill_cover_launch(a, stream);
     if (a.wide)
         launch<true>(a, stream);
     else
