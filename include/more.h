@@ -577,13 +577,15 @@ more_status more_expert_linear_q8_workspace_size(int64_t T, int32_t K, int32_t N
 typedef struct more_linear_plan {
     int32_t tile_rows; /* rows of a tile: 32, 64, 128 or 256; 0: the kernel without tiles               */
     int32_t cols;      /* columns of a step (kind 1: of dx); without tiles: of a workgroup              */
-    int32_t span;      /* columns that a workgroup takes                                                */
-    int32_t stages;    /* of the LDS ring (0 without tiles)                                             */
+    int32_t span;      /* columns that a workgroup takes (kind 1: of dx)                                */
+    int32_t stages;    /* of the LDS ring (0 without tiles; kind 1: of dx)                              */
     int32_t dw_rows;   /* (kind 1, else 0) rows ...                                                     */
-    int32_t dw_cols;   /* ... and columns of a tile of dWt                                              */
+    int32_t dw_cols;   /* ... and columns of a tile of dWt (64 of either: one stage in LDS, else two)   */
     int32_t dw_runs;   /* (kind 1, else 0) runs of an expert's entries that are summed apart            */
-    int32_t dw_span;   /* (kind 1, else 0) columns (dw_cols > 64) or rows of dWt that a workgroup takes */
-    int32_t listed;    /* the tiles are listed by a launch of their own; else workgroups find them       */
+    int32_t dw_span;   /* (kind 1, else 0) rows of dWt that a workgroup takes where dw_cols is 64, or where listed
+                          and both are 128, K <= 128 and N > 128; else columns                          */
+    int32_t listed;    /* the tiles are listed by a launch of their own; else workgroups find them, and
+                          (kind 1, dw_cols < 256) both gradients, where both are asked for, share a launch */
 } more_linear_plan;
 more_status more_expert_linear_plan(int64_t T, int32_t K, int32_t N, int32_t M, int32_t k, int32_t kind,
                                     more_linear_plan* plan);
