@@ -527,7 +527,8 @@ more_status more_expert_linear_workspace_size(int64_t T, int32_t K, int32_t N, i
  *   dWt      bf16 [M][N][K] out, or NULL; zero for experts without entries (all zero when T == 0)
  *                              (not both NULL)
  *   workspace / workspace_bytes   at least more_expert_linear_backward_workspace_size() bytes (it may be
- *                              0), 256-byte aligned
+ *                              0; with k > 1 it holds the entries' shares of dx, 4 T k K bytes, also where
+ *                              dx is NULL), 256-byte aligned
  * Limits as for more_expert_linear.  Numerics: fp32 accumulation of exact bf16 products, each result rounded
  * once.  Nothing is added atomically: a call gives the same bits on every run.
  */

@@ -24,8 +24,10 @@ namespace more {
 // entries' rows of x the N side.  The pipeline runs over (column step, contraction step) pairs, so that a
 // short contraction does not drain it.  Small experts are bound by their weights' way from memory (4096 experts of K = 512,
 // N = 128 with 32 rows 117 us, 587 MB at 5.0 TB/s beside the gathered rows of x; 8-bit, 8192 of K = 4096, N = 128 with a
-// quarter row 140 us), large ones by the matrix cores and their power (32 experts of 2048 x 2048 with 1024 rows 278 us,
-// 990 TFLOP/s, 4.5 rounds of tiles over the chip).
+// quarter row 140 us), large ones by how well the matrix cores are fed: 32 experts of 2048 x 2048 with 1024 rows 282 us a call,
+// 975 TFLOP/s, the kernel 291 to 325 in a trace.  Counters there: the matrix cores work in 44 % of the cycles, waves wait in
+// 38 %, CUs have no tile in 16 % (4.5 rounds of tiles, the last ones of an expert partly empty), the clock is 2.1 GHz.  Full
+// tiles in eight whole rounds (65536 rows) reach 1120 TFLOP/s, a dense library product of 8192^3 1600.
 // LINES: y is stored in whole lines by way of LDS, where a wave has whole lines of a row (us, in halves of lines : whole,
 // 65536 rows, N = 2048, 16 experts, bf16 K = 128 115 : 78, K = 512 194 : 173; 32 experts of 2048 x 2048, 32768 entries 290 : 280).
 template <int BM, int COLS, int STAGES>

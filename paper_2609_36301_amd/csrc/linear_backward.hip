@@ -25,8 +25,9 @@ namespace more {
 // ------------------------------------------------------------------------------ dx
 // The weights lie with the contraction axis (N) slowest: they are a column tile (M side), the entries' rows of dy
 // a row tile (N side).  A workgroup computes `span` columns in steps of COLS; the pipeline runs over (column
-// step, contraction step) pairs.  4096 experts of K = 64, N = 512 with 32 rows 80 us, 419 MB at 5.2 TB/s; 32 of
-// 2048 x 2048 with 1024 rows 330 us, 830 TFLOP/s, and 53 for the fp32 shares' sum.  Up to 128 rows the weights, read
+// step, contraction step) pairs.  4096 experts of K = 64, N = 512 with 32 rows 79 us, 419 MB at 5.3 TB/s; 32 of
+// 2048 x 2048 with 1024 rows 322 us in calls one after the other (352 to 380 in a trace), 850 TFLOP/s, and 53 for the fp32
+// shares' sum; the matrix cores work in 36 % of the cycles, waves wait in 39 %.  Up to 128 rows the weights, read
 // across their rows, come by way of registers; tiles of 256 rows load straight to LDS.
 constexpr int dx_threads(int bm) { return bm == 256 ? 512 : 256; }
 template <int BM, int COLS>
@@ -250,8 +251,9 @@ __global__ __launch_bounds__(256) void linear_sum_kernel(LinearArgs a, const flo
 // rows), dy the N side and x the M side, and both are gathered.  A workgroup computes tiles of RT rows (of N) and CT
 // columns (of K) one after the other over `span` of one side (BY_COLS: of K), and the pipeline runs over (tile, 64
 // entries) pairs, so that the few rows of a small expert do not drain it.
-// Small experts are bound by memory (4096 of K = 64, N = 512, 32 entries 84 us, 419 MB at 5.0 TB/s), large ones by the
-// transposing reads of both operands and power (32 of 2048 x 2048, 1024 entries 344 us, 800 TFLOP/s).
+// Small experts are bound by memory (4096 of K = 64, N = 512, 32 entries 84 to 90 us, 419 MB at 5.0 TB/s), large ones by the
+// transposing reads of both operands, which come by way of registers: 32 of 2048 x 2048, 1024 entries 328 us in calls one
+// after the other (368 to 422 in a trace), 840 TFLOP/s; the matrix cores work in 32 % of the cycles, waves wait in 39 %.
 // PARTS: the entries of an expert are cut into `runs` runs and a workgroup takes one tile and one run; the fp32
 // results of run i go to parts + i M N K.
 struct LinearDw {
