@@ -10,7 +10,7 @@ from test_gpu_distill import close, rows_on_device
 
 pytestmark = pytest.mark.gpu
 
-TAUS = [0.25, 1.0, 20.0, 256.0, 4096.0, 2.0 ** 20, 2.0 ** 40]
+TAUS = [2.0 ** -40, 0.25, 1.0, 20.0, 256.0, 4096.0, 2.0 ** 20, 2.0 ** 40]
 
 
 def case(seed, V, k, bits, repeats=False):
@@ -42,9 +42,9 @@ SHAPES = [(1, 1), (1, 3), (2, 1), (7, 7), (33, 17), (64, 64), (65, 64), (100, 64
           (1500, 800), (2048, 1024)]
 
 
+# (rows of a thousand classes take a second or two to 60 digits: three temperatures of them)
 @pytest.mark.parametrize("bits", [16, 32])
-@pytest.mark.parametrize("tau", TAUS)
-@pytest.mark.parametrize("V,k", SHAPES)
+@pytest.mark.parametrize("V,k,tau", [(V, k, tau) for V, k in SHAPES for tau in (TAUS if V < 600 else TAUS[1::3])])
 def test_covered(V, k, tau, bits):
     torch = require_gpu()
     from paper_2609_36301_amd import distill_backward, distill_loss
