@@ -163,3 +163,31 @@ def test_covered_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((d.loss, d.m, d.Z, d.dlogits), want))
+
+
+@pytest.mark.parametrize("V,k", [(90, 64), (900, 512)])
+def test_covered_each_output_alone(V, k):
+    """The library's call with any of its outputs left out, and gradients that lie otherwise than the logits."""
+    torch = require_gpu()
+    from paper_2609_36301_amd import _lib, distill_loss
+    z, ids, values, w = case(V, V, k, 32, repeats=True)
+    T, tau = len(z), 30.0
+    announce("distill V=%d k=%d, each output alone" % (V, k))
+    logits, ids, values, w = rows_on_device(z, 32, V + 2, 3)[1], to_dev(ids), to_dev(values), to_dev(w)
+    want = distill_loss(logits, ids, values, w, temperature=tau, gradient=True)
+    stream = torch.cuda.current_stream().cuda_stream
+    for given in ("loss", "m", "Z", "dlogits"):
+        outs = {name: torch.full((T,), 5.0, device="cuda") for name in ("loss", "m", "Z")}
+        buffer = torch.full((T * (V + 7),), 5.0, device="cuda")
+        rows = buffer.view(T, V + 7)[:, 2:V + 2]
+        status = _lib.load().more_distill(
+            logits.data_ptr(), 32, T, V, V + 2, ids.data_ptr(), values.data_ptr(), k, tau, w.data_ptr(),
+            *[outs[name].data_ptr() if name == given else None for name in ("loss", "m", "Z")],
+            rows.data_ptr() if given == "dlogits" else None, V + 7, stream)
+        assert status == _lib.OK
+        for name, t in outs.items():
+            assert torch.equal(t, getattr(want, name)) if name == given else (t == 5).all()
+        if given == "dlogits":
+            assert torch.equal(rows, want.dlogits)
+            rows[:] = 5
+        assert (buffer == 5).all()
